@@ -382,6 +382,19 @@ int tkv_add_rmsnorm(int32_t n_rows, int32_t hidden, float eps, float* x, const v
 int tkv_rope_append(const tkv_shape* shape, int32_t n_tok, const void* qkv, const float* cosv, const float* sinv,
                     const int32_t* d_dst, void* q, void* k, void* v, void* hip_stream);
 
+/* The same with a norm of every query and key head first, and rotation of all or the first part of a head:
+ *   q'[h] = rotate(q[h] / sqrt(mean(q[h]^2) + eps) * q_weight),   k'[h] likewise with k_weight,
+ * where rotate turns elements i and i + rot / 2 (i < rot / 2) by the token's i-th angle and passes the rest.
+ *   qkv         token t's heads at qkv + t * qkv_stride elements (bf16; a multiple of 8, at least
+ *               (hq + 2 hkv) d): a slice of a wider product is read in place
+ *   q_weight, k_weight  [d] fp32
+ *   cosv, sinv  [n_tok][rot / 2] fp32; rot a multiple of 16, 0 <= rot <= d (0: norm alone, both may be NULL)
+ * The other arguments and what is written are tkv_rope_append's.  q must not overlap qkv.  A token without a
+ * slot still gets its q.  Tensors 16-byte aligned. */
+int tkv_norm_rope_append(const tkv_shape* shape, int32_t n_tok, const void* qkv, int64_t qkv_stride,
+                         const float* q_weight, const float* k_weight, float eps, const float* cosv, const float* sinv,
+                         int32_t rot, const int32_t* d_dst, void* q, void* k, void* v, void* hip_stream);
+
 /* out[n_rows][inter] bf16 = SiLU(gu[:, :inter]) * gu[:, inter:], gu [n_rows][2 inter] bf16. */
 int tkv_swiglu(int32_t n_rows, int32_t inter, const void* gu, void* out, void* hip_stream);
 

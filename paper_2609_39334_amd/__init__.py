@@ -93,6 +93,8 @@ _SIG = {
     "tkv_kv_append": (ctypes.c_int, [ctypes.POINTER(tkv_shape), _P, _I32, _P, _P, _P, _P, _P]),
     "tkv_add_rmsnorm": (ctypes.c_int, [_I32, _I32, ctypes.c_float, _P, _P, _P, _P, _P]),
     "tkv_rope_append": (ctypes.c_int, [ctypes.POINTER(tkv_shape), _I32, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "tkv_norm_rope_append": (ctypes.c_int, [ctypes.POINTER(tkv_shape), _I32, _P, ctypes.c_int64, _P, _P, ctypes.c_float, _P, _P,
+                                            _I32, _P, _P, _P, _P, _P]),
     "tkv_swiglu": (ctypes.c_int, [_I32, _I32, _P, _P, _P]),
     "tkv_cd_sample": (ctypes.c_int, [_I32, _I32, ctypes.c_float, _I32, _P, _P, _P, _I32, _P, _P, _P, _P]),
     "tkv_search_create": (ctypes.c_int, [_I32, _I32, _I32, _I32, ctypes.POINTER(_P)]),
@@ -451,6 +453,80 @@ def tkv_rope_append(qkv: torch.Tensor, cos: torch.Tensor, sin: torch.Tensor, dst
     shape = tkv_shape(hq, hkv, d, bs, nb)
     _check(lib().tkv_rope_append(ctypes.byref(shape), n, qkv.data_ptr(), cos.data_ptr(), sin.data_ptr(), dst.data_ptr(),
                                  q.data_ptr(), k.data_ptr(), v.data_ptr(), _stream(stream)))
+    return q
+
+
+class _Call:
+    """The device and stream of a call on `device`'s tensors: its outputs and workspaces are allocated for that stream,
+    and its work is enqueued there (the current stream of the tensors' device without a stream; never the
+    current device's, if that is another)."""
+
+    def __init__(self, fn: str, device: torch.device, stream):
+        self.device = device
+        self.current = torch.cuda.current_stream(device)
+        if stream is None:
+            self.stream = self.current
+        elif hasattr(stream, "cuda_stream"):
+            self.stream = stream
+            if stream.device != device:
+                raise ValueError(f"{fn}: the stream is {stream.device}'s, the tensors are on {device}")
+        else:
+            self.stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+        self.handle = self.stream.cuda_stream
+        self.side = self.handle != self.current.cuda_stream
+
+    def empty(self, shape, dtype) -> torch.Tensor:
+        if not self.side:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            t = torch.empty(shape, dtype=dtype, device=self.device)
+        t.record_stream(self.current)  # not handed out again before the current stream's work so far, and later reads
+        return t
+
+    def run(self, entry, *args) -> None:
+        if torch.cuda.current_device() == self.device.index:
+            _check(entry(*args, self.handle))
+        else:
+            with torch.cuda.device(self.device):
+                _check(entry(*args, self.handle))
+
+
+def _on_device(fn: str, device: torch.device, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{fn}: {name} is on {t.device}, not on {device}")
+
+
+def tkv_norm_rope_append(qkv: torch.Tensor, q_weight: torch.Tensor, k_weight: torch.Tensor, eps: float,
+                         cos: torch.Tensor, sin: torch.Tensor, dst: torch.Tensor, hq: int, k: torch.Tensor,
+                         v: torch.Tensor, stream=None) -> torch.Tensor:
+    """tkv_rope_append with a norm of every query and key head (weights [d] fp32) before the rotation.  qkv's rows may
+    be a slice of wider ones (row stride a multiple of 8); cos, sin: [n, rot / 2] fp32, of the first rot <= d elements
+    of a head (rot a multiple of 16; 0: none)."""
+    fn = "tkv_norm_rope_append"
+    if k.dim() != 4 or cos.dim() != 2:
+        raise ValueError(f"{fn}: k must be a pool [num_blocks, hkv, block_size, d], cos [n, rot / 2]")
+    nb, hkv, bs, d = k.shape
+    n, half = int(dst.numel()), int(cos.shape[1])
+    width = (hq + 2 * hkv) * d
+    if (qkv.dtype != torch.bfloat16 or tuple(qkv.shape) != (n, width) or not qkv.is_cuda
+            or (n and (qkv.stride(1) != 1 or (n > 1 and qkv.stride(0) < width)))):
+        raise ValueError(f"{fn}: qkv must be a bfloat16 GPU tensor of shape {(n, width)} with contiguous rows, got "
+                         f"{qkv.dtype} {tuple(qkv.shape)}, strides {qkv.stride()}")
+    _expect(fn, "q_weight", q_weight, torch.float32, (d,))
+    _expect(fn, "k_weight", k_weight, torch.float32, (d,))
+    _expect(fn, "cos", cos, torch.float32, (n, half))
+    _expect(fn, "sin", sin, torch.float32, (n, half))
+    _expect(fn, "k", k, torch.bfloat16, k.shape)
+    _expect(fn, "v", v, torch.bfloat16, k.shape)
+    _expect(fn, "dst", dst, torch.int32, dst.shape)
+    _on_device(fn, k.device, qkv=qkv, q_weight=q_weight, k_weight=k_weight, cos=cos, sin=sin, dst=dst, v=v)
+    call = _Call(fn, k.device, stream)
+    q = call.empty((n, hq, d), torch.bfloat16)
+    shape = tkv_shape(hq, hkv, d, bs, nb)
+    call.run(lib().tkv_norm_rope_append, ctypes.byref(shape), n, qkv.data_ptr(), qkv.stride(0) if n > 1 else width,
+             q_weight.data_ptr(), k_weight.data_ptr(), float(eps), cos.data_ptr(), sin.data_ptr(), 2 * half, dst.data_ptr(),
+             q.data_ptr(), k.data_ptr(), v.data_ptr())
     return q
 
 

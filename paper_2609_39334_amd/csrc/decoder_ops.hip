@@ -1,6 +1,7 @@
 // The elementwise steps of a decoder layer between its matrix products, each as one pass over memory:
 //   add_rmsnorm  x += delta, h = RMSNorm(x)          (residual add, norm and the cast for the next product)
 //   rope_append  RoPE of q and k, q packed for attention, k and v written to their pool slots
+//   norm_rope_append  the same with a norm of each query and key head first
 //   swiglu       a = SiLU(gate) * up
 // All are HBM-bound; written as separate tensor operations every one of them read and wrote its operands
 // three to six times, in fp32.  Arithmetic is fp32 throughout, rounded once to bf16 where the result is
@@ -146,6 +147,77 @@ __global__ __launch_bounds__(kThreads) void rope_append(int64_t n_pieces, int hq
     *reinterpret_cast<uint4*>(out + D / 2 + 8 * c) = ob;
 }
 
+// Norm of each query and key head, rotation and append in one pass over qkv.  D / 16 lanes per head, 16 elements
+// each: the lane's two chunks of eight are chunks j and j + rot / 16 where they rotate together (j < rot / 16), and
+// the next two of the rest past it.  The sum of squares is 16 terms in a lane and log2(D / 16) exchanges; the
+// normed values stay in fp32 through the rotation and are rounded once.
+template <int D>
+__global__ __launch_bounds__(kThreads) void norm_rope_append(
+    int64_t n_pieces, int hq, int hkv, int32_t n_slots, int64_t stride, int rot, float eps, const uint16_t* __restrict__ qkv,
+    const float* __restrict__ wq, const float* __restrict__ wk, const float* __restrict__ cosv, const float* __restrict__ sinv,
+    const int32_t* __restrict__ dst, uint16_t* __restrict__ q, uint16_t* __restrict__ kpool, uint16_t* __restrict__ vpool) {
+    constexpr int PPH = D / 16;  // lanes per head
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    if (i >= n_pieces) return;  // (whole heads: kThreads and n_pieces are multiples of PPH)
+    const int64_t row = i / PPH;
+    const int j = static_cast<int>(i - row * PPH);
+    const int heads = hq + 2 * hkv;
+    const int64_t t = row / heads;
+    const int h = static_cast<int>(row - t * heads);
+    uint16_t* out;
+    if (h < hq) {
+        out = q + (t * hq + h) * D;
+    } else {
+        const int32_t slot = dst[t];
+        if (slot < 0 || slot >= n_slots) return;  // no slot: nothing to write
+        const int64_t blk = slot / tkv::kBlock, pos = slot - blk * tkv::kBlock;
+        const int kh = h < hq + hkv ? h - hq : h - hq - hkv;
+        out = (h < hq + hkv ? kpool : vpool) + ((blk * hkv + kh) * tkv::kBlock + pos) * D;
+    }
+    const bool turns = j < rot / 16;
+    const int e0 = turns ? 8 * j : 16 * j, e1 = turns ? e0 + rot / 2 : e0 + 8;
+    const uint16_t* in = qkv + t * stride + static_cast<int64_t>(h) * D;
+    uint4 oa = *reinterpret_cast<const uint4*>(in + e0), ob = *reinterpret_cast<const uint4*>(in + e1);
+    if (h < hq + hkv) {
+        const uint32_t ua[4] = {oa.x, oa.y, oa.z, oa.w}, ub[4] = {ob.x, ob.y, ob.z, ob.w};
+        float a[8], b[8], sq = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            a[2 * e] = lo_f32(ua[e]), a[2 * e + 1] = hi_f32(ua[e]);
+            b[2 * e] = lo_f32(ub[e]), b[2 * e + 1] = hi_f32(ub[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sq += a[e] * a[e] + b[e] * b[e];
+#pragma unroll
+        for (int o = PPH / 2; o > 0; o >>= 1) sq += __shfl_xor(sq, o);
+        const float r = 1.f / sqrtf(sq / static_cast<float>(D) + eps);
+        const float* w = h < hq ? wq : wk;
+        const float4 w0 = *reinterpret_cast<const float4*>(w + e0), w1 = *reinterpret_cast<const float4*>(w + e0 + 4);
+        const float4 w2 = *reinterpret_cast<const float4*>(w + e1), w3 = *reinterpret_cast<const float4*>(w + e1 + 4);
+        const float wa[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+        const float wb[8] = {w2.x, w2.y, w2.z, w2.w, w3.x, w3.y, w3.z, w3.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] = a[e] * r * wa[e], b[e] = b[e] * r * wb[e];
+        if (turns) {
+            const float4* cp = reinterpret_cast<const float4*>(cosv + t * (rot / 2) + e0);
+            const float4* sp = reinterpret_cast<const float4*>(sinv + t * (rot / 2) + e0);
+            const float4 c0 = cp[0], c1 = cp[1], s0 = sp[0], s1 = sp[1];
+            const float cs[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+            const float sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = a[e], y = b[e];
+                a[e] = x * cs[e] - y * sn[e];
+                b[e] = y * cs[e] + x * sn[e];
+            }
+        }
+        oa = uint4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(a[4], a[5]), pack_bf16x2(a[6], a[7])};
+        ob = uint4{pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3]), pack_bf16x2(b[4], b[5]), pack_bf16x2(b[6], b[7])};
+    }
+    *reinterpret_cast<uint4*>(out + e0) = oa;
+    *reinterpret_cast<uint4*>(out + e1) = ob;
+}
+
 // SiLU(g) u = g / (1 + exp(-g)) u.  exp(-g) is 2^n 2^f: g has the 8 significant bits of bf16 and kHi 13, so
 // g kHi is exact, n its nearest integer, and f rounds once.  For negative g the reciprocal is taken of 2^-64 of
 // the sum, so that nothing is flushed while exp(-g) is finite (exp2 and rcp of the plain values gave 0 for
@@ -241,6 +313,19 @@ TKV_EXPORT int tkv_rope_append(const tkv_shape* shape, int32_t n_tok, const void
                        s.hkv, s.num_blocks * s.block_size, static_cast<const uint16_t*>(qkv), cosv, sinv, d_dst,
                        static_cast<uint16_t*>(q), static_cast<uint16_t*>(k), static_cast<uint16_t*>(v));
     return launched("tkv_rope_append");
+}
+
+int tkv::launch_norm_rope_append(const tkv_shape& s, int32_t n_tok, const void* qkv, int64_t stride, const float* wq,
+                                 const float* wk, float eps, const float* cosv, const float* sinv, int32_t rot,
+                                 const int32_t* dst, void* q, void* k, void* v, void* stream) {
+    const int64_t n = static_cast<int64_t>(n_tok) * (static_cast<int64_t>(s.hq) + 2 * static_cast<int64_t>(s.hkv)) * (s.d / 16);
+    const int64_t grid = (n + kThreads - 1) / kThreads;
+    if (grid > kMaxGrid) return tkv::set_error(TKV_EINVAL, "tkv_norm_rope_append: %d tokens are too many", n_tok);
+    const auto kernel = s.d == 128 ? norm_rope_append<128> : norm_rope_append<64>;
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, static_cast<hipStream_t>(stream), n, s.hq,
+                       s.hkv, s.num_blocks * s.block_size, stride, rot, eps, static_cast<const uint16_t*>(qkv), wq, wk, cosv,
+                       sinv, dst, static_cast<uint16_t*>(q), static_cast<uint16_t*>(k), static_cast<uint16_t*>(v));
+    return launched("tkv_norm_rope_append");
 }
 
 TKV_EXPORT int tkv_swiglu(int32_t n_rows, int32_t inter, const void* gu, void* out, void* stream) {

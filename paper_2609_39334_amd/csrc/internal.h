@@ -184,4 +184,11 @@ int launch_attention(const tkv_plan* p, const void* q, const void* k, const void
 int upload(tkv_plan* p, void* d_ws, size_t bytes, void* stream);
 // Waits until the last copy from the plan's host memory has completed (attn.hip).
 void wait_copies(const tkv_plan* p);
+
+// Device halves of entry points whose arguments capi.cpp has checked.  Weak: a host-only build of the library has
+// none, and those entry points then fail with TKV_EHIP after their checks.
+__attribute__((weak)) int launch_norm_rope_append(const tkv_shape& s, int32_t n_tok, const void* qkv, int64_t stride,
+                                                  const float* wq, const float* wk, float eps, const float* cosv,
+                                                  const float* sinv, int32_t rot, const int32_t* dst, void* q, void* k,
+                                                  void* v, void* stream);
 }  // namespace tkv
