@@ -12,6 +12,7 @@
  *   - row coalescing of identical candidates (host, integer);
  *   - a planner that turns per-row block tables into shared segments and a device work list;
  *   - decode (q_len 1) and verify (q_len >= 1, causal within the step) attention on the GPU;
+ *   - attention of drafted token trees over the same cache (GPU);
  *   - the decode loop's other device steps: K/V append that skips deduplicated blocks, and the
  *     branching sampler of computation deduplication (GPU);
  *   - the controller of early pruning and lazy verification (host).
@@ -361,6 +362,49 @@ int tkv_verify_noalloc(const tkv_plan* plan, const void* q, const void* k, const
  * EINVAL (shape, n_tok < 0, NULL pointers when n_tok > 0), EHIP (launch failure). */
 int tkv_kv_append(const tkv_shape* shape, const int32_t* d_dst, int32_t n_tok, const void* k_new, const void* v_new,
                   void* k, void* v, void* hip_stream);
+
+/* ======================================================================== drafted trees
+ * Verification of a small tree of drafted tokens in one pass.  A row's path ends in its L drafted tokens (their
+ * K/V are in the pool: e.g. tkv_bm_extend with seal = 0, then tkv_norm_rope_append); each continues the
+ * context or another drafted token, and sees the context, its drafted ancestors and itself, but not its
+ * siblings' branches.  tkv_verify is the case of a chain. */
+
+/* Who sees whom: parent[i] is the drafted token that token i continues (parent[i] < i), or -1 for the context.
+ *   mask_out  [n][words] (nullable): bit j % 64 of word j / 64 of token i is set iff j is i or an ancestor of i
+ *   depth_out [n] (nullable): number of drafted ancestors, i.e. token i's position is context length + depth
+ * words >= ceil(n / 64) if mask_out is given.  Host-only.  EINVAL. */
+int tkv_draft_mask(int32_t n, const int32_t* parent, int32_t words, uint64_t* mask_out, int32_t* depth_out);
+
+/* Attention of drafted tokens over the paged pool.  For row r with block table T (N keys in path order, the sum of
+ * block_len over T) and L query tokens, token i attends every key at a position below N - L, and the key at
+ * position N - L + j (drafted token j) iff bit j of its mask is set; any mask will do.
+ *   o[i,h] = softmax(q[i,h] . K^T / sqrt(d)) V,   lse[i,h] = natural log of the softmax denominator
+ * with tensors, types and layouts as for tkv_verify (o and lse are written for the rows' tokens, and nothing else
+ * is).  A token that sees no key gets o = 0, lse = -inf.  L = 1 is single-token decode.
+ * There is no host plan: the batch is device data, so a captured call serves later tables, masks and lengths
+ * within the same maxima.  Every row reads its own path; rows that share long prefixes are better served by a plan.
+ *   n_rows, n_qtok   rows, and query tokens (rows of q, o, lse, mask)
+ *   max_q            most query tokens of a row, 1 .. 1024
+ *   n_kv_blocks      entries of kv_blocks;  max_blocks  most blocks of a row, >= 1
+ *   q_indptr         [n_rows + 1] device: row r's tokens are [q_indptr[r], q_indptr[r + 1])
+ *   kv_indptr        [n_rows + 1] device: its table is kv_blocks[kv_indptr[r] .. kv_indptr[r + 1])
+ *   block_len        [num_blocks] device, tokens per block (tkv_bm_block_len)
+ *   mask             [n_qtok][mask_words] device; mask_words >= ceil(max_q / 64); bits past L are not looked at
+ * Device data is checked by the kernels: a row whose tokens are not inside [0, n_qtok) or are more than max_q is
+ * left out (nothing of it is read or written); one whose table is not inside kv_blocks or is longer than max_blocks
+ * gets o = 0 and lse = NaN; an entry that is no block of the pool, or whose block_len is outside [1, 16], counts
+ * as empty.  K/V slots of the row's keys must be finite; slots past a block's length are never read.
+ * d_workspace: tkv_draft_workspace_bytes of the same numbers (0: none needed), 16-byte aligned; calls that may
+ * overlap need their own.  EINVAL (shape as for tkv_plan_create, sizes, NULL pointers, alignment, workspace too
+ * small), EHIP. */
+typedef struct {
+    int32_t n_rows, n_qtok, max_q, n_kv_blocks, max_blocks, mask_words;
+    const int32_t *q_indptr, *kv_indptr, *kv_blocks, *block_len;
+    const uint64_t* mask;
+} tkv_draft_batch;
+int tkv_draft_workspace_bytes(const tkv_shape* shape, const tkv_draft_batch* batch, size_t* bytes_out);
+int tkv_draft_verify(const tkv_shape* shape, const tkv_draft_batch* batch, const void* q, const void* k, const void* v,
+                     void* o, float* lse, void* d_workspace, size_t bytes, void* hip_stream);
 
 /* ======================================================================== decoder layer
  * The elementwise steps between a decoder layer's matrix products, one pass over memory each: fp32

@@ -55,6 +55,11 @@ class tkv_plan_view(ctypes.Structure):
                [(n, ctypes.c_int32) for n in ("n_items", "n_toks", "n_blks", "n_merge", "n_merge_slots", "n_slots")]
 
 
+class tkv_draft_batch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_rows", "n_qtok", "max_q", "n_kv_blocks", "max_blocks", "mask_words")] + \
+               [(n, ctypes.c_void_p) for n in ("q_indptr", "kv_indptr", "kv_blocks", "block_len", "mask")]
+
+
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
 _PI32 = ctypes.POINTER(ctypes.c_int32)
@@ -91,6 +96,11 @@ _SIG = {
     "tkv_verify": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _P]),
     "tkv_verify_noalloc": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _P]),
     "tkv_kv_append": (ctypes.c_int, [ctypes.POINTER(tkv_shape), _P, _I32, _P, _P, _P, _P, _P]),
+    "tkv_draft_mask": (ctypes.c_int, [_I32, _PI32, _I32, _P, _PI32]),
+    "tkv_draft_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(tkv_shape), ctypes.POINTER(tkv_draft_batch),
+                                                 ctypes.POINTER(ctypes.c_size_t)]),
+    "tkv_draft_verify": (ctypes.c_int, [ctypes.POINTER(tkv_shape), ctypes.POINTER(tkv_draft_batch), _P, _P, _P, _P, _P, _P,
+                                        ctypes.c_size_t, _P]),
     "tkv_add_rmsnorm": (ctypes.c_int, [_I32, _I32, ctypes.c_float, _P, _P, _P, _P, _P]),
     "tkv_rope_append": (ctypes.c_int, [ctypes.POINTER(tkv_shape), _I32, _P, _P, _P, _P, _P, _P, _P, _P]),
     "tkv_norm_rope_append": (ctypes.c_int, [ctypes.POINTER(tkv_shape), _I32, _P, ctypes.c_int64, _P, _P, ctypes.c_float, _P, _P,
@@ -528,6 +538,70 @@ def tkv_norm_rope_append(qkv: torch.Tensor, q_weight: torch.Tensor, k_weight: to
              q_weight.data_ptr(), k_weight.data_ptr(), float(eps), cos.data_ptr(), sin.data_ptr(), 2 * half, dst.data_ptr(),
              q.data_ptr(), k.data_ptr(), v.data_ptr())
     return q
+
+
+def tkv_draft_mask(parents, words: Optional[int] = None):
+    """Who sees whom in one row's drafted tree: (mask [n, words] uint64, depth [n] int32) of parents[i] < i (-1: the
+    context).  words defaults to what n tokens need; a batch uses one number for all its rows."""
+    p = _i32(parents)
+    n = len(p)
+    words = -(-n // 64) if words is None else int(words)
+    mask = np.zeros((n, max(0, words)), dtype=np.uint64)
+    depth = np.zeros(n, dtype=np.int32)
+    _check(lib().tkv_draft_mask(n, _ptr(p), words, mask.ctypes.data_as(_P), _ptr(depth)))
+    return mask, depth
+
+
+def tkv_draft_workspace_bytes(shape, n_rows: int, n_qtok: int, max_q: int, n_kv_blocks: int, max_blocks: int,
+                              mask_words: int) -> int:
+    """Workspace of tkv_draft_verify for these numbers; shape = (hq, hkv, d, block_size, num_blocks)."""
+    sh, n = tkv_shape(*[int(x) for x in shape]), ctypes.c_size_t()
+    batch = tkv_draft_batch(n_rows, n_qtok, max_q, n_kv_blocks, max_blocks, mask_words)
+    _check(lib().tkv_draft_workspace_bytes(ctypes.byref(sh), ctypes.byref(batch), ctypes.byref(n)))
+    return n.value
+
+
+def tkv_draft_verify(q_indptr: torch.Tensor, kv_indptr: torch.Tensor, kv_blocks: torch.Tensor, block_len: torch.Tensor,
+                     mask: torch.Tensor, max_q: int, max_blocks: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                     o: torch.Tensor, lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+    """Attention of drafted trees: row r's tokens [q_indptr[r], q_indptr[r + 1]) over its block table
+    kv_blocks[kv_indptr[r] : kv_indptr[r + 1]], whose last keys are the tokens themselves.  mask [n_qtok, words] int64:
+    bit j of token i's words is set where it sees the row's drafted token j (tkv_draft_mask).  All on the GPU; max_q and
+    max_blocks bound a row's tokens and blocks.  A workspace (uint8, tkv_draft_workspace_bytes) is made for the call
+    if none is given."""
+    fn = "tkv_draft_verify"
+    if k.dim() != 4 or q.dim() != 3 or mask.dim() != 2:
+        raise ValueError(f"{fn}: k must be a pool [num_blocks, hkv, block_size, d], q [n, hq, d], mask [n, words]")
+    nb, hkv, bs, d = k.shape
+    n, hq, words = q.shape[0], q.shape[1], mask.shape[1]
+    n_rows, n_kv = q_indptr.numel() - 1, kv_blocks.numel()
+    _expect(fn, "q", q, torch.bfloat16, (n, hq, d))
+    _expect(fn, "k", k, torch.bfloat16, k.shape)
+    _expect(fn, "v", v, torch.bfloat16, k.shape)
+    _expect(fn, "o", o, torch.bfloat16, q.shape)
+    _expect(fn, "q_indptr", q_indptr, torch.int32, (max(0, n_rows) + 1,))
+    _expect(fn, "kv_indptr", kv_indptr, torch.int32, (n_rows + 1,))
+    _expect(fn, "kv_blocks", kv_blocks, torch.int32, (n_kv,))
+    _expect(fn, "block_len", block_len, torch.int32, (nb,))
+    _expect(fn, "mask", mask, torch.int64, (n, words))
+    if lse is not None:
+        _expect(fn, "lse", lse, torch.float32, (n, hq))
+    _on_device(fn, k.device, q=q, v=v, o=o, q_indptr=q_indptr, kv_indptr=kv_indptr, kv_blocks=kv_blocks, block_len=block_len,
+               mask=mask, lse=lse, workspace=workspace)
+    call = _Call(fn, k.device, stream)
+    sh = tkv_shape(hq, hkv, d, bs, nb)
+    batch = tkv_draft_batch(n_rows, n, int(max_q), n_kv, int(max_blocks), words, q_indptr.data_ptr(), kv_indptr.data_ptr(),
+                            kv_blocks.data_ptr(), block_len.data_ptr(), mask.data_ptr())
+    need = ctypes.c_size_t()
+    _check(lib().tkv_draft_workspace_bytes(ctypes.byref(sh), ctypes.byref(batch), ctypes.byref(need)))
+    if workspace is None and need.value:
+        workspace = call.empty((need.value,), torch.uint8)
+    elif workspace is not None and not workspace.is_contiguous():
+        raise ValueError(f"{fn}: workspace must be contiguous")
+    call.run(lib().tkv_draft_verify, ctypes.byref(sh), ctypes.byref(batch), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+             o.data_ptr(), None if lse is None else lse.data_ptr(), None if workspace is None else workspace.data_ptr(),
+             0 if workspace is None else workspace.numel() * workspace.element_size())
 
 
 def tkv_swiglu(gu: torch.Tensor, stream=None) -> torch.Tensor:

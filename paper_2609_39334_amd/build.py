@@ -18,7 +18,7 @@ ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.path.join(ROCM, "bin", "hipcc")
 
 HOST_SOURCES = ["capi.cpp", "bm.cpp", "plan.cpp", "search.cpp"]
-HIP_SOURCES = ["attn.hip", "kv_append.hip", "cd_sample.hip", "decoder_ops.hip"]
+HIP_SOURCES = ["attn.hip", "kv_append.hip", "cd_sample.hip", "decoder_ops.hip", "draft_attn.hip"]
 
 HOST_FLAGS = ["-std=c++17", "-O2", "-fPIC", "-fvisibility=hidden", "-Wall", "-Wextra", "-Wno-unused-parameter"]
 HIP_FLAGS = [
@@ -29,7 +29,7 @@ HIP_FLAGS = [
 ]
 # attention and sampling: masked scores are -inf, guarded where they could meet, and no NaN enters the
 # arithmetic, so the compiler need not quiet the inputs of every max.  (Activations may hold NaN.)
-FILE_FLAGS = {"attn.hip": ["-fno-honor-nans"], "cd_sample.hip": ["-fno-honor-nans"]}
+FILE_FLAGS = {"attn.hip": ["-fno-honor-nans"], "draft_attn.hip": ["-fno-honor-nans"], "cd_sample.hip": ["-fno-honor-nans"]}
 
 
 def _run_all(cmds, verbose):

@@ -72,3 +72,85 @@ TKV_EXPORT int tkv_norm_rope_append(const tkv_shape* shape, int32_t n_tok, const
     return tkv::launch_norm_rope_append(*shape, n_tok, qkv, qkv_stride, q_weight, k_weight, eps, cosv, sinv, rot, d_dst, q, k,
                                         v, stream);
 }
+
+TKV_EXPORT int tkv_draft_mask(int32_t n, const int32_t* parent, int32_t words, uint64_t* mask_out, int32_t* depth_out) {
+    tkv::clear_error();
+    if (n < 0 || (n > 0 && !parent)) return tkv::set_error(TKV_EINVAL, "tkv_draft_mask: n %d, parent %p", n, static_cast<const void*>(parent));
+    if (mask_out && words < (static_cast<int64_t>(n) + 63) / 64)
+        return tkv::set_error(TKV_EINVAL, "tkv_draft_mask: %d words do not hold %d tokens", words, n);
+    for (int32_t i = 0; i < n; ++i)
+        if (parent[i] < -1 || parent[i] >= i)
+            return tkv::set_error(TKV_EINVAL, "tkv_draft_mask: parent[%d] = %d is not an earlier token or -1", i, parent[i]);
+    for (int32_t i = 0; i < n; ++i) {
+        const int32_t p = parent[i];
+        if (mask_out) {
+            uint64_t* row = mask_out + static_cast<size_t>(i) * words;
+            for (int32_t w = 0; w < words; ++w) row[w] = p < 0 ? 0 : mask_out[static_cast<size_t>(p) * words + w];
+            row[i / 64] |= uint64_t{1} << (i % 64);
+        }
+        if (depth_out) depth_out[i] = p < 0 ? 0 : depth_out[p] + 1;
+    }
+    return TKV_OK;
+}
+
+namespace {
+
+constexpr int32_t kMaxDraft = 1024;  // query tokens of a row
+
+int check_draft(const char* fn, const tkv_shape* s, const tkv_draft_batch* b) {
+    if (const int rc = check_pool(fn, s)) return rc;
+    if (s->hq % s->hkv != 0) return tkv::set_error(TKV_EINVAL, "%s: hq (%d) must be a multiple of hkv (%d)", fn, s->hq, s->hkv);
+    if (s->hq / s->hkv > tkv::kTileRows || s->hq > 256)
+        return tkv::set_error(TKV_EINVAL, "%s: hq = %d (up to 256), hq/hkv = %d (up to %d)", fn, s->hq, s->hq / s->hkv, tkv::kTileRows);
+    if (!b) return tkv::set_error(TKV_EINVAL, "%s: batch is NULL", fn);
+    if (b->n_rows < 0 || b->n_qtok < 0 || b->n_kv_blocks < 0)
+        return tkv::set_error(TKV_EINVAL, "%s: n_rows %d, n_qtok %d, n_kv_blocks %d", fn, b->n_rows, b->n_qtok, b->n_kv_blocks);
+    if (b->max_q < 1 || b->max_q > kMaxDraft) return tkv::set_error(TKV_EINVAL, "%s: max_q = %d is not in [1, %d]", fn, b->max_q, kMaxDraft);
+    if (b->max_blocks < 1) return tkv::set_error(TKV_EINVAL, "%s: max_blocks = %d < 1", fn, b->max_blocks);
+    if (b->mask_words < (b->max_q + 63) / 64)
+        return tkv::set_error(TKV_EINVAL, "%s: %d mask words do not hold %d tokens", fn, b->mask_words, b->max_q);
+    return TKV_OK;
+}
+
+tkv::DraftSplit draft_split(const tkv_shape& s, const tkv_draft_batch& b) {
+    tkv::DraftSplit x{};
+    x.waves = 4;
+    x.chunk = 64;
+    const int64_t rows = static_cast<int64_t>(b.max_q) * (s.hq / s.hkv);
+    x.n_tiles = static_cast<int32_t>((rows + 32 * x.waves - 1) / (32 * x.waves));
+    const int64_t longest = b.max_blocks < b.n_kv_blocks ? b.max_blocks : b.n_kv_blocks;
+    x.n_chunks = static_cast<int32_t>(longest > x.chunk ? (longest + x.chunk - 1) / x.chunk : 1);
+    if (x.n_chunks > 1)
+        x.bytes = static_cast<size_t>(x.n_chunks) * static_cast<size_t>(b.n_qtok) * static_cast<size_t>(s.hq) *
+                  (static_cast<size_t>(s.d) + 1) * sizeof(float);
+    return x;
+}
+
+}  // namespace
+
+TKV_EXPORT int tkv_draft_workspace_bytes(const tkv_shape* shape, const tkv_draft_batch* batch, size_t* bytes_out) {
+    const char* fn = "tkv_draft_workspace_bytes";
+    tkv::clear_error();
+    if (!bytes_out) return tkv::set_error(TKV_EINVAL, "%s: bytes_out is NULL", fn);
+    if (const int rc = check_draft(fn, shape, batch)) return rc;
+    *bytes_out = draft_split(*shape, *batch).bytes;
+    return TKV_OK;
+}
+
+TKV_EXPORT int tkv_draft_verify(const tkv_shape* shape, const tkv_draft_batch* batch, const void* q, const void* k,
+                                const void* v, void* o, float* lse, void* d_workspace, size_t bytes, void* stream) {
+    const char* fn = "tkv_draft_verify";
+    tkv::clear_error();
+    if (const int rc = check_draft(fn, shape, batch)) return rc;
+    const tkv_draft_batch& b = *batch;
+    if (b.n_rows == 0 || b.n_qtok == 0) return TKV_OK;
+    if (!b.q_indptr || !b.kv_indptr || !b.block_len || !b.mask || (b.n_kv_blocks > 0 && !b.kv_blocks) || !q || !k || !v || !o)
+        return tkv::set_error(TKV_EINVAL, "%s: NULL pointer", fn);
+    for (const void* p : {q, k, v, static_cast<const void*>(o), static_cast<const void*>(d_workspace)})
+        if (!aligned16(p)) return tkv::set_error(TKV_EINVAL, "%s: tensors must be 16-byte aligned", fn);
+    const tkv::DraftSplit split = draft_split(*shape, b);
+    if (split.bytes > 0 && (!d_workspace || bytes < split.bytes))
+        return tkv::set_error(TKV_EINVAL, "%s: workspace of %zu bytes < %zu needed", fn, d_workspace ? bytes : 0, split.bytes);
+    if (!tkv::launch_draft_verify) return tkv::set_error(TKV_EHIP, "%s: host-only build, no device", fn);
+    return tkv::launch_draft_verify(*shape, b, split, q, k, v, o, lse, d_workspace, stream);
+}

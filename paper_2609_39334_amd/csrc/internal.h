@@ -191,4 +191,14 @@ __attribute__((weak)) int launch_norm_rope_append(const tkv_shape& s, int32_t n_
                                                   const float* wq, const float* wk, float eps, const float* cosv,
                                                   const float* sinv, int32_t rot, const int32_t* dst, void* q, void* k,
                                                   void* v, void* stream);
+
+// How a drafted batch is cut: blocks a chunk, chunks of the longest row, tiles of the widest row, waves of 32 query
+// rows a workgroup, and the workspace that takes.
+struct DraftSplit {
+    int32_t chunk, n_chunks, n_tiles, waves;
+    size_t bytes;
+};
+__attribute__((weak)) int launch_draft_verify(const tkv_shape& s, const tkv_draft_batch& b, const DraftSplit& split,
+                                              const void* q, const void* k, const void* v, void* o, float* lse, void* ws,
+                                              void* stream);
 }  // namespace tkv

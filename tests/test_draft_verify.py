@@ -1,0 +1,407 @@
+"""Attention of drafted token trees against float64.
+
+Bounds.  With weights w (summing to 1) and values v, the kernel's P is rounded to bf16, a relative error of at most
+2^-8 each, and its denominator sums the rounded P, so o moves by at most 2^-8 sum w |v - o| <= 2^-8 (A + |o|) with
+A = sum w |v|.  The scores' fp32 products (d additions of 2^-24 relative to sum |q k| / sqrt(d), under 16 here), the
+exponentials and the fp32 sums add less than 2^-11 of A.  o is then rounded to bf16: 2^-8 |o|.  lse moves by at most
+2^-8 (the rounded P's sum) plus 2^-11.
+"""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_39334_amd as tkv
+
+BS = 16
+
+
+def _blocks(rng, ctx, L, join):
+    """Lengths of a path's blocks: steps of up to 60 tokens, the last block of a step partial; the draft in the last
+    step's blocks (join) or in its own."""
+    steps, left = [], ctx
+    while left > 0:
+        n = min(left, int(rng.integers(1, 61)))
+        steps.append(n)
+        left -= n
+    if join and steps:
+        steps[-1] += L
+    else:
+        steps.append(L)
+    out = []
+    for n in steps:
+        out += [BS] * ((n - 1) // BS) + [(n - 1) % BS + 1]
+    return out
+
+
+class Batch:
+    """Rows (context length, drafted tokens) with random tables; masks of random trees, or random bits."""
+
+    def __init__(self, rows, hq, hkv, d, seed=0, bits=False, spare=3, extra_words=0, scale=1.0):
+        rng = np.random.default_rng(seed)
+        self.hq, self.hkv, self.d = hq, hkv, d
+        lens = [_blocks(rng, c, L, i % 2 == 0) for i, (c, L) in enumerate(rows)]
+        n = sum(len(x) for x in lens)
+        nb = n + spare
+        ids = rng.permutation(nb)[:n]
+        self.block_len = np.zeros(nb, np.int32)
+        self.block_len[ids] = np.concatenate(lens)
+        cut = np.cumsum([0] + [len(x) for x in lens])
+        self.tables = [ids[a:b].astype(np.int32) for a, b in zip(cut[:-1], cut[1:])]
+        self.q_lens = [L for _, L in rows]
+        self.max_q, self.max_blocks = max(self.q_lens), max(len(t) for t in self.tables)
+        words = -(-self.max_q // 64) + extra_words
+        self.masks = []
+        for L in self.q_lens:
+            if bits:
+                self.masks.append(rng.integers(0, 1 << 63, (L, words), dtype=np.uint64) * 2 + rng.integers(0, 2, (L, words), dtype=np.uint64))
+            else:
+                self.masks.append(tkv.tkv_draft_mask([-1] + [int(rng.integers(max(-1, i - 5), i)) for i in range(1, L)], words)[0])
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        rand = lambda *s: (torch.randn(s, generator=g, device="cuda") * scale).bfloat16()
+        self.q, self.k, self.v = rand(sum(self.q_lens), hq, d), rand(nb, hkv, BS, d), rand(nb, hkv, BS, d)
+        dead = torch.arange(BS, device="cuda")[None, :] >= torch.from_numpy(self.block_len).cuda()[:, None]
+        for pool in (self.k, self.v):  # slots past a block's length may hold anything
+            pool.masked_fill_(dead[:, None, :, None], float("nan"))
+        self.upload()
+
+    def upload(self):
+        dev = lambda x: torch.from_numpy(np.ascontiguousarray(x)).cuda()
+        self.dev = {"q_indptr": dev(np.cumsum([0] + self.q_lens).astype(np.int32)),
+                    "kv_indptr": dev(np.cumsum([0] + [len(t) for t in self.tables]).astype(np.int32)),
+                    "kv_blocks": dev(np.concatenate(self.tables)), "block_len": dev(self.block_len),
+                    "mask": dev(np.concatenate(self.masks).view(np.int64))}
+
+    def run(self, with_lse=True, stream=None, workspace=None, **other):
+        o = torch.full_like(self.q, 7.0)
+        z = torch.full(self.q.shape[:2], 7.0, device="cuda") if with_lse else None
+        args = dict(self.dev, max_q=self.max_q, max_blocks=self.max_blocks, q=self.q, k=self.k, v=self.v, o=o, lse=z,
+                    stream=stream, workspace=workspace)
+        args.update(other)
+        tkv.tkv_draft_verify(**args)
+        return o, z
+
+    def reference(self, r):
+        """o, lse and sum w |v| of row r, float64."""
+        t, L = self.tables[r], self.q_lens[r]
+        at = np.concatenate([np.arange(self.block_len[b]) + b * BS for b in t] + [np.zeros(0, np.int64)])
+        at = torch.from_numpy(at.astype(np.int64)).cuda()
+        N, G = len(at), self.hq // self.hkv
+        a = sum(self.q_lens[:r])
+        keys, vals = (p[at // BS, :, at % BS].double().transpose(0, 1) for p in (self.k, self.v))
+        see = np.ones((L, N), bool)
+        for j in range(L):
+            if N - L + j >= 0:
+                see[:, N - L + j] = (self.masks[r][:, j // 64] >> np.uint64(j % 64)) & np.uint64(1)
+        see = torch.from_numpy(see).cuda()
+        q = self.q[a:a + L].double().view(L, self.hkv, G, self.d).permute(1, 2, 0, 3).reshape(self.hkv, G * L, self.d)
+        x = torch.matmul(q, keys.transpose(1, 2).contiguous()).view(self.hkv, G, L, N) / self.d ** 0.5
+        x = x.masked_fill(~see, -float("inf"))
+        z = torch.logsumexp(x, -1) if N else torch.full((self.hkv, G, L), -float("inf"), device="cuda", dtype=torch.float64)
+        w = torch.exp(x - z.clamp(min=-1e300)[..., None]).view(self.hkv, G * L, N)
+        back = lambda y: y.view(self.hkv, G, L, self.d).permute(2, 0, 1, 3).reshape(L, self.hq, self.d)
+        return back(torch.matmul(w, vals)), z.permute(2, 0, 1).reshape(L, self.hq), back(torch.matmul(w, vals.abs()))
+
+    def check(self, o, lse, rows=None):
+        for r in range(len(self.q_lens)) if rows is None else rows:
+            a, L = sum(self.q_lens[:r]), self.q_lens[r]
+            ref, z, A = self.reference(r)
+            bound = 2.0 ** -8 * (A + 2 * ref.abs()) + 2.0 ** -11 * A
+            err = (o[a:a + L].double() - ref).abs()
+            assert torch.all(err <= bound), (r, self.q_lens[r], (err / bound).nan_to_num(9e9).max())
+            if lse is not None:
+                none = z == -float("inf")
+                assert torch.all(lse[a:a + L][none] == -float("inf"))
+                assert torch.all((lse[a:a + L].double() - z)[~none].abs() <= 2.0 ** -8 + 2.0 ** -11)
+
+
+HEADS = [(28, 4, 128), (4, 4, 64), (16, 1, 64), (12, 2, 128), (15, 5, 64), (64, 1, 128), (40, 8, 128), (8, 2, 64)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d", HEADS)
+@pytest.mark.parametrize("L", [1, 2, 7, 16, 33, 64, 65, 130])
+def test_trees_of_one_size(hq, hkv, d, L):
+    b = Batch([(c, L) for c in (0, 1, 15, 16, 17, 100, 700)], hq, hkv, d, seed=L)
+    b.check(*b.run())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d", HEADS[:4])
+def test_ragged_rows_and_any_mask(hq, hkv, d):
+    rng = np.random.default_rng(hq)
+    rows = [(int(rng.integers(0, 900)), int(rng.integers(1, 90))) for _ in range(23)] + [(3000, 3), (0, 1), (0, 70)]
+    for bits in (False, True):
+        b = Batch(rows, hq, hkv, d, seed=hq, bits=bits, extra_words=1)
+        b.check(*b.run())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [[(30000, 1)], [(20000, 40)], [(9000, 9), (10, 1), (0, 2), (17000, 3)], [(4000, 300)]])
+def test_long_contexts(rows):
+    b = Batch(rows, 12, 2, 128, seed=len(rows))
+    o, lse = b.run()
+    b.check(o, lse)
+    again, _ = b.run(with_lse=False)
+    assert torch.equal(o, again)                          # nothing depends on the order of the workgroups
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("L", [1, 5, 100])
+def test_largest_group_and_drafts_past_the_threads(L):
+    b = Batch([(50, L), (2, 1024)], 4, 2, 64, bits=True, seed=L)
+    b.check(*b.run())
+
+
+@pytest.mark.gpu
+def test_peaked_and_equal_scores():
+    # large scores move the softmax base often; equal ones never
+    for scale in (8.0, 0.0):
+        b = Batch([(500, 20), (3, 5)], 8, 2, 64, scale=scale)
+        if scale:
+            b.q /= 4
+        b.v.copy_(torch.where(b.v.isnan(), b.v, torch.randn_like(b.v.float()).bfloat16()))
+        b.check(*b.run())
+
+
+@pytest.mark.gpu
+def test_tokens_that_see_nothing():
+    b = Batch([(0, 9), (0, 1), (5, 3)], 8, 2, 64)
+    for m in b.masks:
+        m[0] = 0
+    b.masks[0][4] = 0
+    b.upload()
+    o, lse = b.run()
+    b.check(o, lse)
+    for t in (0, 4, 9):
+        assert torch.all(o[t] == 0) and torch.all(lse[t] == -float("inf"))
+    assert torch.all(lse[10] > -float("inf"))
+
+
+@pytest.mark.gpu
+def test_a_draft_longer_than_the_path():
+    # the path's keys are then the last drafted tokens; a row without any key sees nothing
+    b = Batch([(0, 40), (0, 40), (60, 2)], 8, 2, 64, bits=True)
+    b.tables[0], b.tables[1] = b.tables[0][1:], b.tables[1][:0]
+    b.upload()
+    o, lse = b.run()
+    b.check(o, lse)
+    assert torch.all(o[40:80] == 0) and torch.all(lse[40:80] == -float("inf"))
+
+
+@pytest.mark.gpu
+def test_as_tkv_verify_and_tkv_decode_on_chains_and_single_tokens():
+    for rows in ([(300, 17), (40, 5), (1000, 1)], [(300, 1), (17, 1)]):
+        b = Batch(rows, 12, 2, 128)
+        for r, L in enumerate(b.q_lens):
+            b.masks[r] = tkv.tkv_draft_mask(list(range(-1, L - 1)), b.masks[r].shape[1])[0]
+        b.upload()
+        o, lse = b.run()
+        plan = tkv.Plan((12, 2, 128, BS, len(b.block_len)), np.cumsum([0] + b.q_lens), np.cumsum([0] + [len(t) for t in b.tables]),
+                        np.concatenate(b.tables), b.block_len)
+        o2, lse2 = torch.empty_like(o), torch.empty_like(lse)
+        plan.verify(b.q, b.k, b.v, o2, lse2)
+        b.check(o, lse)
+        b.check(o2, lse2)
+
+
+@pytest.mark.gpu
+def test_bad_entries_count_as_empty():
+    b = Batch([(200, 20), (90, 3), (1000, 8)], 8, 2, 64)
+    want = b.run()
+    nb = len(b.block_len)
+    free = np.flatnonzero(b.block_len == 0)
+    b.block_len[free[0]], b.block_len[free[1]] = 17, -3
+    bad = np.array([-1, nb, 1 << 30, -(1 << 31), free[0], free[1], free[2]], np.int32)
+    rng = np.random.default_rng(0)
+    for r, t in enumerate(b.tables):
+        for x in np.concatenate([bad] * (1 if r else 60)):
+            t = np.insert(t, rng.integers(0, len(t) + 1), x)
+        b.tables[r] = t.astype(np.int32)
+    b.tables[1] = np.concatenate([b.tables[1], np.full(300, -1, np.int32)])  # the draft is far from the table's end
+    b.max_blocks = max(len(t) for t in b.tables)
+    b.upload()
+    got = b.run()
+    # the same keys in the same order, in other chunks and stages
+    assert torch.all((got[0].float() - want[0].float()).abs() <= 2.0 ** -6 * (1 + want[0].float().abs()))
+    assert torch.all((got[1] - want[1]).abs() <= 2.0 ** -7)
+
+
+@pytest.mark.gpu
+def test_rows_outside_the_arrays():
+    b = Batch([(100, 4), (100, 6), (100, 8), (1500, 5), (90, 3), (90, 2)], 8, 2, 64)
+    want_o, want_lse = b.run()
+    q, kv = b.dev["q_indptr"].clone(), b.dev["kv_indptr"].clone()
+    total = b.dev["kv_blocks"].numel()
+    qi, ki = q.tolist(), kv.tolist()
+    at = lambda r: slice(qi[r], qi[r + 1])
+    # tables: row 3 is longer than max_blocks, the last one runs past the entries
+    kv[-1] = total + 1
+    o, lse = b.run(max_blocks=40, kv_indptr=kv)
+    for r in (3, 5):
+        assert torch.all(o[at(r)] == 0) and torch.all(lse[at(r)].isnan())
+    b.check(o, lse, rows=(0, 1, 2, 4))
+    for bad in ([-5, ki[1]], [ki[2] + 1, ki[2]]):
+        kv = b.dev["kv_indptr"].clone()
+        kv[0], kv[1] = bad
+        o, lse = b.run(kv_indptr=kv)
+        assert torch.all(o[at(0)] == 0) and torch.all(lse[at(0)].isnan())
+        assert torch.equal(o[at(2)], want_o[at(2)])
+    # tokens: rows whose range leaves the tensors, runs backwards or is longer than max_q are left out
+    n = b.q.shape[0]
+    for ptr, kept in (([0, 4, 10, 18, 23, 26, n + 1], [0, 1, 2, 3, 4]), ([-4, 4, 10, 18, 23, 26, n], [1, 2, 3, 4, 5]),
+                      ([0, 4, 3, 18, 23, 26, n], [0, 3, 4, 5]), ([0, 4, 10, 18, 18, 18, n], [0, 1, 2]),
+                      ([0, 4, 10, 1 << 30, -(1 << 31), 26, n], [0, 1, 5])):
+        o, lse = b.run(q_indptr=torch.tensor(ptr, dtype=torch.int32, device="cuda"))
+        seen = torch.zeros(n, dtype=torch.bool, device="cuda")
+        for r in kept:
+            if ptr[r] == qi[r] and ptr[r + 1] == qi[r + 1]:
+                assert torch.equal(o[at(r)], want_o[at(r)])
+            seen[max(0, ptr[r]):max(0, ptr[r + 1])] = True
+        assert torch.all(o[~seen] == 7) and torch.all(lse[~seen] == 7)
+
+
+@pytest.mark.gpu
+def test_fewer_rows_than_tokens():
+    # tokens behind the last row keep their o and lse
+    b = Batch([(50, 4), (60, 9)], 8, 2, 64)
+    o, lse = b.run(q_indptr=b.dev["q_indptr"][:2].clone(), kv_indptr=b.dev["kv_indptr"][:2].clone())
+    b.check(o, lse, rows=(0,))
+    assert torch.all(o[4:] == 7) and torch.all(lse[4:] == 7)
+    o, lse = b.run(q_indptr=torch.zeros(1, dtype=torch.int32, device="cuda"), kv_indptr=torch.zeros(1, dtype=torch.int32, device="cuda"))
+    assert torch.all(o == 7)
+
+
+@pytest.mark.gpu
+def test_the_same_blocks_twice():
+    # a table may hold a block twice, rows may share blocks
+    b = Batch([(100, 4), (200, 4), (50, 2)], 12, 2, 128)
+    b.tables[0] = np.concatenate([b.tables[1][:3], b.tables[1][:3], b.tables[0]])
+    b.tables[2] = b.tables[0][:-1]
+    b.max_blocks = max(len(t) for t in b.tables)
+    b.upload()
+    b.check(*b.run())
+
+
+@pytest.mark.gpu
+def test_pools_past_four_gib():
+    hkv, d, nb = 8, 128, 140_000
+    b = Batch([(200, 5)], 16, hkv, d)
+    big_k = torch.zeros((nb, hkv, BS, d), dtype=torch.bfloat16, device="cuda")
+    big_v = torch.zeros_like(big_k)
+    want = b.run()
+    ids = torch.arange(nb - len(b.block_len), nb, device="cuda")
+    big_k[ids], big_v[ids] = b.k, b.v
+    lens = torch.zeros(nb, dtype=torch.int32, device="cuda")
+    lens[ids] = b.dev["block_len"]
+    got = b.run(k=big_k, v=big_v, block_len=lens, kv_blocks=b.dev["kv_blocks"] + (nb - len(b.block_len)))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.gpu
+def test_replays_with_other_tables_and_other_streams():
+    first = Batch([(700, 9), (30, 4), (2000, 12)], 12, 2, 128, seed=1)
+    second = Batch([(1900, 3), (640, 12), (0, 10)], 12, 2, 128, seed=2)
+    nb, n_kv = max(len(x.block_len) for x in (first, second)), max(x.dev["kv_blocks"].numel() for x in (first, second))
+    dev = {"q_indptr": torch.zeros(4, dtype=torch.int32, device="cuda"), "kv_indptr": torch.zeros(4, dtype=torch.int32, device="cuda"),
+           "kv_blocks": torch.zeros(n_kv, dtype=torch.int32, device="cuda"), "block_len": torch.zeros(nb, dtype=torch.int32, device="cuda"),
+           "mask": torch.zeros((25, 1), dtype=torch.int64, device="cuda")}
+    q, k, v = (torch.zeros(s, dtype=torch.bfloat16, device="cuda") for s in ((25, 12, 128),) + ((nb, 2, BS, 128),) * 2)
+    o, lse = torch.zeros_like(q), torch.zeros((25, 12), device="cuda")
+    maxima = dict(max_q=12, max_blocks=max(x.max_blocks for x in (first, second)))
+
+    def call(stream=None):
+        tkv.tkv_draft_verify(**dev, **maxima, q=q, k=k, v=v, o=o, lse=lse, stream=stream)
+
+    def fill(b):
+        for name, t in dev.items():
+            t[:len(b.dev[name])].copy_(b.dev[name])
+        q.copy_(b.q)
+        k[:len(b.block_len)].copy_(b.k)
+        v[:len(b.block_len)].copy_(b.v)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    side = torch.cuda.Stream()
+    for b in (first, second, first):
+        fill(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        b.check(o, lse)
+        want = o.clone()
+        for stream in (None, side, side.cuda_stream, 0):
+            o.zero_()
+            torch.cuda.synchronize()
+            call(stream)
+            torch.cuda.synchronize()
+            assert torch.equal(o, want)
+
+
+@pytest.mark.gpu
+def test_a_workspace_of_the_callers():
+    b = Batch([(3000, 9)], 8, 2, 64)
+    want = b.run()
+    need = tkv.tkv_draft_workspace_bytes((8, 2, 64, BS, len(b.block_len)), 1, 9, b.max_q, b.dev["kv_blocks"].numel(), b.max_blocks, 1)
+    assert need > 0
+    room = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")
+    got = b.run(workspace=room[:need])
+    assert torch.equal(got[0], want[0]) and torch.all(room[need:] == 255)
+    with pytest.raises(tkv.TkvError, match="workspace"):
+        b.run(workspace=room[:need - 1])
+    with pytest.raises(tkv.TkvError, match="aligned"):
+        b.run(workspace=room[8:need + 8])
+
+
+@pytest.mark.gpu
+def test_tensors_are_checked():
+    b = Batch([(30, 4)], 8, 2, 64)
+    for name, bad in (("q", b.q.float()), ("k", b.k.transpose(1, 2)), ("v", b.v[1:]), ("mask", b.dev["mask"][:, 0]),
+                      ("mask", b.dev["mask"][1:]), ("mask", b.dev["mask"].int()), ("kv_indptr", b.dev["kv_indptr"][1:]),
+                      ("q_indptr", b.dev["q_indptr"].long()), ("kv_blocks", b.dev["kv_blocks"].cpu()), ("block_len", b.dev["block_len"][1:]),
+                      ("q_indptr", b.dev["q_indptr"][:0]), ("lse", torch.zeros(4, 8, device="cuda", dtype=torch.float64)),
+                      ("o", torch.zeros(4, 8, 128, device="cuda", dtype=torch.bfloat16)[:, :, ::2])):
+        with pytest.raises(ValueError):
+            b.run(**{name: bad})
+    for name, bad in (("max_q", 0), ("max_q", 1025), ("max_q", 65), ("max_blocks", 0)):
+        with pytest.raises(tkv.TkvError):
+            b.run(**{name: bad})
+
+
+def test_draft_mask():
+    mask, depth = tkv.tkv_draft_mask([-1, 0, 0, 1, -1, 4, 3])
+    assert mask[:, 0].tolist() == [0b1, 0b11, 0b101, 0b1011, 0b10000, 0b110000, 0b1001011]
+    assert depth.tolist() == [0, 1, 1, 2, 0, 1, 3]
+    mask, depth = tkv.tkv_draft_mask(list(range(-1, 129)), 4)   # a chain
+    assert mask.shape == (130, 4) and depth.tolist() == list(range(130))
+    for i in (0, 63, 64, 127, 128, 129):
+        assert sum(int(w) << (64 * j) for j, w in enumerate(mask[i])) == (1 << (i + 1)) - 1
+    mask, depth = tkv.tkv_draft_mask([])
+    assert mask.shape == (0, 0) and len(depth) == 0
+    for parents, words in (([0], 1), ([-2], 1), ([-1, 2, 0], 1), ([-1] * 65, 1), ([-1], 0), ([-1], -1)):
+        with pytest.raises(tkv.TkvError) as e:
+            tkv.tkv_draft_mask(parents, words)
+        assert e.value.code == tkv.TKV_EINVAL
+
+
+def test_bad_arguments_are_refused():
+    # refused before any device access (no GPU needed)
+    L, one = tkv.lib(), 16
+
+    def call(sh=(8, 2, 64, 16, 4), n_rows=1, n_qtok=4, max_q=4, n_kv=9, max_blocks=9, words=1, ptr=one, q=one, ws=None, size=0):
+        b = tkv.tkv_draft_batch(n_rows, n_qtok, max_q, n_kv, max_blocks, words, ptr, one, one, one, one)
+        return L.tkv_draft_verify(ctypes.byref(tkv.tkv_shape(*sh)), ctypes.byref(b), q, one, one, one, None, ws, size, None)
+
+    for sh in ((8, 2, 96, 16, 4), (8, 2, 64, 32, 4), (0, 2, 64, 16, 4), (8, 0, 64, 16, 4), (8, 3, 64, 16, 4), (130, 2, 64, 16, 4),
+               (260, 130, 64, 16, 4), (8, 2, 64, 16, 1 << 28), (8, 2, 64, 16, 0)):
+        assert call(sh) == tkv.TKV_EINVAL, sh
+    for bad in (dict(n_rows=-1), dict(n_qtok=-1), dict(max_q=0), dict(max_q=1025), dict(n_kv=-1), dict(max_blocks=0), dict(words=0),
+                dict(max_q=65), dict(ptr=None), dict(q=None), dict(q=one + 2), dict(ws=one + 8), dict(n_kv=100000, max_blocks=100000),
+                dict(n_kv=100000, max_blocks=100000, ws=one, size=64)):
+        assert call(**bad) == tkv.TKV_EINVAL, bad
+    assert call(n_rows=0) == tkv.TKV_OK and call(n_qtok=0) == tkv.TKV_OK
+    assert L.tkv_draft_verify(None, None, one, one, one, one, None, None, 0, None) == tkv.TKV_EINVAL
+    with pytest.raises(tkv.TkvError):
+        tkv.tkv_draft_workspace_bytes((8, 3, 64, 16, 4), 1, 1, 1, 1, 1, 1)
+    assert tkv.tkv_draft_workspace_bytes((8, 2, 64, 16, 4), 1, 1, 1, 1, 1, 1) == 0
