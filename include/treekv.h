@@ -14,7 +14,7 @@
  *   - decode (q_len 1) and verify (q_len >= 1, causal within the step) attention on the GPU;
  *   - attention of drafted token trees over the same cache (GPU);
  *   - the decode loop's other device steps: K/V append that skips deduplicated blocks, and the
- *     branching sampler of computation deduplication (GPU);
+ *     branching sampler of computation deduplication, plain or truncated (top-k, top-p, min-p) (GPU);
  *   - the controller of early pruning and lazy verification (host).
  *
  * Conventions
@@ -467,6 +467,30 @@ int tkv_swiglu(int32_t n_rows, int32_t inter, const void* gu, void* out, void* h
 int tkv_cd_sample(int32_t n_rows, int32_t vocab, float temperature, int32_t max_potential, const float* d_logits,
                   const float* d_uniform, const int32_t* d_draw_off, int32_t n_draws, int32_t* d_token,
                   int32_t* d_count, int32_t* d_n_groups, void* hip_stream);
+
+/* The same draws from a truncated distribution, with settings for each row: temperature, top-k, top-p, min-p.
+ * Row r's weights are w_j = exp((l_j - max l) / T); tokens are ordered by logit, equal logits by index (lowest
+ * first).  Kept are: of the first k tokens, the shortest run from the front whose weights reach top_p times
+ * the k tokens' sum, and of those the ones with w_j >= min_p; the first token always.  A draw at uniform u is the first kept
+ * token in token order whose cumulative weight exceeds u times the kept tokens' sum.  Weights, sums and comparisons
+ * are in 64 bits, and results do not depend on the order in which the row is read.
+ *   d_logits       row r at d_logits + r * stride elements (stride >= vocab), fp32 or bf16 (logit_type)
+ *   d_temperature  [n_rows] fp32, >= 0 and finite; 0: the first token alone
+ *   d_top_k        [n_rows] int32, >= 0, nullable; 0 (or NULL): all tokens
+ *   d_top_p        [n_rows] fp32 in [0, 1], nullable; 1 (or NULL): all of them
+ *   d_min_p        [n_rows] fp32 in [0, 1], nullable; 0 (or NULL): all of them
+ * The draws' arguments and outputs are tkv_cd_sample's (vocab <= 2,097,152); in a row's range the entries past its
+ * groups get token -1, count 0.  A row gets d_n_groups -1 for settings outside their ranges, a logit that is NaN
+ * or +inf, or no finite logit, besides tkv_cd_sample's reasons.
+ * d_workspace: tkv_filter_sample_workspace_bytes(n_rows, vocab), 16-byte aligned; calls that may overlap need
+ * their own.  EINVAL, EHIP. */
+enum { TKV_LOGITS_F32 = 0, TKV_LOGITS_BF16 = 1 };
+size_t tkv_filter_sample_workspace_bytes(int32_t n_rows, int32_t vocab);
+int tkv_filter_sample(int32_t n_rows, int32_t vocab, int32_t logit_type, const void* d_logits, int64_t stride,
+                      const float* d_temperature, const int32_t* d_top_k, const float* d_top_p, const float* d_min_p,
+                      int32_t max_potential, const float* d_uniform, const int32_t* d_draw_off, int32_t n_draws,
+                      int32_t* d_token, int32_t* d_count, int32_t* d_n_groups, void* d_workspace, size_t bytes,
+                      void* hip_stream);
 
 /* ======================================================================== search controller
  * Early pruning (Sec. 4.1) and lazy verification (Sec. 4.3) of a speculative beam search whose

@@ -107,6 +107,9 @@ _SIG = {
                                             _I32, _P, _P, _P, _P, _P]),
     "tkv_swiglu": (ctypes.c_int, [_I32, _I32, _P, _P, _P]),
     "tkv_cd_sample": (ctypes.c_int, [_I32, _I32, ctypes.c_float, _I32, _P, _P, _P, _I32, _P, _P, _P, _P]),
+    "tkv_filter_sample_workspace_bytes": (ctypes.c_size_t, [_I32, _I32]),
+    "tkv_filter_sample": (ctypes.c_int, [_I32, _I32, _I32, _P, ctypes.c_int64, _P, _P, _P, _P, _I32, _P, _P, _I32, _P, _P, _P, _P,
+                                         ctypes.c_size_t, _P]),
     "tkv_search_create": (ctypes.c_int, [_I32, _I32, _I32, _I32, ctypes.POINTER(_P)]),
     "tkv_search_destroy": (None, [_P]),
     "tkv_search_expand": (ctypes.c_int, [_P, _I32, _I32, _PI32]),
@@ -633,6 +636,50 @@ def tkv_cd_sample(logits: torch.Tensor, temperature: float, draw_off: torch.Tens
                                uniform.data_ptr(), draw_off.data_ptr(), int(uniform.numel()), tok.data_ptr(),
                                cnt.data_ptr(), ng.data_ptr(), _stream(stream)))
     return tok, cnt, ng[:n_rows]
+
+
+def tkv_filter_sample_workspace_bytes(n_rows: int, vocab: int) -> int:
+    return int(lib().tkv_filter_sample_workspace_bytes(n_rows, vocab))
+
+
+def tkv_filter_sample(logits: torch.Tensor, temperature: torch.Tensor, draw_off: torch.Tensor, uniform: torch.Tensor,
+                      max_potential: int, top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                      min_p: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """tkv_cd_sample's draws from each row's distribution truncated by top-k, top-p and min-p (in this order), with settings
+    for each row: temperature, top_p, min_p [n_rows] fp32, top_k [n_rows] int32 (None: off).  logits [n_rows, vocab] fp32
+    or bf16, rows may be slices of longer ones.  Returns (tokens, counts, n_groups); the entries of a row's range past
+    its groups are -1 and 0.  A workspace (uint8, tkv_filter_sample_workspace_bytes) is made if none is given."""
+    fn = "tkv_filter_sample"
+    if (logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or not logits.is_cuda
+            or (logits.numel() and logits.shape[1] > 1 and logits.stride(1) != 1)
+            or (logits.shape[0] > 1 and logits.stride(0) < logits.shape[1])):
+        raise ValueError(f"{fn}: logits must be a float32 or bfloat16 GPU tensor [n_rows, vocab] with contiguous rows")
+    n_rows, vocab = logits.shape
+    _expect(fn, "temperature", temperature, torch.float32, (n_rows,))
+    _expect(fn, "draw_off", draw_off, torch.int32, (n_rows + 1,))
+    n = int(uniform.numel())
+    _expect(fn, "uniform", uniform, torch.float32, (n,))
+    for name, t, dtype in (("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if t is not None:
+            _expect(fn, name, t, dtype, (n_rows,))
+    _on_device(fn, logits.device, temperature=temperature, draw_off=draw_off, uniform=uniform, top_k=top_k, top_p=top_p,
+               min_p=min_p, workspace=workspace)
+    call = _Call(fn, logits.device, stream)
+    need = tkv_filter_sample_workspace_bytes(n_rows, vocab)
+    if workspace is None and need:
+        workspace = call.empty((need,), torch.uint8)
+    elif workspace is not None and not workspace.is_contiguous():
+        raise ValueError(f"{fn}: workspace must be contiguous")
+    tok, cnt = call.empty((n,), torch.int32), call.empty((n,), torch.int32)
+    ng = call.empty((n_rows,), torch.int32)
+
+    def ptr(t):
+        return None if t is None else t.data_ptr()
+    call.run(lib().tkv_filter_sample, n_rows, vocab, int(logits.dtype == torch.bfloat16), logits.data_ptr(),
+             logits.stride(0) if n_rows > 1 else vocab, temperature.data_ptr(), ptr(top_k), ptr(top_p), ptr(min_p),
+             int(max_potential), uniform.data_ptr(), draw_off.data_ptr(), n, tok.data_ptr(), cnt.data_ptr(), ng.data_ptr(),
+             ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
+    return tok, cnt, ng
 
 
 def tkv_plan_profile(plan: int, max_calls: int) -> None:

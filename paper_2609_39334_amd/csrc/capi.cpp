@@ -154,3 +154,45 @@ TKV_EXPORT int tkv_draft_verify(const tkv_shape* shape, const tkv_draft_batch* b
     if (!tkv::launch_draft_verify) return tkv::set_error(TKV_EHIP, "%s: host-only build, no device", fn);
     return tkv::launch_draft_verify(*shape, b, split, q, k, v, o, lse, d_workspace, stream);
 }
+
+namespace {
+constexpr int32_t kMaxFilterVocab = 1 << 21, kMaxFilterPotential = 1024;
+}
+
+TKV_EXPORT size_t tkv_filter_sample_workspace_bytes(int32_t n_rows, int32_t vocab) {
+    tkv::clear_error();
+    (void)n_rows, (void)vocab;
+    return 0;
+}
+
+TKV_EXPORT int tkv_filter_sample(int32_t n_rows, int32_t vocab, int32_t logit_type, const void* d_logits, int64_t stride,
+                                 const float* d_temperature, const int32_t* d_top_k, const float* d_top_p,
+                                 const float* d_min_p, int32_t max_potential, const float* d_uniform,
+                                 const int32_t* d_draw_off, int32_t n_draws, int32_t* d_token, int32_t* d_count,
+                                 int32_t* d_n_groups, void* d_workspace, size_t bytes, void* stream) {
+    const char* fn = "tkv_filter_sample";
+    tkv::clear_error();
+    if (n_rows < 0 || vocab < 1) return tkv::set_error(TKV_EINVAL, "%s: n_rows %d, vocab %d", fn, n_rows, vocab);
+    if (vocab > kMaxFilterVocab) return tkv::set_error(TKV_EINVAL, "%s: vocabulary %d exceeds %d", fn, vocab, kMaxFilterVocab);
+    if (logit_type != TKV_LOGITS_F32 && logit_type != TKV_LOGITS_BF16)
+        return tkv::set_error(TKV_EINVAL, "%s: logit_type %d", fn, logit_type);
+    if (stride < vocab) return tkv::set_error(TKV_EINVAL, "%s: stride %lld < vocab %d", fn, static_cast<long long>(stride), vocab);
+    if (max_potential < 0 || max_potential > kMaxFilterPotential)
+        return tkv::set_error(TKV_EINVAL, "%s: potential up to %d per row (got %d)", fn, kMaxFilterPotential, max_potential);
+    if (n_draws < 0) return tkv::set_error(TKV_EINVAL, "%s: n_draws = %d < 0", fn, n_draws);
+    if (n_rows == 0) return TKV_OK;
+    if (!d_logits || !d_temperature || !d_draw_off || !d_n_groups || (n_draws > 0 && (!d_uniform || !d_token || !d_count)))
+        return tkv::set_error(TKV_EINVAL, "%s: NULL pointer", fn);
+    const size_t need = tkv_filter_sample_workspace_bytes(n_rows, vocab);
+    if (need > 0 && (!d_workspace || bytes < need))
+        return tkv::set_error(TKV_EINVAL, "%s: workspace of %zu bytes < %zu needed", fn, d_workspace ? bytes : 0, need);
+    if (!aligned16(d_workspace)) return tkv::set_error(TKV_EINVAL, "%s: workspace not 16-byte aligned", fn);
+    if (!tkv::launch_filter_sample) return tkv::set_error(TKV_EHIP, "%s: host-only build, no device", fn);
+    tkv::FilterCall f{};
+    f.n_rows = n_rows, f.vocab = vocab, f.logit_type = logit_type, f.max_potential = max_potential, f.n_draws = n_draws;
+    f.logits = d_logits, f.stride = stride;
+    f.temperature = d_temperature, f.top_k = d_top_k, f.top_p = d_top_p, f.min_p = d_min_p;
+    f.uniform = d_uniform, f.draw_off = d_draw_off;
+    f.token = d_token, f.count = d_count, f.n_groups = d_n_groups, f.workspace = d_workspace;
+    return tkv::launch_filter_sample(f, stream);
+}

@@ -201,4 +201,18 @@ struct DraftSplit {
 __attribute__((weak)) int launch_draft_verify(const tkv_shape& s, const tkv_draft_batch& b, const DraftSplit& split,
                                               const void* q, const void* k, const void* v, void* o, float* lse, void* ws,
                                               void* stream);
+
+// The arguments of tkv_filter_sample.
+struct FilterCall {
+    int32_t n_rows, vocab, logit_type, max_potential, n_draws;
+    const void* logits;
+    int64_t stride;
+    const float *temperature, *top_p, *min_p;
+    const int32_t* top_k;
+    const float* uniform;
+    const int32_t* draw_off;
+    int32_t *token, *count, *n_groups;
+    void* workspace;
+};
+__attribute__((weak)) int launch_filter_sample(const FilterCall& f, void* stream);
 }  // namespace tkv
