@@ -214,5 +214,6 @@ struct FilterCall {
     int32_t *token, *count, *n_groups;
     void* workspace;
 };
+constexpr int kFilterTile = 2048;  // logits that a wave of its first kernel reads
 __attribute__((weak)) int launch_filter_sample(const FilterCall& f, void* stream);
 }  // namespace tkv
