@@ -162,9 +162,7 @@ constexpr int32_t kMaxFilterVocab = 1 << 21, kMaxFilterPotential = 1024;
 TKV_EXPORT size_t tkv_filter_sample_workspace_bytes(int32_t n_rows, int32_t vocab) {
     tkv::clear_error();
     if (n_rows <= 0 || vocab <= 0) return 0;
-    // a weight for every tile, the largest logit of each of its 64 runs
-    const size_t tiles = (static_cast<size_t>(vocab) + tkv::kFilterTile - 1) / tkv::kFilterTile;
-    return static_cast<size_t>(n_rows) * tiles * (sizeof(double) + 64 * sizeof(float));
+    return tkv::filter_layout(n_rows, vocab).bytes;
 }
 
 TKV_EXPORT int tkv_filter_sample(int32_t n_rows, int32_t vocab, int32_t logit_type, const void* d_logits, int64_t stride,

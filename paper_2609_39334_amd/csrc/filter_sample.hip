@@ -7,18 +7,24 @@
 //   top-p   the number at which the sum of the weights from above reaches top_p times the (top-k) total;
 //   min-p   a bound on the weight itself.
 //
-// Two kernels.  filter_scan streams the logits once, a wave per 2,048: the largest logit of every run of 32, and, for
-// rows whose whole weight is asked for (top-p without top-k, or no truncation), the tile's weight relative to its
-// largest.  filter_draw then takes a workgroup a row.  The runs' maxima bound the threshold from below (the k-th
-// largest of them is at most the k-th largest logit), so only the few runs above that bound are read again, their
-// tokens above it sorted, cut and drawn from.  A row whose threshold lies deeper than kList tokens is read again
-// whole: histograms over the numbers, 2,048 bins of the interval that still holds the threshold, with each bin's count
-// and weight, until that interval holds few enough tokens to sort.
+// filter_scan streams the logits once, a wave per 2,048: the largest logit of every run of 32, and, for rows whose
+// whole weight is asked for (top-p without top-k, or no truncation), the tile's weight relative to its largest and
+// a sample of one logit a run.  filter_draw takes a workgroup a row.  The runs' maxima bound the threshold from below
+// (the k-th largest of them is at most the k-th largest logit), so only the few runs above that bound are read
+// again, their tokens above it sorted, cut and drawn from.  For top-p the bound comes from the sample, which tells how
+// much weight lies below a logit to a few per cent.
+// Where top-p or min-p keeps thousands of tokens the row goes through two more kernels, which find nothing to do
+// otherwise: filter_narrow reads it again, a wave a tile, for the weight above the interval that must hold the
+// threshold and the numbers inside it, and filter_finish cuts among those and draws.  A row that slips through (more
+// tokens at the threshold than a list holds, a large top-k, a threshold outside the interval) is read by one
+// workgroup as often as it takes: histograms over the numbers, 2,048 bins of the interval that still holds the
+// threshold, with each bin's count and weight, until that interval holds few enough tokens to sort.
 //
 // Weights are computed in fp64, w = 2^((l - max) log2(e) / T), and summed in a fixed order.  Histogram sums are
 // integers, w in units of 2^-42, so that they do not depend on the order of the atomics; they decide where top-p ends
 // to 2^-43 of the largest weight a token.
 #include <hip/hip_runtime.h>
+#include <algorithm>
 #include <cstdint>
 
 #include "internal.h"
@@ -34,8 +40,9 @@ constexpr int kRun = 32;              // tokens of a lane in a tile
 constexpr int kTile = tkv::kFilterTile;
 static_assert(kTile == 64 * kRun, "a run a lane");
 constexpr int kScanThreads = 256;
-constexpr int kSparseK = 1024;        // largest top-k that is looked for among the runs' maxima
-constexpr int kSparseP = 256;         // runs looked into for top-p
+constexpr int kSparseP = 64;          // fewest runs looked into for top-p
+constexpr int kSparseRuns = 1024;     // and most, past which filter_narrow reads the row
+constexpr int kHist = 1024;           // bins of the runs' maxima and of the sample
 constexpr int kMaxTiles = (1 << kIdxBits) / kTile;
 constexpr int kMaxPotential = 1024;
 constexpr double kUnit = 4398046511104.0;  // 2^42
@@ -53,10 +60,30 @@ struct Args {
     const int32_t* draw_off;
     int32_t n_draws;
     int32_t *token, *count, *n_groups;
-    int32_t tiles;      // a row's
-    float* run_max;     // [n_rows][tiles][64]
-    double* tile_sum;   // [n_rows][tiles]: weight relative to the tile's largest
+    int32_t tiles, cap;   // a row's tiles; numbers its list holds
+    int32_t* n_again;     // rows that are read again, and which
+    struct Again* again;
+    float *run_max, *sample;          // [n_rows][tiles][64]
+    double *tile_sum, *above, *kept;  // [n_rows][tiles]: weight relative to the tile's largest; filter_narrow's
+    uint64_t* lists;                  // [n_rows][cap]
 };
+
+// A row that is read again.  The interval that holds its threshold is bins [first, last] of equal width below the
+// largest logit.
+struct Again {
+    int32_t row, whole_row;  // whole_row: by one workgroup
+    int32_t first, last;
+    float top, scale;
+    double weight;           // of all tokens, if top-p is to be cut
+    uint32_t n;              // numbers inside the interval
+    uint32_t pad[3];
+};
+static_assert(sizeof(Again) == 48, "the workspace's records");
+
+// Bins of equal width from the largest logit down, the last one open.
+__device__ __forceinline__ int bin_of(float v, float top, float scale) {
+    return static_cast<int>(fminf((top - v) * scale, static_cast<float>(kHist - 1)));
+}
 
 // A row's settings and draws.
 struct Settings {
@@ -233,14 +260,17 @@ struct Shared {
             uint64_t list[kList];  // the tokens above the bound
             union {
                 struct {
-                    uint32_t hist[kBins / 2];
-                    int32_t runs[kList];
+                    uint32_t hist[kHist], sampled[kHist];
+                    int32_t runs[kSparseRuns];
                 };
                 double cdf[kList];
             };
             int32_t hits[kList];  // draws of each kept token
         };
-        double tile[kMaxTiles + 1];  // the draws' tile prefixes
+        struct {
+            double tile[kMaxTiles + 1];  // the draws' tile prefixes
+            uint64_t inside[kMaxTiles];  // weight of the kept tokens inside the interval
+        };
     };
     uint64_t part[kWaves];
     double partd[kWaves];
@@ -262,29 +292,42 @@ struct Row {
     __device__ __forceinline__ uint64_t units(float v) const { return static_cast<uint64_t>(weight(v) * kUnit + 0.5); }
 };
 
-// Where a run from above, of numbers in [lo, hi], reaches a target: its last number, and the run's weight.
-struct Cut {
-    uint64_t number, mass;
+// Sources of numbers: a whole row, or a list.
+template <bool BF16>
+struct RowNumbers {
+    Logits<BF16> x;
+    template <class F>
+    __device__ __forceinline__ void each(F f) const {
+        x.each([&](int i, float v) { f(number_of(v, i)); });
+    }
+};
+struct ListNumbers {
+    const uint64_t* p;
+    int n;
+    template <class F>
+    __device__ __forceinline__ void each(F f) const {
+        for (int i = threadIdx.x; i < n; i += kThreads) f(p[i]);
+    }
 };
 
-// BY_MASS: the target is `share` of the whole weight at or above lo (all of it in the first histogram), else a count.
-template <bool BF16, bool BY_MASS>
-__device__ Cut find_cut(Shared& s, const Row<BF16>& row, uint64_t lo, uint64_t hi, uint64_t target, double share) {
+// The last number of the shortest run from above that reaches a target, among a source's numbers in [lo, hi]; lo if all
+// of them do not.  BY_MASS: the target is `want` units of weight, or (SHARE) that share of the whole weight in [lo, hi];
+// else a count.
+template <bool BY_MASS, bool SHARE, class Src, class W>
+__device__ uint64_t find_cut(Shared& s, const Src& src, const W& units, uint64_t lo, uint64_t hi, uint64_t target, double want) {
     const int t = threadIdx.x;
     uint64_t above_c = 0, above_m = 0;
-    double want = static_cast<double>(target);
     const uint64_t floor = lo;
     for (bool first = true;; first = false) {
         const int bits = 64 - __builtin_clzll(hi - lo | 1), shift = bits > 11 ? bits - 11 : 0;
         __syncthreads();
         for (int i = t; i < kBins; i += kThreads) s.h.mass[i] = 0, s.h.cnt[i] = 0;
         __syncthreads();
-        row.x.each([&](int i, float v) {
-            const uint64_t n = number_of(v, i);
+        src.each([&](uint64_t n) {
             if (n < lo || n > hi) return;
             const int b = static_cast<int>((n - lo) >> shift);
             atomicAdd(&s.h.cnt[b], 1u);
-            atomicAdd(reinterpret_cast<unsigned long long*>(&s.h.mass[b]), static_cast<unsigned long long>(row.units(v)));
+            if (BY_MASS) atomicAdd(reinterpret_cast<unsigned long long*>(&s.h.mass[b]), static_cast<unsigned long long>(units(logit_of(n))));
         });
         __syncthreads();
         // thread t takes bins from the top down: kBins - 1 - per t and the next below
@@ -298,7 +341,7 @@ __device__ Cut find_cut(Shared& s, const Row<BF16>& row, uint64_t lo, uint64_t h
         }
         uint64_t before_c = above_c + block_scan(cs, s.part, total_c);
         uint64_t before_m = above_m + block_scan(ms, s.part, total_m);
-        if (BY_MASS && first) want = share * static_cast<double>(total_m);
+        if (SHARE && first) want *= static_cast<double>(total_m);
         if (t == 0) s.i0 = -1;
         __syncthreads();
         uint64_t bc = before_c, bm = before_m;
@@ -316,7 +359,7 @@ __device__ Cut find_cut(Shared& s, const Row<BF16>& row, uint64_t lo, uint64_t h
             bc = ac, bm = am;
         }
         __syncthreads();
-        if (s.i0 < 0) return Cut{floor, above_m + total_m};  // all of it is less than the target
+        if (s.i0 < 0) return floor;  // all of it is less than the target
         const int bin = s.i0, n = s.i1;
         above_c = s.u0, above_m = s.u1;
         lo += static_cast<uint64_t>(bin) << shift;
@@ -326,8 +369,7 @@ __device__ Cut find_cut(Shared& s, const Row<BF16>& row, uint64_t lo, uint64_t h
         __syncthreads();
         if (t == 0) s.i0 = 0;
         __syncthreads();
-        row.x.each([&](int i, float v) {
-            const uint64_t x = number_of(v, i);
+        src.each([&](uint64_t x) {
             if (x >= lo && x <= hi) s.list[atomicAdd(&s.i0, 1)] = x;
         });
         const int size = pow2_at_least(n);
@@ -338,15 +380,10 @@ __device__ Cut find_cut(Shared& s, const Row<BF16>& row, uint64_t lo, uint64_t h
 #pragma unroll
         for (int e = 0; e < many; ++e) {
             const int i = many * t + e;
-            w[e] = 0;
-            if (i < n) {
-                const int idx = (1 << kIdxBits) - 1 - static_cast<int>(s.list[i] & ((1 << kIdxBits) - 1));
-                w[e] = row.units(row.x.at(idx));
-            }
-            mine += w[e];
+            mine += w[e] = BY_MASS && i < n ? units(logit_of(s.list[i])) : 0;
         }
         uint64_t run = above_m + block_scan(mine, s.part, total);
-        if (t == 0) s.u0 = s.list[n - 1], s.u1 = above_m + total;
+        if (t == 0) s.u0 = s.list[n - 1];
         __syncthreads();
 #pragma unroll
         for (int e = 0; e < many; ++e) {
@@ -354,11 +391,11 @@ __device__ Cut find_cut(Shared& s, const Row<BF16>& row, uint64_t lo, uint64_t h
             const uint64_t next = run + w[e];
             const bool reached = BY_MASS ? static_cast<double>(next) >= want : above_c + i + 1 >= target;
             const bool was = BY_MASS ? static_cast<double>(run) >= want : above_c + i >= target;
-            if (i < n && reached && (!was || above_c + i == 0)) s.u0 = s.list[i], s.u1 = next;
+            if (i < n && reached && (!was || above_c + i == 0)) s.u0 = s.list[i];
             run = next;
         }
         __syncthreads();
-        const Cut cut{s.u0, s.u1};
+        const uint64_t cut = s.u0;
         __syncthreads();
         return cut;
     }
@@ -370,6 +407,7 @@ __global__ __launch_bounds__(kScanThreads) void filter_scan(Args a) {
     const int lane = threadIdx.x & 63;
     const int64_t id = static_cast<int64_t>(blockIdx.x) * (kScanThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = static_cast<int>(id / a.tiles), tile = static_cast<int>(id - static_cast<int64_t>(r) * a.tiles);
+    if (id == 0 && lane == 0) *a.n_again = 0;
     if (r >= a.n_rows) return;
     const Settings s = settings_of(a, r);
     if (!s.inside || !s.valid || s.n == 0) return;
@@ -385,6 +423,7 @@ __global__ __launch_bounds__(kScanThreads) void filter_scan(Args a) {
     if (nan) m = INFINITY;
     a.run_max[id * 64 + lane] = m;
     if (!s.whole(a.vocab)) return;
+    if (s.p < 1.f) a.sample[id * 64 + lane] = x[0][0];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
     double sum = 0.;
@@ -430,7 +469,7 @@ __device__ __forceinline__ void write_groups(Shared& s, const Args& a, int r, in
 
 // Draws over the tiles' prefixes in s.tile, one wave a draw: its tile, the lane in it, the token.
 template <bool BF16, class F>
-__device__ __forceinline__ void draw_from_tiles(Shared& s, const Args& a, const Row<BF16>& row, const Settings& set, F kept) {
+__device__ __forceinline__ void draw_from_tiles(Shared& s, const Args& a, int r, const Row<BF16>& row, const Settings& set, F kept) {
     using L = Logits<BF16>;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int tiles = a.tiles;
@@ -478,7 +517,7 @@ __device__ __forceinline__ void draw_from_tiles(Shared& s, const Args& a, const 
         }
     }
     __syncthreads();
-    write_groups(s, a, blockIdx.x, set.off, set.n);
+    write_groups(s, a, r, set.off, set.n);
 }
 
 // s.tile[i + 1] holds tile i's weight: makes it the prefix.
@@ -508,55 +547,99 @@ __device__ __forceinline__ void prefix(double (&v)[per], double* part) {
     for (int e = 0; e < per; ++e) v[e] = run += v[e];
 }
 
-// The row's draws from the tokens above a bound on the runs' maxima; false if they are more than kList, or do not
-// reach the threshold.
+// What is to be looked at of a row: the tokens in bins up to `last`, or (by_bound) those that min-p keeps.
+struct Bound {
+    bool by_bound;
+    int last, first;  // first: the interval's other end, for top-p
+    int runs;         // runs that hold some
+};
+
+// The bound for a row that top-k or top-p cuts.
 template <bool BF16>
-__device__ bool draw_from_runs(Shared& s, const Args& a, const Row<BF16>& row, const Settings& set, const float* rm,
-                               float top, float low, double whole) {
+__device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, const Settings& set, const float* rm, const float* sample,
+                            float top, float scale, double whole) {
+    const int t = threadIdx.x, n_runs = a.tiles * 64;
+    const bool by_k = set.k < a.vocab;
+    const uint32_t want = by_k ? set.k : kSparseP;
+    constexpr int per = kHist / kThreads;
+    for (int i = t; i < kHist; i += kThreads) s.hist[i] = 0, s.sampled[i] = 0;
+    if (t == 0) s.i0 = kHist - 1, s.i1 = -1, s.i2 = kHist - 1;
+    __syncthreads();
+    for (int i = t; i < n_runs; i += kThreads)
+        if (rm[i] > -INFINITY) atomicAdd(&s.hist[bin_of(rm[i], top, scale)], 1u);
+    // (positions past the row hold -inf)
+    if (!by_k)
+        for (int i = t; i < n_runs; i += kThreads)
+            if (sample[i] > -INFINITY) atomicAdd(&s.sampled[bin_of(sample[i], top, scale)], 1u);
+    __syncthreads();
+    uint32_t c[per], sum = 0, total;
+#pragma unroll
+    for (int e = 0; e < per; ++e) sum += c[e] = s.hist[per * t + e];
+    uint32_t run = block_scan(sum, reinterpret_cast<uint32_t*>(s.part), total);
+#pragma unroll
+    for (int e = 0; e < per; ++e) {
+        if (run < want && run + c[e] >= want) s.i0 = per * t + e;
+        run += c[e];
+        s.hist[per * t + e] = run;  // runs up to this bin
+    }
+    if (!by_k) {
+        // From the smallest logit up (thread t takes bins kHist - 1 - per t and the next above): the weight below a
+        // bin's upper edge, estimated from the sample, and its standard error; both by the weight at the bin's middle.
+        const int left = a.vocab - (a.tiles - 1) * kTile;
+        const int n_sampled = (a.tiles - 1) * 64 + min(64, (left + Logits<BF16>::V - 1) / Logits<BF16>::V);
+        const double each = static_cast<double>(a.vocab) / n_sampled, rest = (1. - static_cast<double>(set.p)) * whole;
+        double m[per], v[per], ms = 0., vs = 0., all;
+#pragma unroll
+        for (int e = 0; e < per; ++e) {
+            const int b = kHist - 1 - (per * t + e);
+            const double w = scale > 0.f ? each * exp2_neg(-(b + .5) / static_cast<double>(scale) * row.c) : each;
+            ms += m[e] = w * s.sampled[b];
+            vs += v[e] = w * w * s.sampled[b];
+        }
+        double mrun = block_scan(ms, s.partd, all);
+        double vrun = block_scan(vs, s.partd, all);
+#pragma unroll
+        for (int e = 0; e < per; ++e) {
+            const int b = kHist - 1 - (per * t + e);
+            mrun += m[e], vrun += v[e];
+            const double err = 4. * sqrt(vrun) + 4. * each * exp2_neg(scale > 0.f ? -b / static_cast<double>(scale) * row.c : 0.);
+            if (mrun + err >= rest) atomicMax(&s.i1, b);   // the lowest bin whose top may be past what is left out
+            if (mrun - err <= rest) atomicMin(&s.i2, b);   // the highest bin whose top may not be
+        }
+    }
+    __syncthreads();
+    Bound r{};
+    r.last = s.i0, r.first = 0;
+    if (!by_k) {
+        r.last = max(s.i0, min(s.i1 + 1, kHist - 1));
+        r.first = max(0, s.i2 - 2);
+    }
+    r.runs = s.hist[r.last];
+    __syncthreads();
+    return r;
+}
+
+// The row's draws from the tokens above a bound; false if they are more than kList, or do not reach the threshold.
+template <bool BF16>
+__device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>& row, const Settings& set, const float* rm,
+                               float top, float scale, double whole, const Bound& at_least) {
     using L = Logits<BF16>;
     const int t = threadIdx.x, n_runs = a.tiles * 64;
     const double bound = static_cast<double>(set.min_p);
     const bool by_k = set.k < a.vocab, by_p = set.p < 1.f;
-    const int want = by_k ? set.k : kSparseP;
-    constexpr int kHist = kBins / 2;
-    // bins of equal width from the largest logit down, the last one open; wide enough for what can be drawn
-    const float width = set.temp > 0.f ? fminf(top - low, 100.f * set.temp) : top - low;
-    const float scale = width > 0.f ? fminf((kHist - 1) / width, 1e30f) : 0.f;
-    auto bin = [&](float v) { return static_cast<int>(fminf((top - v) * scale, static_cast<float>(kHist - 1))); };
-    int last = kHist - 1;
-    if (by_k || by_p) {
-        if (by_k && want > kSparseK) return false;
-        for (int i = t; i < kHist; i += kThreads) s.hist[i] = 0;
-        if (t == 0) s.i0 = kHist - 1;
-        __syncthreads();
-        for (int i = t; i < n_runs; i += kThreads)
-            if (rm[i] > -INFINITY) atomicAdd(&s.hist[bin(rm[i])], 1u);
-        __syncthreads();
-        constexpr int per = kHist / kThreads;
-        uint32_t c[per], sum = 0, total;
-#pragma unroll
-        for (int e = 0; e < per; ++e) sum += c[e] = s.hist[per * t + e];
-        uint32_t run = block_scan(sum, reinterpret_cast<uint32_t*>(s.part), total);
-#pragma unroll
-        for (int e = 0; e < per; ++e) {
-            if (run < static_cast<uint32_t>(want) && run + c[e] >= static_cast<uint32_t>(want)) s.i0 = per * t + e;
-            run += c[e];
-        }
-        __syncthreads();
-        last = s.i0;
-    }
-    auto above = [&](float v) { return v > -INFINITY && (by_k || by_p ? bin(v) <= last : row.weight(v) >= bound); };
-    __syncthreads();
+    auto above = [&](float v) {
+        return v > -INFINITY && (at_least.by_bound ? row.weight(v) >= bound : bin_of(v, top, scale) <= at_least.last);
+    };
     if (t == 0) s.i1 = s.i2 = 0;
     __syncthreads();
     for (int i = t; i < n_runs; i += kThreads)
         if (above(rm[i])) {
             const int at = atomicAdd(&s.i1, 1);
-            if (at < kList) s.runs[at] = i;
+            if (at < kSparseRuns) s.runs[at] = i;
         }
     __syncthreads();
     const int runs = s.i1;
-    if (runs > kList) return false;
+    if (runs > kSparseRuns) return false;
     for (int i = t; i < runs * L::kPieces; i += kThreads) {
         const int run = s.runs[i / L::kPieces];
         const int first = L::token(run / 64 * kTile, run % 64, i % L::kPieces);
@@ -590,7 +673,7 @@ __device__ bool draw_from_runs(Shared& s, const Args& a, const Row<BF16>& row, c
     __syncthreads();
     if (by_p) {
         const double total = by_k ? s.cdf[kList - 1] : whole, target = static_cast<double>(set.p) * total;
-        if (!by_k && s.cdf[n - 1] < target) return false;
+        if (!by_k && !at_least.by_bound && s.cdf[n - 1] < target) return false;
 #pragma unroll
         for (int e = 0; e < per; ++e) {
             const int i = per * t + e;
@@ -655,7 +738,7 @@ __device__ bool draw_from_runs(Shared& s, const Args& a, const Row<BF16>& row, c
             ++at;
         }
     }
-    if (t == 0) a.n_groups[blockIdx.x] = static_cast<int32_t>(groups);
+    if (t == 0) a.n_groups[r] = static_cast<int32_t>(groups);
     return true;
 }
 
@@ -676,12 +759,14 @@ __global__ __launch_bounds__(kThreads) void filter_draw(Args a) {
     const float* rm = a.run_max + static_cast<int64_t>(r) * a.tiles * 64;
     const double* ts = a.tile_sum + static_cast<int64_t>(r) * a.tiles;
 
-    // the largest logit, and the smallest of the runs' largest
+    // the largest logit, and the smallest that is looked at below: of the runs' largest, or of the sample
+    const bool by_k = set.k < a.vocab, by_p = set.p < 1.f;
+    const float* sample = a.sample + static_cast<int64_t>(r) * a.tiles * 64;
     float top = -INFINITY, low = INFINITY;
     for (int i = t; i < a.tiles * 64; i += kThreads) {
-        const float v = rm[i];
+        const float v = rm[i], u = by_p && !by_k ? sample[i] : v;
         top = fmaxf(top, v);
-        low = fminf(low, v == -INFINITY ? INFINITY : v);
+        low = fminf(low, u == -INFINITY ? INFINITY : u);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o)), low = fminf(low, __shfl_xor(low, o));
@@ -708,23 +793,98 @@ __global__ __launch_bounds__(kThreads) void filter_draw(Args a) {
         tile_prefixes(s, a.tiles);
         whole = s.tile[a.tiles];
         if (set.p >= 1.f) {
-            draw_from_tiles<BF16>(s, a, row, set, [&](int, float v) { return row.weight(v); });
+            draw_from_tiles<BF16>(s, a, r, row, set, [&](int, float v) { return row.weight(v); });
             return;
         }
         __syncthreads();
     }
-    if (draw_from_runs<BF16>(s, a, row, set, rm, top, low, whole)) return;
-
-    const uint64_t lo = static_cast<uint64_t>(key_of(-3.4028234663852886e38f)) << kIdxBits;
-    const uint64_t hi = number_of(top, 0);
-    uint64_t cut = 0;
-    if (set.k < a.vocab) cut = find_cut<BF16, false>(s, row, lo, hi, static_cast<uint64_t>(set.k), 0.).number;
-    if (set.p < 1.f) cut = find_cut<BF16, true>(s, row, cut > lo ? cut : lo, hi, 0, static_cast<double>(set.p)).number;
+    // bins wide enough for what can be drawn
+    const float width = set.temp > 0.f ? fminf(top - low, 100.f * set.temp) : top - low;
+    const float scale = width > 0.f ? fminf((kHist - 1) / width, 1e30f) : 0.f;
     const double bound = static_cast<double>(set.min_p);
-    auto kept = [&](int i, float v) {
-        const double x = row.weight(v);
-        return number_of(v, i) >= cut && x >= bound ? x : 0.;
-    };
+    // min-p alone, or the narrower of the two, if few runs reach it
+    Bound at_least{true, -1, kHist, 0};
+    if (!by_k && bound > 0.) {
+        if (t == 0) s.i0 = 0;
+        __syncthreads();
+        int mine = 0;
+        for (int i = t; i < a.tiles * 64; i += kThreads) mine += row.weight(rm[i]) >= bound;
+        if (mine) atomicAdd(&s.i0, mine);
+        __syncthreads();
+        at_least.runs = s.i0;
+        __syncthreads();
+    }
+    if (by_k || (by_p && (bound <= 0. || at_least.runs > kSparseRuns)))
+        at_least = find_bound<BF16>(s, a, row, set, rm, sample, top, scale, whole);
+    if (at_least.runs <= kSparseRuns && draw_from_runs<BF16>(s, a, r, row, set, rm, top, scale, whole, at_least)) return;
+    if (t == 0) {
+        Again again{};
+        again.row = r;
+        again.whole_row = by_k || at_least.runs <= kSparseRuns || a.cap == 0;
+        again.first = at_least.first, again.last = at_least.last;
+        again.top = top, again.scale = scale, again.weight = whole;
+        a.again[atomicAdd(a.n_again, 1)] = again;
+    }
+}
+
+// A wave a tile of the rows that are read again: the weight above the interval, of what min-p keeps of it, and the
+// numbers inside.
+template <bool BF16>
+__global__ __launch_bounds__(kScanThreads) void filter_narrow(Args a) {
+    using L = Logits<BF16>;
+    const int lane = threadIdx.x & 63;
+    const int64_t items = static_cast<int64_t>(*a.n_again) * a.tiles;
+    const int waves = gridDim.x * (kScanThreads / 64);
+    for (int64_t id = blockIdx.x * (kScanThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); id < items; id += waves) {
+        const int d = static_cast<int>(id / a.tiles), tile = static_cast<int>(id - static_cast<int64_t>(d) * a.tiles);
+        const Again g = a.again[d];
+        if (g.whole_row) continue;
+        const Settings set = settings_of(a, g.row);
+        const Row<BF16> row{{static_cast<const char*>(a.logits) + g.row * a.stride * (BF16 ? 2 : 4), a.vocab},
+                            static_cast<double>(g.top), set.scale()};
+        const double bound = static_cast<double>(set.min_p);
+        float x[L::kPieces][L::V];
+        row.x.run(tile * kTile, lane, x);
+        double above = 0., kept = 0.;
+        uint32_t in = 0;
+#pragma unroll
+        for (int j = 0; j < L::kPieces; ++j)
+#pragma unroll
+            for (int e = 0; e < L::V; ++e) {
+                const int b = bin_of(x[j][e], g.top, g.scale);
+                if (b < g.first) {
+                    const double y = row.weight(x[j][e]);
+                    above += y;
+                    kept += y >= bound ? y : 0.;
+                } else if (b <= g.last && x[j][e] > -INFINITY) {
+                    in |= 1u << (j * L::V + e);
+                }
+            }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) above += __shfl_xor(above, o), kept += __shfl_xor(kept, o);
+        const int64_t at = static_cast<int64_t>(g.row) * a.tiles + tile;
+        if (lane == 0) a.above[at] = above, a.kept[at] = kept;
+        const int mine = __builtin_popcount(in), incl = wave_scan(mine, lane);
+        uint32_t base = 0;
+        if (lane == 63 && incl > 0) base = atomicAdd(&a.again[d].n, static_cast<uint32_t>(incl));
+        base = __shfl(base, 63) + incl - mine;
+        uint64_t* list = a.lists + static_cast<int64_t>(g.row) * a.cap;
+#pragma unroll
+        for (int j = 0; j < L::kPieces; ++j)
+#pragma unroll
+            for (int e = 0; e < L::V; ++e)
+                if (in >> (j * L::V + e) & 1) {
+                    if (base < static_cast<uint32_t>(a.cap)) list[base] = number_of(x[j][e], L::token(tile * kTile, lane, j) + e);
+                    ++base;
+                }
+    }
+}
+
+// The kept weight of a row's tiles, read whole by the workgroup.
+template <bool BF16, class F>
+__device__ __forceinline__ void sum_tiles(Shared& s, const Args& a, const Row<BF16>& row, F kept) {
+    using L = Logits<BF16>;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     __syncthreads();
     for (int i = w; i < a.tiles; i += kWaves) {
         float x[L::kPieces][L::V];
@@ -738,8 +898,94 @@ __global__ __launch_bounds__(kThreads) void filter_draw(Args a) {
         for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
         if (lane == 0) s.tile[i + 1] = sum;
     }
-    tile_prefixes(s, a.tiles);
-    draw_from_tiles<BF16>(s, a, row, set, kept);
+}
+
+// The threshold of a row that filter_narrow has read; false if it is not in the row's list.  s.tile then holds the
+// tiles' kept weights.
+template <bool BF16>
+__device__ bool cut_in_list(Shared& s, const Args& a, const Row<BF16>& row, const Settings& set, const Again& g, uint64_t& cut) {
+    const int t = threadIdx.x;
+    const int64_t at = static_cast<int64_t>(g.row) * a.tiles;
+    const double bound = static_cast<double>(set.min_p);
+    cut = 0;
+    if (set.p < 1.f) {
+        if (g.n > static_cast<uint32_t>(a.cap)) return false;
+        const ListNumbers list{a.lists + static_cast<int64_t>(g.row) * a.cap, static_cast<int>(g.n)};
+        double sum = 0., above;
+        for (int i = t; i < a.tiles; i += kThreads) sum += a.above[at + i];
+        block_scan(sum, s.partd, above);
+        const double want = static_cast<double>(set.p) * g.weight - above;
+        // the list's weight in units, and its smallest and largest number
+        uint64_t units = 0, all, lo = ~uint64_t{0}, hi = 0;
+        list.each([&](uint64_t n) {
+            units += row.units(logit_of(n));
+            lo = n < lo ? n : lo, hi = n > hi ? n : hi;
+        });
+        block_scan(units, s.part, all);
+        if (!(want > 0.) || static_cast<double>(all) < want * kUnit) return false;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            const uint64_t l2 = __shfl_xor(lo, o), h2 = __shfl_xor(hi, o);
+            lo = l2 < lo ? l2 : lo, hi = h2 > hi ? h2 : hi;
+        }
+        __syncthreads();
+        if (t == 0) s.u0 = ~uint64_t{0}, s.u1 = 0;
+        __syncthreads();
+        if ((t & 63) == 0) {
+            atomicMin(reinterpret_cast<unsigned long long*>(&s.u0), static_cast<unsigned long long>(lo));
+            atomicMax(reinterpret_cast<unsigned long long*>(&s.u1), static_cast<unsigned long long>(hi));
+        }
+        __syncthreads();
+        lo = s.u0, hi = s.u1;
+        cut = find_cut<true, false>(s, list, [&](float v) { return row.units(v); }, lo, hi, 0, want * kUnit);
+        // kept tokens of the list, by tile: integers, whatever their order (at most 4,096 of a weight up to 1)
+        constexpr double kFine = 1125899906842624.0;  // 2^50
+        __syncthreads();
+        for (int i = t; i < a.tiles; i += kThreads) s.inside[i] = 0;
+        __syncthreads();
+        list.each([&](uint64_t n) {
+            const double y = row.weight(logit_of(n));
+            if (n < cut || y < bound) return;
+            const int i = (1 << kIdxBits) - 1 - static_cast<int>(n & ((1 << kIdxBits) - 1));
+            atomicAdd(reinterpret_cast<unsigned long long*>(&s.inside[i / kTile]), static_cast<unsigned long long>(y * kFine + .5));
+        });
+        __syncthreads();
+        for (int i = t; i < a.tiles; i += kThreads) s.tile[i + 1] = a.kept[at + i] + static_cast<double>(s.inside[i]) / kFine;
+    } else {
+        for (int i = t; i < a.tiles; i += kThreads) s.tile[i + 1] = a.kept[at + i];
+    }
+    return true;
+}
+
+// Cuts and draws of the rows that are read again, a workgroup a row.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void filter_finish(Args a) {
+    __shared__ Shared s;
+    for (int d = blockIdx.x; d < *a.n_again; d += gridDim.x) {
+        __syncthreads();
+        const Again g = a.again[d];
+        const Settings set = settings_of(a, g.row);
+        const Row<BF16> row{{static_cast<const char*>(a.logits) + g.row * a.stride * (BF16 ? 2 : 4), a.vocab},
+                            static_cast<double>(g.top), set.scale()};
+        const double bound = static_cast<double>(set.min_p);
+        uint64_t cut = 0;
+        auto kept = [&](int i, float v) {
+            const double x = row.weight(v);
+            return number_of(v, i) >= cut && x >= bound ? x : 0.;
+        };
+        if (g.whole_row || !cut_in_list<BF16>(s, a, row, set, g, cut)) {
+            const RowNumbers<BF16> all{row.x};
+            auto units = [&](float v) { return row.units(v); };
+            const uint64_t lo = static_cast<uint64_t>(key_of(-3.4028234663852886e38f)) << kIdxBits;
+            const uint64_t hi = number_of(g.top, 0);
+            cut = 0;
+            if (set.k < a.vocab) cut = find_cut<false, false>(s, all, units, lo, hi, static_cast<uint64_t>(set.k), 0.);
+            if (set.p < 1.f) cut = find_cut<true, true>(s, all, units, cut > lo ? cut : lo, hi, 0, static_cast<double>(set.p));
+            sum_tiles<BF16>(s, a, row, kept);
+        }
+        tile_prefixes(s, a.tiles);
+        draw_from_tiles<BF16>(s, a, g.row, row, set, kept);
+    }
 }
 
 }  // namespace
@@ -750,21 +996,31 @@ int tkv::launch_filter_sample(const FilterCall& f, void* stream) {
     a.temperature = f.temperature, a.top_k = f.top_k, a.top_p = f.top_p, a.min_p = f.min_p;
     a.uniform = f.uniform, a.draw_off = f.draw_off, a.n_draws = f.n_draws;
     a.token = f.token, a.count = f.count, a.n_groups = f.n_groups;
-    a.tiles = (f.vocab + kTile - 1) / kTile;
-    a.tile_sum = static_cast<double*>(f.workspace);
-    a.run_max = reinterpret_cast<float*>(a.tile_sum + static_cast<int64_t>(f.n_rows) * a.tiles);
+    const FilterLayout l = filter_layout(f.n_rows, f.vocab);
+    uint8_t* ws = static_cast<uint8_t*>(f.workspace);
+    a.tiles = l.tiles, a.cap = l.list;
+    a.n_again = reinterpret_cast<int32_t*>(ws);
+    a.again = reinterpret_cast<Again*>(ws + l.rows);
+    a.tile_sum = reinterpret_cast<double*>(ws + l.tile_sum);
+    a.above = reinterpret_cast<double*>(ws + l.above);
+    a.kept = reinterpret_cast<double*>(ws + l.kept);
+    a.run_max = reinterpret_cast<float*>(ws + l.run_max);
+    a.sample = reinterpret_cast<float*>(ws + l.sample);
+    a.lists = reinterpret_cast<uint64_t*>(ws + l.lists);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     constexpr int waves = kScanThreads / 64;
     const int64_t grid = (static_cast<int64_t>(f.n_rows) * a.tiles + waves - 1) / waves;
     if (grid > INT32_MAX) return set_error(TKV_EINVAL, "tkv_filter_sample: %d rows are too many", f.n_rows);
-    const auto launch = [&](auto scan, auto draw) {
+    const auto launch = [&](auto scan, auto draw, auto narrow, auto finish) {
         scan<<<dim3(static_cast<unsigned>(grid)), dim3(kScanThreads), 0, st>>>(a);
         draw<<<dim3(static_cast<unsigned>(f.n_rows)), dim3(kThreads), 0, st>>>(a);
+        narrow<<<dim3(static_cast<unsigned>(std::min<int64_t>(grid, 2048))), dim3(kScanThreads), 0, st>>>(a);
+        finish<<<dim3(static_cast<unsigned>(std::min(f.n_rows, 1024))), dim3(kThreads), 0, st>>>(a);
     };
     if (f.logit_type == TKV_LOGITS_BF16)
-        launch(filter_scan<true>, filter_draw<true>);
+        launch(filter_scan<true>, filter_draw<true>, filter_narrow<true>, filter_finish<true>);
     else
-        launch(filter_scan<false>, filter_draw<false>);
+        launch(filter_scan<false>, filter_draw<false>, filter_narrow<false>, filter_finish<false>);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? TKV_OK : set_error(TKV_EHIP, "tkv_filter_sample launch: %s", hipGetErrorString(e));
 }
