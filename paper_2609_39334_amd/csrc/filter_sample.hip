@@ -63,7 +63,8 @@ struct Args {
     int32_t tiles, cap;   // a row's tiles; numbers its list holds
     int32_t* n_again;     // rows that are read again, and which
     struct Again* again;
-    float *run_max, *sample;          // [n_rows][tiles][64]
+    float2* tile_max;                 // [n_rows][tiles]: the largest logit, the smallest that filter_draw's bins are to hold
+    float *run_max, *sample;          // [n_rows][tiles][64], sample: two of them
     double *tile_sum, *above, *kept;  // [n_rows][tiles]: weight relative to the tile's largest; filter_narrow's
     uint64_t* lists;                  // [n_rows][cap]
 };
@@ -234,17 +235,30 @@ __device__ __forceinline__ T block_scan(T v, T* part, T& total) {
     return before + incl - v;
 }
 
-// Bitonic sort of n (a power of two) numbers, descending.
+// Orders a wave's LDS accesses (they run in program order: this only keeps the compiler from moving them).
+__device__ __forceinline__ void lanes_agree() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Bitonic sort of n (a power of two) numbers, descending.  Where pairs are at most 64 apart a wave works on 128
+// numbers of its own, and its lanes need no barrier between steps.
 template <class T>
 __device__ __forceinline__ void sort_down(T* a, int n) {
+    __syncthreads();
     for (int k = 2; k <= n; k <<= 1)
         for (int j = k >> 1; j > 0; j >>= 1) {
-            __syncthreads();
             for (int t = threadIdx.x; t < n / 2; t += kThreads) {
-                const int i = 2 * j * (t / j) + t % j, p = i + j;
+                const int i = 2 * (t & ~(j - 1)) + (t & (j - 1)), p = i + j;
                 const T x = a[i], y = a[p];
                 if ((x < y) == ((i & k) == 0)) a[i] = y, a[p] = x;
             }
+            // the next step's pairs are j / 2 apart, or k after the last
+            if (j > 64 || (j == 1 && k > 64))
+                __syncthreads();
+            else
+                lanes_agree();
         }
     __syncthreads();
 }
@@ -422,10 +436,15 @@ __global__ __launch_bounds__(kScanThreads) void filter_scan(Args a) {
         for (int e = 0; e < Logits<BF16>::V; ++e) m = fmaxf(m, x[j][e]), nan |= x[j][e] != x[j][e];
     if (nan) m = INFINITY;
     a.run_max[id * 64 + lane] = m;
-    if (!s.whole(a.vocab)) return;
-    if (s.p < 1.f) a.sample[id * 64 + lane] = x[0][0];
+    const bool whole = s.whole(a.vocab), samples = whole && s.p < 1.f;
+    const float s0 = x[0][0], s1 = x[Logits<BF16>::kPieces / 2][0];
+    if (samples) a.sample[id * 128 + lane] = s0, a.sample[id * 128 + 64 + lane] = s1;
+    const auto finite = [](float v) { return v == -INFINITY ? INFINITY : v; };
+    float low = samples ? fminf(finite(s0), finite(s1)) : finite(m);
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o)), low = fminf(low, __shfl_xor(low, o));
+    if (lane == 0) a.tile_max[id] = make_float2(m, low);
+    if (!whole) return;
     double sum = 0.;
     if (m > -INFINITY && m < INFINITY) {
         const double base = m, c = s.scale();
@@ -547,6 +566,19 @@ __device__ __forceinline__ void prefix(double (&v)[per], double* part) {
     for (int e = 0; e < per; ++e) v[e] = run += v[e];
 }
 
+// f(i, p[i]) for i < n, eight loads ahead.
+template <class F>
+__device__ __forceinline__ void each_of(const float* p, int n, F f) {
+    for (int i0 = threadIdx.x; i0 < n; i0 += 8 * kThreads) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = p[min(i0 + e * kThreads, n - 1)];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (i0 + e * kThreads < n) f(i0 + e * kThreads, v[e]);
+    }
+}
+
 // What is to be looked at of a row: the tokens in bins up to `last`, or (by_bound) those that min-p keeps.
 struct Bound {
     bool by_bound;
@@ -563,14 +595,16 @@ __device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, cons
     const uint32_t want = by_k ? set.k : kSparseP;
     constexpr int per = kHist / kThreads;
     for (int i = t; i < kHist; i += kThreads) s.hist[i] = 0, s.sampled[i] = 0;
-    if (t == 0) s.i0 = kHist - 1, s.i1 = -1, s.i2 = kHist - 1;
+    if (t == 0) s.i0 = kHist - 1, s.i1 = s.i2 = -1;
     __syncthreads();
-    for (int i = t; i < n_runs; i += kThreads)
-        if (rm[i] > -INFINITY) atomicAdd(&s.hist[bin_of(rm[i], top, scale)], 1u);
+    each_of(rm, n_runs, [&](int, float v) {
+        if (v > -INFINITY) atomicAdd(&s.hist[bin_of(v, top, scale)], 1u);
+    });
     // (positions past the row hold -inf)
     if (!by_k)
-        for (int i = t; i < n_runs; i += kThreads)
-            if (sample[i] > -INFINITY) atomicAdd(&s.sampled[bin_of(sample[i], top, scale)], 1u);
+        each_of(sample, 2 * n_runs, [&](int, float v) {
+            if (v > -INFINITY) atomicAdd(&s.sampled[bin_of(v, top, scale)], 1u);
+        });
     __syncthreads();
     uint32_t c[per], sum = 0, total;
 #pragma unroll
@@ -585,17 +619,22 @@ __device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, cons
     if (!by_k) {
         // From the smallest logit up (thread t takes bins kHist - 1 - per t and the next above): the weight below a
         // bin's upper edge, estimated from the sample, and its standard error; both by the weight at the bin's middle.
+        // The largest of them may be wide off (few tokens, much weight): what matters is where it passes `rest`.
+        constexpr int V = Logits<BF16>::V;
         const int left = a.vocab - (a.tiles - 1) * kTile;
-        const int n_sampled = (a.tiles - 1) * 64 + min(64, (left + Logits<BF16>::V - 1) / Logits<BF16>::V);
+        const int n_sampled = (a.tiles - 1) * 128 + min(64, (left + V - 1) / V) + max(0, min(64, (left - kTile / 2 + V - 1) / V));
         const double each = static_cast<double>(a.vocab) / n_sampled, rest = (1. - static_cast<double>(set.p)) * whole;
         double m[per], v[per], ms = 0., vs = 0., all;
+        uint32_t cs = 0, every;
 #pragma unroll
         for (int e = 0; e < per; ++e) {
             const int b = kHist - 1 - (per * t + e);
             const double w = scale > 0.f ? each * exp2_neg(-(b + .5) / static_cast<double>(scale) * row.c) : each;
             ms += m[e] = w * s.sampled[b];
             vs += v[e] = w * w * s.sampled[b];
+            cs += c[e] = s.sampled[b];
         }
+        uint32_t crun = block_scan(cs, reinterpret_cast<uint32_t*>(s.part), every);
         double mrun = block_scan(ms, s.partd, all);
         double vrun = block_scan(vs, s.partd, all);
 #pragma unroll
@@ -603,8 +642,10 @@ __device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, cons
             const int b = kHist - 1 - (per * t + e);
             mrun += m[e], vrun += v[e];
             const double err = 4. * sqrt(vrun) + 4. * each * exp2_neg(scale > 0.f ? -b / static_cast<double>(scale) * row.c : 0.);
-            if (mrun + err >= rest) atomicMax(&s.i1, b);   // the lowest bin whose top may be past what is left out
-            if (mrun - err <= rest) atomicMin(&s.i2, b);   // the highest bin whose top may not be
+            if (mrun + err >= rest) atomicMax(&s.i1, b);  // the last bin that may hold the threshold: past it there is too little
+            if (mrun - err > rest) atomicMax(&s.i2, b);   // the first: from it on there is too much
+            s.sampled[b] = every - crun;                  // samples in bins above
+            crun += c[e];
         }
     }
     __syncthreads();
@@ -612,9 +653,11 @@ __device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, cons
     r.last = s.i0, r.first = 0;
     if (!by_k) {
         r.last = max(s.i0, min(s.i1 + 1, kHist - 1));
-        r.first = max(0, s.i2 - 2);
+        r.first = max(0, s.i2 - 1);
     }
     r.runs = s.hist[r.last];
+    // (twice the sample's estimate has to fit the list)
+    if (!by_k && r.last + 1 < kHist && 64 * static_cast<int64_t>(s.sampled[r.last]) / 2 > kList / 2) r.runs = kSparseRuns + 1;
     __syncthreads();
     return r;
 }
@@ -632,25 +675,34 @@ __device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>&
     };
     if (t == 0) s.i1 = s.i2 = 0;
     __syncthreads();
-    for (int i = t; i < n_runs; i += kThreads)
-        if (above(rm[i])) {
+    each_of(rm, n_runs, [&](int i, float v) {
+        if (above(v)) {
             const int at = atomicAdd(&s.i1, 1);
             if (at < kSparseRuns) s.runs[at] = i;
         }
+    });
     __syncthreads();
     const int runs = s.i1;
     if (runs > kSparseRuns) return false;
-    for (int i = t; i < runs * L::kPieces; i += kThreads) {
-        const int run = s.runs[i / L::kPieces];
-        const int first = L::token(run / 64 * kTile, run % 64, i % L::kPieces);
-        float x[L::V];
-        row.x.piece(first, x);
+    constexpr int kAhead = 4;
+    for (int i0 = t; i0 < runs * L::kPieces; i0 += kAhead * kThreads) {
+        float x[kAhead][L::V];
+        int first[kAhead];
 #pragma unroll
-        for (int e = 0; e < L::V; ++e)
-            if (above(x[e])) {
-                const int at = atomicAdd(&s.i2, 1);
-                if (at < kList) s.list[at] = number_of(x[e], first + e);
-            }
+        for (int q = 0; q < kAhead; ++q) {
+            const int i = min(i0 + q * kThreads, runs * L::kPieces - 1);
+            const int run = s.runs[i / L::kPieces];
+            first[q] = L::token(run / 64 * kTile, run % 64, i % L::kPieces);
+            row.x.piece(first[q], x[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+#pragma unroll
+            for (int e = 0; e < L::V; ++e)
+                if (i0 + q * kThreads < runs * L::kPieces && above(x[q][e])) {
+                    const int at = atomicAdd(&s.i2, 1);
+                    if (at < kList) s.list[at] = number_of(x[q][e], first[q] + e);
+                }
     }
     __syncthreads();
     const int n = s.i2;
@@ -759,14 +811,14 @@ __global__ __launch_bounds__(kThreads) void filter_draw(Args a) {
     const float* rm = a.run_max + static_cast<int64_t>(r) * a.tiles * 64;
     const double* ts = a.tile_sum + static_cast<int64_t>(r) * a.tiles;
 
-    // the largest logit, and the smallest that is looked at below: of the runs' largest, or of the sample
+    // the largest logit, the smallest for the bins below, and the tiles' weights relative to the row's largest
     const bool by_k = set.k < a.vocab, by_p = set.p < 1.f;
-    const float* sample = a.sample + static_cast<int64_t>(r) * a.tiles * 64;
+    const float* sample = a.sample + static_cast<int64_t>(r) * a.tiles * 128;
+    const float2* tm = a.tile_max + static_cast<int64_t>(r) * a.tiles;
     float top = -INFINITY, low = INFINITY;
-    for (int i = t; i < a.tiles * 64; i += kThreads) {
-        const float v = rm[i], u = by_p && !by_k ? sample[i] : v;
-        top = fmaxf(top, v);
-        low = fminf(low, u == -INFINITY ? INFINITY : u);
+    for (int i = t; i < a.tiles; i += kThreads) {
+        const float2 v = tm[i];
+        top = fmaxf(top, v.x), low = fminf(low, v.y);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o)), low = fminf(low, __shfl_xor(low, o));
@@ -780,19 +832,12 @@ __global__ __launch_bounds__(kThreads) void filter_draw(Args a) {
     }
     __syncthreads();
     row.top = top;
-
     double whole = 0.;
     if (set.whole(a.vocab)) {
-        // the tiles' weights, relative to the row's largest
-        for (int i = w; i < a.tiles; i += kWaves) {
-            float m = rm[i * 64 + lane];
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-            if (lane == 0) s.tile[i + 1] = m > -INFINITY ? ts[i] * row.weight(m) : 0.;
-        }
+        for (int i = t; i < a.tiles; i += kThreads) s.tile[i + 1] = ts[i] * row.weight(tm[i].x);
         tile_prefixes(s, a.tiles);
         whole = s.tile[a.tiles];
-        if (set.p >= 1.f) {
+        if (!by_p) {
             draw_from_tiles<BF16>(s, a, r, row, set, [&](int, float v) { return row.weight(v); });
             return;
         }
@@ -802,25 +847,27 @@ __global__ __launch_bounds__(kThreads) void filter_draw(Args a) {
     const float width = set.temp > 0.f ? fminf(top - low, 100.f * set.temp) : top - low;
     const float scale = width > 0.f ? fminf((kHist - 1) / width, 1e30f) : 0.f;
     const double bound = static_cast<double>(set.min_p);
-    // min-p alone, or the narrower of the two, if few runs reach it
+    // min-p alone, or before top-p, if few runs reach it
     Bound at_least{true, -1, kHist, 0};
     if (!by_k && bound > 0.) {
         if (t == 0) s.i0 = 0;
         __syncthreads();
         int mine = 0;
-        for (int i = t; i < a.tiles * 64; i += kThreads) mine += row.weight(rm[i]) >= bound;
+        each_of(rm, a.tiles * 64, [&](int, float v) { mine += row.weight(v) >= bound; });
         if (mine) atomicAdd(&s.i0, mine);
         __syncthreads();
         at_least.runs = s.i0;
         __syncthreads();
+        if (at_least.runs <= kSparseRuns && draw_from_runs<BF16>(s, a, r, row, set, rm, top, scale, whole, at_least)) return;
     }
-    if (by_k || (by_p && (bound <= 0. || at_least.runs > kSparseRuns)))
+    if (by_k || by_p) {
         at_least = find_bound<BF16>(s, a, row, set, rm, sample, top, scale, whole);
-    if (at_least.runs <= kSparseRuns && draw_from_runs<BF16>(s, a, r, row, set, rm, top, scale, whole, at_least)) return;
+        if (at_least.runs <= kSparseRuns && draw_from_runs<BF16>(s, a, r, row, set, rm, top, scale, whole, at_least)) return;
+    }
     if (t == 0) {
         Again again{};
         again.row = r;
-        again.whole_row = by_k || at_least.runs <= kSparseRuns || a.cap == 0;
+        again.whole_row = by_k || a.cap == 0;
         again.first = at_least.first, again.last = at_least.last;
         again.top = top, again.scale = scale, again.weight = whole;
         a.again[atomicAdd(a.n_again, 1)] = again;
@@ -938,7 +985,7 @@ __device__ bool cut_in_list(Shared& s, const Args& a, const Row<BF16>& row, cons
         __syncthreads();
         lo = s.u0, hi = s.u1;
         cut = find_cut<true, false>(s, list, [&](float v) { return row.units(v); }, lo, hi, 0, want * kUnit);
-        // kept tokens of the list, by tile: integers, whatever their order (at most 4,096 of a weight up to 1)
+        // kept tokens of the list, by tile: integers, whatever their order (at most 8,192 of a weight up to 1)
         constexpr double kFine = 1125899906842624.0;  // 2^50
         __syncthreads();
         for (int i = t; i < a.tiles; i += kThreads) s.inside[i] = 0;
@@ -1004,6 +1051,7 @@ int tkv::launch_filter_sample(const FilterCall& f, void* stream) {
     a.tile_sum = reinterpret_cast<double*>(ws + l.tile_sum);
     a.above = reinterpret_cast<double*>(ws + l.above);
     a.kept = reinterpret_cast<double*>(ws + l.kept);
+    a.tile_max = reinterpret_cast<float2*>(ws + l.tile_max);
     a.run_max = reinterpret_cast<float*>(ws + l.run_max);
     a.sample = reinterpret_cast<float*>(ws + l.sample);
     a.lists = reinterpret_cast<uint64_t*>(ws + l.lists);

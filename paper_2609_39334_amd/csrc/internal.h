@@ -218,13 +218,13 @@ struct FilterCall {
 constexpr int kFilterTile = 2048;  // logits that a wave of its first kernel reads
 struct FilterLayout {
     int32_t tiles, list;  // a row's tiles; entries of its list of tokens near the threshold
-    size_t rows, tile_sum, above, kept, run_max, sample, lists, bytes;
+    size_t rows, tile_sum, above, kept, tile_max, run_max, sample, lists, bytes;
 };
 inline FilterLayout filter_layout(int32_t n_rows, int32_t vocab) {
     const size_t n = static_cast<size_t>(n_rows);
     FilterLayout l{};
     l.tiles = static_cast<int32_t>((static_cast<int64_t>(vocab) + kFilterTile - 1) / kFilterTile);
-    l.list = vocab <= kFilterTile ? 0 : vocab <= 8 * 512 ? 512 : vocab < 8 * 4096 ? vocab / 8 : 4096;
+    l.list = vocab <= kFilterTile ? 0 : vocab <= 6 * 1024 ? 1024 : vocab < 6 * 8192 ? vocab / 6 : 8192;
     size_t at = 16;  // the number of rows that are read again
     const auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -235,8 +235,9 @@ inline FilterLayout filter_layout(int32_t n_rows, int32_t vocab) {
     l.tile_sum = take(n * l.tiles * sizeof(double));
     l.above = take(n * l.tiles * sizeof(double));
     l.kept = take(n * l.tiles * sizeof(double));
+    l.tile_max = take(n * l.tiles * 2 * sizeof(float));
     l.run_max = take(n * l.tiles * 64 * sizeof(float));
-    l.sample = take(n * l.tiles * 64 * sizeof(float));
+    l.sample = take(n * l.tiles * 128 * sizeof(float));
     l.lists = take(n * static_cast<size_t>(l.list) * sizeof(uint64_t));
     l.bytes = at;
     return l;
