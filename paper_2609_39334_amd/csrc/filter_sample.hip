@@ -242,10 +242,34 @@ __device__ __forceinline__ void lanes_agree() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Bitonic sort of n (a power of two) numbers, descending.  Where pairs are at most 64 apart a wave works on 128
-// numbers of its own, and its lanes need no barrier between steps.
+__device__ __forceinline__ int pow2_at_least(int n) { return n <= 1 ? 1 : 1 << (32 - __builtin_clz(n - 1)); }
+
+// Sorts n numbers (of which 0 is none), descending; room for the next power of two.  Up to one a thread, each counts
+// those before its own: 64 numbers take 0.5 us, 4 us as a bitonic sort.  More are sorted bitonically: where pairs are
+// at most 64 apart a wave works on 128 numbers of its own, and its lanes need no barrier between steps.
 template <class T>
 __device__ __forceinline__ void sort_down(T* a, int n) {
+    const int size = pow2_at_least(n);
+    for (int i = n + threadIdx.x; i < size; i += kThreads) a[i] = 0;
+    if (n <= kThreads) {
+        __syncthreads();
+        const int t = threadIdx.x;
+        T mine = 0;
+        int rank = 0;
+        if (t < n) {
+            mine = a[t];
+            for (int i = 0; i < n; i += 4) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (i + e < size) rank += a[i + e] > mine || (a[i + e] == mine && i + e < t);
+            }
+        }
+        __syncthreads();
+        if (t < n) a[rank] = mine;
+        __syncthreads();
+        return;
+    }
+    n = size;
     __syncthreads();
     for (int k = 2; k <= n; k <<= 1)
         for (int j = k >> 1; j > 0; j >>= 1) {
@@ -262,7 +286,6 @@ __device__ __forceinline__ void sort_down(T* a, int n) {
         }
     __syncthreads();
 }
-__device__ __forceinline__ int pow2_at_least(int n) { return n <= 1 ? 1 : 1 << (32 - __builtin_clz(n - 1)); }
 
 struct Shared {
     union {
@@ -386,9 +409,7 @@ __device__ uint64_t find_cut(Shared& s, const Src& src, const W& units, uint64_t
         src.each([&](uint64_t x) {
             if (x >= lo && x <= hi) s.list[atomicAdd(&s.i0, 1)] = x;
         });
-        const int size = pow2_at_least(n);
-        for (int i = n + t; i < size; i += kThreads) s.list[i] = 0;
-        sort_down(s.list, size);
+        sort_down(s.list, n);
         constexpr int many = kList / kThreads;
         uint64_t mine = 0, total, w[many];
 #pragma unroll
@@ -461,9 +482,7 @@ __global__ __launch_bounds__(kScanThreads) void filter_scan(Args a) {
 // The groups of n draws, sorted in s.draw (complements of tokens).
 __device__ __forceinline__ void write_groups(Shared& s, const Args& a, int r, int off, int n) {
     const int t = threadIdx.x;
-    const int size = pow2_at_least(n);
-    for (int i = n + t; i < size; i += kThreads) s.draw[i] = 0;
-    sort_down(s.draw, size);
+    sort_down(s.draw, n);
     constexpr int per = kMaxPotential / kThreads;
     uint64_t firsts = 0, groups;
     bool is[per];
@@ -517,23 +536,15 @@ __device__ __forceinline__ void draw_from_tiles(Shared& s, const Args& a, int r,
         const uint64_t has = __builtin_amdgcn_ballot_w64(sum > 0.);
         const uint64_t past = has & __builtin_amdgcn_ballot_w64(incl > target);
         const int who = past ? __builtin_ctzll(past) : has ? 63 - __builtin_clzll(has) : 0;
-        if (lane == who) {
-            double acc = incl - sum;
-            int pick = -1, last = 0;
-#pragma unroll
-            for (int j = 0; j < L::kPieces; ++j)
-#pragma unroll
-                for (int q = 0; q < L::V; ++q) {
-                    const int i = first + j * L::V + q;
-                    const double y = kept(i, x[j][q]);
-                    acc += y;
-                    if (y > 0.) {
-                        last = i;
-                        if (pick < 0 && acc > target) pick = i;
-                    }
-                }
-            s.draw[d] = ~static_cast<uint32_t>(pick >= 0 ? pick : last);
-        }
+        // that lane's tokens, one a lane
+        static_assert(kRun == 32, "half a wave");
+        const int i = b * kTile + who * kRun + (lane & 31);
+        const double y = lane < kRun && i < a.vocab ? kept(i, row.x.at(i)) : 0.;
+        const double acc = __shfl(incl - sum, who) + wave_scan(y, lane);
+        const uint64_t some = __builtin_amdgcn_ballot_w64(y > 0.);
+        const uint64_t over = some & __builtin_amdgcn_ballot_w64(acc > target);
+        const int pick = over ? __builtin_ctzll(over) : some ? 63 - __builtin_clzll(some) : 0;
+        if (lane == 0) s.draw[d] = ~static_cast<uint32_t>(b * kTile + who * kRun + pick);
     }
     __syncthreads();
     write_groups(s, a, r, set.off, set.n);
@@ -579,12 +590,17 @@ __device__ __forceinline__ void each_of(const float* p, int n, F f) {
     }
 }
 
-// What is to be looked at of a row: the tokens in bins up to `last`, or (by_bound) those that min-p keeps.
+// What is to be looked at of a row: the tokens from a logit up.
 struct Bound {
-    bool by_bound;
-    int last, first;  // first: the interval's other end, for top-p
-    int runs;         // runs that hold some
+    float low;
+    bool min_p;       // all that min-p keeps are among them, wherever top-p ends
+    int first, last;  // the bins that may hold the threshold
+    int runs;         // runs that hold some of the tokens
 };
+// A logit in or below a bin, by a little (all for the last bin).
+__device__ __forceinline__ float foot_of(int bin, float top, float scale) {
+    return bin >= kHist - 1 || scale == 0.f ? -3.4028234663852886e38f : top - (bin + 1.01f) / scale;
+}
 
 // The bound for a row that top-k or top-p cuts.
 template <bool BF16>
@@ -656,6 +672,7 @@ __device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, cons
         r.first = max(0, s.i2 - 1);
     }
     r.runs = s.hist[r.last];
+    r.low = foot_of(r.last, top, scale);
     // (twice the sample's estimate has to fit the list)
     if (!by_k && r.last + 1 < kHist && 64 * static_cast<int64_t>(s.sampled[r.last]) / 2 > kList / 2) r.runs = kSparseRuns + 1;
     __syncthreads();
@@ -665,18 +682,16 @@ __device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, cons
 // The row's draws from the tokens above a bound; false if they are more than kList, or do not reach the threshold.
 template <bool BF16>
 __device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>& row, const Settings& set, const float* rm,
-                               float top, float scale, double whole, const Bound& at_least) {
+                               double whole, const Bound& at_least) {
     using L = Logits<BF16>;
     const int t = threadIdx.x, n_runs = a.tiles * 64;
     const double bound = static_cast<double>(set.min_p);
     const bool by_k = set.k < a.vocab, by_p = set.p < 1.f;
-    auto above = [&](float v) {
-        return v > -INFINITY && (at_least.by_bound ? row.weight(v) >= bound : bin_of(v, top, scale) <= at_least.last);
-    };
+    const float low = at_least.low;
     if (t == 0) s.i1 = s.i2 = 0;
     __syncthreads();
     each_of(rm, n_runs, [&](int i, float v) {
-        if (above(v)) {
+        if (v >= low) {
             const int at = atomicAdd(&s.i1, 1);
             if (at < kSparseRuns) s.runs[at] = i;
         }
@@ -699,7 +714,7 @@ __device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>&
         for (int q = 0; q < kAhead; ++q)
 #pragma unroll
             for (int e = 0; e < L::V; ++e)
-                if (i0 + q * kThreads < runs * L::kPieces && above(x[q][e])) {
+                if (i0 + q * kThreads < runs * L::kPieces && x[q][e] >= low) {
                     const int at = atomicAdd(&s.i2, 1);
                     if (at < kList) s.list[at] = number_of(x[q][e], first[q] + e);
                 }
@@ -707,8 +722,7 @@ __device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>&
     __syncthreads();
     const int n = s.i2;
     if (n > kList) return false;
-    for (int i = n + t; i < pow2_at_least(n); i += kThreads) s.list[i] = 0;
-    sort_down(s.list, pow2_at_least(n));
+    sort_down(s.list, n);
     // weights from above, and where they are cut
     constexpr int per = kList / kThreads;
     double w[per], sum[per];
@@ -725,7 +739,7 @@ __device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>&
     __syncthreads();
     if (by_p) {
         const double total = by_k ? s.cdf[kList - 1] : whole, target = static_cast<double>(set.p) * total;
-        if (!by_k && !at_least.by_bound && s.cdf[n - 1] < target) return false;
+        if (!by_k && !at_least.min_p && s.cdf[n - 1] < target) return false;
 #pragma unroll
         for (int e = 0; e < per; ++e) {
             const int i = per * t + e;
@@ -745,12 +759,11 @@ __device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>&
         keep = s.i0;
     }
     // the kept tokens in token order, their prefixes, the draws' places among them
-    const int size = pow2_at_least(keep);
-    for (int i = t; i < size; i += kThreads) {
-        const uint64_t x = i < keep ? s.list[i] : 0;  // (complemented index above the logit's key)
-        s.list[i] = i < keep ? (x & ((1 << kIdxBits) - 1)) << 32 | x >> kIdxBits : 0;
+    for (int i = t; i < keep; i += kThreads) {
+        const uint64_t x = s.list[i];  // (complemented index above the logit's key)
+        s.list[i] = (x & ((1 << kIdxBits) - 1)) << 32 | x >> kIdxBits;
     }
-    sort_down(s.list, size);
+    sort_down(s.list, keep);
 #pragma unroll
     for (int e = 0; e < per; ++e) {
         const int i = per * t + e;
@@ -848,21 +861,24 @@ __global__ __launch_bounds__(kThreads) void filter_draw(Args a) {
     const float scale = width > 0.f ? fminf((kHist - 1) / width, 1e30f) : 0.f;
     const double bound = static_cast<double>(set.min_p);
     // min-p alone, or before top-p, if few runs reach it
-    Bound at_least{true, -1, kHist, 0};
+    Bound at_least{0.f, true, kHist, -1, 0};
     if (!by_k && bound > 0.) {
+        // (by a little, and to the next float below)
+        const double foot = row.top + (log2(bound) - 1e-6) / row.c;
+        at_least.low = foot > -3.4e38 ? __double2float_rd(foot) : -3.4028234663852886e38f;
         if (t == 0) s.i0 = 0;
         __syncthreads();
         int mine = 0;
-        each_of(rm, a.tiles * 64, [&](int, float v) { mine += row.weight(v) >= bound; });
+        each_of(rm, a.tiles * 64, [&](int, float v) { mine += v >= at_least.low; });
         if (mine) atomicAdd(&s.i0, mine);
         __syncthreads();
         at_least.runs = s.i0;
         __syncthreads();
-        if (at_least.runs <= kSparseRuns && draw_from_runs<BF16>(s, a, r, row, set, rm, top, scale, whole, at_least)) return;
+        if (at_least.runs <= kSparseRuns && draw_from_runs<BF16>(s, a, r, row, set, rm, whole, at_least)) return;
     }
     if (by_k || by_p) {
         at_least = find_bound<BF16>(s, a, row, set, rm, sample, top, scale, whole);
-        if (at_least.runs <= kSparseRuns && draw_from_runs<BF16>(s, a, r, row, set, rm, top, scale, whole, at_least)) return;
+        if (at_least.runs <= kSparseRuns && draw_from_runs<BF16>(s, a, r, row, set, rm, whole, at_least)) return;
     }
     if (t == 0) {
         Again again{};
