@@ -235,56 +235,93 @@ __device__ __forceinline__ T block_scan(T v, T* part, T& total) {
     return before + incl - v;
 }
 
-// Orders a wave's LDS accesses (they run in program order: this only keeps the compiler from moving them).
-__device__ __forceinline__ void lanes_agree() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+// v of the lane whose index differs in one bit.
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v, int bit) { return static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), bit)); }
+__device__ __forceinline__ uint64_t lane_xor(uint64_t v, int bit) {
+    return static_cast<uint64_t>(lane_xor(static_cast<uint32_t>(v >> 32), bit)) << 32 | lane_xor(static_cast<uint32_t>(v), bit);
 }
 
-__device__ __forceinline__ int pow2_at_least(int n) { return n <= 1 ? 1 : 1 << (32 - __builtin_clz(n - 1)); }
+// Bitonic sort of E * kThreads numbers, descending, in registers: number e * kThreads + t is thread t's.  Pairs within a
+// wave go over the lanes, pairs within a thread stay, the rest go through LDS.
+template <int E, class T>
+__device__ __forceinline__ void sort_registers(T* a) {
+    const int t = threadIdx.x;
+    T x[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = a[e * kThreads + t];
+#pragma unroll 1
+    for (int k = 2; k <= E * kThreads; k <<= 1) {
+        int j = k >> 1;
+#pragma unroll
+        for (int d = E / 2; d > 0; d >>= 1)
+            if (j == d * kThreads) {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if ((e & d) == 0) {
+                        const bool down = ((e * kThreads + t) & k) == 0;
+                        const T p = x[e], q = x[e + d];
+                        if ((p < q) == down) x[e] = q, x[e + d] = p;
+                    }
+                j >>= 1;
+            }
+#pragma unroll 1
+        for (; j >= 64; j >>= 1) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < E; ++e) a[e * kThreads + t] = x[e];
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const T y = a[e * kThreads + (t ^ j)];
+                const bool larger = ((t & j) == 0) == (((e * kThreads + t) & k) == 0);
+                x[e] = (x[e] < y) == larger ? y : x[e];
+            }
+        }
+#pragma unroll 1
+        for (; j > 0; j >>= 1) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const T y = lane_xor(x[e], j);
+                const bool larger = ((t & j) == 0) == (((e * kThreads + t) & k) == 0);
+                x[e] = (x[e] < y) == larger ? y : x[e];
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e) a[e * kThreads + t] = x[e];
+    __syncthreads();
+}
 
-// Sorts n numbers (of which 0 is none), descending; room for the next power of two.  Up to one a thread, each counts
-// those before its own: 64 numbers take 0.5 us, 4 us as a bitonic sort.  More are sorted bitonically: where pairs are
-// at most 64 apart a wave works on 128 numbers of its own, and its lanes need no barrier between steps.
+// Sorts n numbers (0 is none), descending; a has room for the next multiple of kThreads.  Few are counted: each
+// thread those before its own.
 template <class T>
 __device__ __forceinline__ void sort_down(T* a, int n) {
-    const int size = pow2_at_least(n);
-    for (int i = n + threadIdx.x; i < size; i += kThreads) a[i] = 0;
-    if (n <= kThreads) {
-        __syncthreads();
-        const int t = threadIdx.x;
+    constexpr int kCounted = 192;
+    const int t = threadIdx.x;
+    const int size = n <= kCounted ? (n + 7) & ~7 : n <= kThreads ? kThreads : n <= 2 * kThreads ? 2 * kThreads : 4 * kThreads;
+    for (int i = n + t; i < size; i += kThreads) a[i] = 0;
+    __syncthreads();
+    if (n <= kCounted) {
         T mine = 0;
         int rank = 0;
         if (t < n) {
             mine = a[t];
-            for (int i = 0; i < n; i += 4) {
+            for (int i = 0; i < n; i += 8) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (i + e < size) rank += a[i + e] > mine || (a[i + e] == mine && i + e < t);
+                for (int e = 0; e < 8; ++e) rank += a[i + e] > mine || (a[i + e] == mine && i + e < t);
             }
         }
         __syncthreads();
         if (t < n) a[rank] = mine;
         __syncthreads();
-        return;
+    } else if (n <= kThreads) {
+        sort_registers<1>(a);
+    } else if (n <= 2 * kThreads) {
+        sort_registers<2>(a);
+    } else {
+        sort_registers<4>(a);
     }
-    n = size;
-    __syncthreads();
-    for (int k = 2; k <= n; k <<= 1)
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            for (int t = threadIdx.x; t < n / 2; t += kThreads) {
-                const int i = 2 * (t & ~(j - 1)) + (t & (j - 1)), p = i + j;
-                const T x = a[i], y = a[p];
-                if ((x < y) == ((i & k) == 0)) a[i] = y, a[p] = x;
-            }
-            // the next step's pairs are j / 2 apart, or k after the last
-            if (j > 64 || (j == 1 && k > 64))
-                __syncthreads();
-            else
-                lanes_agree();
-        }
-    __syncthreads();
 }
 
 struct Shared {
@@ -640,12 +677,13 @@ __device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, cons
         const int left = a.vocab - (a.tiles - 1) * kTile;
         const int n_sampled = (a.tiles - 1) * 128 + min(64, (left + V - 1) / V) + max(0, min(64, (left - kTile / 2 + V - 1) / V));
         const double each = static_cast<double>(a.vocab) / n_sampled, rest = (1. - static_cast<double>(set.p)) * whole;
+        const double slope = scale > 0.f ? -row.c / static_cast<double>(scale) : 0.;
         double m[per], v[per], ms = 0., vs = 0., all;
         uint32_t cs = 0, every;
 #pragma unroll
         for (int e = 0; e < per; ++e) {
             const int b = kHist - 1 - (per * t + e);
-            const double w = scale > 0.f ? each * exp2_neg(-(b + .5) / static_cast<double>(scale) * row.c) : each;
+            const double w = each * exp2_neg((b + .5) * slope);
             ms += m[e] = w * s.sampled[b];
             vs += v[e] = w * w * s.sampled[b];
             cs += c[e] = s.sampled[b];
@@ -657,7 +695,7 @@ __device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, cons
         for (int e = 0; e < per; ++e) {
             const int b = kHist - 1 - (per * t + e);
             mrun += m[e], vrun += v[e];
-            const double err = 4. * sqrt(vrun) + 4. * each * exp2_neg(scale > 0.f ? -b / static_cast<double>(scale) * row.c : 0.);
+            const double err = 4. * sqrt(vrun) + 4. * each * exp2_neg(b * slope);
             if (mrun + err >= rest) atomicMax(&s.i1, b);  // the last bin that may hold the threshold: past it there is too little
             if (mrun - err > rest) atomicMax(&s.i2, b);   // the first: from it on there is too much
             s.sampled[b] = every - crun;                  // samples in bins above
