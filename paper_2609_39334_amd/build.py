@@ -29,7 +29,8 @@ HIP_FLAGS = [
 ]
 # attention and sampling: masked scores are -inf, guarded where they could meet, and no NaN enters the
 # arithmetic, so the compiler need not quiet the inputs of every max.  (Activations may hold NaN.)
-FILE_FLAGS = {"attn.hip": ["-fno-honor-nans"], "draft_attn.hip": ["-fno-honor-nans"], "cd_sample.hip": ["-fno-honor-nans"]}
+FILE_FLAGS = {"attn.hip": ["-fno-honor-nans"], "draft_attn.hip": ["-fno-honor-nans"], "cd_sample.hip": ["-fno-honor-nans"],
+              "filter_sample.hip": ["-fno-honor-nans"]}
 
 
 def _run_all(cmds, verbose):

@@ -41,7 +41,8 @@ constexpr int kTile = tkv::kFilterTile;
 static_assert(kTile == 64 * kRun, "a run a lane");
 constexpr int kScanThreads = 256;
 constexpr int kSparseP = 64;          // fewest runs looked into for top-p
-constexpr int kSparseRuns = 1024;     // and most, past which filter_narrow reads the row
+constexpr int kSparseRuns = 1024;     // most runs that are looked into for top-k
+constexpr int kSparseFew = 384;       // and for top-p and min-p, past which filter_narrow reads the row
 constexpr int kHist = 1024;           // bins of the runs' maxima and of the sample
 constexpr int kMaxTiles = (1 << kIdxBits) / kTile;
 constexpr int kMaxPotential = 1024;
@@ -65,7 +66,8 @@ struct Args {
     struct Again* again;
     float2* tile_max;                 // [n_rows][tiles]: the largest logit, the smallest that filter_draw's bins are to hold
     float *run_max, *sample;          // [n_rows][tiles][64], sample: two of them
-    double *tile_sum, *above, *kept;  // [n_rows][tiles]: weight relative to the tile's largest; filter_narrow's
+    double* part_sum;                 // [n_rows][tiles][8]: weight of a tile's parts relative to the tile's largest logit
+    double *above, *kept;             // [n_rows][tiles] and its parts: filter_narrow's
     uint64_t* lists;                  // [n_rows][cap]
 };
 
@@ -76,14 +78,14 @@ struct Again {
     int32_t first, last;
     float top, scale;
     double weight;           // of all tokens, if top-p is to be cut
-    uint32_t n;              // numbers inside the interval
-    uint32_t pad[3];
+    int32_t n;               // numbers inside the interval
+    int32_t pad[3];
 };
 static_assert(sizeof(Again) == 48, "the workspace's records");
 
 // Bins of equal width from the largest logit down, the last one open.
 __device__ __forceinline__ int bin_of(float v, float top, float scale) {
-    return static_cast<int>(fminf((top - v) * scale, static_cast<float>(kHist - 1)));
+    return static_cast<int>(fminf(fminf(top - v, 3.4028234663852886e38f) * scale, static_cast<float>(kHist - 1)));
 }
 
 // A row's settings and draws.
@@ -107,34 +109,34 @@ __device__ __forceinline__ Settings settings_of(const Args& a, int r) {
     s.p = a.top_p ? a.top_p[r] : 1.f;
     s.min_p = a.min_p ? a.min_p[r] : 0.f;
     s.k = a.top_k ? a.top_k[r] : 0;
-    s.valid = s.temp >= 0.f && s.temp < INFINITY && s.p >= 0.f && s.p <= 1.f && s.min_p >= 0.f && s.min_p <= 1.f && s.k >= 0;
+    // (by their bits: the compiler may assume that a number is no NaN)
+    const auto below = [](float v, uint32_t end) { return __float_as_uint(v) == 0x80000000u || __float_as_uint(v) < end; };
+    s.valid = below(s.temp, 0x7f800000u) && below(s.p, 0x3f800001u) && below(s.min_p, 0x3f800001u) && s.k >= 0;
     if (s.temp == 0.f) s.k = 1;
     if (s.k == 0 || s.k > a.vocab) s.k = a.vocab;
     return s;
 }
 
-// 2^t for t <= 0, to 2^-52: t's nearest integer by adding 1.5 * 2^52, and the series of exp on [-ln 2 / 2, ln 2 / 2],
-// whose first omitted term is below 2^-52.
+// 2^t for t <= 0, to 2^-50: t's nearest integer n by adding 1.5 * 2^52, and 2^(t - n) as 1 + f p(f), p the polynomial
+// that meets (2^f - 1) / f at ten Chebyshev nodes of [-1/2, 1/2].  (2^0 is 1 exactly: equal logits have equal sums.)
 __device__ __forceinline__ double exp2_neg(double t) {
     constexpr double kRound = 6755399441055744.0;
     t = fmax(t, -1100.);
     const double r = t + kRound;
     const int n = static_cast<int>(__double_as_longlong(r));
-    const double f = (t - (r - kRound)) * 0.6931471805599453;
-    double y = 1. / 479001600.;
-    y = fma(y, f, 1. / 39916800.);
-    y = fma(y, f, 1. / 3628800.);
-    y = fma(y, f, 1. / 362880.);
-    y = fma(y, f, 1. / 40320.);
-    y = fma(y, f, 1. / 5040.);
-    y = fma(y, f, 1. / 720.);
-    y = fma(y, f, 1. / 120.);
-    y = fma(y, f, 1. / 24.);
-    y = fma(y, f, 1. / 6.);
-    y = fma(y, f, .5);
+    const double f = t - (r - kRound);
+    double y = 0x1.e5e9f548e5725p-28;
+    y = fma(y, f, 0x1.b6571de2f2351p-24);
+    y = fma(y, f, 0x1.62bfe46117445p-20);
+    y = fma(y, f, 0x1.ffcb76789860fp-17);
+    y = fma(y, f, 0x1.4309130378460p-13);
+    y = fma(y, f, 0x1.5d87fe908f88ap-10);
+    y = fma(y, f, 0x1.3b2ab6fba385fp-7);
+    y = fma(y, f, 0x1.c6b08d7044119p-5);
+    y = fma(y, f, 0x1.ebfbdff82c590p-3);
+    y = fma(y, f, 0x1.62e42fefa39f7p-1);
     y = fma(y, f, 1.);
-    y = fma(y, f, 1.);
-    return ldexp(y, n);
+    return __builtin_amdgcn_ldexp(y, n);
 }
 
 // Larger logits have larger keys; -0 and 0 have one.
@@ -177,16 +179,20 @@ struct Logits {
         for (int i = V * whole + threadIdx.x; i < vocab; i += kThreads) f(i, at(i));
     }
     // this lane's run of the tile that starts at a0: kPieces pieces of V tokens, 64 V apart (-inf past the row)
+    // (a piece of all 64 lanes is a part of the tile, consecutive tokens)
     static constexpr int V = BF16 ? 8 : 4, kPieces = kRun / V;
     static __device__ __forceinline__ int token(int a0, int lane, int piece) { return a0 + (piece * 64 + lane) * V; }
+    template <bool NT = false>
     __device__ __forceinline__ void piece(int a, float (&x)[V]) const {
         if (a + V <= vocab) {
             if constexpr (BF16) {
-                const u16x8_t y = *reinterpret_cast<const u16x8_t*>(static_cast<const uint16_t*>(p) + a);
+                const u16x8_t* from = reinterpret_cast<const u16x8_t*>(static_cast<const uint16_t*>(p) + a);
+                const u16x8_t y = NT ? __builtin_nontemporal_load(from) : *from;
 #pragma unroll
                 for (int e = 0; e < V; ++e) x[e] = bf16_f32(y[e]);
             } else {
-                const f32x4_t y = *reinterpret_cast<const f32x4_t*>(static_cast<const float*>(p) + a);
+                const f32x4_t* from = reinterpret_cast<const f32x4_t*>(static_cast<const float*>(p) + a);
+                const f32x4_t y = NT ? __builtin_nontemporal_load(from) : *from;
 #pragma unroll
                 for (int e = 0; e < V; ++e) x[e] = y[e];
             }
@@ -195,16 +201,32 @@ struct Logits {
             for (int e = 0; e < V; ++e) x[e] = a + e < vocab ? at(a + e) : -INFINITY;
         }
     }
-    // kRun consecutive tokens of a tile for each lane
-    __device__ __forceinline__ void consecutive(int a0, int lane, float (&x)[kPieces][V]) const {
-#pragma unroll
-        for (int j = 0; j < kPieces; ++j) piece(a0 + lane * kRun + j * V, x[j]);
-    }
+    template <bool NT = false>
     __device__ __forceinline__ void run(int a0, int lane, float (&x)[kPieces][V]) const {
 #pragma unroll
-        for (int j = 0; j < kPieces; ++j) piece(token(a0, lane, j), x[j]);
+        for (int j = 0; j < kPieces; ++j) piece<NT>(token(a0, lane, j), x[j]);
     }
 };
+
+// Sums of v[0], v[1], .. over the wave, in a fixed pattern: lane 64 / N j .. 64 / N (j + 1) - 1 gets v[j]'s.
+template <int N, int O = 32>
+__device__ __forceinline__ double wave_sums(const double (&v)[N], int lane) {
+    if constexpr (N > 1) {
+        const bool upper = lane & O;
+        double u[N / 2];
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) {
+            const double mine = upper ? v[j + N / 2] : v[j], other = upper ? v[j] : v[j + N / 2];
+            u[j] = mine + __shfl_xor(other, O);
+        }
+        return wave_sums<N / 2, O / 2>(u, lane);
+    } else {
+        double sum = v[0];
+#pragma unroll
+        for (int o = O; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+        return sum;
+    }
+}
 
 // Inclusive scan over a wave, in a fixed pattern.
 template <class T>
@@ -297,30 +319,38 @@ __device__ __forceinline__ void sort_registers(T* a) {
 // thread those before its own.
 template <class T>
 __device__ __forceinline__ void sort_down(T* a, int n) {
-    constexpr int kCounted = 192;
+    constexpr int kCounted = 256;
     const int t = threadIdx.x;
-    const int size = n <= kCounted ? (n + 7) & ~7 : n <= kThreads ? kThreads : n <= 2 * kThreads ? 2 * kThreads : 4 * kThreads;
+    static_assert(kList == 8 * kThreads || kList == 4 * kThreads, "the sizes below");
+    int size = (n + 63) & ~63;
+    if (n > kCounted)
+        for (size = kThreads; size < n;) size *= 2;
     for (int i = n + t; i < size; i += kThreads) a[i] = 0;
     __syncthreads();
     if (n <= kCounted) {
-        T mine = 0;
+        // `parts` threads a number, each over its share of the others
+        const int parts = kThreads / (n <= 64 ? 64 : n <= 128 ? 128 : 256), i = t / parts, share = size / parts, from = (t & (parts - 1)) * share;
+        const T mine = i < n ? a[i] : 0;
         int rank = 0;
-        if (t < n) {
-            mine = a[t];
-            for (int i = 0; i < n; i += 8) {
+        for (int q = from; q < from + share; q += 8) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) rank += a[i + e] > mine || (a[i + e] == mine && i + e < t);
+            for (int e = 0; e < 8; ++e) {
+                rank += a[q + e] > mine;
+                if constexpr (sizeof(T) == 4) rank += a[q + e] == mine && q + e < i;  // (only draws repeat)
             }
         }
+        for (int o = parts / 2; o > 0; o >>= 1) rank += __shfl_xor(rank, o);
         __syncthreads();
-        if (t < n) a[rank] = mine;
+        if (i < n && (t & (parts - 1)) == 0) a[rank] = mine;
         __syncthreads();
-    } else if (n <= kThreads) {
+    } else if (size == kThreads) {
         sort_registers<1>(a);
-    } else if (n <= 2 * kThreads) {
+    } else if (size == 2 * kThreads) {
         sort_registers<2>(a);
-    } else {
+    } else if (size == 4 * kThreads) {
         sort_registers<4>(a);
+    } else {
+        sort_registers<kList / kThreads>(a);
     }
 }
 
@@ -339,12 +369,9 @@ struct Shared {
                 };
                 double cdf[kList];
             };
-            int32_t hits[kList];  // draws of each kept token
+            uint32_t hits[kList / 2];  // draws of each kept token, 16 bits each
         };
-        struct {
-            double tile[kMaxTiles + 1];  // the draws' tile prefixes
-            uint64_t inside[kMaxTiles];  // weight of the kept tokens inside the interval
-        };
+        double tile[kMaxTiles + 1];  // the draws' tile prefixes
     };
     uint64_t part[kWaves];
     double partd[kWaves];
@@ -380,7 +407,14 @@ struct ListNumbers {
     int n;
     template <class F>
     __device__ __forceinline__ void each(F f) const {
-        for (int i = threadIdx.x; i < n; i += kThreads) f(p[i]);
+        for (int i0 = threadIdx.x; i0 < n; i0 += 8 * kThreads) {
+            uint64_t v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = p[min(i0 + e * kThreads, n - 1)];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (i0 + e * kThreads < n) f(v[e]);
+        }
     }
 };
 
@@ -474,8 +508,8 @@ __device__ uint64_t find_cut(Shared& s, const Src& src, const W& units, uint64_t
 }
 
 // A wave a tile: the runs' maxima (+inf where a logit is NaN), and the tile's weight where the row asks for it.
-template <bool BF16>
-__global__ __launch_bounds__(kScanThreads) void filter_scan(Args a) {
+template <bool BF16, bool NT>
+__global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(5))) void filter_scan(Args a) {
     const int lane = threadIdx.x & 63;
     const int64_t id = static_cast<int64_t>(blockIdx.x) * (kScanThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = static_cast<int>(id / a.tiles), tile = static_cast<int>(id - static_cast<int64_t>(r) * a.tiles);
@@ -485,13 +519,13 @@ __global__ __launch_bounds__(kScanThreads) void filter_scan(Args a) {
     if (!s.inside || !s.valid || s.n == 0) return;
     const Logits<BF16> row{static_cast<const char*>(a.logits) + r * a.stride * (BF16 ? 2 : 4), a.vocab};
     float x[Logits<BF16>::kPieces][Logits<BF16>::V];
-    row.run(tile * kTile, lane, x);
+    row.template run<NT>(tile * kTile, lane, x);
     float m = -INFINITY;
     bool nan = false;
 #pragma unroll
     for (int j = 0; j < Logits<BF16>::kPieces; ++j)
 #pragma unroll
-        for (int e = 0; e < Logits<BF16>::V; ++e) m = fmaxf(m, x[j][e]), nan |= x[j][e] != x[j][e];
+        for (int e = 0; e < Logits<BF16>::V; ++e) m = fmaxf(m, x[j][e]), nan |= (__float_as_uint(x[j][e]) & 0x7fffffffu) > 0x7f800000u;
     if (nan) m = INFINITY;
     a.run_max[id * 64 + lane] = m;
     const bool whole = s.whole(a.vocab), samples = whole && s.p < 1.f;
@@ -503,17 +537,19 @@ __global__ __launch_bounds__(kScanThreads) void filter_scan(Args a) {
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o)), low = fminf(low, __shfl_xor(low, o));
     if (lane == 0) a.tile_max[id] = make_float2(m, low);
     if (!whole) return;
-    double sum = 0.;
-    if (m > -INFINITY && m < INFINITY) {
-        const double base = m, c = s.scale();
+    constexpr int N = Logits<BF16>::kPieces;
+    double sum[N];
+    const bool some = m > -INFINITY && m < INFINITY;
+    const double base = some ? m : 0., c = s.scale();
 #pragma unroll
-        for (int j = 0; j < Logits<BF16>::kPieces; ++j)
+    for (int j = 0; j < N; ++j) {
+        sum[j] = 0.;
+        if (some)
 #pragma unroll
-            for (int e = 0; e < Logits<BF16>::V; ++e) sum += exp2_neg((static_cast<double>(x[j][e]) - base) * c);
+            for (int e = 0; e < Logits<BF16>::V; ++e) sum[j] += exp2_neg((static_cast<double>(x[j][e]) - base) * c);
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    if (lane == 0) a.tile_sum[id] = sum;
+    const double part = wave_sums(sum, lane);
+    if (lane % (64 / N) == 0) a.part_sum[id * N + lane / (64 / N)] = part;
 }
 
 // The groups of n draws, sorted in s.draw (complements of tokens).
@@ -542,13 +578,20 @@ __device__ __forceinline__ void write_groups(Shared& s, const Args& a, int r, in
     if (t == 0) a.n_groups[r] = static_cast<int32_t>(groups);
 }
 
-// Draws over the tiles' prefixes in s.tile, one wave a draw: its tile, the lane in it, the token.
-template <bool BF16, class F>
-__device__ __forceinline__ void draw_from_tiles(Shared& s, const Args& a, int r, const Row<BF16>& row, const Settings& set, F kept) {
+// Draws over the tiles' prefixes in s.tile, one wave a draw: its tile, the part (by part(tile, j), its weight), the lane
+// that has it, the token.
+template <bool BF16, class P, class F>
+__device__ __forceinline__ void draw_from_tiles(Shared& s, const Args& a, int r, const Row<BF16>& row, const Settings& set, P part, F kept) {
     using L = Logits<BF16>;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int tiles = a.tiles;
     const double total = s.tile[tiles];
+    // the first of the lanes with a weight whose inclusive sum is past the target, else the last with a weight
+    const auto choose = [&](double weight, double incl, double target) {
+        const uint64_t has = __builtin_amdgcn_ballot_w64(weight > 0.);
+        const uint64_t past = has & __builtin_amdgcn_ballot_w64(incl > target);
+        return past ? __builtin_ctzll(past) : has ? 63 - __builtin_clzll(has) : 0;
+    };
     for (int d = w; d < set.n; d += kWaves) {
         const double target = static_cast<double>(a.uniform[set.off + d]) * total;
         int b = 0, e = tiles;  // the first tile that ends past the target
@@ -561,27 +604,30 @@ __device__ __forceinline__ void draw_from_tiles(Shared& s, const Args& a, int r,
             while (b > 0 && !(s.tile[b + 1] > s.tile[b])) --b;
         }
         b = __builtin_amdgcn_readfirstlane(b);
-        float x[L::kPieces][L::V];
-        const int first = b * kTile + lane * kRun;
-        row.x.consecutive(b * kTile, lane, x);
-        double sum = 0.;
+        const double pw = lane < L::kPieces ? part(b, lane) : 0.;
+        double incl = s.tile[b] + wave_scan(pw, lane);
+        const int j = choose(pw, incl, target);
+        double start = __shfl(incl - pw, j);
+        const int first = L::token(b * kTile, lane, j);
+        float x[L::V];
+        row.x.piece(first, x);
+        double y[L::V], sum = 0.;
 #pragma unroll
-        for (int j = 0; j < L::kPieces; ++j)
+        for (int q = 0; q < L::V; ++q) sum += y[q] = kept(first + q, x[q]);
+        incl = start + wave_scan(sum, lane);
+        if (lane == choose(sum, incl, target)) {
+            double acc = incl - sum;
+            int pick = -1, last = 0;
 #pragma unroll
-            for (int q = 0; q < L::V; ++q) sum += kept(first + j * L::V + q, x[j][q]);
-        const double incl = s.tile[b] + wave_scan(sum, lane);
-        const uint64_t has = __builtin_amdgcn_ballot_w64(sum > 0.);
-        const uint64_t past = has & __builtin_amdgcn_ballot_w64(incl > target);
-        const int who = past ? __builtin_ctzll(past) : has ? 63 - __builtin_clzll(has) : 0;
-        // that lane's tokens, one a lane
-        static_assert(kRun == 32, "half a wave");
-        const int i = b * kTile + who * kRun + (lane & 31);
-        const double y = lane < kRun && i < a.vocab ? kept(i, row.x.at(i)) : 0.;
-        const double acc = __shfl(incl - sum, who) + wave_scan(y, lane);
-        const uint64_t some = __builtin_amdgcn_ballot_w64(y > 0.);
-        const uint64_t over = some & __builtin_amdgcn_ballot_w64(acc > target);
-        const int pick = over ? __builtin_ctzll(over) : some ? 63 - __builtin_clzll(some) : 0;
-        if (lane == 0) s.draw[d] = ~static_cast<uint32_t>(b * kTile + who * kRun + pick);
+            for (int q = 0; q < L::V; ++q) {
+                acc += y[q];
+                if (y[q] > 0.) {
+                    last = first + q;
+                    if (pick < 0 && acc > target) pick = last;
+                }
+            }
+            s.draw[d] = ~static_cast<uint32_t>(pick >= 0 ? pick : last);
+        }
     }
     __syncthreads();
     write_groups(s, a, r, set.off, set.n);
@@ -612,6 +658,24 @@ __device__ __forceinline__ void prefix(double (&v)[per], double* part) {
     double run = block_scan(sum, part, total);
 #pragma unroll
     for (int e = 0; e < per; ++e) v[e] = run += v[e];
+}
+
+// Room for this lane's set bits behind what `counter` counts, with one atomic for the wave's lanes that are here.
+__device__ __forceinline__ int append(int* counter, uint32_t bits) {
+    const int mine = __builtin_popcount(bits);
+    int before = 0, total = 0;
+    const uint64_t here = __builtin_amdgcn_ballot_w64(true);
+    // (bit by bit of the counts, which are at most 32)
+#pragma unroll
+    for (int k = 0; k < 6; ++k) {
+        const uint64_t b = __builtin_amdgcn_ballot_w64(mine >> k & 1);
+        before += static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(b >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(b), 0))) << k;
+        total += __builtin_popcountll(b) << k;
+    }
+    int base = 0;
+    const int leader = __builtin_ctzll(here);
+    if (static_cast<int>(threadIdx.x & 63) == leader && total > 0) base = atomicAdd(counter, total);
+    return __builtin_amdgcn_readlane(base, leader) + before;
 }
 
 // f(i, p[i]) for i < n, eight loads ahead.
@@ -711,8 +775,8 @@ __device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, cons
     }
     r.runs = s.hist[r.last];
     r.low = foot_of(r.last, top, scale);
-    // (twice the sample's estimate has to fit the list)
-    if (!by_k && r.last + 1 < kHist && 64 * static_cast<int64_t>(s.sampled[r.last]) / 2 > kList / 2) r.runs = kSparseRuns + 1;
+    // (a sampled token stands for 16)
+    if (!by_k && (r.runs > kSparseFew || 16 * s.sampled[r.last] > kSparseFew)) r.runs = kSparseRuns + 1;
     __syncthreads();
     return r;
 }
@@ -728,16 +792,25 @@ __device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>&
     const float low = at_least.low;
     if (t == 0) s.i1 = s.i2 = 0;
     __syncthreads();
-    each_of(rm, n_runs, [&](int i, float v) {
-        if (v >= low) {
-            const int at = atomicAdd(&s.i1, 1);
-            if (at < kSparseRuns) s.runs[at] = i;
-        }
-    });
+    for (int i0 = t; i0 < n_runs; i0 += 8 * kThreads) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = rm[min(i0 + e * kThreads, n_runs - 1)];
+        uint32_t in = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) in |= static_cast<uint32_t>(i0 + e * kThreads < n_runs && v[e] >= low) << e;
+        int at = append(&s.i1, in);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (in >> e & 1) {
+                if (at < kSparseRuns) s.runs[at] = i0 + e * kThreads;
+                ++at;
+            }
+    }
     __syncthreads();
     const int runs = s.i1;
     if (runs > kSparseRuns) return false;
-    constexpr int kAhead = 4;
+    constexpr int kAhead = 16 / L::V;
     for (int i0 = t; i0 < runs * L::kPieces; i0 += kAhead * kThreads) {
         float x[kAhead][L::V];
         int first[kAhead];
@@ -748,13 +821,20 @@ __device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>&
             first[q] = L::token(run / 64 * kTile, run % 64, i % L::kPieces);
             row.x.piece(first[q], x[q]);
         }
+        uint32_t in = 0;
 #pragma unroll
         for (int q = 0; q < kAhead; ++q)
 #pragma unroll
             for (int e = 0; e < L::V; ++e)
-                if (i0 + q * kThreads < runs * L::kPieces && x[q][e] >= low) {
-                    const int at = atomicAdd(&s.i2, 1);
+                in |= static_cast<uint32_t>(i0 + q * kThreads < runs * L::kPieces && x[q][e] >= low) << (q * L::V + e);
+        int at = append(&s.i2, in);
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+#pragma unroll
+            for (int e = 0; e < L::V; ++e)
+                if (in >> (q * L::V + e) & 1) {
                     if (at < kList) s.list[at] = number_of(x[q][e], first[q] + e);
+                    ++at;
                 }
     }
     __syncthreads();
@@ -806,7 +886,7 @@ __device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>&
     for (int e = 0; e < per; ++e) {
         const int i = per * t + e;
         sum[e] = i < keep ? row.weight(logit_of(s.list[i] << kIdxBits)) : 0.;
-        s.hits[i] = 0;
+        if (i < kList / 2) s.hits[i] = 0;
     }
     prefix(sum, s.partd);
     __syncthreads();
@@ -825,19 +905,20 @@ __device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>&
             b = keep - 1;
             while (b > 0 && !(s.cdf[b] > s.cdf[b - 1])) --b;
         }
-        atomicAdd(&s.hits[b], 1);
+        atomicAdd(&s.hits[b / 2], 1u << (16 * (b & 1)));
     }
     __syncthreads();
+    const auto hits = [&](int i) { return static_cast<int32_t>(s.hits[i / 2] >> (16 * (i & 1)) & 0xffff); };
     uint32_t mine = 0, groups;
 #pragma unroll
-    for (int e = 0; e < per; ++e) mine += s.hits[per * t + e] > 0;
+    for (int e = 0; e < per; ++e) mine += hits(per * t + e) > 0;
     uint32_t at = block_scan(mine, reinterpret_cast<uint32_t*>(s.part), groups);
 #pragma unroll
     for (int e = 0; e < per; ++e) {
         const int i = per * t + e;
-        if (s.hits[i] > 0) {
+        if (hits(i) > 0) {
             a.token[set.off + at] = (1 << kIdxBits) - 1 - static_cast<int32_t>(s.list[i] >> 32);
-            a.count[set.off + at] = s.hits[i];
+            a.count[set.off + at] = hits(i);
             ++at;
         }
     }
@@ -846,7 +927,7 @@ __device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>&
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void filter_draw(Args a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) void filter_draw(Args a) {
     using L = Logits<BF16>;
     __shared__ Shared s;
     const int r = blockIdx.x, t = threadIdx.x, lane = t & 63;
@@ -860,7 +941,7 @@ __global__ __launch_bounds__(kThreads) void filter_draw(Args a) {
     }
     Row<BF16> row{{static_cast<const char*>(a.logits) + r * a.stride * (BF16 ? 2 : 4), a.vocab}, 0., set.scale()};
     const float* rm = a.run_max + static_cast<int64_t>(r) * a.tiles * 64;
-    const double* ts = a.tile_sum + static_cast<int64_t>(r) * a.tiles;
+    const double* ps = a.part_sum + static_cast<int64_t>(r) * a.tiles * L::kPieces;
 
     // the largest logit, the smallest for the bins below, and the tiles' weights relative to the row's largest
     const bool by_k = set.k < a.vocab, by_p = set.p < 1.f;
@@ -885,11 +966,18 @@ __global__ __launch_bounds__(kThreads) void filter_draw(Args a) {
     row.top = top;
     double whole = 0.;
     if (set.whole(a.vocab)) {
-        for (int i = t; i < a.tiles; i += kThreads) s.tile[i + 1] = ts[i] * row.weight(tm[i].x);
+        for (int i = t; i < a.tiles; i += kThreads) {
+            double sum = 0.;
+#pragma unroll
+            for (int j = 0; j < L::kPieces; ++j) sum += ps[i * L::kPieces + j];
+            s.tile[i + 1] = sum * row.weight(tm[i].x);
+        }
         tile_prefixes(s, a.tiles);
         whole = s.tile[a.tiles];
         if (!by_p) {
-            draw_from_tiles<BF16>(s, a, r, row, set, [&](int, float v) { return row.weight(v); });
+            draw_from_tiles<BF16>(
+                s, a, r, row, set, [&](int tile, int j) { return ps[tile * L::kPieces + j] * row.weight(tm[tile].x); },
+                [&](int, float v) { return row.weight(v); });
             return;
         }
         __syncthreads();
@@ -912,7 +1000,7 @@ __global__ __launch_bounds__(kThreads) void filter_draw(Args a) {
         __syncthreads();
         at_least.runs = s.i0;
         __syncthreads();
-        if (at_least.runs <= kSparseRuns && draw_from_runs<BF16>(s, a, r, row, set, rm, whole, at_least)) return;
+        if (at_least.runs <= kSparseFew && draw_from_runs<BF16>(s, a, r, row, set, rm, whole, at_least)) return;
     }
     if (by_k || by_p) {
         at_least = find_bound<BF16>(s, a, row, set, rm, sample, top, scale, whole);
@@ -946,72 +1034,73 @@ __global__ __launch_bounds__(kScanThreads) void filter_narrow(Args a) {
         const double bound = static_cast<double>(set.min_p);
         float x[L::kPieces][L::V];
         row.x.run(tile * kTile, lane, x);
-        double above = 0., kept = 0.;
+        double above = 0., kept[L::kPieces];
         uint32_t in = 0;
 #pragma unroll
-        for (int j = 0; j < L::kPieces; ++j)
+        for (int j = 0; j < L::kPieces; ++j) {
+            kept[j] = 0.;
 #pragma unroll
             for (int e = 0; e < L::V; ++e) {
                 const int b = bin_of(x[j][e], g.top, g.scale);
                 if (b < g.first) {
                     const double y = row.weight(x[j][e]);
                     above += y;
-                    kept += y >= bound ? y : 0.;
+                    kept[j] += y >= bound ? y : 0.;
                 } else if (b <= g.last && x[j][e] > -INFINITY) {
                     in |= 1u << (j * L::V + e);
                 }
             }
+        }
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) above += __shfl_xor(above, o), kept += __shfl_xor(kept, o);
+        for (int o = 32; o > 0; o >>= 1) above += __shfl_xor(above, o);
+        const double part = wave_sums(kept, lane);
         const int64_t at = static_cast<int64_t>(g.row) * a.tiles + tile;
-        if (lane == 0) a.above[at] = above, a.kept[at] = kept;
-        const int mine = __builtin_popcount(in), incl = wave_scan(mine, lane);
-        uint32_t base = 0;
-        if (lane == 63 && incl > 0) base = atomicAdd(&a.again[d].n, static_cast<uint32_t>(incl));
-        base = __shfl(base, 63) + incl - mine;
+        if (lane == 0) a.above[at] = above;
+        if (lane % (64 / L::kPieces) == 0) a.kept[at * L::kPieces + lane / (64 / L::kPieces)] = part;
+        int base = append(&a.again[d].n, in);
+        // (few of a lane's 32, so read again from the cache rather than picked out of the registers one by one)
         uint64_t* list = a.lists + static_cast<int64_t>(g.row) * a.cap;
-#pragma unroll
-        for (int j = 0; j < L::kPieces; ++j)
-#pragma unroll
-            for (int e = 0; e < L::V; ++e)
-                if (in >> (j * L::V + e) & 1) {
-                    if (base < static_cast<uint32_t>(a.cap)) list[base] = number_of(x[j][e], L::token(tile * kTile, lane, j) + e);
-                    ++base;
-                }
+        for (; in != 0; in &= in - 1, ++base) {
+            const int q = __builtin_ctz(in), i = L::token(tile * kTile, lane, q / L::V) + q % L::V;
+            if (base < a.cap) list[base] = number_of(row.x.at(i), i);
+        }
     }
 }
 
-// The kept weight of a row's tiles, read whole by the workgroup.
+// The kept weight of a row's parts, read whole by the workgroup.
 template <bool BF16, class F>
-__device__ __forceinline__ void sum_tiles(Shared& s, const Args& a, const Row<BF16>& row, F kept) {
+__device__ __forceinline__ void sum_parts(const Args& a, const Row<BF16>& row, double* parts, F kept) {
     using L = Logits<BF16>;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    __syncthreads();
     for (int i = w; i < a.tiles; i += kWaves) {
         float x[L::kPieces][L::V];
         row.x.run(i * kTile, lane, x);
-        double sum = 0.;
+        double sum[L::kPieces];
 #pragma unroll
-        for (int j = 0; j < L::kPieces; ++j)
+        for (int j = 0; j < L::kPieces; ++j) {
+            sum[j] = 0.;
 #pragma unroll
-            for (int e = 0; e < L::V; ++e) sum += kept(L::token(i * kTile, lane, j) + e, x[j][e]);
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-        if (lane == 0) s.tile[i + 1] = sum;
+            for (int e = 0; e < L::V; ++e) sum[j] += kept(L::token(i * kTile, lane, j) + e, x[j][e]);
+        }
+        const double part = wave_sums(sum, lane);
+        if (lane % (64 / L::kPieces) == 0) parts[i * L::kPieces + lane / (64 / L::kPieces)] = part;
     }
 }
 
-// The threshold of a row that filter_narrow has read; false if it is not in the row's list.  s.tile then holds the
-// tiles' kept weights.
+constexpr double kFine = 1125899906842624.0;  // 2^50: units of a list's kept weights (at most 8,192 of weight 1)
+
+// The threshold of a row that filter_narrow has read, and the kept weight of its list in each part (`inside`, zero
+// before); false if the threshold is not in the list.
 template <bool BF16>
-__device__ bool cut_in_list(Shared& s, const Args& a, const Row<BF16>& row, const Settings& set, const Again& g, uint64_t& cut) {
+__device__ bool cut_in_list(Shared& s, const Args& a, const Row<BF16>& row, const Settings& set, const Again& g, uint64_t* inside,
+                            uint64_t& cut) {
     const int t = threadIdx.x;
     const int64_t at = static_cast<int64_t>(g.row) * a.tiles;
     const double bound = static_cast<double>(set.min_p);
     cut = 0;
     if (set.p < 1.f) {
-        if (g.n > static_cast<uint32_t>(a.cap)) return false;
-        const ListNumbers list{a.lists + static_cast<int64_t>(g.row) * a.cap, static_cast<int>(g.n)};
+        if (g.n > a.cap) return false;
+        const ListNumbers list{a.lists + static_cast<int64_t>(g.row) * a.cap, g.n};
         double sum = 0., above;
         for (int i = t; i < a.tiles; i += kThreads) sum += a.above[at + i];
         block_scan(sum, s.partd, above);
@@ -1039,21 +1128,13 @@ __device__ bool cut_in_list(Shared& s, const Args& a, const Row<BF16>& row, cons
         __syncthreads();
         lo = s.u0, hi = s.u1;
         cut = find_cut<true, false>(s, list, [&](float v) { return row.units(v); }, lo, hi, 0, want * kUnit);
-        // kept tokens of the list, by tile: integers, whatever their order (at most 8,192 of a weight up to 1)
-        constexpr double kFine = 1125899906842624.0;  // 2^50
-        __syncthreads();
-        for (int i = t; i < a.tiles; i += kThreads) s.inside[i] = 0;
-        __syncthreads();
+        // kept tokens of the list, by part: integers, whatever their order
         list.each([&](uint64_t n) {
             const double y = row.weight(logit_of(n));
             if (n < cut || y < bound) return;
             const int i = (1 << kIdxBits) - 1 - static_cast<int>(n & ((1 << kIdxBits) - 1));
-            atomicAdd(reinterpret_cast<unsigned long long*>(&s.inside[i / kTile]), static_cast<unsigned long long>(y * kFine + .5));
+            atomicAdd(reinterpret_cast<unsigned long long*>(&inside[i / (64 * Logits<BF16>::V)]), static_cast<unsigned long long>(y * kFine + .5));
         });
-        __syncthreads();
-        for (int i = t; i < a.tiles; i += kThreads) s.tile[i + 1] = a.kept[at + i] + static_cast<double>(s.inside[i]) / kFine;
-    } else {
-        for (int i = t; i < a.tiles; i += kThreads) s.tile[i + 1] = a.kept[at + i];
     }
     return true;
 }
@@ -1061,20 +1142,25 @@ __device__ bool cut_in_list(Shared& s, const Args& a, const Row<BF16>& row, cons
 // Cuts and draws of the rows that are read again, a workgroup a row.
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void filter_finish(Args a) {
+    using L = Logits<BF16>;
     __shared__ Shared s;
+    __shared__ uint64_t inside[kMaxTiles * L::kPieces];
+    const int t = threadIdx.x;
     for (int d = blockIdx.x; d < *a.n_again; d += gridDim.x) {
         __syncthreads();
+        for (int i = t; i < a.tiles * L::kPieces; i += kThreads) inside[i] = 0;
         const Again g = a.again[d];
         const Settings set = settings_of(a, g.row);
         const Row<BF16> row{{static_cast<const char*>(a.logits) + g.row * a.stride * (BF16 ? 2 : 4), a.vocab},
                             static_cast<double>(g.top), set.scale()};
         const double bound = static_cast<double>(set.min_p);
+        double* parts = a.kept + static_cast<int64_t>(g.row) * a.tiles * L::kPieces;
         uint64_t cut = 0;
         auto kept = [&](int i, float v) {
             const double x = row.weight(v);
             return number_of(v, i) >= cut && x >= bound ? x : 0.;
         };
-        if (g.whole_row || !cut_in_list<BF16>(s, a, row, set, g, cut)) {
+        if (g.whole_row || !cut_in_list<BF16>(s, a, row, set, g, inside, cut)) {
             const RowNumbers<BF16> all{row.x};
             auto units = [&](float v) { return row.units(v); };
             const uint64_t lo = static_cast<uint64_t>(key_of(-3.4028234663852886e38f)) << kIdxBits;
@@ -1082,10 +1168,20 @@ __global__ __launch_bounds__(kThreads) void filter_finish(Args a) {
             cut = 0;
             if (set.k < a.vocab) cut = find_cut<false, false>(s, all, units, lo, hi, static_cast<uint64_t>(set.k), 0.);
             if (set.p < 1.f) cut = find_cut<true, true>(s, all, units, cut > lo ? cut : lo, hi, 0, static_cast<double>(set.p));
-            sum_tiles<BF16>(s, a, row, kept);
+            sum_parts<BF16>(a, row, parts, kept);
+        }
+        __syncthreads();
+        const auto part = [&](int tile, int j) {
+            return parts[tile * L::kPieces + j] + static_cast<double>(inside[tile * L::kPieces + j]) / kFine;
+        };
+        for (int i = t; i < a.tiles; i += kThreads) {
+            double sum = 0.;
+#pragma unroll
+            for (int j = 0; j < L::kPieces; ++j) sum += part(i, j);
+            s.tile[i + 1] = sum;
         }
         tile_prefixes(s, a.tiles);
-        draw_from_tiles<BF16>(s, a, g.row, row, set, kept);
+        draw_from_tiles<BF16>(s, a, g.row, row, set, part, kept);
     }
 }
 
@@ -1102,7 +1198,7 @@ int tkv::launch_filter_sample(const FilterCall& f, void* stream) {
     a.tiles = l.tiles, a.cap = l.list;
     a.n_again = reinterpret_cast<int32_t*>(ws);
     a.again = reinterpret_cast<Again*>(ws + l.rows);
-    a.tile_sum = reinterpret_cast<double*>(ws + l.tile_sum);
+    a.part_sum = reinterpret_cast<double*>(ws + l.part_sum);
     a.above = reinterpret_cast<double*>(ws + l.above);
     a.kept = reinterpret_cast<double*>(ws + l.kept);
     a.tile_max = reinterpret_cast<float2*>(ws + l.tile_max);
@@ -1119,10 +1215,11 @@ int tkv::launch_filter_sample(const FilterCall& f, void* stream) {
         narrow<<<dim3(static_cast<unsigned>(std::min<int64_t>(grid, 2048))), dim3(kScanThreads), 0, st>>>(a);
         finish<<<dim3(static_cast<unsigned>(std::min(f.n_rows, 1024))), dim3(kThreads), 0, st>>>(a);
     };
+    const bool past = static_cast<int64_t>(f.n_rows) * f.vocab * (f.logit_type == TKV_LOGITS_BF16 ? 2 : 4) > int64_t{256} << 20;
     if (f.logit_type == TKV_LOGITS_BF16)
-        launch(filter_scan<true>, filter_draw<true>, filter_narrow<true>, filter_finish<true>);
+        launch(past ? filter_scan<true, true> : filter_scan<true, false>, filter_draw<true>, filter_narrow<true>, filter_finish<true>);
     else
-        launch(filter_scan<false>, filter_draw<false>, filter_narrow<false>, filter_finish<false>);
+        launch(past ? filter_scan<false, true> : filter_scan<false, false>, filter_draw<false>, filter_narrow<false>, filter_finish<false>);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? TKV_OK : set_error(TKV_EHIP, "tkv_filter_sample launch: %s", hipGetErrorString(e));
 }

@@ -218,7 +218,7 @@ struct FilterCall {
 constexpr int kFilterTile = 2048;  // logits that a wave of its first kernel reads
 struct FilterLayout {
     int32_t tiles, list;  // a row's tiles; entries of its list of tokens near the threshold
-    size_t rows, tile_sum, above, kept, tile_max, run_max, sample, lists, bytes;
+    size_t rows, part_sum, above, kept, tile_max, run_max, sample, lists, bytes;
 };
 inline FilterLayout filter_layout(int32_t n_rows, int32_t vocab) {
     const size_t n = static_cast<size_t>(n_rows);
@@ -232,9 +232,9 @@ inline FilterLayout filter_layout(int32_t n_rows, int32_t vocab) {
         return here;
     };
     l.rows = take(n * 48);
-    l.tile_sum = take(n * l.tiles * sizeof(double));
+    l.part_sum = take(n * l.tiles * 8 * sizeof(double));
     l.above = take(n * l.tiles * sizeof(double));
-    l.kept = take(n * l.tiles * sizeof(double));
+    l.kept = take(n * l.tiles * 8 * sizeof(double));
     l.tile_max = take(n * l.tiles * 2 * sizeof(float));
     l.run_max = take(n * l.tiles * 64 * sizeof(float));
     l.sample = take(n * l.tiles * 128 * sizeof(float));
