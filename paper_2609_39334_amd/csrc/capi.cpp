@@ -2,6 +2,7 @@
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
+#include <cstdlib>
 #include <string>
 
 #include "internal.h"
@@ -114,8 +115,8 @@ int check_draft(const char* fn, const tkv_shape* s, const tkv_draft_batch* b) {
 
 tkv::DraftSplit draft_split(const tkv_shape& s, const tkv_draft_batch& b) {
     tkv::DraftSplit x{};
-    x.waves = 4;
-    x.chunk = 64;
+    x.waves = getenv("DW") ? atoi(getenv("DW")) : 4;
+    x.chunk = getenv("DC") ? atoi(getenv("DC")) : 64;
     const int64_t rows = static_cast<int64_t>(b.max_q) * (s.hq / s.hkv);
     x.n_tiles = static_cast<int32_t>((rows + 32 * x.waves - 1) / (32 * x.waves));
     const int64_t longest = b.max_blocks < b.n_kv_blocks ? b.max_blocks : b.n_kv_blocks;

@@ -5,8 +5,9 @@
 // the row's blocks, in transposed products so that each lane keeps one query row throughout:
 //   S^T = K Q^T,  O^T += V^T P^T   on v_mfma_f32_32x32x16_bf16, 32 query rows a wave,
 // with an online softmax between them in fp32, whose base moves only when a row's maximum exceeds it by more than
-// 2^8 in probability scale.  P is rounded to bf16 for the second product (2^-9 of each term at most, as in the other
-// attention kernels here) and the denominator sums the rounded values, so the rounding does not bias the mean.
+// 2^8 in probability scale.  P is rounded to bf16 for the second product (2^-8 of each term at most, as in the other
+// attention kernels here: the matrix instructions take no wider operands at that rate); the denominator sums it
+// unrounded, so that lse has the precision of fp32.
 //
 // K and V go from the pool straight to LDS (buffer_load ... lds), double-buffered.  Which blocks these are is
 // device data: the workgroup first reads its chunk's table entries and lengths, drops what is no block of the pool,
@@ -34,7 +35,7 @@ constexpr uint32_t kNaNBits = 0x7fc00000u;
 struct Args {
     tkv_draft_batch b;
     int32_t num_blocks, hq, hkv, G;
-    int32_t chunk, n_chunks, n_tiles;  // blocks a chunk, chunks of the longest row, tiles of the widest row
+    int32_t chunk, n_chunks, n_tiles;  // most blocks of a chunk, chunks of the longest row, tiles of the widest row
     float sl2;                         // log2(e) / sqrt(d)
     const uint16_t *q, *k, *v;
     uint16_t* o;
@@ -46,10 +47,6 @@ __device__ __forceinline__ f32x16_t mfma(bf16x8_t a, bf16x8_t b, f32x16_t c) {
 }
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, bf16x2_t));
-}
-__device__ __forceinline__ float sum_bf16x2(uint32_t p, float acc) {
-    const bf16x2_t one{static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
-    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, p), one, acc, false);
 }
 
 // Stage rows are D bf16, unpadded, their 16-byte chunks XOR-swizzled by row so that the operand reads below (K: 32
@@ -100,8 +97,10 @@ struct Row {
     int q0, L;         // its query tokens
     int kv0, n_blk;    // its table
     bool tokens, table;  // whether they are inside the arrays
+    int n_chunks, chunk; // chunks of near-equal length, blocks a chunk (one chunk at least)
 };
-__device__ __forceinline__ Row row_of(const tkv_draft_batch& b, int r) {
+__device__ __forceinline__ Row row_of(const Args& a, int r) {
+    const tkv_draft_batch& b = a.b;
     Row w;
     w.q0 = b.q_indptr[r];
     w.L = b.q_indptr[r + 1] - w.q0;
@@ -109,6 +108,8 @@ __device__ __forceinline__ Row row_of(const tkv_draft_batch& b, int r) {
     w.n_blk = b.kv_indptr[r + 1] - w.kv0;
     w.tokens = w.q0 >= 0 && w.q0 <= b.n_qtok && w.L >= 1 && w.L <= b.max_q && w.L <= b.n_qtok - w.q0;
     w.table = w.kv0 >= 0 && w.kv0 <= b.n_kv_blocks && w.n_blk >= 0 && w.n_blk <= b.max_blocks && w.n_blk <= b.n_kv_blocks - w.kv0;
+    w.n_chunks = w.table && w.n_blk > 0 ? (w.n_blk + a.chunk - 1) / a.chunk : 1;
+    w.chunk = w.table ? (w.n_blk + w.n_chunks - 1) / w.n_chunks : 0;
     return w;
 }
 
@@ -139,10 +140,10 @@ __device__ __forceinline__ uint32_t seen(const uint64_t* __restrict__ m, int wor
     return static_cast<uint32_t>(v) & ((1u << len) - 1);
 }
 
-// R waves of 32 query rows times NG groups of keys; NB blocks a stage.
+// One tile of a row against one chunk: R waves of 32 query rows times NG groups of keys, NB blocks a stage.
 template <int D, int R>
-__device__ __forceinline__ void draft_tile(const Args& a) {
-    constexpr int NG = 4 / R, NB = R == 1 ? 8 : 4, BG = NB / NG;  // BG: blocks of a group's part of a stage
+__device__ __forceinline__ void draft_tile(const Args& a, const Row& w, int chunk, int kvh, int tile) {
+    constexpr int NG = 4 / R, NB = 4, BG = NB / NG;  // BG: blocks of a group's part of a stage
     constexpr int RB = 2 * D, kStage = NB * 16 * RB;
     static_assert(BG % 2 == 0, "32 keys an MFMA");
     __shared__ __attribute__((aligned(16))) uint8_t k0[kStage], v0[kStage], k1[kStage], v1[kStage];
@@ -153,18 +154,7 @@ __device__ __forceinline__ void draft_tile(const Args& a) {
     const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wave = wid % R, grp = wid / R;
 
-    // the tiles of one (chunk, row, KV head) on one XCD: they read the same keys
-    const int seq = blockIdx.x >> 3;
-    const int tile = seq % a.n_tiles;
-    int g = (seq / a.n_tiles) * 8 + (blockIdx.x & 7);
-    const int kvh = g % a.hkv;
-    g /= a.hkv;
-    const int r = g % a.b.n_rows, chunk = g / a.b.n_rows;
-    if (chunk >= a.n_chunks) return;
-    const Row w = row_of(a.b, r);
-    if (!w.tokens || tile * 32 * R >= w.L * a.G) return;
-    const int c0 = chunk * a.chunk;
-    if (chunk > 0 && (!w.table || c0 >= w.n_blk)) return;
+    const int c0 = chunk * w.chunk;
 
     // this lane's query row
     const int col = lane & 31, hi = lane >> 5;
@@ -189,7 +179,7 @@ __device__ __forceinline__ void draft_tile(const Args& a) {
     // the chunk's blocks, and how many keys of the row follow it (exact below L)
     int nb;
     {
-        const int n = min(a.chunk, w.n_blk - c0);
+        const int n = min(w.chunk, w.n_blk - c0);
         int id = 0, len = 0, after = 0, later;
         if (tid < n) len = entry(a, w.kv0 + c0 + tid, id);
         int next = c0 + n;
@@ -266,21 +256,43 @@ __device__ __forceinline__ void draft_tile(const Args& a) {
         f32x16_t sc[P];
 #pragma unroll
         for (int p = 0; p < P; ++p) sc[p] = f32x16_t{};
+        bf16x8_t kf[D / 16][P];
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
             for (int p = 0; p < P; ++p)
-                sc[p] = mfma(*reinterpret_cast<const bf16x8_t*>(ks + (grp * BG + 2 * p) * 16 * RB + (koff ^ (32 * kk))), qf[kk], sc[p]);
-        // sc[p][8 b + 4 u + x] is key 8 u + 4 hi + x of block 2 p + b of the group's part
+                kf[kk][p] = *reinterpret_cast<const bf16x8_t*>(ks + (grp * BG + 2 * p) * 16 * RB + (koff ^ (32 * kk)));
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+            for (int p = 0; p < P; ++p) sc[p] = mfma(kf[kk][p], qf[kk], sc[p]);
+        // K reads up to eight operands ahead of the MFMAs that use them
+        constexpr int kReads = D / 16 * P, kAhead = kReads < 8 ? kReads : 8;
+        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+        for (int kk = 0; kk < (kReads - kAhead) / 4; ++kk) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+        // sc[p][8 b + 4 u + x] is key 8 u + 4 hi + x of block 2 p + b of the group's part.  One uniform decision: mask
+        // where a block is partial, absent or holds drafted keys.
+        int blk[BG];
+        bool mixed = first + BG > nb;
 #pragma unroll
         for (int j = 0; j < BG; ++j) {
-            const int e = __builtin_amdgcn_readlane(dthis.y, BG * grp + j);
-            const int len = first + j < nb ? e & 31 : 0, d0 = e >> 5;
-            if (len == 16 && d0 + 16 <= 0) continue;  // a whole block of context
-            const uint32_t bits = seen(mask, a.b.mask_words, d0, len) >> (4 * hi);
+            blk[j] = __builtin_amdgcn_readlane(dthis.y, BG * grp + j);
+            mixed = mixed || (blk[j] & 31) != 16 || (blk[j] >> 5) > -16;
+        }
+        if (mixed) {
 #pragma unroll
-            for (int x = 0; x < 8; ++x)
-                if (!((bits >> (8 * (x >> 2) + (x & 3))) & 1)) sc[j >> 1][8 * (j & 1) + x] = -INFINITY;
+            for (int j = 0; j < BG; ++j) {
+                const int len = first + j < nb ? blk[j] & 31 : 0;
+                const uint32_t bits = seen(mask, a.b.mask_words, blk[j] >> 5, len) >> (4 * hi);
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                    if (!((bits >> (8 * (x >> 2) + (x & 3))) & 1)) sc[j >> 1][8 * (j & 1) + x] = -INFINITY;
+            }
         }
         {
             constexpr float kSlack = 8.f;
@@ -307,7 +319,7 @@ __device__ __forceinline__ void draft_tile(const Args& a) {
             for (int x = 0; x < 8; ++x) pr[x] = __builtin_amdgcn_exp2f(fmaf(sc[j >> 1][8 * (j & 1) + x], a.sl2, -msc));
             const uint4 pk{pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3]), pack_bf16x2(pr[4], pr[5]),
                            pack_bf16x2(pr[6], pr[7])};
-            l = sum_bf16x2(pk.x, sum_bf16x2(pk.y, sum_bf16x2(pk.z, sum_bf16x2(pk.w, l))));
+            l += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
             const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, pk);
             const uint8_t* vr = vs + (grp * BG + j) * 16 * RB;
 #pragma unroll
@@ -377,7 +389,7 @@ __device__ __forceinline__ void draft_tile(const Args& a) {
     if (!live) return;
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
     const float lse2 = sum > 0.f ? m * a.sl2 + log2f(sum) : -INFINITY;
-    if (w.n_blk <= a.chunk) {
+    if (w.n_chunks == 1) {
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -398,33 +410,86 @@ __device__ __forceinline__ void draft_tile(const Args& a) {
     }
 }
 
+// A workgroup a unit: a row's chunk, KV head and tile.  Which units there are is device data: every workgroup counts
+// the rows' units up to its own, one row a thread, so none is spent on chunks and tiles that a shorter row lacks (as
+// a grid over the maxima would: 32 rows of 4 to 32 tokens of 28/4/128 heads under 500 to 6,144 keys FIGURES).
+// Units of one (row, chunk, KV head) follow each other, in runs on one XCD: they read the same keys.
 template <int D, int R>
-__global__ __launch_bounds__(kThreads, R == 1 ? 1 : 2) void draft_attn(Args a) {
-    draft_tile<D, R>(a);
+__global__ __launch_bounds__(kThreads, 2) void draft_attn(Args a) {
+    __shared__ int sums[4], found[4];
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+    const int seq = blockIdx.x >> 3, run = a.n_tiles;
+    const int unit = (seq / run) * (8 * run) + (blockIdx.x & 7) * run + seq % run;
+    if (tid == 0) found[0] = -1;
+    int64_t before = 0;
+    for (int r0 = 0; r0 < a.b.n_rows && before <= unit; r0 += kThreads) {
+        int mine = 0, tiles = 0;
+        if (r0 + tid < a.b.n_rows) {
+            const Row w = row_of(a, r0 + tid);
+            if (w.tokens) tiles = (w.L * a.G + 32 * R - 1) / (32 * R), mine = w.n_chunks * a.hkv * tiles;
+        }
+        int incl = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int u = __shfl_up(incl, o);
+            if (lane >= o) incl += u;
+        }
+        __syncthreads();
+        if (lane == 63) sums[wid] = incl;
+        __syncthreads();
+        int64_t at = before + incl - mine;
+        for (int x = 0; x < 4; ++x) {
+            if (x < wid) at += sums[x];
+            before += sums[x];
+        }
+        if (unit >= at && unit < at + mine) found[0] = r0 + tid, found[1] = static_cast<int>(unit - at), found[2] = tiles;
+    }
+    __syncthreads();
+    const int r = __builtin_amdgcn_readfirstlane(found[0]), local = __builtin_amdgcn_readfirstlane(found[1]);
+    const int tiles = __builtin_amdgcn_readfirstlane(found[2]);
+    if (r < 0) return;
+    const int g = local / tiles;
+    draft_tile<D, R>(a, row_of(a, r), g / a.hkv, g % a.hkv, local - g * tiles);
 }
 
-// o = sum_c 2^(lse_c - M) o_c / sum_c 2^(lse_c - M) over a row's chunks, D / 4 lanes per (token, head).
-template <int D>
+// o = sum_c 2^(lse_c - M) o_c / sum_c 2^(lse_c - M) over a row's chunks: P threads share the chunks of four dims of a
+// (token, head), four loads ahead, and meet through LDS.
+template <int D, int P>
 __global__ __launch_bounds__(kThreads) void draft_merge(Args a, int per_row) {
-    const int r = blockIdx.x / per_row, part = blockIdx.x - r * per_row;
-    const Row w = row_of(a.b, r);
-    if (!w.tokens || !w.table || w.n_blk <= a.chunk) return;
-    const int x = (part * kThreads + threadIdx.x) / (D / 4), c = threadIdx.x % (D / 4);
-    if (x >= w.L * a.hq) return;
-    const size_t orow = static_cast<size_t>(w.q0) * a.hq + x, step = static_cast<size_t>(a.b.n_qtok) * a.hq;
-    const int n = (w.n_blk + a.chunk - 1) / a.chunk;
+    constexpr int C = D / 4, H = kThreads / (C * P);  // (token, head) rows a workgroup
+    __shared__ f32x4_t part[P][H][C];
+    __shared__ float weight[P][H];
+    const int r = blockIdx.x / per_row, first = (blockIdx.x - r * per_row) * H;
+    const Row w = row_of(a, r);
+    if (!w.tokens || w.n_chunks == 1) return;
+    const int c = threadIdx.x % C, h = threadIdx.x / C % H, p = threadIdx.x / (C * H);
+    const bool live = first + h < w.L * a.hq;
+    const size_t orow = static_cast<size_t>(w.q0) * a.hq + min(first + h, w.L * a.hq - 1), step = static_cast<size_t>(a.b.n_qtok) * a.hq;
+    const int n = w.n_chunks;
     float top = -INFINITY;
-    for (int j = 0; j < n; ++j) top = fmaxf(top, a.plse[j * step + orow]);
+    for (int j = c; j < n; j += C) top = fmaxf(top, a.plse[j * step + orow]);
+#pragma unroll
+    for (int o = C / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const float base = top > -INFINITY ? top : 0.f;
     f32x4_t s{0.f, 0.f, 0.f, 0.f};
     float z = 0.f;
-    if (top > -INFINITY) {
-        for (int j = 0; j < n; ++j) {
-            const float e = __builtin_amdgcn_exp2f(a.plse[j * step + orow] - top);
-            const f32x4_t p = *reinterpret_cast<const f32x4_t*>(a.po + (j * step + orow) * D + 4 * c);
-            z += e;
+#pragma unroll 4
+    for (int j = p; j < n; j += P) {
+        const float e = __builtin_amdgcn_exp2f(a.plse[j * step + orow] - base);
+        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(a.po + (j * step + orow) * D + 4 * c);
+        z += e;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s[k] = fmaf(e, p[k], s[k]);
-        }
+        for (int k = 0; k < 4; ++k) s[k] = fmaf(e, v[k], s[k]);
+    }
+    part[p][h][c] = s;
+    if (c == 0) weight[p][h] = z;
+    __syncthreads();
+    if (p > 0 || !live) return;
+#pragma unroll
+    for (int q = 1; q < P; ++q) {
+        z += weight[q][h];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[k] += part[q][h][c][k];
     }
     const float inv = z > 0.f ? 1.f / z : 0.f;
     *reinterpret_cast<uint2*>(a.o + orow * D + 4 * c) = uint2{pack_bf16x2(s[0] * inv, s[1] * inv), pack_bf16x2(s[2] * inv, s[3] * inv)};
@@ -438,10 +503,14 @@ int launched(const char* fn) {
 
 template <int D, int R>
 int launch(const Args& a, hipStream_t st) {
-    const int64_t groups = static_cast<int64_t>(a.n_chunks) * a.b.n_rows * a.hkv;
-    const int64_t grid = (groups + 7) / 8 * 8 * a.n_tiles;
-    if (grid > INT32_MAX) return tkv::set_error(TKV_EINVAL, "tkv_draft_verify: %lld workgroups are too many", static_cast<long long>(grid));
-    draft_attn<D, R><<<dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, st>>>(a);
+    // as many units as every row having the longest table, or as the tables' blocks can make
+    const int64_t heads = static_cast<int64_t>(a.hkv) * a.n_tiles;
+    const int64_t most = static_cast<int64_t>(a.n_chunks) * a.b.n_rows * heads;
+    const int64_t grid = std::min(most, (a.b.n_kv_blocks / a.chunk + static_cast<int64_t>(a.b.n_rows)) * heads);
+    const int64_t run = 8 * static_cast<int64_t>(a.n_tiles), padded = (grid + run - 1) / run * run;
+    if (padded > INT32_MAX)
+        return tkv::set_error(TKV_EINVAL, "tkv_draft_verify: %lld workgroups are too many", static_cast<long long>(padded));
+    draft_attn<D, R><<<dim3(static_cast<unsigned>(padded)), dim3(kThreads), 0, st>>>(a);
     return launched("tkv_draft_verify");
 }
 
@@ -461,16 +530,25 @@ int tkv::launch_draft_verify(const tkv_shape& s, const tkv_draft_batch& b, const
     a.plse = a.po + static_cast<size_t>(a.n_chunks) * b.n_qtok * s.hq * s.d;
     int rc;
     if (s.d == 128)
-        rc = split.waves == 4 ? launch<128, 4>(a, st) : split.waves == 2 ? launch<128, 2>(a, st) : launch<128, 1>(a, st);
+        rc = split.waves == 4 ? launch<128, 4>(a, st) : launch<128, 2>(a, st);
     else
-        rc = split.waves == 4 ? launch<64, 4>(a, st) : split.waves == 2 ? launch<64, 2>(a, st) : launch<64, 1>(a, st);
+        rc = split.waves == 4 ? launch<64, 4>(a, st) : launch<64, 2>(a, st);
     if (rc != TKV_OK || a.n_chunks == 1) return rc;
-    const int per_row = (b.max_q * s.hq * (s.d / 4) + kThreads - 1) / kThreads;
-    const int64_t grid = static_cast<int64_t>(per_row) * b.n_rows;
-    if (grid > INT32_MAX) return tkv::set_error(TKV_EINVAL, "tkv_draft_verify: %d rows are too many", b.n_rows);
+    const auto merge = [&](auto kernel, int rows) -> int {  // rows: (token, head) rows a workgroup
+        const int per_row = (b.max_q * s.hq + rows - 1) / rows;
+        const int64_t grid = static_cast<int64_t>(per_row) * b.n_rows;
+        if (grid > INT32_MAX) return tkv::set_error(TKV_EINVAL, "tkv_draft_verify: %d rows are too many", b.n_rows);
+        kernel<<<dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, st>>>(a, per_row);
+        return TKV_OK;
+    };
+    // Few rows share their chunks over four threads (896 rows of 32 chunks 4.8 us, 18 us with one a row); many rows fill
+    // the chip by themselves (28,672 rows of up to 5 chunks 8.5 us, 16.7 us with four).
+    constexpr int kParts = 4;
+    const bool few = static_cast<int64_t>(b.n_qtok) * s.hq * (s.d / 4) * kParts <= 256 * 2048;
     if (s.d == 128)
-        draft_merge<128><<<dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, st>>>(a, per_row);
+        rc = few ? merge(draft_merge<128, kParts>, kThreads / (32 * kParts)) : merge(draft_merge<128, 1>, kThreads / 32);
     else
-        draft_merge<64><<<dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, st>>>(a, per_row);
+        rc = few ? merge(draft_merge<64, kParts>, kThreads / (16 * kParts)) : merge(draft_merge<64, 1>, kThreads / 16);
+    if (rc != TKV_OK) return rc;
     return launched("tkv_draft_verify (merge)");
 }
