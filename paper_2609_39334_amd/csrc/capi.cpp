@@ -1,8 +1,8 @@
 // Error reporting shared by every C entry point: a thread-local message behind tkv_last_error().
+#include <algorithm>
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
-#include <cstdlib>
 #include <string>
 
 #include "internal.h"
@@ -97,6 +97,8 @@ TKV_EXPORT int tkv_draft_mask(int32_t n, const int32_t* parent, int32_t words, u
 namespace {
 
 constexpr int32_t kMaxDraft = 1024;  // query tokens of a row
+constexpr int32_t kMinDraftChunk = 16, kLongDraftChunk = 192, kMaxDraftChunk = 256, kShortDraft = 32;  // blocks
+constexpr int64_t kFewDraftRows = 4096;
 
 int check_draft(const char* fn, const tkv_shape* s, const tkv_draft_batch* b) {
     if (const int rc = check_pool(fn, s)) return rc;
@@ -113,13 +115,37 @@ int check_draft(const char* fn, const tkv_shape* s, const tkv_draft_batch* b) {
     return TKV_OK;
 }
 
+// Tiles of 64 query rows, whose two pairs of waves share the keys, where the batch has no wider row or few rows in all
+// (one row of 32 tokens, 28/4/128 heads, 30,000 keys: 36 us against 37 with tiles of 128; 64 single tokens of 12/2/128
+// heads under 300 to 6,144 keys: 39 against 40), else 128 (32 rows of 4 to 32 tokens, 28/4/128: 64 against 70).
+// Chunks as long as they can be with a unit for every slot of the chip (two workgroups a CU for heads of 128, three
+// for 64): a unit costs about 7 us beside its stages, and one past the slots waits for a whole round (those 32 rows:
+// 484 units of up to 104 blocks 66 us, 528 of up to 93 78 us, 728 of 64 83 us).  Chunks that would pass 192 blocks
+// are cut for two rounds, or more (8 rows of 64 to 150 tokens, 32/8/128, 2,000 to 12,000 keys: 178 us with 150
+// blocks, 211 with 240).  A row's last chunk is short, so tables make more units than their blocks fill: `uneven`.
+// Where the longest table has 32 blocks the merge costs more than a split saves (64 rows under 20 to 300 keys 13.5 us,
+// 20 us in chunks of 16).
 tkv::DraftSplit draft_split(const tkv_shape& s, const tkv_draft_batch& b) {
     tkv::DraftSplit x{};
-    x.waves = getenv("DW") ? atoi(getenv("DW")) : 4;
-    x.chunk = getenv("DC") ? atoi(getenv("DC")) : 64;
-    const int64_t rows = static_cast<int64_t>(b.max_q) * (s.hq / s.hkv);
-    x.n_tiles = static_cast<int32_t>((rows + 32 * x.waves - 1) / (32 * x.waves));
-    const int64_t longest = b.max_blocks < b.n_kv_blocks ? b.max_blocks : b.n_kv_blocks;
+    const int64_t G = s.hq / s.hkv, rows = b.max_q * G;
+    x.waves = rows <= 64 || static_cast<int64_t>(b.n_qtok) * s.hq <= kFewDraftRows ? 2 : 4;
+    const int64_t tile_rows = 32 * x.waves;
+    x.n_tiles = static_cast<int32_t>((rows + tile_rows - 1) / tile_rows);
+    const double n_rows = b.n_rows > 0 ? b.n_rows : 1;
+    const double tiles = std::min<double>(x.n_tiles, std::max(1., b.n_qtok / n_rows * static_cast<double>(G) / static_cast<double>(tile_rows) + .5));
+    const double work = b.n_kv_blocks * tiles * s.hkv, uneven = .8 * n_rows * s.hkv * tiles, slots = s.d == 128 ? 512 : 768;
+    double chunk = kMaxDraftChunk;
+    for (int k = 1; k <= 64; ++k) {
+        const double units = slots * k - uneven;
+        if (units > 0 && work / units <= kLongDraftChunk) {
+            chunk = work / units;
+            break;
+        }
+    }
+    x.chunk = static_cast<int32_t>(std::min<double>(kMaxDraftChunk, std::max<double>(kMinDraftChunk, chunk)));
+    x.chunk = (x.chunk + 3) & ~3;
+    const int64_t longest = std::min(b.max_blocks, b.n_kv_blocks);
+    if (longest <= kShortDraft) x.chunk = kMaxDraftChunk;
     x.n_chunks = static_cast<int32_t>(longest > x.chunk ? (longest + x.chunk - 1) / x.chunk : 1);
     if (x.n_chunks > 1)
         x.bytes = static_cast<size_t>(x.n_chunks) * static_cast<size_t>(b.n_qtok) * static_cast<size_t>(s.hq) *

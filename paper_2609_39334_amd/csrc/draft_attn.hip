@@ -109,7 +109,8 @@ __device__ __forceinline__ Row row_of(const Args& a, int r) {
     w.tokens = w.q0 >= 0 && w.q0 <= b.n_qtok && w.L >= 1 && w.L <= b.max_q && w.L <= b.n_qtok - w.q0;
     w.table = w.kv0 >= 0 && w.kv0 <= b.n_kv_blocks && w.n_blk >= 0 && w.n_blk <= b.max_blocks && w.n_blk <= b.n_kv_blocks - w.kv0;
     w.n_chunks = w.table && w.n_blk > 0 ? (w.n_blk + a.chunk - 1) / a.chunk : 1;
-    w.chunk = w.table ? (w.n_blk + w.n_chunks - 1) / w.n_chunks : 0;
+    w.chunk = w.table ? ((w.n_blk + w.n_chunks - 1) / w.n_chunks + 3) & ~3 : 0;  // whole stages (a.chunk is a multiple of four)
+    if (w.n_chunks > 1) w.n_chunks = (w.n_blk + w.chunk - 1) / w.chunk;
     return w;
 }
 
@@ -411,8 +412,9 @@ __device__ __forceinline__ void draft_tile(const Args& a, const Row& w, int chun
 }
 
 // A workgroup a unit: a row's chunk, KV head and tile.  Which units there are is device data: every workgroup counts
-// the rows' units up to its own, one row a thread, so none is spent on chunks and tiles that a shorter row lacks (as
-// a grid over the maxima would: 32 rows of 4 to 32 tokens of 28/4/128 heads under 500 to 6,144 keys FIGURES).
+// the rows' units up to its own, one row a thread, so that no slot of the chip is held by a chunk or tile that a
+// shorter row lacks (32 rows of 4 to 32 tokens of 28/4/128 heads under 500 to 6,144 keys: 64 us, 90 with a grid over
+// the maxima).
 // Units of one (row, chunk, KV head) follow each other, in runs on one XCD: they read the same keys.
 template <int D, int R>
 __global__ __launch_bounds__(kThreads, 2) void draft_attn(Args a) {
@@ -453,12 +455,12 @@ __global__ __launch_bounds__(kThreads, 2) void draft_attn(Args a) {
 }
 
 // o = sum_c 2^(lse_c - M) o_c / sum_c 2^(lse_c - M) over a row's chunks: P threads share the chunks of four dims of a
-// (token, head), four loads ahead, and meet through LDS.
+// (token, head), and meet through LDS.
 template <int D, int P>
 __global__ __launch_bounds__(kThreads) void draft_merge(Args a, int per_row) {
     constexpr int C = D / 4, H = kThreads / (C * P);  // (token, head) rows a workgroup
-    __shared__ f32x4_t part[P][H][C];
-    __shared__ float weight[P][H];
+    __shared__ f32x4_t part[P > 1 ? P : 1][H][C];
+    __shared__ float weight[P][H], base[P][H];
     const int r = blockIdx.x / per_row, first = (blockIdx.x - r * per_row) * H;
     const Row w = row_of(a, r);
     if (!w.tokens || w.n_chunks == 1) return;
@@ -466,31 +468,63 @@ __global__ __launch_bounds__(kThreads) void draft_merge(Args a, int per_row) {
     const bool live = first + h < w.L * a.hq;
     const size_t orow = static_cast<size_t>(w.q0) * a.hq + min(first + h, w.L * a.hq - 1), step = static_cast<size_t>(a.b.n_qtok) * a.hq;
     const int n = w.n_chunks;
-    float top = -INFINITY;
-    for (int j = c; j < n; j += C) top = fmaxf(top, a.plse[j * step + orow]);
-#pragma unroll
-    for (int o = C / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float base = top > -INFINITY ? top : 0.f;
+    // eight chunks' results in flight, over a running maximum
+    constexpr int U = 8;
+    float top = -INFINITY, z = 0.f;
     f32x4_t s{0.f, 0.f, 0.f, 0.f};
-    float z = 0.f;
-#pragma unroll 4
-    for (int j = p; j < n; j += P) {
-        const float e = __builtin_amdgcn_exp2f(a.plse[j * step + orow] - base);
-        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(a.po + (j * step + orow) * D + 4 * c);
-        z += e;
+    for (int j0 = p; j0 < n; j0 += U * P) {
+        float l[U];
+        f32x4_t v[U];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s[k] = fmaf(e, v[k], s[k]);
+        for (int u = 0; u < U; ++u) {
+            const size_t at = min(j0 + u * P, n - 1) * step + orow;
+            l[u] = a.plse[at];
+            v[u] = *reinterpret_cast<const f32x4_t*>(a.po + at * D + 4 * c);
+        }
+        float now = top;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (j0 + u * P >= n) l[u] = -INFINITY;
+            now = fmaxf(now, l[u]);
+        }
+        if (now == -INFINITY) continue;
+        const float keep = __builtin_amdgcn_exp2f(top - now);
+        z *= keep;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[k] *= keep;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float e = __builtin_amdgcn_exp2f(l[u] - now);
+            z += e;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[k] = fmaf(e, v[u][k], s[k]);
+        }
+        top = now;
     }
-    part[p][h][c] = s;
-    if (c == 0) weight[p][h] = z;
-    __syncthreads();
-    if (p > 0 || !live) return;
+    if constexpr (P > 1) {
+        part[p][h][c] = s;
+        if (c == 0) weight[p][h] = z, base[p][h] = top;
+        __syncthreads();
+        if (p > 0) return;
+        float now = top;
 #pragma unroll
-    for (int q = 1; q < P; ++q) {
-        z += weight[q][h];
+        for (int q = 1; q < P; ++q) now = fmaxf(now, base[q][h]);
+        if (now > -INFINITY) {
+            const float keep = __builtin_amdgcn_exp2f(top - now);
+            z *= keep;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s[k] += part[q][h][c][k];
+            for (int k = 0; k < 4; ++k) s[k] *= keep;
+#pragma unroll
+            for (int q = 1; q < P; ++q) {
+                const float e = __builtin_amdgcn_exp2f(base[q][h] - now);
+                z = fmaf(e, weight[q][h], z);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s[k] = fmaf(e, part[q][h][c][k], s[k]);
+            }
+            top = now;
+        }
     }
+    if (!live) return;
     const float inv = z > 0.f ? 1.f / z : 0.f;
     *reinterpret_cast<uint2*>(a.o + orow * D + 4 * c) = uint2{pack_bf16x2(s[0] * inv, s[1] * inv), pack_bf16x2(s[2] * inv, s[3] * inv)};
     if (a.lse && c == 0) a.lse[orow] = z > 0.f ? (top + log2f(z)) * 0.6931471805599453f : -INFINITY;
