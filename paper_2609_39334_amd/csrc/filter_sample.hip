@@ -228,22 +228,51 @@ __device__ __forceinline__ double wave_sums(const double (&v)[N], int lane) {
     }
 }
 
-// Inclusive scan over a wave, in a fixed pattern.
-template <class T>
-__device__ __forceinline__ T wave_scan(T v, int lane) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const T u = __shfl_up(v, o);
-        if (lane >= o) v += u;
+// v of another lane by a data-parallel move (within a row of 16, or a row's last lane to the rows behind), `none` where
+// that lane does not exist or the row is not in ROWS.
+template <int CTRL, int ROWS, class T>
+__device__ __forceinline__ T moved(T v, T none) {
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+    } else {
+        const int2 x = __builtin_bit_cast(int2, v), n = __builtin_bit_cast(int2, none);
+        return __builtin_bit_cast(T, int2{__builtin_amdgcn_update_dpp(n.x, x.x, CTRL, ROWS, 0xf, false),
+                                          __builtin_amdgcn_update_dpp(n.y, x.y, CTRL, ROWS, 0xf, false)});
     }
-    return v;
+}
+// Inclusive scan over a wave (all lanes there), in a fixed pattern: within rows of 16, then the rows before.
+template <class T, class Op>
+__device__ __forceinline__ T wave_scan(T v, T none, Op op) {
+    v = op(v, moved<0x111, 0xf>(v, none));
+    v = op(v, moved<0x112, 0xf>(v, none));
+    v = op(v, moved<0x114, 0xf>(v, none));
+    v = op(v, moved<0x118, 0xf>(v, none));
+    v = op(v, moved<0x142, 0xa>(v, none));  // lane 15 to row 1, lane 47 to row 3
+    return op(v, moved<0x143, 0xc>(v, none));  // lane 31 to rows 2 and 3
+}
+template <class T>
+__device__ __forceinline__ T wave_scan(T v) {
+    return wave_scan(v, T{0}, [](T a, T b) { return a + b; });
+}
+// v of one lane, for all.
+template <class T>
+__device__ __forceinline__ T lane_of(T v, int lane) {
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+    } else {
+        const int2 x = __builtin_bit_cast(int2, v);
+        return __builtin_bit_cast(T, int2{__builtin_amdgcn_readlane(x.x, lane), __builtin_amdgcn_readlane(x.y, lane)});
+    }
+}
+__device__ __forceinline__ float wave_max(float v) {
+    return lane_of(wave_scan(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); }), 63);
 }
 
 // Exclusive scan over the workgroup and the total; `part` holds a value a wave.
 template <class T>
 __device__ __forceinline__ T block_scan(T v, T* part, T& total) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const T incl = wave_scan(v, lane);
+    const T incl = wave_scan(v);
     __syncthreads();  // part is free
     if (lane == 63) part[w] = incl;
     __syncthreads();
@@ -399,43 +428,41 @@ struct RowNumbers {
     Logits<BF16> x;
     template <class F>
     __device__ __forceinline__ void each(F f) const {
-        x.each([&](int i, float v) { f(number_of(v, i)); });
+        x.each([&](int i, float v) { f(number_of(v, i), uint64_t{0}); });
     }
 };
+// (in registers, with each number's weight in units; 0 is none)
+constexpr int kMine = 8192 / kThreads;
 struct ListNumbers {
-    const uint64_t* p;
-    int n;
+    uint64_t n[kMine], w[kMine];
     template <class F>
     __device__ __forceinline__ void each(F f) const {
-        for (int i0 = threadIdx.x; i0 < n; i0 += 8 * kThreads) {
-            uint64_t v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = p[min(i0 + e * kThreads, n - 1)];
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (i0 + e * kThreads < n) f(v[e]);
-        }
+        for (int e = 0; e < kMine; ++e)
+            if (n[e] != 0) f(n[e], w[e]);
     }
 };
 
 // The last number of the shortest run from above that reaches a target, among a source's numbers in [lo, hi]; lo if all
 // of them do not.  BY_MASS: the target is `want` units of weight, or (SHARE) that share of the whole weight in [lo, hi];
 // else a count.
+// fresh(logit): a token's weight, where the source has none.
 template <bool BY_MASS, bool SHARE, class Src, class W>
-__device__ uint64_t find_cut(Shared& s, const Src& src, const W& units, uint64_t lo, uint64_t hi, uint64_t target, double want) {
+__device__ uint64_t find_cut(Shared& s, const Src& src, const W& fresh, uint64_t lo, uint64_t hi, uint64_t target, double want) {
     const int t = threadIdx.x;
     uint64_t above_c = 0, above_m = 0;
     const uint64_t floor = lo;
+    const auto units = [&](uint64_t n, uint64_t w) { return w != 0 ? w : fresh(logit_of(n)); };
     for (bool first = true;; first = false) {
         const int bits = 64 - __builtin_clzll(hi - lo | 1), shift = bits > 11 ? bits - 11 : 0;
         __syncthreads();
         for (int i = t; i < kBins; i += kThreads) s.h.mass[i] = 0, s.h.cnt[i] = 0;
         __syncthreads();
-        src.each([&](uint64_t n) {
+        src.each([&](uint64_t n, uint64_t w) {
             if (n < lo || n > hi) return;
             const int b = static_cast<int>((n - lo) >> shift);
             atomicAdd(&s.h.cnt[b], 1u);
-            if (BY_MASS) atomicAdd(reinterpret_cast<unsigned long long*>(&s.h.mass[b]), static_cast<unsigned long long>(units(logit_of(n))));
+            if (BY_MASS) atomicAdd(reinterpret_cast<unsigned long long*>(&s.h.mass[b]), static_cast<unsigned long long>(units(n, w)));
         });
         __syncthreads();
         // thread t takes bins from the top down: kBins - 1 - per t and the next below
@@ -477,7 +504,7 @@ __device__ uint64_t find_cut(Shared& s, const Src& src, const W& units, uint64_t
         __syncthreads();
         if (t == 0) s.i0 = 0;
         __syncthreads();
-        src.each([&](uint64_t x) {
+        src.each([&](uint64_t x, uint64_t) {
             if (x >= lo && x <= hi) s.list[atomicAdd(&s.i0, 1)] = x;
         });
         sort_down(s.list, n);
@@ -486,7 +513,7 @@ __device__ uint64_t find_cut(Shared& s, const Src& src, const W& units, uint64_t
 #pragma unroll
         for (int e = 0; e < many; ++e) {
             const int i = many * t + e;
-            mine += w[e] = BY_MASS && i < n ? units(logit_of(s.list[i])) : 0;
+            mine += w[e] = BY_MASS && i < n ? fresh(logit_of(s.list[i])) : 0;
         }
         uint64_t run = above_m + block_scan(mine, s.part, total);
         if (t == 0) s.u0 = s.list[n - 1];
@@ -533,8 +560,7 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(5)
     if (samples) a.sample[id * 128 + lane] = s0, a.sample[id * 128 + 64 + lane] = s1;
     const auto finite = [](float v) { return v == -INFINITY ? INFINITY : v; };
     float low = samples ? fminf(finite(s0), finite(s1)) : finite(m);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o)), low = fminf(low, __shfl_xor(low, o));
+    m = wave_max(m), low = -wave_max(-low);
     if (lane == 0) a.tile_max[id] = make_float2(m, low);
     if (!whole) return;
     constexpr int N = Logits<BF16>::kPieces;
@@ -605,16 +631,16 @@ __device__ __forceinline__ void draw_from_tiles(Shared& s, const Args& a, int r,
         }
         b = __builtin_amdgcn_readfirstlane(b);
         const double pw = lane < L::kPieces ? part(b, lane) : 0.;
-        double incl = s.tile[b] + wave_scan(pw, lane);
+        double incl = s.tile[b] + wave_scan(pw);
         const int j = choose(pw, incl, target);
-        double start = __shfl(incl - pw, j);
+        const double start = lane_of(incl - pw, j);
         const int first = L::token(b * kTile, lane, j);
         float x[L::V];
         row.x.piece(first, x);
         double y[L::V], sum = 0.;
 #pragma unroll
         for (int q = 0; q < L::V; ++q) sum += y[q] = kept(first + q, x[q]);
-        incl = start + wave_scan(sum, lane);
+        incl = start + wave_scan(sum);
         if (lane == choose(sum, incl, target)) {
             double acc = incl - sum;
             int pick = -1, last = 0;
@@ -640,9 +666,9 @@ __device__ __forceinline__ void tile_prefixes(Shared& s, int tiles) {
     if (threadIdx.x < 64) {
         double run = 0.;
         for (int i0 = 0; i0 < tiles; i0 += 64) {
-            const double incl = run + wave_scan(i0 + lane < tiles ? s.tile[i0 + lane + 1] : 0., lane);
+            const double incl = run + wave_scan(i0 + lane < tiles ? s.tile[i0 + lane + 1] : 0.);
             if (i0 + lane < tiles) s.tile[i0 + lane + 1] = incl;
-            run = __shfl(incl, 63);
+            run = lane_of(incl, 63);
         }
         if (lane == 0) s.tile[0] = 0.;
     }
@@ -952,8 +978,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) v
         const float2 v = tm[i];
         top = fmaxf(top, v.x), low = fminf(low, v.y);
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o)), low = fminf(low, __shfl_xor(low, o));
+    top = wave_max(top), low = -wave_max(-low);
     if (lane == 0) s.red[w] = top, s.red[kWaves + w] = low;
     __syncthreads();
 #pragma unroll
@@ -1051,8 +1076,7 @@ __global__ __launch_bounds__(kScanThreads) void filter_narrow(Args a) {
                 }
             }
         }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) above += __shfl_xor(above, o);
+        above = lane_of(wave_scan(above), 63);
         const double part = wave_sums(kept, lane);
         const int64_t at = static_cast<int64_t>(g.row) * a.tiles + tile;
         if (lane == 0) a.above[at] = above;
@@ -1100,17 +1124,25 @@ __device__ bool cut_in_list(Shared& s, const Args& a, const Row<BF16>& row, cons
     cut = 0;
     if (set.p < 1.f) {
         if (g.n > a.cap) return false;
-        const ListNumbers list{a.lists + static_cast<int64_t>(g.row) * a.cap, g.n};
+        static_assert(kMine * kThreads >= 8192, "a list of any length");
+        const uint64_t* from = a.lists + static_cast<int64_t>(g.row) * a.cap;
+        ListNumbers list;
+#pragma unroll
+        for (int e = 0; e < kMine; ++e) list.n[e] = t + e * kThreads < g.n ? from[t + e * kThreads] : 0;
         double sum = 0., above;
         for (int i = t; i < a.tiles; i += kThreads) sum += a.above[at + i];
         block_scan(sum, s.partd, above);
         const double want = static_cast<double>(set.p) * g.weight - above;
         // the list's weight in units, and its smallest and largest number
         uint64_t units = 0, all, lo = ~uint64_t{0}, hi = 0;
-        list.each([&](uint64_t n) {
-            units += row.units(logit_of(n));
-            lo = n < lo ? n : lo, hi = n > hi ? n : hi;
-        });
+#pragma unroll
+        for (int e = 0; e < kMine; ++e) {
+            list.w[e] = 0;
+            if (t + e * kThreads < g.n) {
+                units += list.w[e] = row.units(logit_of(list.n[e]));
+                lo = list.n[e] < lo ? list.n[e] : lo, hi = list.n[e] > hi ? list.n[e] : hi;
+            }
+        }
         block_scan(units, s.part, all);
         if (!(want > 0.) || static_cast<double>(all) < want * kUnit) return false;
 #pragma unroll
@@ -1129,9 +1161,10 @@ __device__ bool cut_in_list(Shared& s, const Args& a, const Row<BF16>& row, cons
         lo = s.u0, hi = s.u1;
         cut = find_cut<true, false>(s, list, [&](float v) { return row.units(v); }, lo, hi, 0, want * kUnit);
         // kept tokens of the list, by part: integers, whatever their order
-        list.each([&](uint64_t n) {
+        list.each([&](uint64_t n, uint64_t) {
+            if (n < cut) return;
             const double y = row.weight(logit_of(n));
-            if (n < cut || y < bound) return;
+            if (y < bound) return;
             const int i = (1 << kIdxBits) - 1 - static_cast<int>(n & ((1 << kIdxBits) - 1));
             atomicAdd(reinterpret_cast<unsigned long long*>(&inside[i / (64 * Logits<BF16>::V)]), static_cast<unsigned long long>(y * kFine + .5));
         });
