@@ -879,6 +879,46 @@ class Plan:
         tkv_verify(self.h, q, k, v, o, lse, stream)
 
 
+class DraftBatch:
+    """The device arrays of a drafted batch for tkv_draft_verify, in one upload: row r's block table (its last keys are the
+    drafted tokens), the parents of its drafted tokens (earlier ones, or -1 for the context), and every block's length.
+    A batch serves every layer.  positions, depth: each token's position in its path (int64, device) and its
+    number of drafted ancestors (host)."""
+
+    def __init__(self, tables, parents, block_len, device="cuda"):
+        if len(tables) != len(parents):
+            raise ValueError("DraftBatch: a table and a tree for every row")
+        lens, n_blk = [len(p) for p in parents], [len(t) for t in tables]
+        bl = _i32(block_len)
+        self.max_q, self.max_blocks = max(lens, default=1), max(n_blk, default=1)
+        if any(n < 1 for n in lens):
+            raise ValueError("DraftBatch: every row needs a drafted token")
+        words = -(-self.max_q // 64)
+        trees = [tkv_draft_mask(p, words) for p in parents]
+        self.depth = np.concatenate([d for _, d in trees]) if trees else np.zeros(0, np.int32)
+        kv = np.concatenate([_i32(t) for t in tables]) if tables else np.zeros(0, np.int32)
+        if len(kv) and (kv.min() < 0 or kv.max() >= len(bl)):
+            raise ValueError("DraftBatch: a table names a block outside block_len")
+        context = [int(bl[_i32(t)].sum()) - n for t, n in zip(tables, lens)]
+        if any(c < 0 for c in context):
+            raise ValueError("DraftBatch: a row's path is shorter than its draft")
+        positions = np.repeat(np.asarray(context, np.int64), lens) + self.depth
+        mask = np.concatenate([m for m, _ in trees]) if trees else np.zeros((0, words), np.uint64)
+        parts = [positions.astype(np.int64).view(np.int32), mask.view(np.int32).reshape(-1),
+                 np.cumsum([0] + lens).astype(np.int32), np.cumsum([0] + n_blk).astype(np.int32), kv, bl]
+        flat = torch.from_numpy(np.concatenate(parts)).to(device)
+        at = np.cumsum([0] + [len(p) for p in parts])
+        cut = [flat[a:b] for a, b in zip(at[:-1], at[1:])]
+        n = len(positions)
+        self.positions = cut[0].view(torch.int64) if n else torch.zeros(0, dtype=torch.int64, device=device)
+        self.mask = cut[1].view(torch.int64).view(n, words) if n else torch.zeros((0, words), dtype=torch.int64, device=device)
+        self.q_indptr, self.kv_indptr, self.kv_blocks, self.block_len = cut[2:]
+
+    def verify(self, q, k, v, o, lse=None, workspace=None, stream=None):
+        tkv_draft_verify(self.q_indptr, self.kv_indptr, self.kv_blocks, self.block_len, self.mask, self.max_q, self.max_blocks,
+                         q, k, v, o, lse, workspace, stream)
+
+
 class Search:
     """Owns a tkv_search handle (speculative beam-search controller); methods forward to the C
     entry points."""
