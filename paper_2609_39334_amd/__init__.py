@@ -470,44 +470,48 @@ def tkv_rope_append(qkv: torch.Tensor, cos: torch.Tensor, sin: torch.Tensor, dst
 
 
 class _Call:
-    """The device and stream of a call on `device`'s tensors: its outputs and workspaces are allocated for that stream,
-    and its work is enqueued there (the current stream of the tensors' device without a stream; never the
-    current device's, if that is another)."""
+    """The device and stream of a call: its outputs and workspaces are allocated for that stream, and its work is enqueued
+    there (the current stream of the tensors' device without a stream; never the current device's, if that is
+    another)."""
+    __slots__ = ("index", "device", "side", "handle")
 
-    def __init__(self, fn: str, device: torch.device, stream):
-        self.device = device
-        self.current = torch.cuda.current_stream(device)
+    def __init__(self, fn: str, pool: torch.Tensor, stream):
+        self.index, self.device = pool.get_device(), pool.device
+        self.handle = torch.cuda.current_stream(self.device).cuda_stream
+        self.side = None  # another stream than the current one
         if stream is None:
-            self.stream = self.current
-        elif hasattr(stream, "cuda_stream"):
-            self.stream = stream
-            if stream.device != device:
-                raise ValueError(f"{fn}: the stream is {stream.device}'s, the tensors are on {device}")
+            return
+        if hasattr(stream, "cuda_stream"):
+            if stream.device != self.device:
+                raise ValueError(f"{fn}: the stream is {stream.device}'s, the tensors are on {self.device}")
         else:
-            self.stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
-        self.handle = self.stream.cuda_stream
-        self.side = self.handle != self.current.cuda_stream
+            stream = torch.cuda.ExternalStream(stream, device=self.device) if stream else torch.cuda.default_stream(self.device)
+        if stream.cuda_stream != self.handle:
+            self.side, self.handle = stream, stream.cuda_stream
 
     def empty(self, shape, dtype) -> torch.Tensor:
-        if not self.side:
+        if self.side is None:
             return torch.empty(shape, dtype=dtype, device=self.device)
-        with torch.cuda.stream(self.stream):
+        with torch.cuda.stream(self.side):
             t = torch.empty(shape, dtype=dtype, device=self.device)
-        t.record_stream(self.current)  # not handed out again before the current stream's work so far, and later reads
+        # not handed out again before the current stream's work so far, and its later reads
+        t.record_stream(torch.cuda.current_stream(self.device))
         return t
 
     def run(self, entry, *args) -> None:
-        if torch.cuda.current_device() == self.device.index:
+        if torch.cuda.current_device() == self.index:
             _check(entry(*args, self.handle))
         else:
             with torch.cuda.device(self.device):
                 _check(entry(*args, self.handle))
 
 
-def _on_device(fn: str, device: torch.device, **tensors) -> None:
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{fn}: {name} is on {t.device}, not on {device}")
+def _tensors(fn: str, index: int, *specs) -> None:
+    """Checks (name, tensor, dtype, shape): contiguous, of that type and shape, on GPU `index`."""
+    for name, t, dtype, shape in specs:
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != index or index < 0 or not t.is_contiguous():
+            raise ValueError(f"{fn}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on GPU {max(index, 0)}, got "
+                             f"{t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
 
 
 def tkv_norm_rope_append(qkv: torch.Tensor, q_weight: torch.Tensor, k_weight: torch.Tensor, eps: float,
@@ -522,19 +526,16 @@ def tkv_norm_rope_append(qkv: torch.Tensor, q_weight: torch.Tensor, k_weight: to
     nb, hkv, bs, d = k.shape
     n, half = int(dst.numel()), int(cos.shape[1])
     width = (hq + 2 * hkv) * d
-    if (qkv.dtype != torch.bfloat16 or tuple(qkv.shape) != (n, width) or not qkv.is_cuda
+    if (qkv.dtype is not torch.bfloat16 or qkv.shape != (n, width) or qkv.get_device() != k.get_device()
             or (n and (qkv.stride(1) != 1 or (n > 1 and qkv.stride(0) < width)))):
-        raise ValueError(f"{fn}: qkv must be a bfloat16 GPU tensor of shape {(n, width)} with contiguous rows, got "
-                         f"{qkv.dtype} {tuple(qkv.shape)}, strides {qkv.stride()}")
-    _expect(fn, "q_weight", q_weight, torch.float32, (d,))
-    _expect(fn, "k_weight", k_weight, torch.float32, (d,))
-    _expect(fn, "cos", cos, torch.float32, (n, half))
-    _expect(fn, "sin", sin, torch.float32, (n, half))
-    _expect(fn, "k", k, torch.bfloat16, k.shape)
-    _expect(fn, "v", v, torch.bfloat16, k.shape)
-    _expect(fn, "dst", dst, torch.int32, dst.shape)
-    _on_device(fn, k.device, qkv=qkv, q_weight=q_weight, k_weight=k_weight, cos=cos, sin=sin, dst=dst, v=v)
-    call = _Call(fn, k.device, stream)
+        raise ValueError(f"{fn}: qkv must be a bfloat16 tensor of shape {(n, width)} with contiguous rows on the pools' GPU, got "
+                         f"{qkv.dtype} {tuple(qkv.shape)}, strides {qkv.stride()}, on {qkv.device}")
+    index = k.get_device()
+    pool = k.shape
+    _tensors(fn, index, ("k", k, torch.bfloat16, pool), ("v", v, torch.bfloat16, pool), ("q_weight", q_weight, torch.float32, (d,)),
+             ("k_weight", k_weight, torch.float32, (d,)), ("cos", cos, torch.float32, (n, half)),
+             ("sin", sin, torch.float32, (n, half)), ("dst", dst, torch.int32, dst.shape))
+    call = _Call(fn, k, stream)
     q = call.empty((n, hq, d), torch.bfloat16)
     shape = tkv_shape(hq, hkv, d, bs, nb)
     call.run(lib().tkv_norm_rope_append, ctypes.byref(shape), n, qkv.data_ptr(), qkv.stride(0) if n > 1 else width,
@@ -579,20 +580,16 @@ def tkv_draft_verify(q_indptr: torch.Tensor, kv_indptr: torch.Tensor, kv_blocks:
     nb, hkv, bs, d = k.shape
     n, hq, words = q.shape[0], q.shape[1], mask.shape[1]
     n_rows, n_kv = q_indptr.numel() - 1, kv_blocks.numel()
-    _expect(fn, "q", q, torch.bfloat16, (n, hq, d))
-    _expect(fn, "k", k, torch.bfloat16, k.shape)
-    _expect(fn, "v", v, torch.bfloat16, k.shape)
-    _expect(fn, "o", o, torch.bfloat16, q.shape)
-    _expect(fn, "q_indptr", q_indptr, torch.int32, (max(0, n_rows) + 1,))
-    _expect(fn, "kv_indptr", kv_indptr, torch.int32, (n_rows + 1,))
-    _expect(fn, "kv_blocks", kv_blocks, torch.int32, (n_kv,))
-    _expect(fn, "block_len", block_len, torch.int32, (nb,))
-    _expect(fn, "mask", mask, torch.int64, (n, words))
+    index, pool, head = k.get_device(), k.shape, q.shape
+    _tensors(fn, index, ("k", k, torch.bfloat16, pool), ("v", v, torch.bfloat16, pool), ("q", q, torch.bfloat16, head),
+             ("o", o, torch.bfloat16, head), ("q_indptr", q_indptr, torch.int32, (max(0, n_rows) + 1,)),
+             ("kv_indptr", kv_indptr, torch.int32, (n_rows + 1,)), ("kv_blocks", kv_blocks, torch.int32, (n_kv,)),
+             ("block_len", block_len, torch.int32, (nb,)), ("mask", mask, torch.int64, (n, words)))
     if lse is not None:
-        _expect(fn, "lse", lse, torch.float32, (n, hq))
-    _on_device(fn, k.device, q=q, v=v, o=o, q_indptr=q_indptr, kv_indptr=kv_indptr, kv_blocks=kv_blocks, block_len=block_len,
-               mask=mask, lse=lse, workspace=workspace)
-    call = _Call(fn, k.device, stream)
+        _tensors(fn, index, ("lse", lse, torch.float32, (n, hq)))
+    if workspace is not None and (workspace.get_device() != index or not workspace.is_contiguous()):
+        raise ValueError(f"{fn}: workspace must be contiguous, on GPU {index}")
+    call = _Call(fn, k, stream)
     sh = tkv_shape(hq, hkv, d, bs, nb)
     batch = tkv_draft_batch(n_rows, n, int(max_q), n_kv, int(max_blocks), words, q_indptr.data_ptr(), kv_indptr.data_ptr(),
                             kv_blocks.data_ptr(), block_len.data_ptr(), mask.data_ptr())
@@ -600,8 +597,6 @@ def tkv_draft_verify(q_indptr: torch.Tensor, kv_indptr: torch.Tensor, kv_blocks:
     _check(lib().tkv_draft_workspace_bytes(ctypes.byref(sh), ctypes.byref(batch), ctypes.byref(need)))
     if workspace is None and need.value:
         workspace = call.empty((need.value,), torch.uint8)
-    elif workspace is not None and not workspace.is_contiguous():
-        raise ValueError(f"{fn}: workspace must be contiguous")
     call.run(lib().tkv_draft_verify, ctypes.byref(sh), ctypes.byref(batch), q.data_ptr(), k.data_ptr(), v.data_ptr(),
              o.data_ptr(), None if lse is None else lse.data_ptr(), None if workspace is None else workspace.data_ptr(),
              0 if workspace is None else workspace.numel() * workspace.element_size())
@@ -655,23 +650,19 @@ def tkv_filter_sample(logits: torch.Tensor, temperature: torch.Tensor, draw_off:
             or (logits.shape[0] > 1 and logits.stride(0) < logits.shape[1])):
         raise ValueError(f"{fn}: logits must be a float32 or bfloat16 GPU tensor [n_rows, vocab] with contiguous rows")
     n_rows, vocab = logits.shape
-    _expect(fn, "temperature", temperature, torch.float32, (n_rows,))
-    _expect(fn, "draw_off", draw_off, torch.int32, (n_rows + 1,))
-    n = int(uniform.numel())
-    _expect(fn, "uniform", uniform, torch.float32, (n,))
+    index, n = logits.get_device(), uniform.numel()
+    _tensors(fn, index, ("temperature", temperature, torch.float32, (n_rows,)), ("draw_off", draw_off, torch.int32, (n_rows + 1,)),
+             ("uniform", uniform, torch.float32, (n,)))
     for name, t, dtype in (("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
         if t is not None:
-            _expect(fn, name, t, dtype, (n_rows,))
-    _on_device(fn, logits.device, temperature=temperature, draw_off=draw_off, uniform=uniform, top_k=top_k, top_p=top_p,
-               min_p=min_p, workspace=workspace)
-    call = _Call(fn, logits.device, stream)
+            _tensors(fn, index, (name, t, dtype, (n_rows,)))
+    if workspace is not None and (workspace.get_device() != index or not workspace.is_contiguous()):
+        raise ValueError(f"{fn}: workspace must be contiguous, on GPU {index}")
+    call = _Call(fn, logits, stream)
     need = tkv_filter_sample_workspace_bytes(n_rows, vocab)
     if workspace is None and need:
         workspace = call.empty((need,), torch.uint8)
-    elif workspace is not None and not workspace.is_contiguous():
-        raise ValueError(f"{fn}: workspace must be contiguous")
-    tok, cnt = call.empty((n,), torch.int32), call.empty((n,), torch.int32)
-    ng = call.empty((n_rows,), torch.int32)
+    tok, cnt, ng = call.empty((n,), torch.int32), call.empty((n,), torch.int32), call.empty((n_rows,), torch.int32)
 
     def ptr(t):
         return None if t is None else t.data_ptr()
