@@ -147,11 +147,31 @@ __global__ __launch_bounds__(kThreads) void rope_append(int64_t n_pieces, int hq
     *reinterpret_cast<uint4*>(out + D / 2 + 8 * c) = ob;
 }
 
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+template <bool STREAM>
+__device__ __forceinline__ uint4 load16(const uint16_t* p) {
+    const u32x4_t* from = reinterpret_cast<const u32x4_t*>(p);
+    return __builtin_bit_cast(uint4, STREAM ? __builtin_nontemporal_load(from) : *from);
+}
+template <bool STREAM>
+__device__ __forceinline__ void store16(uint16_t* p, uint4 v) {
+    u32x4_t* to = reinterpret_cast<u32x4_t*>(p);
+    if constexpr (STREAM)
+        __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, v), to);
+    else
+        *to = __builtin_bit_cast(u32x4_t, v);
+}
+
 // Norm of each query and key head, rotation and append in one pass over qkv.  D / 16 lanes per head, 16 elements
 // each: the lane's two chunks of eight are chunks j and j + rot / 16 where they rotate together (j < rot / 16), and
 // the next two of the rest past it.  The sum of squares is 16 terms in a lane and log2(D / 16) exchanges; the
 // normed values stay in fp32 through the rotation and are rounded once.
-template <int D>
+// What bounds it: memory.  16,480 tokens of 32/8/128 heads, a fifth of them without a slot (387 MB): 65 us, 5.9 TB/s; 72 us
+// through the caches.  STREAM: heads are read and written past the caches, for calls of 256 MiB and more, as
+// kv_append is (254 MB of such heads run at 6.2 TB/s through them); heads of 64 gain nothing from it (422 MB 88 us
+// either way).
+template <int D, bool STREAM>
 __global__ __launch_bounds__(kThreads) void norm_rope_append(
     int64_t n_pieces, int hq, int hkv, int32_t n_slots, int64_t stride, int rot, float eps, const uint16_t* __restrict__ qkv,
     const float* __restrict__ wq, const float* __restrict__ wk, const float* __restrict__ cosv, const float* __restrict__ sinv,
@@ -177,7 +197,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append(
     const bool turns = j < rot / 16;
     const int e0 = turns ? 8 * j : 16 * j, e1 = turns ? e0 + rot / 2 : e0 + 8;
     const uint16_t* in = qkv + t * stride + static_cast<int64_t>(h) * D;
-    uint4 oa = *reinterpret_cast<const uint4*>(in + e0), ob = *reinterpret_cast<const uint4*>(in + e1);
+    uint4 oa = load16<STREAM>(in + e0), ob = load16<STREAM>(in + e1);
     if (h < hq + hkv) {
         const uint32_t ua[4] = {oa.x, oa.y, oa.z, oa.w}, ub[4] = {ob.x, ob.y, ob.z, ob.w};
         float a[8], b[8], sq = 0.f;
@@ -214,8 +234,8 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append(
         oa = uint4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(a[4], a[5]), pack_bf16x2(a[6], a[7])};
         ob = uint4{pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3]), pack_bf16x2(b[4], b[5]), pack_bf16x2(b[6], b[7])};
     }
-    *reinterpret_cast<uint4*>(out + e0) = oa;
-    *reinterpret_cast<uint4*>(out + e1) = ob;
+    store16<STREAM>(out + e0, oa);
+    store16<STREAM>(out + e1, ob);
 }
 
 // SiLU(g) u = g / (1 + exp(-g)) u.  exp(-g) is 2^n 2^f: g has the 8 significant bits of bf16 and kHi 13, so
@@ -321,7 +341,8 @@ int tkv::launch_norm_rope_append(const tkv_shape& s, int32_t n_tok, const void* 
     const int64_t n = static_cast<int64_t>(n_tok) * (static_cast<int64_t>(s.hq) + 2 * static_cast<int64_t>(s.hkv)) * (s.d / 16);
     const int64_t grid = (n + kThreads - 1) / kThreads;
     if (grid > kMaxGrid) return tkv::set_error(TKV_EINVAL, "tkv_norm_rope_append: %d tokens are too many", n_tok);
-    const auto kernel = s.d == 128 ? norm_rope_append<128> : norm_rope_append<64>;
+    const bool stream_past = 64 * n >= int64_t{256} << 20;  // (a lane reads 32 bytes and writes 32)
+    const auto kernel = s.d == 64 ? norm_rope_append<64, false> : stream_past ? norm_rope_append<128, true> : norm_rope_append<128, false>;
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, static_cast<hipStream_t>(stream), n, s.hq,
                        s.hkv, s.num_blocks * s.block_size, stride, rot, eps, static_cast<const uint16_t*>(qkv), wq, wk, cosv,
                        sinv, dst, static_cast<uint16_t*>(q), static_cast<uint16_t*>(k), static_cast<uint16_t*>(v));

@@ -46,7 +46,8 @@ constexpr int kSparseFew = 384;       // and for top-p and min-p, past which fil
 constexpr int kHist = 1024;           // bins of the runs' maxima and of the sample
 constexpr int kMaxTiles = (1 << kIdxBits) / kTile;
 constexpr int kMaxPotential = 1024;
-constexpr double kUnit = 4398046511104.0;  // 2^42
+constexpr double kUnit = 4398046511104.0;     // 2^42: units of weights that histograms add up (2^21 of 1 at most)
+constexpr double kFine = 1125899906842624.0;  // 2^50: of a list's kept weights (8,192 of 1 at most)
 
 typedef float f32x4_t __attribute__((ext_vector_type(4), aligned(4)));        // rows may start at any element
 typedef uint16_t u16x8_t __attribute__((ext_vector_type(8), aligned(2)));
@@ -400,7 +401,11 @@ struct Shared {
             };
             uint32_t hits[kList / 2];  // draws of each kept token, 16 bits each
         };
-        double tile[kMaxTiles + 1];  // the draws' tile prefixes
+        struct {
+            double tile[kMaxTiles + 1];   // the draws' tile prefixes
+            double want[kMaxPotential];   // each draw's target past its part's start
+            uint32_t found[kMaxPotential];  // and its token's complement
+        };
     };
     uint64_t part[kWaves];
     double partd[kWaves];
@@ -448,7 +453,7 @@ struct ListNumbers {
 // else a count.
 // fresh(logit): a token's weight, where the source has none.
 template <bool BY_MASS, bool SHARE, class Src, class W>
-__device__ uint64_t find_cut(Shared& s, const Src& src, const W& fresh, uint64_t lo, uint64_t hi, uint64_t target, double want) {
+__device__ __forceinline__ uint64_t find_cut(Shared& s, const Src& src, const W& fresh, uint64_t lo, uint64_t hi, uint64_t target, double want) {
     const int t = threadIdx.x;
     uint64_t above_c = 0, above_m = 0;
     const uint64_t floor = lo;
@@ -604,21 +609,16 @@ __device__ __forceinline__ void write_groups(Shared& s, const Args& a, int r, in
     if (t == 0) a.n_groups[r] = static_cast<int32_t>(groups);
 }
 
-// Draws over the tiles' prefixes in s.tile, one wave a draw: its tile, the part (by part(tile, j), its weight), the lane
-// that has it, the token.
+// Draws over the tiles' prefixes in s.tile, and the parts' weights part(tile, j).  A sum that rounding leaves short of the
+// target falls to the last one with a weight.
 template <bool BF16, class P, class F>
 __device__ __forceinline__ void draw_from_tiles(Shared& s, const Args& a, int r, const Row<BF16>& row, const Settings& set, P part, F kept) {
     using L = Logits<BF16>;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int tiles = a.tiles;
     const double total = s.tile[tiles];
-    // the first of the lanes with a weight whose inclusive sum is past the target, else the last with a weight
-    const auto choose = [&](double weight, double incl, double target) {
-        const uint64_t has = __builtin_amdgcn_ballot_w64(weight > 0.);
-        const uint64_t past = has & __builtin_amdgcn_ballot_w64(incl > target);
-        return past ? __builtin_ctzll(past) : has ? 63 - __builtin_clzll(has) : 0;
-    };
-    for (int d = w; d < set.n; d += kWaves) {
+    // a thread a draw: its tile and part
+    for (int d = threadIdx.x; d < set.n; d += kThreads) {
         const double target = static_cast<double>(a.uniform[set.off + d]) * total;
         int b = 0, e = tiles;  // the first tile that ends past the target
         while (b < e) {
@@ -629,32 +629,61 @@ __device__ __forceinline__ void draw_from_tiles(Shared& s, const Args& a, int r,
             b = tiles - 1;
             while (b > 0 && !(s.tile[b + 1] > s.tile[b])) --b;
         }
-        b = __builtin_amdgcn_readfirstlane(b);
-        const double pw = lane < L::kPieces ? part(b, lane) : 0.;
-        double incl = s.tile[b] + wave_scan(pw);
-        const int j = choose(pw, incl, target);
-        const double start = lane_of(incl - pw, j);
-        const int first = L::token(b * kTile, lane, j);
-        float x[L::V];
-        row.x.piece(first, x);
-        double y[L::V], sum = 0.;
+        double weight[L::kPieces], run = s.tile[b], start = run;
 #pragma unroll
-        for (int q = 0; q < L::V; ++q) sum += y[q] = kept(first + q, x[q]);
-        incl = start + wave_scan(sum);
-        if (lane == choose(sum, incl, target)) {
-            double acc = incl - sum;
-            int pick = -1, last = 0;
+        for (int j = 0; j < L::kPieces; ++j) weight[j] = part(b, j);
+        int in = 0;
+        bool past = false;
 #pragma unroll
-            for (int q = 0; q < L::V; ++q) {
-                acc += y[q];
-                if (y[q] > 0.) {
-                    last = first + q;
-                    if (pick < 0 && acc > target) pick = last;
+        for (int j = 0; j < L::kPieces; ++j) {
+            if (!past && weight[j] > 0.) in = j, start = run;
+            run += weight[j];
+            past = past || (weight[j] > 0. && run > target);
+        }
+        s.draw[d] = static_cast<uint32_t>(b * L::kPieces + in);
+        s.want[d] = target - start;
+    }
+    __syncthreads();
+    // a wave a draw, two on their way at once: the lane that has it, and the token
+    constexpr int kAtOnce = 2;
+    for (int d0 = w; d0 < set.n; d0 += kAtOnce * kWaves) {
+        int first[kAtOnce];
+        float x[kAtOnce][L::V];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int p = __builtin_amdgcn_readfirstlane(static_cast<int>(s.draw[min(d0 + u * kWaves, set.n - 1)]));
+            first[u] = (p * 64 + lane) * L::V;
+            row.x.piece(first[u], x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int d = d0 + u * kWaves;
+            if (d >= set.n) break;
+            const double target = s.want[d];
+            double y[L::V], sum = 0.;
+#pragma unroll
+            for (int q = 0; q < L::V; ++q) sum += y[q] = kept(first[u] + q, x[u][q]);
+            const double incl = wave_scan(sum);
+            const uint64_t has = __builtin_amdgcn_ballot_w64(sum > 0.);
+            const uint64_t past = has & __builtin_amdgcn_ballot_w64(incl > target);
+            const int who = past ? __builtin_ctzll(past) : has ? 63 - __builtin_clzll(has) : 0;
+            if (lane == who) {
+                double acc = incl - sum;
+                int pick = -1, last = 0;
+#pragma unroll
+                for (int q = 0; q < L::V; ++q) {
+                    acc += y[q];
+                    if (y[q] > 0.) {
+                        last = first[u] + q;
+                        if (pick < 0 && acc > target) pick = last;
+                    }
                 }
+                s.found[d] = ~static_cast<uint32_t>(pick >= 0 ? pick : last);
             }
-            s.draw[d] = ~static_cast<uint32_t>(pick >= 0 ? pick : last);
         }
     }
+    __syncthreads();
+    for (int d = threadIdx.x; d < set.n; d += kThreads) s.draw[d] = s.found[d];
     __syncthreads();
     write_groups(s, a, r, set.off, set.n);
 }
@@ -1082,7 +1111,7 @@ __global__ __launch_bounds__(kScanThreads) void filter_narrow(Args a) {
         if (lane == 0) a.above[at] = above;
         if (lane % (64 / L::kPieces) == 0) a.kept[at * L::kPieces + lane / (64 / L::kPieces)] = part;
         int base = append(&a.again[d].n, in);
-        // (few of a lane's 32, so read again from the cache rather than picked out of the registers one by one)
+        // (few of a lane's 32, read again from the cache: 38 us of 129 rows of 151,936, 45 us picked out of the registers)
         uint64_t* list = a.lists + static_cast<int64_t>(g.row) * a.cap;
         for (; in != 0; in &= in - 1, ++base) {
             const int q = __builtin_ctz(in), i = L::token(tile * kTile, lane, q / L::V) + q % L::V;
@@ -1111,7 +1140,6 @@ __device__ __forceinline__ void sum_parts(const Args& a, const Row<BF16>& row, d
     }
 }
 
-constexpr double kFine = 1125899906842624.0;  // 2^50: units of a list's kept weights (at most 8,192 of weight 1)
 
 // The threshold of a row that filter_narrow has read, and the kept weight of its list in each part (`inside`, zero
 // before); false if the threshold is not in the list.
