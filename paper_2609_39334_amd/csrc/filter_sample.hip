@@ -619,7 +619,9 @@ __device__ __forceinline__ void draw_from_tiles(Shared& s, const Args& a, int r,
     const double total = s.tile[tiles];
     // a thread a draw: its tile and part
     for (int d = threadIdx.x; d < set.n; d += kThreads) {
-        const double target = static_cast<double>(a.uniform[set.off + d]) * total;
+        // (at least 2^-1000, total being 1 or more: a uniform of 0 passes over a tile whose weight is positive only as a
+        // sum, its tokens' own weights having rounded to 0)
+        const double target = fmax(static_cast<double>(a.uniform[set.off + d]) * total, 0x1p-1000);
         int b = 0, e = tiles;  // the first tile that ends past the target
         while (b < e) {
             const int mid = (b + e) >> 1;

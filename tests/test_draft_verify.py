@@ -354,6 +354,51 @@ def test_a_workspace_of_the_callers():
 
 
 @pytest.mark.gpu
+def test_hundreds_of_rows():
+    # more rows than a workgroup counts at once, empty ones among them
+    rng = np.random.default_rng(5)
+    b = Batch([(int(c), int(L)) for c, L in zip(rng.integers(0, 90, 700), rng.integers(1, 6, 700))], 12, 2, 128)
+    b.check(*b.run(), rows=list(range(0, 700, 23)) + [255, 256, 511, 512, 699])
+    b = Batch([(int(c), 1) for c in rng.integers(0, 90, 600)] + [(5000, 3)] * 2, 8, 2, 64)   # with a split
+    b.check(*b.run(), rows=list(range(0, 600, 37)) + [600, 601])
+
+
+@pytest.mark.gpu
+def test_two_graphs_replayed_in_turn_and_two_streams_at_once():
+    batches = [Batch([(3000, 9), (500, 3)], 12, 2, 128, seed=s) for s in (1, 2)]
+    want = [b.run() for b in batches]
+    graphs, got = [torch.cuda.CUDAGraph() for _ in batches], []
+    for graph, b in zip(graphs, batches):
+        with torch.cuda.graph(graph):
+            got.append(b.run())
+    for _ in range(3):
+        for graph in graphs:
+            graph.replay()
+        eager = batches[0].run()
+        torch.cuda.synchronize()
+        for g, w in zip(got + [eager], want + [want[0]]):
+            assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])
+            g[0].zero_()
+    streams = [torch.cuda.Stream() for _ in batches]
+    for _ in range(5):
+        outs = [(torch.empty_like(b.q), torch.empty(b.q.shape[:2], device="cuda")) for b in batches]
+        torch.cuda.synchronize()
+        for b, s, (o, z) in zip(batches, streams, outs):
+            b.run(stream=s, o=o, lse=z)
+        torch.cuda.synchronize()
+        assert all(torch.equal(g[0], w[0]) and torch.equal(g[1], w[1]) for g, w in zip(outs, want))
+
+
+@pytest.mark.gpu
+def test_tables_of_the_largest_capacity():
+    # maxima and arrays far above what the rows use (a captured call's capacity)
+    b = Batch([(300, 5), (90, 2)], 28, 4, 128)
+    spare = torch.zeros(20000, dtype=torch.int32, device="cuda")
+    o, lse = b.run(kv_blocks=torch.cat([b.dev["kv_blocks"], spare]), max_blocks=4000, max_q=64)
+    b.check(o, lse)
+
+
+@pytest.mark.gpu
 def test_tensors_are_checked():
     b = Batch([(30, 4)], 8, 2, 64)
     for name, bad in (("q", b.q.float()), ("k", b.k.transpose(1, 2)), ("v", b.v[1:]), ("mask", b.dev["mask"][:, 0]),

@@ -172,6 +172,17 @@ def test_uniforms_at_the_ends():
 
 
 @pytest.mark.gpu
+def test_a_uniform_of_zero_and_weights_that_round_to_zero():
+    # the first tile's weights are below the smallest 64-bit number each (e^-746), though not as a sum
+    for vocab, m in ((9000, None), (100000, None), (100000, 1e-30)):
+        x = torch.zeros((2, vocab), device="cuda")
+        x[:, :2048] = -746.0
+        x[:, 0] = float("-inf")
+        x[:, 2048:2050] = torch.tensor([-746.0, -100.0], device="cuda")
+        _check(x, [1.0, 1.0], None, None, None if m is None else [m, m], [1, 2], us=[0.0, 0.0, 0.5])
+
+
+@pytest.mark.gpu
 def test_temperatures_at_the_ends():
     x = _logits("normal", 8, 3001, torch.float32)
     T = [1e-45, 1e-30, 1e-3, 0.05, 100.0, 1e6, 1e30, 3e38]
@@ -249,6 +260,68 @@ def test_other_streams_and_replays():
         want = call()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.gpu
+def test_more_rows_read_again_than_workgroups():
+    # 1,100 rows whose top-p keeps thousands of tokens, and a top-k past the runs that are looked into
+    rows, vocab = 1100, 8200
+    x = _logits("normal", rows, vocab, torch.bfloat16)
+    k = np.where(np.arange(rows) % 11 == 0, 3500, 0)
+    off, us, tok, cnt, ng = _run(x, np.full(rows, 1.0), k, np.full(rows, 0.95), None, [2] * rows)
+    host = x.float().cpu().numpy()
+    for r in list(range(0, rows, 61)) + list(range(1020, 1100, 7)):
+        t, c = _plain(host[r], 1.0, k[r], 0.95, 0.0, us[2 * r:2 * r + 2])
+        assert tok[2 * r:2 * r + ng[r]].tolist() == t.tolist() and cnt[2 * r:2 * r + ng[r]].tolist() == c.tolist(), r
+
+
+@pytest.mark.gpu
+def test_a_workspace_of_the_callers():
+    x = _logits("normal", 9, 20000, torch.float32)
+    T, p = torch.ones(9, device="cuda"), torch.full((9,), 0.9, device="cuda")
+    off, u = torch.arange(10, dtype=torch.int32, device="cuda") * 2, torch.rand(18, device="cuda")
+    want = tkv.tkv_filter_sample(x, T, off, u, 2, None, p)
+    n = tkv.tkv_filter_sample_workspace_bytes(9, 20000)
+    ws = torch.full((n + 64,), 0xA5, dtype=torch.uint8, device="cuda")
+    for _ in range(2):                                               # what it holds before a call does not matter
+        got = tkv.tkv_filter_sample(x, T, off, u, 2, None, p, workspace=ws[16:16 + n])
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert bool((ws[:16] == 0xA5).all()) and bool((ws[16 + n:] == 0xA5).all())
+    for bad in (ws[:n - 1], ws[1:n + 1], ws[:0]):
+        with pytest.raises(tkv.TkvError):
+            tkv.tkv_filter_sample(x, T, off, u, 2, None, p, workspace=bad)
+    with pytest.raises(ValueError):
+        tkv.tkv_filter_sample(x, T, off, u, 2, None, p, workspace=ws.cpu())
+
+
+@pytest.mark.gpu
+def test_two_graphs_replayed_in_turn_and_two_streams_at_once():
+    sets = []
+    for seed, vocab in ((1, 30000), (2, 30000)):
+        x = _logits("normal", 40, vocab, torch.float32, seed=seed)
+        T, p = torch.full((40,), 0.9, device="cuda"), torch.full((40,), 0.8, device="cuda")
+        off = torch.arange(41, dtype=torch.int32, device="cuda") * 3
+        u = torch.rand(120, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda")
+        sets.append((x, T, off, u, 3, None, p))
+    want = [tkv.tkv_filter_sample(*a) for a in sets]
+    graphs, got = [torch.cuda.CUDAGraph() for _ in sets], []
+    for graph, a in zip(graphs, sets):
+        with torch.cuda.graph(graph):
+            got.append(tkv.tkv_filter_sample(*a))
+    for _ in range(3):
+        for g in got:
+            g[0].zero_()
+        for graph in graphs:
+            graph.replay()
+        eager = tkv.tkv_filter_sample(*sets[0])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g, w in zip(got + [eager], want + [want[0]]) for a, b in zip(g, w))
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        both = [tkv.tkv_filter_sample(*a, stream=s) for a, s in zip(sets, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g, w in zip(both, want) for a, b in zip(g, w))
 
 
 @pytest.mark.gpu
