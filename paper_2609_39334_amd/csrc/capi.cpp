@@ -1,4 +1,5 @@
-// Error reporting shared by every C entry point: a thread-local message behind tkv_last_error().
+// Error reporting shared by every C entry point (a thread-local message behind tkv_last_error()), and the host halves of
+// the entry points that take device data alone: their checks of arguments, and how a drafted batch is cut.
 #include <algorithm>
 #include <cstdarg>
 #include <cstdint>
@@ -29,7 +30,7 @@ void clear_error() { g_error.clear(); }
 
 TKV_EXPORT const char* tkv_last_error(void) { return g_error.c_str(); }
 
-// ------------------------------------------------------------------ drafted trees: argument checks
+// ------------------------------------------------------------------ norms with the append, drafted trees, truncated draws
 namespace {
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }

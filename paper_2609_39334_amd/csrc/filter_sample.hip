@@ -7,12 +7,13 @@
 //   top-p   the number at which the sum of the weights from above reaches top_p times the (top-k) total;
 //   min-p   a bound on the weight itself.
 //
-// filter_scan streams the logits once, a wave per 2,048: the largest logit of every run of 32, and, for rows whose
-// whole weight is asked for (top-p without top-k, or no truncation), the tile's weight relative to its largest and
-// a sample of one logit a run.  filter_draw takes a workgroup a row.  The runs' maxima bound the threshold from below
-// (the k-th largest of them is at most the k-th largest logit), so only the few runs above that bound are read
-// again, their tokens above it sorted, cut and drawn from.  For top-p the bound comes from the sample, which tells how
-// much weight lies below a logit to a few per cent.
+// filter_scan streams the logits once, a wave per tile of 2,048: the largest logit of every run of 32 and, for rows whose
+// whole weight is asked for (top-p without top-k, or no truncation), the weights of the tile's parts (64 lanes x 16
+// bytes: 512 tokens of bf16, 256 of fp32) relative to the tile's largest logit, and a sample of two logits a run.
+// filter_draw takes a workgroup a row.  The runs' maxima bound the threshold from below (the k-th largest of them is at
+// most the k-th largest logit), so only the few runs above that bound are read again, their tokens above it sorted, cut
+// and drawn from.  For top-p the bound comes from the sample, which tells how much weight lies below a logit to a few
+// per cent.
 // Where top-p or min-p keeps thousands of tokens the row goes through two more kernels, which find nothing to do
 // otherwise: filter_narrow reads it again, a wave a tile, for the weight above the interval that must hold the
 // threshold and the numbers inside it, and filter_finish cuts among those and draws.  A row that slips through (more
@@ -23,6 +24,13 @@
 // Weights are computed in fp64, w = 2^((l - max) log2(e) / T), and summed in a fixed order.  Histogram sums are
 // integers, w in units of 2^-42, so that they do not depend on the order of the atomics; they decide where top-p ends
 // to 2^-43 of the largest weight a token.
+//
+// What bounds it (MI355X).  The scan: memory, 608 MB of fp32 logits (1,000 rows of 151,936) in 98 us, 6.2 TB/s, past the
+// caches; where a third of the rows ask for their whole weight the fp64 exponentials (ten FMAs each) hide behind it.
+// The draw: latency, one workgroup's chain of barriers, 14 us for 5 rows, 26 us for 250 (a workgroup a CU), 59 us for
+// 1,000 (three on a CU at once).  filter_narrow and filter_finish find nothing in 2.3 and 1.5 us; 129 rows of the 1,000
+// take them 37 and 26 us: a second read of 78 MB with an exponential for each logit above the interval, then 20 us of one
+// workgroup's chain (a list of some thousand numbers weighed, a histogram, a sort, the draws).
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cstdint>
@@ -31,7 +39,7 @@
 
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 512;         // a row's workgroup
 constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 2048;
 constexpr int kList = 2048;           // tokens that are sorted
@@ -42,7 +50,8 @@ static_assert(kTile == 64 * kRun, "a run a lane");
 constexpr int kScanThreads = 256;
 constexpr int kSparseP = 64;          // fewest runs looked into for top-p
 constexpr int kSparseRuns = 1024;     // most runs that are looked into for top-k
-constexpr int kSparseFew = 384;       // and for top-p and min-p, past which filter_narrow reads the row
+constexpr int kSparseFew = 384;       // and for top-p and min-p, past which filter_narrow reads the row (250 rows of 152,064
+                                      // 101 us, 192: 100, 768: 101; 333 of 32,003 90, 88 and 90; 1,000 of 151,936 230, 236, 230)
 constexpr int kHist = 1024;           // bins of the runs' maxima and of the sample
 constexpr int kMaxTiles = (1 << kIdxBits) / kTile;
 constexpr int kMaxPotential = 1024;
@@ -539,7 +548,9 @@ __device__ __forceinline__ uint64_t find_cut(Shared& s, const Src& src, const W&
     }
 }
 
-// A wave a tile: the runs' maxima (+inf where a logit is NaN), and the tile's weight where the row asks for it.
+// A wave a tile: the runs' maxima (+inf where a logit is NaN), and the parts' weights where the row asks for them.
+// NT: logits are read past the caches, from 192 MiB on.  The whole call on logits just written, read through and past:
+// 61 MB 75 and 76 us, 152 MB 104 and 105, 243 MB 142 and 135, 365 MB 226 and 198, 608 MB 338 and 306.
 template <bool BF16, bool NT>
 __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(5))) void filter_scan(Args a) {
     const int lane = threadIdx.x & 63;
@@ -1142,7 +1153,6 @@ __device__ __forceinline__ void sum_parts(const Args& a, const Row<BF16>& row, d
     }
 }
 
-
 // The threshold of a row that filter_narrow has read, and the kept weight of its list in each part (`inside`, zero
 // before); false if the threshold is not in the list.
 template <bool BF16>
@@ -1278,7 +1288,7 @@ int tkv::launch_filter_sample(const FilterCall& f, void* stream) {
         narrow<<<dim3(static_cast<unsigned>(std::min<int64_t>(grid, 2048))), dim3(kScanThreads), 0, st>>>(a);
         finish<<<dim3(static_cast<unsigned>(std::min(f.n_rows, 1024))), dim3(kThreads), 0, st>>>(a);
     };
-    const bool past = static_cast<int64_t>(f.n_rows) * f.vocab * (f.logit_type == TKV_LOGITS_BF16 ? 2 : 4) > int64_t{256} << 20;
+    const bool past = static_cast<int64_t>(f.n_rows) * f.vocab * (f.logit_type == TKV_LOGITS_BF16 ? 2 : 4) >= int64_t{192} << 20;
     if (f.logit_type == TKV_LOGITS_BF16)
         launch(past ? filter_scan<true, true> : filter_scan<true, false>, filter_draw<true>, filter_narrow<true>, filter_finish<true>);
     else
