@@ -469,6 +469,10 @@ def tkv_rope_append(qkv: torch.Tensor, cos: torch.Tensor, sin: torch.Tensor, dst
     return q
 
 
+# A device's current stream as a raw handle, without the stream object around it (0.1 us instead of 1.7).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 class _Call:
     """The device and stream of a call: its outputs and workspaces are allocated for that stream, and its work is enqueued
     there (the current stream of the tensors' device without a stream; never the current device's, if that is
@@ -477,7 +481,7 @@ class _Call:
 
     def __init__(self, fn: str, pool: torch.Tensor, stream):
         self.index, self.device = pool.get_device(), pool.device
-        self.handle = torch.cuda.current_stream(self.device).cuda_stream
+        self.handle = _raw_stream(self.index)
         self.side = None  # another stream than the current one
         if stream is None:
             return
@@ -662,7 +666,7 @@ def tkv_filter_sample(logits: torch.Tensor, temperature: torch.Tensor, draw_off:
     need = tkv_filter_sample_workspace_bytes(n_rows, vocab)
     if workspace is None and need:
         workspace = call.empty((need,), torch.uint8)
-    tok, cnt, ng = call.empty((n,), torch.int32), call.empty((n,), torch.int32), call.empty((n_rows,), torch.int32)
+    tok, cnt, ng = call.empty((2 * n + n_rows,), torch.int32).split((n, n, n_rows))  # (one allocation: 1.4 us each)
 
     def ptr(t):
         return None if t is None else t.data_ptr()

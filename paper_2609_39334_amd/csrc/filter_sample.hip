@@ -1285,7 +1285,8 @@ int tkv::launch_filter_sample(const FilterCall& f, void* stream) {
     const auto launch = [&](auto scan, auto draw, auto narrow, auto finish) {
         scan<<<dim3(static_cast<unsigned>(grid)), dim3(kScanThreads), 0, st>>>(a);
         draw<<<dim3(static_cast<unsigned>(f.n_rows)), dim3(kThreads), 0, st>>>(a);
-        narrow<<<dim3(static_cast<unsigned>(std::min<int64_t>(grid, 2048))), dim3(kScanThreads), 0, st>>>(a);
+        if (f.top_p || f.min_p)  // (top-k alone narrows nothing)
+            narrow<<<dim3(static_cast<unsigned>(std::min<int64_t>(grid, 2048))), dim3(kScanThreads), 0, st>>>(a);
         finish<<<dim3(static_cast<unsigned>(std::min(f.n_rows, 1024))), dim3(kThreads), 0, st>>>(a);
     };
     const bool past = static_cast<int64_t>(f.n_rows) * f.vocab * (f.logit_type == TKV_LOGITS_BF16 ? 2 : 4) >= int64_t{192} << 20;
