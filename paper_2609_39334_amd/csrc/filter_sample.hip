@@ -277,6 +277,9 @@ __device__ __forceinline__ T lane_of(T v, int lane) {
 __device__ __forceinline__ float wave_max(float v) {
     return lane_of(wave_scan(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); }), 63);
 }
+__device__ __forceinline__ int wave_max(int v) {
+    return lane_of(wave_scan(v, INT32_MIN, [](int a, int b) { return a > b ? a : b; }), 63);
+}
 
 // Exclusive scan over the workgroup and the total; `part` holds a value a wave.
 template <class T>
@@ -823,16 +826,19 @@ __device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, cons
         uint32_t crun = block_scan(cs, reinterpret_cast<uint32_t*>(s.part), every);
         double mrun = block_scan(ms, s.partd, all);
         double vrun = block_scan(vs, s.partd, all);
+        int may = -1, must = -1;
 #pragma unroll
         for (int e = 0; e < per; ++e) {
             const int b = kHist - 1 - (per * t + e);
             mrun += m[e], vrun += v[e];
             const double err = 4. * sqrt(vrun) + 4. * each * exp2_neg(b * slope);
-            if (mrun + err >= rest) atomicMax(&s.i1, b);  // the last bin that may hold the threshold: past it there is too little
-            if (mrun - err > rest) atomicMax(&s.i2, b);   // the first: from it on there is too much
-            s.sampled[b] = every - crun;                  // samples in bins above
+            if (mrun + err >= rest) may = max(may, b);   // the last bin that may hold the threshold: past it there is too little
+            if (mrun - err > rest) must = max(must, b);  // the first: from it on there is too much
+            s.sampled[b] = every - crun;                 // samples in bins above
             crun += c[e];
         }
+        may = wave_max(may), must = wave_max(must);
+        if ((t & 63) == 0) atomicMax(&s.i1, may), atomicMax(&s.i2, must);
     }
     __syncthreads();
     Bound r{};
@@ -936,11 +942,14 @@ __device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>&
     __syncthreads();
     int keep = s.i0;
     if (bound > 0.) {
+        int end = INT32_MIN;  // (negated: the first below the bound)
 #pragma unroll
         for (int e = 0; e < per; ++e) {
             const int i = per * t + e;
-            if (i > 0 && i < n && w[e] < bound) atomicMin(&s.i0, i);
+            if (i > 0 && i < n && w[e] < bound) end = max(end, -i);
         }
+        end = wave_max(end);
+        if ((t & 63) == 0 && end > INT32_MIN) atomicMin(&s.i0, -end);
         __syncthreads();
         keep = s.i0;
     }
