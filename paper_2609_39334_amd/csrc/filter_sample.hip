@@ -25,10 +25,10 @@
 // integers, w in units of 2^-42, so that they do not depend on the order of the atomics; they decide where top-p ends
 // to 2^-43 of the largest weight a token.
 //
-// What bounds it (MI355X).  The scan: memory, 608 MB of fp32 logits (1,000 rows of 151,936) in 98 us, 6.2 TB/s, past the
+// What bounds it (MI355X).  The scan: memory, 608 MB of fp32 logits (1,000 rows of 151,936) in 102 us, 6.0 TB/s, past the
 // caches; where a third of the rows ask for their whole weight the fp64 exponentials (ten FMAs each) hide behind it.
-// The draw: latency, one workgroup's chain of barriers, 14 us for 5 rows, 26 us for 250 (a workgroup a CU), 59 us for
-// 1,000 (three on a CU at once).  filter_narrow and filter_finish find nothing in 2.3 and 1.5 us; 129 rows of the 1,000
+// The draw: latency, one workgroup's chain of barriers, 13 us for 5 rows, 24 us for 250 (a workgroup a CU), 48 us for
+// 1,000 (three on a CU at once; 44 of them for a row under a top-k of 1,000).  filter_narrow and filter_finish find nothing in 2.3 and 1.5 us; 129 rows of the 1,000
 // take them 37 and 26 us: a second read of 78 MB with an exponential for each logit above the interval, then 20 us of one
 // workgroup's chain (a list of some thousand numbers weighed, a histogram, a sort, the draws).
 #include <hip/hip_runtime.h>
@@ -44,9 +44,9 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 2048;
 constexpr int kList = 2048;           // tokens that are sorted
 constexpr int kIdxBits = 21;          // vocabularies of up to 2^21 tokens
-constexpr int kRun = 32;              // tokens of a lane in a tile
+constexpr int kRun = 32;              // consecutive tokens whose largest logit is kept
 constexpr int kTile = tkv::kFilterTile;
-static_assert(kTile == 64 * kRun, "a run a lane");
+static_assert(kTile == 64 * kRun, "as many runs as lanes");
 constexpr int kScanThreads = 256;
 constexpr int kSparseP = 64;          // fewest runs looked into for top-p
 constexpr int kSparseRuns = 1024;     // most runs that are looked into for top-k
@@ -188,10 +188,15 @@ struct Logits {
         }
         for (int i = V * whole + threadIdx.x; i < vocab; i += kThreads) f(i, at(i));
     }
-    // this lane's run of the tile that starts at a0: kPieces pieces of V tokens, 64 V apart (-inf past the row)
-    // (a piece of all 64 lanes is a part of the tile, consecutive tokens)
+    // this lane's tokens of the tile that starts at a0: kPieces pieces of V tokens, 64 V apart (-inf past the row)
+    // (a piece of all 64 lanes is a part of the tile, consecutive tokens; kPieces lanes of one are a run)
     static constexpr int V = BF16 ? 8 : 4, kPieces = kRun / V;
     static __device__ __forceinline__ int token(int a0, int lane, int piece) { return a0 + (piece * 64 + lane) * V; }
+    // the first of the `sub`-th V tokens of run r
+    static __device__ __forceinline__ int token_of_run(int r, int sub) {
+        const int in = r % 64;
+        return token(r / 64 * kTile, in / kPieces * kPieces + sub, in % kPieces);
+    }
     template <bool NT = false>
     __device__ __forceinline__ void piece(int a, float (&x)[V]) const {
         if (a + V <= vocab) {
@@ -212,7 +217,7 @@ struct Logits {
         }
     }
     template <bool NT = false>
-    __device__ __forceinline__ void run(int a0, int lane, float (&x)[kPieces][V]) const {
+    __device__ __forceinline__ void tile(int a0, int lane, float (&x)[kPieces][V]) const {
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) piece<NT>(token(a0, lane, j), x[j]);
     }
@@ -370,15 +375,21 @@ __device__ __forceinline__ void sort_down(T* a, int n) {
     for (int i = n + t; i < size; i += kThreads) a[i] = 0;
     __syncthreads();
     if (n <= kCounted) {
-        // `parts` threads a number, each over its share of the others
-        const int parts = kThreads / (n <= 64 ? 64 : n <= 128 ? 128 : 256), i = t / parts, share = size / parts, from = (t & (parts - 1)) * share;
+        // `parts` threads a number, each over its share of the others, 16 in flight
+        const int parts = kThreads / (n <= 128 ? 128 : 256), i = t / parts, share = size / parts, from = (t & (parts - 1)) * share;
         const T mine = i < n ? a[i] : 0;
         int rank = 0;
-        for (int q = from; q < from + share; q += 8) {
+        constexpr int P = 16 / sizeof(T);
+        typedef T pack_t __attribute__((ext_vector_type(P)));
+        for (int q = from; q < from + share; q += 16) {
+            pack_t v[16 / P];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                rank += a[q + e] > mine;
-                if constexpr (sizeof(T) == 4) rank += a[q + e] == mine && q + e < i;  // (only draws repeat)
+            for (int e = 0; e < 16 / P; ++e) v[e] = *reinterpret_cast<const pack_t*>(a + q + e * P);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const T other = v[e / P][e % P];
+                rank += other > mine;
+                if constexpr (sizeof(T) == 4) rank += other == mine && q + e < i;  // (only draws repeat)
             }
         }
         for (int o = parts / 2; o > 0; o >>= 1) rank += __shfl_xor(rank, o);
@@ -396,7 +407,7 @@ __device__ __forceinline__ void sort_down(T* a, int n) {
     }
 }
 
-struct Shared {
+struct __attribute__((aligned(16))) Shared {
     union {
         struct {
             uint64_t mass[kBins];
@@ -422,7 +433,7 @@ struct Shared {
     uint64_t part[kWaves];
     double partd[kWaves];
     union {
-        uint32_t draw[kMaxPotential];  // complements of the tokens drawn
+        __attribute__((aligned(16))) uint32_t draw[kMaxPotential];  // complements of the tokens drawn
         float red[2 * kWaves];
     };
     int32_t start[kMaxPotential + 1];
@@ -565,14 +576,33 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(5)
     if (!s.inside || !s.valid || s.n == 0) return;
     const Logits<BF16> row{static_cast<const char*>(a.logits) + r * a.stride * (BF16 ? 2 : 4), a.vocab};
     float x[Logits<BF16>::kPieces][Logits<BF16>::V];
-    row.template run<NT>(tile * kTile, lane, x);
-    float m = -INFINITY;
-    bool nan = false;
+    row.template tile<NT>(tile * kTile, lane, x);
+    // Run l is piece l % N of the lanes l / N * N .. + N - 1 (consecutive tokens, so that filter_draw reads few lines; a
+    // lane's own pieces as a run cost this kernel 4 us less of 102 and filter_draw 6 to 12 more).  The N pieces' maxima over
+    // N lanes by halving: each exchange leaves a lane half of the pieces over twice the lanes.
+    constexpr int N = Logits<BF16>::kPieces;
+    float p[N];
 #pragma unroll
-    for (int j = 0; j < Logits<BF16>::kPieces; ++j)
+    for (int j = 0; j < N; ++j) {
+        p[j] = -INFINITY;
+        bool nan = false;
 #pragma unroll
-        for (int e = 0; e < Logits<BF16>::V; ++e) m = fmaxf(m, x[j][e]), nan |= (__float_as_uint(x[j][e]) & 0x7fffffffu) > 0x7f800000u;
-    if (nan) m = INFINITY;
+        for (int e = 0; e < Logits<BF16>::V; ++e) p[j] = fmaxf(p[j], x[j][e]), nan |= (__float_as_uint(x[j][e]) & 0x7fffffffu) > 0x7f800000u;
+        if (nan) p[j] = INFINITY;
+    }
+    if constexpr (N == 8) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float keep = lane & 4 ? p[j + 4] : p[j], give = lane & 4 ? p[j] : p[j + 4];
+            p[j] = fmaxf(keep, moved<0x141, 0xf>(give, -INFINITY));  // lane 7 - l of eight
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const float keep = lane & 2 ? p[j + 2] : p[j], give = lane & 2 ? p[j] : p[j + 2];
+        p[j] = fmaxf(keep, moved<0x4e, 0xf>(give, -INFINITY));  // quad_perm 2 3 0 1
+    }
+    float m = fmaxf(lane & 1 ? p[1] : p[0], moved<0xb1, 0xf>(lane & 1 ? p[0] : p[1], -INFINITY));  // quad_perm 1 0 3 2
     a.run_max[id * 64 + lane] = m;
     const bool whole = s.whole(a.vocab), samples = whole && s.p < 1.f;
     const float s0 = x[0][0], s1 = x[Logits<BF16>::kPieces / 2][0];
@@ -582,7 +612,6 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(5)
     m = wave_max(m), low = -wave_max(-low);
     if (lane == 0) a.tile_max[id] = make_float2(m, low);
     if (!whole) return;
-    constexpr int N = Logits<BF16>::kPieces;
     double sum[N];
     const bool some = m > -INFINITY && m < INFINITY;
     const double base = some ? m : 0., c = s.scale();
@@ -891,8 +920,7 @@ __device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>&
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
             const int i = min(i0 + q * kThreads, runs * L::kPieces - 1);
-            const int run = s.runs[i / L::kPieces];
-            first[q] = L::token(run / 64 * kTile, run % 64, i % L::kPieces);
+            first[q] = L::token_of_run(s.runs[i / L::kPieces], i % L::kPieces);
             row.x.piece(first[q], x[q]);
         }
         uint32_t in = 0;
@@ -901,15 +929,18 @@ __device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>&
 #pragma unroll
             for (int e = 0; e < L::V; ++e)
                 in |= static_cast<uint32_t>(i0 + q * kThreads < runs * L::kPieces && x[q][e] >= low) << (q * L::V + e);
-        int at = append(&s.i2, in);
+        // (few of a lane's 16, picked one at a time)
+        for (int at = append(&s.i2, in); in != 0; in &= in - 1, ++at) {
+            const int b = __builtin_ctz(in);
+            float v = 0.f;
+            int from = 0;
 #pragma unroll
-        for (int q = 0; q < kAhead; ++q)
+            for (int q = 0; q < kAhead; ++q)
 #pragma unroll
-            for (int e = 0; e < L::V; ++e)
-                if (in >> (q * L::V + e) & 1) {
-                    if (at < kList) s.list[at] = number_of(x[q][e], first[q] + e);
-                    ++at;
-                }
+                for (int e = 0; e < L::V; ++e)
+                    if (b == q * L::V + e) v = x[q][e], from = first[q] + e;
+            if (at < kList) s.list[at] = number_of(v, from);
+        }
     }
     __syncthreads();
     const int n = s.i2;
@@ -1109,7 +1140,7 @@ __global__ __launch_bounds__(kScanThreads) void filter_narrow(Args a) {
                             static_cast<double>(g.top), set.scale()};
         const double bound = static_cast<double>(set.min_p);
         float x[L::kPieces][L::V];
-        row.x.run(tile * kTile, lane, x);
+        row.x.tile(tile * kTile, lane, x);
         double above = 0., kept[L::kPieces];
         uint32_t in = 0;
 #pragma unroll
@@ -1149,7 +1180,7 @@ __device__ __forceinline__ void sum_parts(const Args& a, const Row<BF16>& row, d
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (int i = w; i < a.tiles; i += kWaves) {
         float x[L::kPieces][L::V];
-        row.x.run(i * kTile, lane, x);
+        row.x.tile(i * kTile, lane, x);
         double sum[L::kPieces];
 #pragma unroll
         for (int j = 0; j < L::kPieces; ++j) {
