@@ -12,6 +12,13 @@
 // K and V go from the pool straight to LDS (buffer_load ... lds), double-buffered.  Which blocks these are is
 // device data: the workgroup first reads its chunk's table entries and lengths, drops what is no block of the pool,
 // and counts the keys from the row's end, which tells each block's place among the drafted tokens.
+//
+// What bounds it (MI355X).  Single tokens: memory, 198 MB of keys (64 rows of 12/2/128 heads under 300 to 6,144 keys) in
+// 34 us, 5.8 TB/s, and 4 us of merge.  Trees: the chain of a stage (K from LDS, MFMAs, exponentials, V, MFMAs) with two
+// waves a SIMD.  8 rows of 64 to 150 tokens of 32/8/128 heads under 2,000 to 12,000 keys take 176 us, 610 TFLOP/s of seen
+// keys; without the stages' loads 163, with the loads alone 98.  32 rows of 4 to 32 tokens, 28/4/128: 63 us, 57 and 41;
+// 32 tokens under 30,000 keys 33 us, 33 and 23.  A unit costs 7 us beside its stages (its row, its table, the first
+// stage, the partial result), a stage 1.4 to 2 us.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cstdint>
