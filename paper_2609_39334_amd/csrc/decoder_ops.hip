@@ -167,7 +167,7 @@ __device__ __forceinline__ void store16(uint16_t* p, uint4 v) {
 // each: the lane's two chunks of eight are chunks j and j + rot / 16 where they rotate together (j < rot / 16), and
 // the next two of the rest past it.  The sum of squares is 16 terms in a lane and log2(D / 16) exchanges; the
 // normed values stay in fp32 through the rotation and are rounded once.
-// What bounds it: memory.  16,480 tokens of 32/8/128 heads, a fifth of them without a slot (387 MB): 65 us, 5.9 TB/s; 72 us
+// What bounds it: memory.  16,340 tokens of 32/8/128 heads, a fifth of them without a slot (387 MB): 65 us, 5.9 TB/s; 72 us
 // through the caches.  STREAM: heads are read and written past the caches, for calls of 256 MiB and more, as
 // kv_append is (254 MB of such heads run at 6.2 TB/s through them); heads of 64 gain nothing from it (422 MB 88 us
 // either way).
