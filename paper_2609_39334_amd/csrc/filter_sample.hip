@@ -52,6 +52,7 @@ constexpr int kSparseP = 64;          // fewest runs looked into for top-p
 constexpr int kSparseRuns = 1024;     // most runs that are looked into for top-k
 constexpr int kSparseFew = 384;       // and for top-p and min-p, past which filter_narrow reads the row (250 rows of 152,064
                                       // 101 us, 192: 100, 768: 101; 333 of 32,003 90, 88 and 90; 1,000 of 151,936 230, 236, 230)
+constexpr int kSparseK = 256;         // largest top-k that they are looked into for where a list holds twice as many numbers
 constexpr int kHist = 1024;           // bins of the runs' maxima and of the sample
 constexpr int kMaxTiles = (1 << kIdxBits) / kTile;
 constexpr int kMaxPotential = 1024;
@@ -107,6 +108,8 @@ struct Settings {
     bool valid;
     // the weight of all of the row's tokens decides something
     __device__ __forceinline__ bool whole(int vocab) const { return k >= vocab && (p < 1.f || min_p <= 0.f); }
+    // top-k by a sample: too many runs would hold some of the k tokens
+    __device__ __forceinline__ bool many(int vocab, int cap) const { return k < vocab && k > kSparseK && 2 * static_cast<int64_t>(k) <= cap; }
     __device__ __forceinline__ double scale() const { return temp == 0.f ? 1. : 1.4426950408889634 / static_cast<double>(temp); }
 };
 __device__ __forceinline__ Settings settings_of(const Args& a, int r) {
@@ -472,11 +475,12 @@ struct ListNumbers {
 };
 
 // The last number of the shortest run from above that reaches a target, among a source's numbers in [lo, hi]; lo if all
-// of them do not.  BY_MASS: the target is `want` units of weight, or (SHARE) that share of the whole weight in [lo, hi];
+// of them do not.  by_mass: the target is `want` units of weight, or (share) that share of the whole weight in [lo, hi];
 // else a count.
 // fresh(logit): a token's weight, where the source has none.
-template <bool BY_MASS, bool SHARE, class Src, class W>
-__device__ __forceinline__ uint64_t find_cut(Shared& s, const Src& src, const W& fresh, uint64_t lo, uint64_t hi, uint64_t target, double want) {
+template <class Src, class W>
+__device__ __forceinline__ uint64_t find_cut(Shared& s, const Src& src, const W& fresh, bool by_mass, bool share, uint64_t lo, uint64_t hi, uint64_t target,
+                                             double want) {
     const int t = threadIdx.x;
     uint64_t above_c = 0, above_m = 0;
     const uint64_t floor = lo;
@@ -490,7 +494,7 @@ __device__ __forceinline__ uint64_t find_cut(Shared& s, const Src& src, const W&
             if (n < lo || n > hi) return;
             const int b = static_cast<int>((n - lo) >> shift);
             atomicAdd(&s.h.cnt[b], 1u);
-            if (BY_MASS) atomicAdd(reinterpret_cast<unsigned long long*>(&s.h.mass[b]), static_cast<unsigned long long>(units(n, w)));
+            if (by_mass) atomicAdd(reinterpret_cast<unsigned long long*>(&s.h.mass[b]), static_cast<unsigned long long>(units(n, w)));
         });
         __syncthreads();
         // thread t takes bins from the top down: kBins - 1 - per t and the next below
@@ -504,15 +508,15 @@ __device__ __forceinline__ uint64_t find_cut(Shared& s, const Src& src, const W&
         }
         uint64_t before_c = above_c + block_scan(cs, s.part, total_c);
         uint64_t before_m = above_m + block_scan(ms, s.part, total_m);
-        if (SHARE && first) want *= static_cast<double>(total_m);
+        if (share && first) want *= static_cast<double>(total_m);
         if (t == 0) s.i0 = -1;
         __syncthreads();
         uint64_t bc = before_c, bm = before_m;
 #pragma unroll
         for (int e = 0; e < per; ++e) {
             const uint64_t ac = bc + c[e], am = bm + m[e];
-            const bool reached = BY_MASS ? static_cast<double>(am) >= want : ac >= target;
-            const bool was = BY_MASS ? static_cast<double>(bm) >= want : bc >= target;
+            const bool reached = by_mass ? static_cast<double>(am) >= want : ac >= target;
+            const bool was = by_mass ? static_cast<double>(bm) >= want : bc >= target;
             // (the first bin that holds anything, if nothing is wanted)
             if (c[e] > 0 && reached && (!was || bc == 0)) {
                 s.i0 = kBins - 1 - (per * t + e);
@@ -541,7 +545,7 @@ __device__ __forceinline__ uint64_t find_cut(Shared& s, const Src& src, const W&
 #pragma unroll
         for (int e = 0; e < many; ++e) {
             const int i = many * t + e;
-            mine += w[e] = BY_MASS && i < n ? fresh(logit_of(s.list[i])) : 0;
+            mine += w[e] = by_mass && i < n ? fresh(logit_of(s.list[i])) : 0;
         }
         uint64_t run = above_m + block_scan(mine, s.part, total);
         if (t == 0) s.u0 = s.list[n - 1];
@@ -550,8 +554,8 @@ __device__ __forceinline__ uint64_t find_cut(Shared& s, const Src& src, const W&
         for (int e = 0; e < many; ++e) {
             const int i = many * t + e;
             const uint64_t next = run + w[e];
-            const bool reached = BY_MASS ? static_cast<double>(next) >= want : above_c + i + 1 >= target;
-            const bool was = BY_MASS ? static_cast<double>(run) >= want : above_c + i >= target;
+            const bool reached = by_mass ? static_cast<double>(next) >= want : above_c + i + 1 >= target;
+            const bool was = by_mass ? static_cast<double>(run) >= want : above_c + i >= target;
             if (i < n && reached && (!was || above_c + i == 0)) s.u0 = s.list[i];
             run = next;
         }
@@ -604,7 +608,7 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(5)
     }
     float m = fmaxf(lane & 1 ? p[1] : p[0], moved<0xb1, 0xf>(lane & 1 ? p[0] : p[1], -INFINITY));  // quad_perm 1 0 3 2
     a.run_max[id * 64 + lane] = m;
-    const bool whole = s.whole(a.vocab), samples = whole && s.p < 1.f;
+    const bool whole = s.whole(a.vocab), samples = (whole && s.p < 1.f) || s.many(a.vocab, a.cap);
     const float s0 = x[0][0], s1 = x[Logits<BF16>::kPieces / 2][0];
     if (samples) a.sample[id * 128 + lane] = s0, a.sample[id * 128 + 64 + lane] = s1;
     const auto finite = [](float v) { return v == -INFINITY ? INFINITY : v; };
@@ -808,17 +812,17 @@ template <bool BF16>
 __device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, const Settings& set, const float* rm, const float* sample,
                             float top, float scale, double whole) {
     const int t = threadIdx.x, n_runs = a.tiles * 64;
-    const bool by_k = set.k < a.vocab;
+    const bool by_k = set.k < a.vocab, sampled = !by_k || set.many(a.vocab, a.cap);
     const uint32_t want = by_k ? set.k : kSparseP;
     constexpr int per = kHist / kThreads;
     for (int i = t; i < kHist; i += kThreads) s.hist[i] = 0, s.sampled[i] = 0;
-    if (t == 0) s.i0 = kHist - 1, s.i1 = s.i2 = -1;
+    if (t == 0) s.i0 = kHist - 1, s.i1 = s.i2 = by_k ? kHist - 1 : -1;
     __syncthreads();
     each_of(rm, n_runs, [&](int, float v) {
         if (v > -INFINITY) atomicAdd(&s.hist[bin_of(v, top, scale)], 1u);
     });
     // (positions past the row hold -inf)
-    if (!by_k)
+    if (sampled)
         each_of(sample, 2 * n_runs, [&](int, float v) {
             if (v > -INFINITY) atomicAdd(&s.sampled[bin_of(v, top, scale)], 1u);
         });
@@ -833,14 +837,29 @@ __device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, cons
         run += c[e];
         s.hist[per * t + e] = run;  // runs up to this bin
     }
+    constexpr int V = Logits<BF16>::V;
+    const int left = a.vocab - (a.tiles - 1) * kTile;
+    const int n_sampled = (a.tiles - 1) * 128 + min(64, (left + V - 1) / V) + max(0, min(64, (left - kTile / 2 + V - 1) / V));
+    const double each = static_cast<double>(a.vocab) / n_sampled;  // tokens that a sampled one stands for
+    if (by_k && sampled) {
+        // the bin from which on, by the sample and four standard errors of it, there are k tokens
+        uint32_t c[per], sum = 0, total;
+#pragma unroll
+        for (int e = 0; e < per; ++e) sum += c[e] = s.sampled[per * t + e];
+        uint32_t run = block_scan(sum, reinterpret_cast<uint32_t*>(s.part), total);
+        const float most = static_cast<float>(set.k / each);
+        const auto enough = [&](uint32_t n) { return static_cast<float>(n) - 4.f * sqrtf(static_cast<float>(n)) >= most; };
+#pragma unroll
+        for (int e = 0; e < per; ++e) {
+            if (!enough(run) && enough(run + c[e])) s.i1 = per * t + e;
+            run += c[e];
+        }
+    }
     if (!by_k) {
         // From the smallest logit up (thread t takes bins kHist - 1 - per t and the next above): the weight below a
         // bin's upper edge, estimated from the sample, and its standard error; both by the weight at the bin's middle.
         // The largest of them may be wide off (few tokens, much weight): what matters is where it passes `rest`.
-        constexpr int V = Logits<BF16>::V;
-        const int left = a.vocab - (a.tiles - 1) * kTile;
-        const int n_sampled = (a.tiles - 1) * 128 + min(64, (left + V - 1) / V) + max(0, min(64, (left - kTile / 2 + V - 1) / V));
-        const double each = static_cast<double>(a.vocab) / n_sampled, rest = (1. - static_cast<double>(set.p)) * whole;
+        const double rest = (1. - static_cast<double>(set.p)) * whole;
         const double slope = scale > 0.f ? -row.c / static_cast<double>(scale) : 0.;
         double m[per], v[per], ms = 0., vs = 0., all;
         uint32_t cs = 0, every;
@@ -872,6 +891,7 @@ __device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, cons
     __syncthreads();
     Bound r{};
     r.last = s.i0, r.first = 0;
+    if (by_k && sampled) r.last = min(r.last, s.i1);
     if (!by_k) {
         r.last = max(s.i0, min(s.i1 + 1, kHist - 1));
         r.first = max(0, s.i2 - 1);
@@ -879,7 +899,7 @@ __device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, cons
     r.runs = s.hist[r.last];
     r.low = foot_of(r.last, top, scale);
     // (a sampled token stands for 16)
-    if (!by_k && (r.runs > kSparseFew || 16 * s.sampled[r.last] > kSparseFew)) r.runs = kSparseRuns + 1;
+    if (sampled && (by_k || r.runs > kSparseFew || 16 * s.sampled[r.last] > kSparseFew)) r.runs = kSparseRuns + 1;
     __syncthreads();
     return r;
 }
@@ -1116,7 +1136,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) v
     if (t == 0) {
         Again again{};
         again.row = r;
-        again.whole_row = by_k || a.cap == 0;
+        again.whole_row = a.cap == 0 || (by_k && set.k > a.cap);
         again.first = at_least.first, again.last = at_least.last;
         again.top = top, again.scale = scale, again.weight = whole;
         a.again[atomicAdd(a.n_again, 1)] = again;
@@ -1202,8 +1222,9 @@ __device__ bool cut_in_list(Shared& s, const Args& a, const Row<BF16>& row, cons
     const int64_t at = static_cast<int64_t>(g.row) * a.tiles;
     const double bound = static_cast<double>(set.min_p);
     cut = 0;
-    if (set.p < 1.f) {
-        if (g.n > a.cap) return false;
+    const bool by_k = set.k < a.vocab;
+    if (by_k || set.p < 1.f) {
+        if (g.n > a.cap || (by_k && g.n < set.k && g.last < kHist - 1)) return false;
         static_assert(kMine * kThreads >= 8192, "a list of any length");
         const uint64_t* from = a.lists + static_cast<int64_t>(g.row) * a.cap;
         ListNumbers list;
@@ -1224,7 +1245,7 @@ __device__ bool cut_in_list(Shared& s, const Args& a, const Row<BF16>& row, cons
             }
         }
         block_scan(units, s.part, all);
-        if (!(want > 0.) || static_cast<double>(all) < want * kUnit) return false;
+        if (!by_k && (!(want > 0.) || static_cast<double>(all) < want * kUnit)) return false;
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) {
             const uint64_t l2 = __shfl_xor(lo, o), h2 = __shfl_xor(hi, o);
@@ -1239,7 +1260,12 @@ __device__ bool cut_in_list(Shared& s, const Args& a, const Row<BF16>& row, cons
         }
         __syncthreads();
         lo = s.u0, hi = s.u1;
-        cut = find_cut<true, false>(s, list, [&](float v) { return row.units(v); }, lo, hi, 0, want * kUnit);
+        const auto units_of = [&](float v) { return row.units(v); };
+        // the k-th, then the end of top-p from there up
+        cut = lo;
+#pragma unroll 1
+        for (int by_mass = by_k ? 0 : 1; by_mass <= (set.p < 1.f ? 1 : 0); ++by_mass)
+            cut = find_cut(s, list, units_of, by_mass != 0, by_k, cut, hi, static_cast<uint64_t>(set.k), by_k ? static_cast<double>(set.p) : want * kUnit);
         // kept tokens of the list, by part: integers, whatever their order
         list.each([&](uint64_t n, uint64_t) {
             if (n < cut) return;
@@ -1278,9 +1304,11 @@ __global__ __launch_bounds__(kThreads) void filter_finish(Args a) {
             auto units = [&](float v) { return row.units(v); };
             const uint64_t lo = static_cast<uint64_t>(key_of(-3.4028234663852886e38f)) << kIdxBits;
             const uint64_t hi = number_of(g.top, 0);
-            cut = 0;
-            if (set.k < a.vocab) cut = find_cut<false, false>(s, all, units, lo, hi, static_cast<uint64_t>(set.k), 0.);
-            if (set.p < 1.f) cut = find_cut<true, true>(s, all, units, cut > lo ? cut : lo, hi, 0, static_cast<double>(set.p));
+            cut = lo;
+            if (set.k >= a.vocab && set.p >= 1.f) cut = 0;
+#pragma unroll 1
+            for (int by_mass = set.k < a.vocab ? 0 : 1; by_mass <= (set.p < 1.f ? 1 : 0); ++by_mass)
+                cut = find_cut(s, all, units, by_mass != 0, true, cut, hi, static_cast<uint64_t>(set.k), static_cast<double>(set.p));
             sum_parts<BF16>(a, row, parts, kept);
         }
         __syncthreads();
@@ -1325,8 +1353,7 @@ int tkv::launch_filter_sample(const FilterCall& f, void* stream) {
     const auto launch = [&](auto scan, auto draw, auto narrow, auto finish) {
         scan<<<dim3(static_cast<unsigned>(grid)), dim3(kScanThreads), 0, st>>>(a);
         draw<<<dim3(static_cast<unsigned>(f.n_rows)), dim3(kThreads), 0, st>>>(a);
-        if (f.top_p || f.min_p)  // (top-k alone narrows nothing)
-            narrow<<<dim3(static_cast<unsigned>(std::min<int64_t>(grid, 2048))), dim3(kScanThreads), 0, st>>>(a);
+        narrow<<<dim3(static_cast<unsigned>(std::min<int64_t>(grid, 2048))), dim3(kScanThreads), 0, st>>>(a);
         finish<<<dim3(static_cast<unsigned>(std::min(f.n_rows, 1024))), dim3(kThreads), 0, st>>>(a);
     };
     const bool past = static_cast<int64_t>(f.n_rows) * f.vocab * (f.logit_type == TKV_LOGITS_BF16 ? 2 : 4) >= int64_t{192} << 20;
