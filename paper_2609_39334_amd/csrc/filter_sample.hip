@@ -14,12 +14,13 @@
 // most the k-th largest logit), so only the few runs above that bound are read again, their tokens above it sorted, cut
 // and drawn from.  For top-p the bound comes from the sample, which tells how much weight lies below a logit to a few
 // per cent.
-// Where top-p or min-p keeps thousands of tokens the row goes through two more kernels, which find nothing to do
-// otherwise: filter_narrow reads it again, a wave a tile, for the weight above the interval that must hold the
-// threshold and the numbers inside it, and filter_finish cuts among those and draws.  A row that slips through (more
-// tokens at the threshold than a list holds, a large top-k, a threshold outside the interval) is read by one
-// workgroup as often as it takes: histograms over the numbers, 2,048 bins of the interval that still holds the
-// threshold, with each bin's count and weight, until that interval holds few enough tokens to sort.
+// Where thousands of tokens are kept the row goes through two more kernels, which find nothing to do otherwise:
+// filter_narrow reads it again, a wave a tile, for the weight above the interval that must hold the threshold and the
+// numbers inside it (top-k: all from the interval's end up, which by the sample are k and a few), and filter_finish cuts
+// among those and draws.  A row that slips through (more tokens at the threshold than a list holds, a top-k of more than
+// half a list, a threshold outside the interval) is read by one workgroup as often as it takes: histograms over the
+// numbers, 2,048 bins of the interval that still holds the threshold, with each bin's count and weight, until that
+// interval holds few enough tokens to sort.
 //
 // Weights are computed in fp64, w = 2^((l - max) log2(e) / T), and summed in a fixed order.  Histogram sums are
 // integers, w in units of 2^-42, so that they do not depend on the order of the atomics; they decide where top-p ends
@@ -27,9 +28,9 @@
 //
 // What bounds it (MI355X).  The scan: memory, 608 MB of fp32 logits (1,000 rows of 151,936) in 102 us, 6.0 TB/s, past the
 // caches; where a third of the rows ask for their whole weight the fp64 exponentials (ten FMAs each) hide behind it.
-// The draw: latency, one workgroup's chain of barriers, 13 us for 5 rows, 24 us for 250 (a workgroup a CU), 48 us for
-// 1,000 (three on a CU at once; 44 of them for a row under a top-k of 1,000).  filter_narrow and filter_finish find nothing in 2.3 and 1.5 us; 129 rows of the 1,000
-// take them 37 and 26 us: a second read of 78 MB with an exponential for each logit above the interval, then 20 us of one
+// The draw: latency, one workgroup's chain of barriers, 13 us for 5 rows, 24 us for 250 (a workgroup a CU), 40 us for
+// 1,000 (three on a CU at once).  filter_narrow and filter_finish find nothing in 2.3 and 1.5 us; 136 rows of the 1,000
+// take them 38 and 30 us: a second read of 83 MB with an exponential for each logit above the interval, then 20 us of one
 // workgroup's chain (a list of some thousand numbers weighed, a histogram, a sort, the draws).
 #include <hip/hip_runtime.h>
 #include <algorithm>
@@ -52,7 +53,10 @@ constexpr int kSparseP = 64;          // fewest runs looked into for top-p
 constexpr int kSparseRuns = 1024;     // most runs that are looked into for top-k
 constexpr int kSparseFew = 384;       // and for top-p and min-p, past which filter_narrow reads the row (250 rows of 152,064
                                       // 101 us, 192: 100, 768: 101; 333 of 32,003 90, 88 and 90; 1,000 of 151,936 230, 236, 230)
-constexpr int kSparseK = 256;         // largest top-k that they are looked into for where a list holds twice as many numbers
+constexpr int kSparseK = 512;         // largest top-k that they are looked into for where a list holds twice as many numbers:
+                                      // 8 rows of 151,936 under a top-k of 500 31 us, 44 by the sample; of 1,000 41 and 45.
+                                      // 200 rows of 32,000 (1,000 runs) under a top-k of 1,000 112 and 49, of 151,936 59 and
+                                      // 87, but where a few do and others keep thousands of tokens anyway 101 and 85
 constexpr int kHist = 1024;           // bins of the runs' maxima and of the sample
 constexpr int kMaxTiles = (1 << kIdxBits) / kTile;
 constexpr int kMaxPotential = 1024;

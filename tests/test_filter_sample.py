@@ -276,6 +276,19 @@ def test_more_rows_read_again_than_workgroups():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kind", ["normal", "peaked", "steps", "masked"])
+@pytest.mark.parametrize("vocab", [12000, 32000, 128256])
+def test_large_top_k(vocab, kind, dtype):
+    n = 20
+    k = np.array([512, 513, 700, 1000, 1024, 1500, 2500, 4000, 5000, 11000] * 2)
+    p = np.array([1.0] * 7 + [0.95, 0.5, 0.999, 0.9, 0.0, 0.95, 0.99, 1.0, 0.7, 0.9, 1.0, 1.0, 0.95])
+    m = np.where(np.arange(n) % 6 == 5, 0.02, 0.0)
+    T = np.array([0.8, 1.3, 0.3, 1.0, 30.0] * 4)
+    _check(_logits(kind, n, vocab, dtype, seed=vocab + 1), T, k, p, m, [1, 3, 20, 2] * 5, seed=vocab + 1)
+
+
+@pytest.mark.gpu
 def test_a_workspace_of_the_callers():
     x = _logits("normal", 9, 20000, torch.float32)
     T, p = torch.ones(9, device="cuda"), torch.full((9,), 0.9, device="cuda")
