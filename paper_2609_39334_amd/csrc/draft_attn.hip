@@ -11,7 +11,9 @@
 //
 // K and V go from the pool straight to LDS (buffer_load ... lds), double-buffered.  Which blocks these are is
 // device data: the workgroup first reads its chunk's table entries and lengths, drops what is no block of the pool,
-// and counts the keys from the row's end, which tells each block's place among the drafted tokens.
+// and counts the keys from the row's end, which tells each block's place among the drafted tokens.  Stages of context
+// alone run first, without looking at masks; in the others V is cleared of what is not finite, so that a hidden key may
+// hold anything (under 1% of the time of the cases below).
 //
 // What bounds it (MI355X).  Single tokens: memory, 198 MB of keys (64 rows of 12/2/128 heads under 300 to 6,144 keys) in
 // 34 us, 5.8 TB/s, and 4 us of merge.  Trees: the chain of a stage (K from LDS, MFMAs, exponentials, V, MFMAs) with two
@@ -22,6 +24,7 @@
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "internal.h"
 
@@ -33,6 +36,7 @@ typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) void* lds_void_ptr;
 
 constexpr int kThreads = 256;      // four waves
@@ -92,11 +96,42 @@ __device__ __forceinline__ void fetch_part(const uint16_t* __restrict__ kpool, c
     }
 }
 
-__device__ __forceinline__ void stage_barrier() {
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+// A barrier over what is in LDS, loads on their way left alone.
+__device__ __forceinline__ void local_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+__device__ __forceinline__ void stage_barrier() {
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    local_barrier();
+}
+
+// This wave's block of a stage of V in LDS: what is not finite becomes 0.  (A key that a row does not see has weight 0 there,
+// and 0 times infinity or NaN would be NaN.)
+template <int D>
+__device__ __forceinline__ void clear_block(uint8_t* blk, int lane) {
+    constexpr int N = D / 32;  // 16-byte pieces a lane
+    uint4 x[N];
+    u16x2_t most{0, 0};
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] = *reinterpret_cast<const uint4*>(blk + (i * 64 + lane) * 16);
+        const uint32_t* w = &x[i].x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2_t, w[e] & 0x7fff7fffu));
+    }
+    if (__builtin_amdgcn_ballot_w64(most.x >= 0x7f80 || most.y >= 0x7f80) == 0) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        uint32_t* w = &x[i].x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool hi = (w[e] & 0x7f800000u) == 0x7f800000u, lo = (w[e] & 0x7f80u) == 0x7f80u;
+            w[e] = (hi ? 0u : w[e] & 0xffff0000u) | (lo ? 0u : w[e] & 0xffffu);
+        }
+        *reinterpret_cast<uint4*>(blk + (i * 64 + lane) * 16) = x[i];
+    }
 }
 
 // A row of the batch as the device arrays give it.
@@ -156,7 +191,7 @@ __device__ __forceinline__ void draft_tile(const Args& a, const Row& w, int chun
     static_assert(BG % 2 == 0, "32 keys an MFMA");
     __shared__ __attribute__((aligned(16))) uint8_t k0[kStage], v0[kStage], k1[kStage], v1[kStage];
     __shared__ int2 list[kMaxChunk];     // the chunk's blocks: {id, 32 (first key's drafted number) + length}
-    __shared__ int wsum[3][4];
+    __shared__ int wsum[4][4];
     __shared__ float xml[NG > 1 ? (NG - 1) * R * 128 : 1];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -183,9 +218,10 @@ __device__ __forceinline__ void draft_tile(const Args& a, const Row& w, int chun
     for (int ks = 0; ks < D / 16; ++ks)
         qf[ks] = *reinterpret_cast<const bf16x8_t*>(a.q + orow * D + hi * 8 + ks * 16);
     const uint64_t* mask = a.b.mask + static_cast<size_t>(w.q0 + i) * a.b.mask_words;
+    const bool hides = w.L > 1 || (a.b.mask[static_cast<size_t>(w.q0) * a.b.mask_words] & 1) == 0;  // (a lone token sees itself)
 
     // the chunk's blocks, and how many keys of the row follow it (exact below L)
-    int nb;
+    int nb, before_draft;  // blocks, and those of them that hold no drafted key (the first)
     {
         const int n = min(w.chunk, w.n_blk - c0);
         int id = 0, len = 0, after = 0, later;
@@ -225,7 +261,10 @@ __device__ __forceinline__ void draft_tile(const Args& a, const Row& w, int chun
         }
         const int d0 = w.L - (after + total - (before + incl - len));  // drafted number of this block's first key
         if (len > 0) list[at + __builtin_popcountll(has & ((uint64_t{1} << lane) - 1))] = int2{id, 32 * max(d0, -64) + len};
+        const uint64_t context = __builtin_amdgcn_ballot_w64(len > 0 && d0 <= -len);
+        if (lane == 0) wsum[3][wid] = __builtin_popcountll(context);
         __syncthreads();
+        before_draft = wsum[3][0] + wsum[3][1] + wsum[3][2] + wsum[3][3];
     }
     const int n_stages = (nb + NB - 1) / NB;
     const size_t blk_stride = static_cast<size_t>(a.hkv) * (16 * D), kvh_off = static_cast<size_t>(kvh) * (16 * D);
@@ -252,12 +291,17 @@ __device__ __forceinline__ void draft_tile(const Args& a, const Row& w, int chun
         fetch(dcur, k0, v0);
         dnxt = stage_desc(1);
     }
-    auto stage = [&](int st, const uint8_t* ks, const uint8_t* vs, uint8_t* kn, uint8_t* vn) {
+    auto stage = [&](auto drafted, int st, const uint8_t* ks, uint8_t* vs, uint8_t* kn, uint8_t* vn) {
+        constexpr bool kDrafted = decltype(drafted)::value;
         stage_barrier();
         if (st + 1 < n_stages) fetch(dnxt, kn, vn);
         const int2 dthis = dcur;
         dcur = dnxt;
         dnxt = stage_desc(st + 2);
+        if (kDrafted && hides) {
+            clear_block<D>(vs + wid * 16 * RB, lane);
+            local_barrier();
+        }
         const int first = NB * st + BG * grp;
         if (!wave_live || first >= nb) return;
         constexpr int P = BG / 2;
@@ -290,13 +334,14 @@ __device__ __forceinline__ void draft_tile(const Args& a, const Row& w, int chun
 #pragma unroll
         for (int j = 0; j < BG; ++j) {
             blk[j] = __builtin_amdgcn_readlane(dthis.y, BG * grp + j);
-            mixed = mixed || (blk[j] & 31) != 16 || (blk[j] >> 5) > -16;
+            mixed = mixed || (blk[j] & 31) != 16 || (kDrafted && (blk[j] >> 5) > -16);
         }
         if (mixed) {
+            asm volatile("");  // (a branch, not selects in every stage)
 #pragma unroll
             for (int j = 0; j < BG; ++j) {
                 const int len = first + j < nb ? blk[j] & 31 : 0;
-                const uint32_t bits = seen(mask, a.b.mask_words, blk[j] >> 5, len) >> (4 * hi);
+                const uint32_t bits = (kDrafted ? seen(mask, a.b.mask_words, blk[j] >> 5, len) : (1u << len) - 1) >> (4 * hi);
 #pragma unroll
                 for (int x = 0; x < 8; ++x)
                     if (!((bits >> (8 * (x >> 2) + (x & 3))) & 1)) sc[j >> 1][8 * (j & 1) + x] = -INFINITY;
@@ -341,9 +386,15 @@ __device__ __forceinline__ void draft_tile(const Args& a, const Row& w, int chun
             }
         }
     };
-    for (int st = 0; st < n_stages; st += 2) {
-        stage(st, k0, v0, k1, v1);
-        if (st + 1 < n_stages) stage(st + 1, k1, v1, k0, v0);
+    // the stages of context alone, in pairs, then the rest
+    int st = 0;
+    for (const int end = before_draft / NB; st + 1 < end; st += 2) {
+        stage(std::false_type{}, st, k0, v0, k1, v1);
+        stage(std::false_type{}, st + 1, k1, v1, k0, v0);
+    }
+    for (; st < n_stages; st += 2) {
+        stage(std::true_type{}, st, k0, v0, k1, v1);
+        if (st + 1 < n_stages) stage(std::true_type{}, st + 1, k1, v1, k0, v0);
     }
     if constexpr (NG > 1) {
         // the other groups' results over their keys join the first's through LDS, 32 x D fp32 a wave

@@ -179,6 +179,54 @@ def test_tokens_that_see_nothing():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("hq,hkv,d,L", [(28, 4, 128, 9), (8, 2, 64, 40), (40, 8, 128, 150), (64, 1, 128, 70)])
+def test_hidden_keys_may_hold_anything(hq, hkv, d, L, bad):
+    # a draft padded with tokens that the others do not see, in slots that were never written; and a token that only its
+    # own branch sees
+    b = Batch([(700, L), (0, L), (33, L), (2000, L)], hq, hkv, d, seed=L)
+    used, first = L - L // 3, [sum(b.q_lens[:r]) for r in range(4)]
+    keep = np.zeros(b.masks[0].shape[1], np.uint64)
+    for j in range(used):
+        keep[j // 64] |= np.uint64(1) << np.uint64(j % 64)
+    for m in b.masks:
+        m[:used] &= keep
+    b.upload()
+    refs = [b.reference(r) for r in range(4)]
+    for t in b.tables:
+        at = np.concatenate([np.arange(b.block_len[x]) + x * BS for x in t])[-L:]
+        for j in [2] + list(range(used, L)):
+            b.k[at[j] // BS, :, at[j] % BS] = bad
+            b.v[at[j] // BS, :, at[j] % BS] = bad
+    o, lse = b.run()
+    for r, (ref, z, A) in enumerate(refs):
+        rows = [i for i in range(used) if not b.masks[r][i, 0] & np.uint64(4)]
+        assert len(rows) >= 2
+        got, bound = o[first[r]:first[r] + L].double(), 2.0 ** -8 * (A + 2 * ref.abs()) + 2.0 ** -11 * A
+        assert torch.all((got - ref).abs()[rows] <= bound[rows])
+        assert torch.all((lse[first[r]:first[r] + L].double() - z)[rows].abs() <= 2.0 ** -11)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d", [(28, 4, 128), (8, 2, 64)])
+def test_a_lone_token_that_does_not_see_itself(hq, hkv, d):
+    b = Batch([(700, 1), (0, 1), (31, 1)], hq, hkv, d)
+    for m in b.masks:
+        m[:] = 0
+    b.upload()
+    refs = [b.reference(r) for r in range(3)]
+    for t in b.tables:
+        b.k[t[-1], :, b.block_len[t[-1]] - 1] = float("inf")
+        b.v[t[-1], :, b.block_len[t[-1]] - 1] = float("nan")
+    o, lse = b.run()
+    assert torch.all(o[1] == 0) and torch.all(lse[1] == -float("inf"))
+    for r in (0, 2):
+        ref, z, A = refs[r]
+        assert torch.all((o[r:r + 1].double() - ref).abs() <= 2.0 ** -8 * (A + 2 * ref.abs()) + 2.0 ** -11 * A)
+        assert torch.all((lse[r:r + 1].double() - z).abs() <= 2.0 ** -11)
+
+
+@pytest.mark.gpu
 def test_a_draft_longer_than_the_path():
     # the path's keys are then the last drafted tokens; a row without any key sees nothing
     b = Batch([(0, 40), (0, 40), (60, 2)], 8, 2, 64, bits=True)
