@@ -908,7 +908,8 @@ __device__ Bound find_bound(Shared& s, const Args& a, const Row<BF16>& row, cons
     return r;
 }
 
-// The row's draws from the tokens above a bound; false if they are more than kList, or do not reach the threshold.
+// The row's draws from the tokens above a bound; false if they are more than kList, or do not reach the threshold (waves may
+// then still be reading `s`).
 template <bool BF16>
 __device__ bool draw_from_runs(Shared& s, const Args& a, int r, const Row<BF16>& row, const Settings& set, const float* rm,
                                double whole, const Bound& at_least) {
@@ -1131,7 +1132,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(6))) v
         __syncthreads();
         at_least.runs = s.i0;
         __syncthreads();
-        if (at_least.runs <= kSparseFew && draw_from_runs<BF16>(s, a, r, row, set, rm, whole, at_least)) return;
+        if (at_least.runs <= kSparseFew) {
+            if (draw_from_runs<BF16>(s, a, r, row, set, rm, whole, at_least)) return;
+            __syncthreads();  // every wave has read the count that made it fail
+        }
     }
     if (by_k || by_p) {
         at_least = find_bound<BF16>(s, a, row, set, rm, sample, top, scale, whole);

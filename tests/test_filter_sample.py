@@ -289,6 +289,21 @@ def test_large_top_k(vocab, kind, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [2049, 3001, 8200, 12288])
+def test_min_p_that_keeps_more_than_a_list_before_top_p(vocab, dtype):
+    # at most 384 runs of 32 reach the min-p bound and hold more than 2,048 tokens: the rows turn to top-p's own bound
+    rows = 600
+    x = _logits("flat", rows, vocab, dtype, seed=vocab)
+    p, m = np.tile([0.95, 0.02, 0.5, 0.999], rows // 4), np.tile([0.01, 0.3, 0.02], rows // 3)
+    off, us, tok, cnt, ng = _run(x, np.full(rows, 1.0), None, p, m, [3] * rows, seed=vocab)
+    host = x.float().cpu().numpy()
+    for r in range(rows):
+        t, c = _plain(host[r], 1.0, 0, p[r], m[r], us[3 * r:3 * r + 3])
+        assert tok[3 * r:3 * r + ng[r]].tolist() == t.tolist() and cnt[3 * r:3 * r + ng[r]].tolist() == c.tolist(), (r, p[r], m[r])
+
+
+@pytest.mark.gpu
 def test_a_workspace_of_the_callers():
     x = _logits("normal", 9, 20000, torch.float32)
     T, p = torch.ones(9, device="cuda"), torch.full((9,), 0.9, device="cuda")
