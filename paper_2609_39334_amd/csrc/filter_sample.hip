@@ -1307,7 +1307,16 @@ __global__ __launch_bounds__(kThreads) void filter_finish(Args a) {
             const double x = row.weight(v);
             return number_of(v, i) >= cut && x >= bound ? x : 0.;
         };
-        if (g.whole_row || !cut_in_list<BF16>(s, a, row, set, g, inside, cut)) {
+        bool sums = g.whole_row || !cut_in_list<BF16>(s, a, row, set, g, inside, cut);
+        if (!sums) {
+            // `inside` misses weights below 2^-51, up to 2^-38 together: draws that fall so low (one in 2^30) take the parts'
+            // own sums instead
+            int low = 0;
+            for (int i = t; i < set.n; i += kThreads) low |= a.uniform[set.off + i] < 0x1p-30f;
+            sums = __syncthreads_or(low);
+            if (sums)
+                for (int i = t; i < a.tiles * L::kPieces; i += kThreads) inside[i] = 0;
+        } else {
             const RowNumbers<BF16> all{row.x};
             auto units = [&](float v) { return row.units(v); };
             const uint64_t lo = static_cast<uint64_t>(key_of(-3.4028234663852886e38f)) << kIdxBits;
@@ -1317,8 +1326,8 @@ __global__ __launch_bounds__(kThreads) void filter_finish(Args a) {
 #pragma unroll 1
             for (int by_mass = set.k < a.vocab ? 0 : 1; by_mass <= (set.p < 1.f ? 1 : 0); ++by_mass)
                 cut = find_cut(s, all, units, by_mass != 0, true, cut, hi, static_cast<uint64_t>(set.k), static_cast<double>(set.p));
-            sum_parts<BF16>(a, row, parts, kept);
         }
+        if (sums) sum_parts<BF16>(a, row, parts, kept);
         __syncthreads();
         const auto part = [&](int tile, int j) {
             return parts[tile * L::kPieces + j] + static_cast<double>(inside[tile * L::kPieces + j]) / kFine;

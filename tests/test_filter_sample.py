@@ -183,6 +183,30 @@ def test_a_uniform_of_zero_and_weights_that_round_to_zero():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_low_draws_among_tiny_weights_under_a_large_top_k(dtype):
+    # logits fall by 0.05 a rank: of 1,000 kept tokens the last 293 weigh less than 2^-51, and no other kept token lies
+    # in the first 2,048, where a uniform of 0 and the smallest ones draw
+    rng = np.random.default_rng(7)
+    vocab, rows = 32003, 4
+    x = np.empty((rows, vocab), np.float32)
+    for r in range(rows):
+        rank = rng.permutation(vocab)
+        tiny = np.flatnonzero((rank >= 720) & (rank < 1000))[:200]
+        front = rng.permutation(2048)
+        others = np.flatnonzero(rank[:2048] < 2500)               # these ranks leave the front
+        away = 2048 + np.flatnonzero(rank[2048:] >= 2500)[:len(others)]
+        rank[others], rank[away] = rank[away].copy(), rank[others].copy()
+        tiny = np.flatnonzero((rank >= 720) & (rank < 1000))[:200]
+        rank[front[:200]], rank[tiny] = rank[tiny].copy(), rank[front[:200]].copy()
+        assert rank[:2048].min() >= 720 and np.sum(rank[:2048] < 1000) == 200
+        x[r] = -0.05 * rank
+    us = [0.0, 2.0 ** -149, 2.0 ** -100, 2.0 ** -70, 1.1 * 2.0 ** -60, 2.0 ** -40, 2.0 ** -24, 0.25, 0.9] * rows
+    _check(torch.from_numpy(x).to(dtype).cuda(), [1.0] * rows, [1000, 900, 1000, 800], [1.0, 1.0, 1.0, 1.0], [0.0, 0.0, 1e-20, 0.0],
+           [9] * rows, us=us)
+
+
+@pytest.mark.gpu
 def test_temperatures_at_the_ends():
     x = _logits("normal", 8, 3001, torch.float32)
     T = [1e-45, 1e-30, 1e-3, 0.05, 100.0, 1e6, 1e30, 3e38]
