@@ -394,8 +394,9 @@ int tkv_draft_mask(int32_t n, const int32_t* parent, int32_t words, uint64_t* ma
  * left out (nothing of it is read or written); one whose table is not inside kv_blocks or is longer than max_blocks
  * gets o = 0 and lse = NaN; an entry that is no block of the pool, or whose block_len is outside [1, 16], counts
  * as empty.  (Where kv_indptr decreases somewhere, so that rows share entries, o and lse of rows behind it are
- * unspecified.)  K/V of the keys that a token sees must be finite; what the others hold does not
- * matter (drafts may be padded with tokens whose slots were never written); slots past a block's length are never read.
+ * unspecified.)  K of the keys that a token sees must be finite; an element of their V that is not makes that element of
+ * the token's o infinite or NaN.  What the other keys hold does not matter (drafts may be padded with tokens whose slots
+ * were never written); slots past a block's length are never read.
  * d_workspace: tkv_draft_workspace_bytes of the same numbers (0: none needed), 16-byte aligned; calls that may
  * overlap need their own.  EINVAL (shape as for tkv_plan_create, sizes, NULL pointers, alignment, workspace too
  * small), EHIP. */

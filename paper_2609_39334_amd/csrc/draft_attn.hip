@@ -13,7 +13,7 @@
 // device data: the workgroup first reads its chunk's table entries and lengths, drops what is no block of the pool,
 // and counts the keys from the row's end, which tells each block's place among the drafted tokens.  Stages of context
 // alone run first, without looking at masks; in the others V is cleared of what is not finite, so that a hidden key may
-// hold anything (under 1% of the time of the cases below).
+// hold anything (under 1% of the time of the cases below), and what was cleared is added to the rows that see it.
 //
 // What bounds it (MI355X).  Single tokens: memory, 198 MB of keys (64 rows of 12/2/128 heads under 300 to 6,144 keys) in
 // 34 us, 5.8 TB/s, and 4 us of merge.  Trees: the chain of a stage (K from LDS, MFMAs, exponentials, V, MFMAs) with two
@@ -107,10 +107,10 @@ __device__ __forceinline__ void stage_barrier() {
     local_barrier();
 }
 
-// This wave's block of a stage of V in LDS: what is not finite becomes 0.  (A key that a row does not see has weight 0 there,
-// and 0 times infinity or NaN would be NaN.)
+// This wave's block of a stage of V in LDS: what is not finite becomes 0; returns whether anything was.  (A key that a row
+// does not see has weight 0 there, and 0 times infinity or NaN would be NaN.)
 template <int D>
-__device__ __forceinline__ void clear_block(uint8_t* blk, int lane) {
+__device__ __forceinline__ bool clear_block(uint8_t* blk, int lane) {
     constexpr int N = D / 32;  // 16-byte pieces a lane
     uint4 x[N];
     u16x2_t most{0, 0};
@@ -121,7 +121,7 @@ __device__ __forceinline__ void clear_block(uint8_t* blk, int lane) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2_t, w[e] & 0x7fff7fffu));
     }
-    if (__builtin_amdgcn_ballot_w64(most.x >= 0x7f80 || most.y >= 0x7f80) == 0) return;
+    if (__builtin_amdgcn_ballot_w64(most.x >= 0x7f80 || most.y >= 0x7f80) == 0) return false;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         uint32_t* w = &x[i].x;
@@ -132,6 +132,7 @@ __device__ __forceinline__ void clear_block(uint8_t* blk, int lane) {
         }
         *reinterpret_cast<uint4*>(blk + (i * 64 + lane) * 16) = x[i];
     }
+    return true;
 }
 
 // A row of the batch as the device arrays give it.
@@ -183,6 +184,26 @@ __device__ __forceinline__ uint32_t seen(const uint64_t* __restrict__ m, int wor
     return static_cast<uint32_t>(v) & ((1u << len) - 1);
 }
 
+// Those values for the rows that see them, added as they are in the pool (a weight would not change what they make of a sum;
+// a row that sees a key whose weight rounds to 0 gets them too).  row: the block's first row of this KV head; bits: the
+// keys that this lane's row sees.
+template <int D>
+__device__ __forceinline__ void add_not_finite(f32x16_t (&acc)[D / 32], const uint16_t* __restrict__ row, uint32_t bits, int hi) {
+#pragma unroll 1
+    for (int key = 0; key < tkv::kBlock; ++key, row += D) {
+        if (!(bits >> key & 1)) continue;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint2 x = *reinterpret_cast<const uint2*>(row + 32 * dt + 8 * u + 4 * hi);
+                const uint32_t w[4] = {x.x << 16, x.x & 0xffff0000u, x.y << 16, x.y & 0xffff0000u};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[dt][4 * u + e] += __uint_as_float((w[e] & 0x7f800000u) == 0x7f800000u ? w[e] : 0u);
+            }
+    }
+}
+
 // One tile of a row against one chunk: R waves of 32 query rows times NG groups of keys, NB blocks a stage.
 template <int D, int R>
 __device__ __forceinline__ void draft_tile(const Args& a, const Row& w, int chunk, int kvh, int tile) {
@@ -192,6 +213,7 @@ __device__ __forceinline__ void draft_tile(const Args& a, const Row& w, int chun
     __shared__ __attribute__((aligned(16))) uint8_t k0[kStage], v0[kStage], k1[kStage], v1[kStage];
     __shared__ int2 list[kMaxChunk];     // the chunk's blocks: {id, 32 (first key's drafted number) + length}
     __shared__ int wsum[4][4];
+    __shared__ int odd[NB];              // blocks of the stage whose V was cleared of something
     __shared__ float xml[NG > 1 ? (NG - 1) * R * 128 : 1];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -299,7 +321,8 @@ __device__ __forceinline__ void draft_tile(const Args& a, const Row& w, int chun
         dcur = dnxt;
         dnxt = stage_desc(st + 2);
         if (kDrafted && hides) {
-            clear_block<D>(vs + wid * 16 * RB, lane);
+            const bool some = clear_block<D>(vs + wid * 16 * RB, lane);
+            if (lane == 0) odd[wid] = some;
             local_barrier();
         }
         const int first = NB * st + BG * grp;
@@ -383,6 +406,18 @@ __device__ __forceinline__ void draft_tile(const Args& a, const Row& w, int chun
                 const s16x4_t vb = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                     (__attribute__((address_space(3))) s16x4_t*)(const_cast<uint8_t*>(vr + 8 * RB + off)));
                 acc[dt] = mfma(__builtin_bit_cast(bf16x8_t, __builtin_shufflevector(va, vb, 0, 1, 2, 3, 4, 5, 6, 7)), pb, acc[dt]);
+            }
+        }
+        if (kDrafted && hides) {
+            int some = 0;
+#pragma unroll
+            for (int j = 0; j < BG; ++j) some |= odd[BG * grp + j] << j;
+            some = __builtin_amdgcn_readfirstlane(some);
+            for (int j = 0; some != 0; ++j, some >>= 1) {
+                if (!(some & 1) || first + j >= nb) continue;
+                const int at = __builtin_amdgcn_readlane(dthis.y, BG * grp + j);
+                add_not_finite<D>(acc, a.v + static_cast<size_t>(__builtin_amdgcn_readlane(dthis.x, BG * grp + j)) * blk_stride + kvh_off,
+                                  seen(mask, a.b.mask_words, at >> 5, at & 31), hi);
             }
         }
     };

@@ -208,6 +208,33 @@ def test_hidden_keys_may_hold_anything(hq, hkv, d, L, bad):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("hq,hkv,d,L", [(28, 4, 128, 9), (8, 2, 64, 40), (40, 8, 128, 150), (64, 1, 128, 70)])
+def test_values_that_are_not_finite_reach_those_who_see_them(hq, hkv, d, L, bad):
+    # one element of a drafted key's value, one of the last context key's (in the draft's first block or stage), one of a key far ahead
+    b = Batch([(700, L), (40, L), (33, L), (2000, L)], hq, hkv, d, seed=L)
+    refs, a = [b.reference(r) for r in range(4)], 0
+    far, near, own = 3, d // 2 + 5, d - 2
+    for t in b.tables:
+        at = np.concatenate([np.arange(b.block_len[x]) + x * BS for x in t])
+        for j, e in ((2, far), (len(at) - L - 1, near), (len(at) - L + 1, own)):
+            b.v[at[j] // BS, hkv - 1, at[j] % BS, e] = bad
+    o, lse = b.run()
+    G = hq // hkv
+    for r, (ref, z, A) in enumerate(refs):
+        got, bound = o[a:a + L].double(), 2.0 ** -8 * (A + 2 * ref.abs()) + 2.0 ** -11 * A
+        hit = torch.zeros_like(got, dtype=torch.bool)
+        sees = torch.from_numpy((b.masks[r][:, 0] & np.uint64(2)) != 0).cuda()
+        assert bool(sees.any()) and not bool(sees.all())
+        hit[:, hq - G:, far] = hit[:, hq - G:, near] = True
+        hit[:, hq - G:, own] = sees[:, None]
+        assert torch.equal(~got.isfinite(), hit), r
+        assert torch.all(((got - ref).abs() <= bound)[~hit])
+        assert torch.all((lse[a:a + L].double() - z).abs() <= 2.0 ** -11)
+        a += L
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("hq,hkv,d", [(28, 4, 128), (8, 2, 64)])
 def test_a_lone_token_that_does_not_see_itself(hq, hkv, d):
     b = Batch([(700, 1), (0, 1), (31, 1)], hq, hkv, d)
