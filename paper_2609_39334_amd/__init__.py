@@ -502,6 +502,14 @@ class _Call:
         t.record_stream(torch.cuda.current_stream(self.device))
         return t
 
+    def uses(self, *tensors) -> None:
+        """The call's tensors (None: not given): dropped after it, they are not handed out again before another stream's
+        work."""
+        if self.side is not None:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.side)
+
     def run(self, entry, *args) -> None:
         if torch.cuda.current_device() == self.index:
             _check(entry(*args, self.handle))
@@ -540,6 +548,7 @@ def tkv_norm_rope_append(qkv: torch.Tensor, q_weight: torch.Tensor, k_weight: to
              ("k_weight", k_weight, torch.float32, (d,)), ("cos", cos, torch.float32, (n, half)),
              ("sin", sin, torch.float32, (n, half)), ("dst", dst, torch.int32, dst.shape))
     call = _Call(fn, k, stream)
+    call.uses(qkv, q_weight, k_weight, cos, sin, dst, k, v)
     q = call.empty((n, hq, d), torch.bfloat16)
     shape = tkv_shape(hq, hkv, d, bs, nb)
     call.run(lib().tkv_norm_rope_append, ctypes.byref(shape), n, qkv.data_ptr(), qkv.stride(0) if n > 1 else width,
@@ -594,6 +603,7 @@ def tkv_draft_verify(q_indptr: torch.Tensor, kv_indptr: torch.Tensor, kv_blocks:
     if workspace is not None and (workspace.get_device() != index or not workspace.is_contiguous()):
         raise ValueError(f"{fn}: workspace must be contiguous, on GPU {index}")
     call = _Call(fn, k, stream)
+    call.uses(q_indptr, kv_indptr, kv_blocks, block_len, mask, q, k, v, o, lse, workspace)
     sh = tkv_shape(hq, hkv, d, bs, nb)
     batch = tkv_draft_batch(n_rows, n, int(max_q), n_kv, int(max_blocks), words, q_indptr.data_ptr(), kv_indptr.data_ptr(),
                             kv_blocks.data_ptr(), block_len.data_ptr(), mask.data_ptr())
@@ -663,6 +673,7 @@ def tkv_filter_sample(logits: torch.Tensor, temperature: torch.Tensor, draw_off:
     if workspace is not None and (workspace.get_device() != index or not workspace.is_contiguous()):
         raise ValueError(f"{fn}: workspace must be contiguous, on GPU {index}")
     call = _Call(fn, logits, stream)
+    call.uses(logits, temperature, draw_off, uniform, top_k, top_p, min_p, workspace)
     need = tkv_filter_sample_workspace_bytes(n_rows, vocab)
     if workspace is None and need:
         workspace = call.empty((need,), torch.uint8)

@@ -414,6 +414,26 @@ def test_replays_with_other_tables_and_other_streams():
 
 
 @pytest.mark.gpu
+def test_inputs_dropped_after_a_call_on_another_stream():
+    # their memory is not handed out again while that stream may still read it
+    b, side = Batch([(3000, 9), (400, 200)], 12, 2, 128), torch.cuda.Stream()
+    b.run()
+    kept = dict(b.dev, q=b.q, k=b.k, v=b.v, o=torch.empty_like(b.q), lse=torch.empty(b.q.shape[:2], device="cuda"))
+    for name in ("mask", "q", "k", "v", "o", "lse"):
+        args = dict(kept, **{name: kept[name].clone()})
+        torch.cuda.synchronize()
+        at = args[name].data_ptr()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)
+        tkv.tkv_draft_verify(**args, max_q=b.max_q, max_blocks=b.max_blocks, stream=side)
+        del args
+        new = torch.empty_like(kept[name])
+        busy = not side.query()
+        torch.cuda.synchronize()
+        assert busy and new.data_ptr() != at, name
+
+
+@pytest.mark.gpu
 def test_a_workspace_of_the_callers():
     b = Batch([(3000, 9)], 8, 2, 64)
     want = b.run()

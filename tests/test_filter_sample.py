@@ -287,6 +287,26 @@ def test_other_streams_and_replays():
 
 
 @pytest.mark.gpu
+def test_inputs_dropped_after_a_call_on_another_stream():
+    # their memory is not handed out again while that stream may still read it
+    side = torch.cuda.Stream()
+    off, u = torch.arange(31, dtype=torch.int32, device="cuda") * 4, torch.rand(120, device="cuda")
+    kept = dict(x=_logits("peaked", 30, 90000, torch.float32), T=torch.full((30,), 0.8, device="cuda"))
+    torch.cuda.synchronize()
+    for name in ("x", "T"):
+        args = dict(kept, **{name: kept[name].clone()})
+        torch.cuda.synchronize()
+        at = args[name].data_ptr()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)
+        tkv.tkv_filter_sample(args["x"], args["T"], off, u, 4, stream=side)
+        del args
+        new = torch.empty_like(kept[name])
+        busy = not side.query()
+        torch.cuda.synchronize()
+        assert busy and new.data_ptr() != at, name
+
+@pytest.mark.gpu
 def test_more_rows_read_again_than_workgroups():
     # 1,100 rows whose top-p keeps thousands of tokens, and a top-k past the runs that are looked into
     rows, vocab = 1100, 8200

@@ -148,7 +148,21 @@ def test_other_streams_and_replays():
 
 
 @pytest.mark.gpu
-def test_tensors_are_checked():
+def test_inputs_dropped_after_a_call_on_another_stream():
+    # their memory is not handed out again while that stream may still read it
+    a, side = _inputs(700, 12, 2, 128, 128), torch.cuda.Stream()
+    for name in ("qkv", "cos", "dst", "q_weight", "v"):
+        args = dict(a, **{name: a[name].clone()})
+        torch.cuda.synchronize()
+        at = args[name].data_ptr()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)
+        tkv.tkv_norm_rope_append(**args, stream=side)
+        del args
+        new = torch.empty_like(a[name])
+        busy = not side.query()
+        torch.cuda.synchronize()
+        assert busy and new.data_ptr() != at, namedef test_tensors_are_checked():
     a = _inputs(4, 4, 2, 64, 64)
     for name, bad in (("qkv", a["qkv"].float()), ("qkv", a["qkv"].t()), ("qkv", a["qkv"][:, :-64]), ("qkv", a["qkv"][:1].expand(4, -1)),
                       ("q_weight", a["q_weight"].bfloat16()), ("k_weight", a["k_weight"][:32]), ("cos", a["cos"][:, ::2]),
