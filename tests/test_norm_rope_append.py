@@ -162,7 +162,23 @@ def test_inputs_dropped_after_a_call_on_another_stream():
         new = torch.empty_like(a[name])
         busy = not side.query()
         torch.cuda.synchronize()
-        assert busy and new.data_ptr() != at, namedef test_tensors_are_checked():
+        assert busy and new.data_ptr() != at, name
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rot,extra", [(128, 0), (32, 48)])
+def test_calls_of_more_than_256_mib(rot, extra):
+    # heads of 128 are then read and written past the caches
+    n, hq, hkv, d = 9500, 40, 8, 128
+    assert n * (hq + 2 * hkv) * d * 4 >= 256 << 20
+    a = _inputs(n, hq, hkv, d, rot, seed=rot, extra=extra)
+    a["dst"][::5], a["dst"][7] = -1, a["k"].shape[0] * 16
+    k0, v0 = a["k"].clone(), a["v"].clone()
+    _check(a, tkv.tkv_norm_rope_append(**a), k0, v0)
+
+
+@pytest.mark.gpu
+def test_tensors_are_checked():
     a = _inputs(4, 4, 2, 64, 64)
     for name, bad in (("qkv", a["qkv"].float()), ("qkv", a["qkv"].t()), ("qkv", a["qkv"][:, :-64]), ("qkv", a["qkv"][:1].expand(4, -1)),
                       ("q_weight", a["q_weight"].bfloat16()), ("k_weight", a["k_weight"][:32]), ("cos", a["cos"][:, ::2]),
