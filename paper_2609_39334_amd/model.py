@@ -110,10 +110,11 @@ class SyntheticDecoder:
         other = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream)
         other.wait_stream(current)
         with torch.cuda.stream(other):
-            logits = run()
+            out = run()
         current.wait_stream(other)
-        logits.record_stream(current)
-        return logits
+        for t in out if isinstance(out, tuple) else (out,):
+            t.record_stream(current)
+        return out
 
     def _forward(self, tokens, positions, dst, attend, k_pools, v_pools, on_layer):
         """The head's logits (bf16) on the current stream; attend(q, k, v, o): the attention of the rows' queries."""
@@ -143,5 +144,6 @@ class SyntheticDecoder:
 
     def sample_filtered(self, logits, temperature, draw_off, uniform, max_potential, top_k=None, top_p=None, min_p=None,
                         stream=None):
-        """Draws under per-row temperature, top-k, top-p and min-p: (tokens, counts, groups per row)."""
-        return tkv_filter_sample(logits, temperature, draw_off, uniform, max_potential, top_k, top_p, min_p, stream=stream)
+        """Draws under per-row temperature, top-k, top-p and min-p: (tokens, counts, groups per row).  stream as for step."""
+        return self._on(stream, lambda: tkv_filter_sample(logits, temperature, draw_off, uniform, max_potential, top_k, top_p, min_p,
+                                                          stream=stream))

@@ -185,6 +185,27 @@ def test_a_chain_draft_is_the_decode_step():
     assert err.max() <= 2e-2 * want.abs().max() and err.mean() <= 1e-2 * want.abs().mean()
 
 
+@pytest.mark.gpu
+def test_draws_on_another_stream_follow_the_logits_and_come_before_their_use():
+    model = SyntheticDecoder(DecoderShape(layers=1, hidden=64, hq=1, hkv=1, d=64, inter=64, vocab=64))
+    g = torch.Generator(device="cuda").manual_seed(2)
+    n, vocab = 200, 30000
+    new = torch.randn((n, vocab), generator=g, device="cuda") * 3
+    logits = torch.zeros_like(new)
+    T, off, u = torch.ones(n, device="cuda"), torch.arange(n + 1, dtype=torch.int32, device="cuda"), torch.rand(n, generator=g, device="cuda")
+    p = torch.full((n,), 0.9, device="cuda")
+    want = [t.clone() for t in model.sample_filtered(new, T, off, u, 1, top_p=p)]
+    for stream in (torch.cuda.Stream(), torch.cuda.Stream().cuda_stream, 0, None):
+        logits.zero_()
+        torch.cuda.synchronize()
+        torch.cuda._sleep(100_000_000)
+        logits.copy_(new)                              # the draws read these
+        got = model.sample_filtered(logits, T, off, u, 1, top_p=p, stream=stream)
+        got = [t.clone() for t in got]                 # and are complete for the current stream
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_draft_batch():
     bl = np.array([16, 16, 5, 3, 0], np.int32)
     b = tkv.DraftBatch([[0, 3], [1, 2]], [[-1, 0, 0], [-1, 0, 1, -1]], bl, device="cpu")
