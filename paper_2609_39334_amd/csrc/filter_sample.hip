@@ -1366,18 +1366,22 @@ int tkv::launch_filter_sample(const FilterCall& f, void* stream) {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     constexpr int waves = kScanThreads / 64;
     const int64_t grid = (static_cast<int64_t>(f.n_rows) * a.tiles + waves - 1) / waves;
-    if (grid > INT32_MAX) return set_error(TKV_EINVAL, "tkv_filter_sample: %d rows are too many", f.n_rows);
+    // (a launch takes less than 2^32 threads)
+    if (grid * kScanThreads > UINT32_MAX || static_cast<int64_t>(f.n_rows) * kThreads > UINT32_MAX)
+        return set_error(TKV_EINVAL, "tkv_filter_sample: %d rows are too many", f.n_rows);
     const auto launch = [&](auto scan, auto draw, auto narrow, auto finish) {
         scan<<<dim3(static_cast<unsigned>(grid)), dim3(kScanThreads), 0, st>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;  // (the others read what it writes)
         draw<<<dim3(static_cast<unsigned>(f.n_rows)), dim3(kThreads), 0, st>>>(a);
         narrow<<<dim3(static_cast<unsigned>(std::min<int64_t>(grid, 2048))), dim3(kScanThreads), 0, st>>>(a);
         finish<<<dim3(static_cast<unsigned>(std::min(f.n_rows, 1024))), dim3(kThreads), 0, st>>>(a);
+        return hipGetLastError();
     };
     const bool past = static_cast<int64_t>(f.n_rows) * f.vocab * (f.logit_type == TKV_LOGITS_BF16 ? 2 : 4) >= int64_t{192} << 20;
-    if (f.logit_type == TKV_LOGITS_BF16)
-        launch(past ? filter_scan<true, true> : filter_scan<true, false>, filter_draw<true>, filter_narrow<true>, filter_finish<true>);
-    else
-        launch(past ? filter_scan<false, true> : filter_scan<false, false>, filter_draw<false>, filter_narrow<false>, filter_finish<false>);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e =
+        f.logit_type == TKV_LOGITS_BF16
+            ? launch(past ? filter_scan<true, true> : filter_scan<true, false>, filter_draw<true>, filter_narrow<true>, filter_finish<true>)
+            : launch(past ? filter_scan<false, true> : filter_scan<false, false>, filter_draw<false>, filter_narrow<false>, filter_finish<false>);
     return e == hipSuccess ? TKV_OK : set_error(TKV_EHIP, "tkv_filter_sample launch: %s", hipGetErrorString(e));
 }

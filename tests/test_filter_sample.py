@@ -306,6 +306,7 @@ def test_inputs_dropped_after_a_call_on_another_stream():
         torch.cuda.synchronize()
         assert busy and new.data_ptr() != at, name
 
+
 @pytest.mark.gpu
 def test_more_rows_read_again_than_workgroups():
     # 1,100 rows whose top-p keeps thousands of tokens, and a top-k past the runs that are looked into
@@ -428,3 +429,11 @@ def test_bad_arguments_are_refused():
                 dict(logits=None), dict(T=None), dict(most=-1), dict(most=1025), dict(n_draws=-1), dict(u=None), dict(off=None)):
         assert call(**bad) == tkv.TKV_EINVAL, bad
     assert call(n=0) == tkv.TKV_OK and call(n=0, logits=None) == tkv.TKV_OK
+
+
+def test_more_rows_than_a_launch_takes_are_refused():
+    # before any device access: 512 threads a row, under 2^32 in a launch; a wave a tile of 2,048 logits
+    L, one = tkv.lib(), 16
+    for n, vocab in ((1 << 23, 1), ((1 << 31) - 1, 1), (1 << 22, 16 * 2048)):
+        assert L.tkv_filter_sample(n, vocab, 0, one, vocab, one, one, one, one, 1, one, one, 1, one, one, one, one, 1 << 62, None) == tkv.TKV_EINVAL
+        assert "too many" in tkv.tkv_last_error()
