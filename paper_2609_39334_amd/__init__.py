@@ -905,6 +905,8 @@ class DraftBatch:
         kv = np.concatenate([_i32(t) for t in tables]) if tables else np.zeros(0, np.int32)
         if len(kv) and (kv.min() < 0 or kv.max() >= len(bl)):
             raise ValueError("DraftBatch: a table names a block outside block_len")
+        if len(kv) and (bl[kv].min() < 0 or bl[kv].max() > 16):
+            raise ValueError("DraftBatch: a table's block has a length outside [0, 16]")
         context = [int(bl[_i32(t)].sum()) - n for t, n in zip(tables, lens)]
         if any(c < 0 for c in context):
             raise ValueError("DraftBatch: a row's path is shorter than its draft")

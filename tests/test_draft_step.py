@@ -206,6 +206,15 @@ def test_draws_on_another_stream_follow_the_logits_and_come_before_their_use():
         assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_draft_batch_of_bad_lengths():
+    # a length outside [0, 16] would count for the positions and not for the attention
+    for bad in (17, -1):
+        with pytest.raises(ValueError, match="length"):
+            tkv.DraftBatch([[0, 1]], [[-1]], np.array([16, bad, 3], np.int32), device="cpu")
+    b = tkv.DraftBatch([[0, 2]], [[-1]], np.array([16, 17, 3], np.int32), device="cpu")    # not in a table
+    assert b.positions.tolist() == [18]
+
+
 def test_draft_batch():
     bl = np.array([16, 16, 5, 3, 0], np.int32)
     b = tkv.DraftBatch([[0, 3], [1, 2]], [[-1, 0, 0], [-1, 0, 1, -1]], bl, device="cpu")
