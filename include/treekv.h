@@ -483,8 +483,8 @@ int tkv_cd_sample(int32_t n_rows, int32_t vocab, float temperature, int32_t max_
  *   d_top_p        [n_rows] fp32 in [0, 1], nullable; 1 (or NULL): all of them
  *   d_min_p        [n_rows] fp32 in [0, 1], nullable; 0 (or NULL): all of them
  * The draws' arguments and outputs are tkv_cd_sample's (vocab <= 2,097,152, n_rows < 2^23, and below 2^26 tiles of 2,048
- * logits in all); in a row's range the entries past its
- * groups get token -1, count 0.  A row gets d_n_groups -1 for settings outside their ranges, a logit that is NaN
+ * logits in all); max_potential is checked for its range alone, and rows of up to 1,024 draws are served whatever it is.
+ * In a row's range the entries past its groups get token -1, count 0.  A row gets d_n_groups -1 for settings outside their ranges, a logit that is NaN
  * or +inf, or no finite logit, besides tkv_cd_sample's reasons.
  * d_workspace: tkv_filter_sample_workspace_bytes(n_rows, vocab), 16-byte aligned; calls that may overlap need
  * their own.  EINVAL, EHIP. */

@@ -217,7 +217,7 @@ TKV_EXPORT int tkv_filter_sample(int32_t n_rows, int32_t vocab, int32_t logit_ty
     if (!aligned16(d_workspace)) return tkv::set_error(TKV_EINVAL, "%s: workspace not 16-byte aligned", fn);
     if (!tkv::launch_filter_sample) return tkv::set_error(TKV_EHIP, "%s: host-only build, no device", fn);
     tkv::FilterCall f{};
-    f.n_rows = n_rows, f.vocab = vocab, f.logit_type = logit_type, f.max_potential = max_potential, f.n_draws = n_draws;
+    f.n_rows = n_rows, f.vocab = vocab, f.logit_type = logit_type, f.n_draws = n_draws;
     f.logits = d_logits, f.stride = stride;
     f.temperature = d_temperature, f.top_k = d_top_k, f.top_p = d_top_p, f.min_p = d_min_p;
     f.uniform = d_uniform, f.draw_off = d_draw_off;

@@ -204,7 +204,7 @@ __attribute__((weak)) int launch_draft_verify(const tkv_shape& s, const tkv_draf
 
 // The arguments of tkv_filter_sample.
 struct FilterCall {
-    int32_t n_rows, vocab, logit_type, max_potential, n_draws;
+    int32_t n_rows, vocab, logit_type, n_draws;
     const void* logits;
     int64_t stride;
     const float *temperature, *top_p, *min_p;

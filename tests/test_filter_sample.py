@@ -249,6 +249,18 @@ def test_rows_outside_the_arrays():
 
 
 @pytest.mark.gpu
+def test_rows_of_more_draws_than_max_potential_are_served():
+    # as tkv_cd_sample does: the argument's own range is checked, a row is refused past 1,024 draws
+    x = _logits("normal", 2, 4000, torch.float32)
+    off, u = torch.tensor([0, 3, 103], dtype=torch.int32, device="cuda"), torch.rand(103, device="cuda")
+    T = torch.ones(2, device="cuda")
+    want = tkv.tkv_filter_sample(x, T, off, u, 100)
+    assert want[2].min() > 0 and int(want[1].sum()) == 103
+    for most in (0, 2):
+        assert all(torch.equal(a, b) for a, b in zip(tkv.tkv_filter_sample(x, T, off, u, most), want))
+
+
+@pytest.mark.gpu
 def test_as_tkv_cd_sample_without_filters():
     # the plain sampler's sums are in 32 bits: a draw in reach of a border may differ
     x = _logits("normal", 40, 32000, torch.float32)
