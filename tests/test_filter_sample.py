@@ -320,6 +320,23 @@ def test_inputs_dropped_after_a_call_on_another_stream():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,rows", [(torch.float32, 335), (torch.bfloat16, 670)])
+def test_logits_of_more_than_192_mib(dtype, rows):
+    # read past the caches; an odd vocabulary, rows that start at any element
+    vocab = 151937
+    assert rows * vocab * dtype.itemsize >= 192 << 20
+    x = _logits("normal", rows, vocab + 6, dtype, seed=3)[:, 3:3 + vocab]
+    x[::2, ::997] += 9
+    rng = np.random.default_rng(3)
+    T, k = rng.choice([0.3, 0.8, 1.0], rows), rng.choice([0, 0, 1, 50, 1000], rows)
+    p, m = rng.choice([1.0, 0.9, 0.5], rows), rng.choice([0.0, 0.0, 0.05], rows)
+    off, us, tok, cnt, ng = _run(x, T, k, p, m, [3] * rows, seed=3)
+    for r in list(range(0, rows, 17)) + [1, rows - 2, rows - 1]:
+        t, c = _plain(x[r].float().cpu().numpy(), T[r], int(k[r]), p[r], m[r], us[3 * r:3 * r + 3])
+        assert tok[3 * r:3 * r + ng[r]].tolist() == t.tolist() and cnt[3 * r:3 * r + ng[r]].tolist() == c.tolist(), r
+
+
+@pytest.mark.gpu
 def test_more_rows_read_again_than_workgroups():
     # 1,100 rows whose top-p keeps thousands of tokens, and a top-k past the runs that are looked into
     rows, vocab = 1100, 8200
