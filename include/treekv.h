@@ -475,8 +475,10 @@ int tkv_cd_sample(int32_t n_rows, int32_t vocab, float temperature, int32_t max_
  * Row r's weights are w_j = exp((l_j - max l) / T); tokens are ordered by logit, equal logits by index (lowest
  * first).  Kept are: of the first k tokens, the shortest run from the front whose weights reach top_p times
  * the k tokens' sum, and of those the ones with w_j >= min_p; the first token always.  A draw at uniform u is the first kept
- * token in token order whose cumulative weight exceeds u times the kept tokens' sum.  Weights, sums and comparisons
- * are in 64 bits, and results do not depend on the order in which the row is read.
+ * token in token order whose cumulative weight exceeds u times the kept tokens' sum (u = 0 may pass over tokens whose
+ * weight is below 2^-1000).  Weights and sums are in 64 bits, and results do not depend on the order in which the row is
+ * read.  Where more than 2,048 tokens come into question, top-p's end is found in units of 2^-42 of the largest weight a
+ * token, and draws at 2^-30 and above among sums that are off by 2^-38 of it at most.
  *   d_logits       row r at d_logits + r * stride elements (stride >= vocab), fp32 or bf16 (logit_type)
  *   d_temperature  [n_rows] fp32, >= 0 and finite; 0: the first token alone
  *   d_top_k        [n_rows] int32, >= 0, nullable; 0 (or NULL): all tokens

@@ -117,13 +117,16 @@ int check_draft(const char* fn, const tkv_shape* s, const tkv_draft_batch* b) {
 }
 
 // Tiles of 64 query rows, whose two pairs of waves share the keys, where the batch has no wider row or few rows in all
-// (one row of 32 tokens, 28/4/128 heads, 30,000 keys: 36 us against 37 with tiles of 128; 64 single tokens of 12/2/128
-// heads under 300 to 6,144 keys: 39 against 40), else 128 (32 rows of 4 to 32 tokens, 28/4/128: 64 against 70).
+// (little between them there: one row of 32 tokens, 28/4/128 heads, 30,000 keys 36 us against 37 with tiles of 128; 64
+// single tokens of 12/2/128 heads under 300 to 6,144 keys 39 against 40), else 128 (32 rows of 4 to 32 tokens, 28/4/128:
+// 64 against 70).
 // Chunks as long as they can be with a unit for every slot of the chip (two workgroups a CU for heads of 128, three
 // for 64): a unit costs about 7 us beside its stages, and one past the slots waits for a whole round (those 32 rows:
 // 484 units of up to 104 blocks 66 us, 528 of up to 93 78 us, 728 of 64 83 us).  Chunks that would pass 192 blocks
 // are cut for two rounds, or more (8 rows of 64 to 150 tokens, 32/8/128, 2,000 to 12,000 keys: 178 us with 150
-// blocks, 211 with 240).  A row's last chunk is short, so tables make more units than their blocks fill: `uneven`.
+// blocks, 211 with 240).  A row's chunks are whole in number, of near-equal length, so tables make more units than their
+// blocks fill: `uneven`, too much for long rows (those 8 rows: 856 units of 128 to 164 blocks on the 1,024 slots of two
+// rounds).
 // Where the longest table has 32 blocks the merge costs more than a split saves (64 rows under 20 to 300 keys 13.5 us,
 // 20 us in chunks of 16).
 tkv::DraftSplit draft_split(const tkv_shape& s, const tkv_draft_batch& b) {

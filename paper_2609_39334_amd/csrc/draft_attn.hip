@@ -16,7 +16,8 @@
 // hold anything (under 1% of the time of the cases below), and what was cleared is added to the rows that see it.
 //
 // What bounds it (MI355X).  Single tokens: memory, 198 MB of keys (64 rows of 12/2/128 heads under 300 to 6,144 keys) in
-// 34 us, 5.8 TB/s, and 4 us of merge.  Trees: the chain of a stage (K from LDS, MFMAs, exponentials, V, MFMAs) with two
+// 42 us, 4.7 TB/s, and 4.6 us of merge; where the last-level cache holds the keys from the call before, 34 us.  Trees (with
+// their keys in the cache; 32 rows take 4 us more without): the chain of a stage (K from LDS, MFMAs, exponentials, V, MFMAs) with two
 // waves a SIMD.  8 rows of 64 to 150 tokens of 32/8/128 heads under 2,000 to 12,000 keys take 176 us, 610 TFLOP/s of seen
 // keys; without the stages' loads 163, with the loads alone 98.  32 rows of 4 to 32 tokens, 28/4/128: 63 us, 57 and 41;
 // 32 tokens under 30,000 keys 33 us, 33 and 23.  A unit costs 7 us beside its stages (its row, its table, the first
@@ -508,7 +509,8 @@ __device__ __forceinline__ void draft_tile(const Args& a, const Row& w, int chun
 // the rows' units up to its own, one row a thread, so that no slot of the chip is held by a chunk or tile that a
 // shorter row lacks (32 rows of 4 to 32 tokens of 28/4/128 heads under 500 to 6,144 keys: 64 us, 90 with a grid over
 // the maxima).
-// Units of one (row, chunk, KV head) follow each other, in runs on one XCD: they read the same keys.
+// Units of one (row, chunk, KV head) read the same keys and follow each other, in runs on one XCD as long as the widest row
+// has tiles; where rows differ in width a run may end among them, and the rest reads the keys on the next XCD.
 template <int D, int R>
 __global__ __launch_bounds__(kThreads, 2) void draft_attn(Args a) {
     __shared__ int sums[4], found[4];

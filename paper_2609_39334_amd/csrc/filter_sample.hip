@@ -20,17 +20,19 @@
 // among those and draws.  A row that slips through (more tokens at the threshold than a list holds, a top-k of more than
 // half a list, a threshold outside the interval) is read by one workgroup as often as it takes: histograms over the
 // numbers, 2,048 bins of the interval that still holds the threshold, with each bin's count and weight, until that
-// interval holds few enough tokens to sort.
+// interval holds few enough tokens to sort.  The sample's positions are fixed, so a row whose logits follow them goes this
+// way: 8 rows of 151,936 under a top-p of 0.9 take 48 us, 259 where the sampled tokens lie 30 below the others and 227 where
+// they lie 4 above; 100 rows 84, 313 and 288.
 //
 // Weights are computed in fp64, w = 2^((l - max) log2(e) / T), and summed in a fixed order.  Histogram sums are
 // integers, w in units of 2^-42, so that they do not depend on the order of the atomics; they decide where top-p ends
 // to 2^-43 of the largest weight a token.
 //
-// What bounds it (MI355X).  The scan: memory, 608 MB of fp32 logits (1,000 rows of 151,936) in 102 us, 6.0 TB/s, past the
-// caches; where a third of the rows ask for their whole weight the fp64 exponentials (ten FMAs each) hide behind it.
-// The draw: latency, one workgroup's chain of barriers, 13 us for 5 rows, 24 us for 250 (a workgroup a CU), 40 us for
-// 1,000 (three on a CU at once).  filter_narrow and filter_finish find nothing in 2.3 and 1.5 us; 136 rows of the 1,000
-// take them 38 and 30 us: a second read of 83 MB with an exponential for each logit above the interval, then 20 us of one
+// What bounds it (MI355X).  The scan: memory, 608 MB of fp32 logits (1,000 rows of 151,936) in 98 to 107 us, 5.7 to 6.2 TB/s,
+// past the caches; where a third of the rows ask for their whole weight the fp64 exponentials (ten FMAs each) hide behind it.
+// The draw: latency, one workgroup's chain of barriers, 14 us for 5 rows, 25 us for 250 (a workgroup a CU), 42 us for
+// 1,000 (three on a CU at once).  filter_narrow and filter_finish find nothing in 2 to 4 and 1.6 us; 136 rows of the 1,000
+// take them 42 and 31 us: a second read of 83 MB with an exponential for each logit above the interval, then 20 us of one
 // workgroup's chain (a list of some thousand numbers weighed, a histogram, a sort, the draws).
 #include <hip/hip_runtime.h>
 #include <algorithm>
@@ -51,8 +53,9 @@ static_assert(kTile == 64 * kRun, "as many runs as lanes");
 constexpr int kScanThreads = 256;
 constexpr int kSparseP = 64;          // fewest runs looked into for top-p
 constexpr int kSparseRuns = 1024;     // most runs that are looked into for top-k
-constexpr int kSparseFew = 384;       // and for top-p and min-p, past which filter_narrow reads the row (250 rows of 152,064
-                                      // 101 us, 192: 100, 768: 101; 333 of 32,003 90, 88 and 90; 1,000 of 151,936 230, 236, 230)
+constexpr int kSparseFew = 384;       // and for top-p and min-p, past which filter_narrow reads the row; within 3% whatever it is
+                                      // (250 rows of 152,064 101 us, 192: 100, 768: 101; 333 of 32,003 90, 88 and 90; 1,000 of
+                                      // 151,936 230, 236, 230)
 constexpr int kSparseK = 512;         // largest top-k that they are looked into for where a list holds twice as many numbers:
                                       // 8 rows of 151,936 under a top-k of 500 31 us, 44 by the sample; of 1,000 41 and 45.
                                       // 200 rows of 32,000 (1,000 runs) under a top-k of 1,000 112 and 49, of 151,936 59 and
