@@ -102,12 +102,12 @@ class SyntheticDecoder:
         return self._on(stream, lambda: self._forward(tokens, batch.positions, dst, batch.verify, k_pools, v_pools, on_layer))
 
     @staticmethod
-    def _on(stream, run):
-        """run() on a stream, after the current stream's work so far and before its later work."""
-        current = torch.cuda.current_stream()
+    def _on(stream, run, device=None):
+        """run() on a stream, after the current stream's (of the device) work so far and before its later work."""
+        current = torch.cuda.current_stream(device)
         if stream is None or getattr(stream, "cuda_stream", stream) == current.cuda_stream:
             return run()
-        other = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream)
+        other = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device=device)
         other.wait_stream(current)
         with torch.cuda.stream(other):
             out = run()
@@ -146,4 +146,4 @@ class SyntheticDecoder:
                         stream=None):
         """Draws under per-row temperature, top-k, top-p and min-p: (tokens, counts, groups per row).  stream as for step."""
         return self._on(stream, lambda: tkv_filter_sample(logits, temperature, draw_off, uniform, max_potential, top_k, top_p, min_p,
-                                                          stream=stream))
+                                                          stream=stream), logits.device)
