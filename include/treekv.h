@@ -13,6 +13,8 @@
  *   - a planner that turns per-row block tables into shared segments and a device work list;
  *   - decode (q_len 1) and verify (q_len >= 1, causal within the step) attention on the GPU;
  *   - attention of drafted token trees over the same cache (GPU);
+ *   - what a long generation carries from step to step: the attention weight that each key has got, eviction of
+ *     the lightest keys, penalties for the tokens of a path, biases and grammar masks on the next logits (GPU);
  *   - the decode loop's other device steps: K/V append that skips deduplicated blocks, and the
  *     branching sampler of computation deduplication, plain or truncated (top-k, top-p, min-p) (GPU);
  *   - the controller of early pruning and lazy verification (host).
@@ -409,6 +411,56 @@ int tkv_draft_workspace_bytes(const tkv_shape* shape, const tkv_draft_batch* bat
 int tkv_draft_verify(const tkv_shape* shape, const tkv_draft_batch* batch, const void* q, const void* k, const void* v,
                      void* o, float* lse, void* d_workspace, size_t bytes, void* hip_stream);
 
+/* ======================================================================== key weights and eviction
+ * A long generation bounds its cache by what its keys have been worth: the attention weight that the queries so far gave
+ * them.  After attention over a batch (tkv_draft_verify, or tkv_decode or tkv_verify on the same tables) its queries' weights
+ * are added to the keys'; a path that has grown past its budget keeps its first keys, its last ones and the heaviest of
+ * those between, each KV head its own. */
+
+/* Adds up the attention weight of the batch's queries.  For row r, KV head g and the key x in slot s of entry e of the row's
+ * table, the sum over the tokens i that see x (as in tkv_draft_verify) and the query heads h of g:
+ *   out[r][g][16 e + s] = decay * before[r][g][16 e + s] + sum_i coef[i] sum_h exp(q[i,h] . k[x] / sqrt(d) - lse[i,h]),
+ * in fp32, the first term for the keys of the context alone: a key among the row's last L enters with this call.
+ *   q, k     as in tkv_draft_verify;  lse  [n_qtok][hq] fp32, of the same attention (natural log); a query head whose lse is
+ *            not finite gives nothing
+ *   coef     [n_qtok] fp32, >= 0 (nullable: 1): 0 leaves a token out (a draft that was not accepted, padding); a
+ *            coefficient that is not above 0 leaves it out too
+ *   decay    finite; before is not read where it is 0
+ *   before   [n_rows][hkv][keys] fp32 (nullable: zeros);  out  the same, and may be the same memory
+ *   keys     at least 16 * max_blocks
+ * What no key of a row's table has a place for is not written (slots past a block's length, entries that are no blocks, rows
+ * that are left out: tokens or table outside the arrays, or longer than max_q or max_blocks).  K of the keys that a token
+ * sees must be finite; what the others hold does not matter.  Results do not depend on how the work is cut.  No workspace.
+ * EINVAL (shape and batch as for tkv_draft_verify, keys, decay, NULL pointers, q or k not 16-byte aligned), EHIP. */
+int tkv_key_weights(const tkv_shape* shape, const tkv_draft_batch* batch, const void* q, const void* k, const float* lse,
+                    const float* coef, float decay, const float* before, float* out, int64_t keys, void* hip_stream);
+
+/* Moves the keys that stay to new tables.  Of row r's path of N keys, each KV head keeps n = min(N, budget[r]): all of
+ * them if N <= budget[r], else the first min(sink, n), of the rest the last min(recent, ...), and of those between the
+ * ones with the largest weights, the lowest index first among equal weights (NaN is below everything).  They go, in path
+ * order, to the slots 0 .. n - 1 of the row's new table (16 a block; block_len is the caller's to bring up to date).
+ *   n_rows, n_kv_blocks, max_blocks, kv_indptr, kv_blocks, block_len   the rows' tables, as in tkv_draft_batch
+ *   new_indptr  [n_rows + 1] device: row r's new table is new_blocks[new_indptr[r] .. new_indptr[r + 1]), at least
+ *               ceil(n / 16) blocks of the pool (tkv_bm_extend of n tokens without a parent and with seal = 0), each
+ *               named once, and in no table of the call
+ *   budget      [n_rows] int32 device, 0 .. max_budget (0: the row keeps nothing);  sink, recent >= 0
+ *   weights     [n_rows][hkv][keys] fp32, keys >= 16 * max_blocks: as tkv_key_weights writes them
+ *   out         the same: kept key i's weight goes to out[r][g][i], its place in the new table; the rest is not written.
+ *               Must not overlap weights.
+ *   k, v        the pool, read and written
+ *   kept        [n_rows][hkv][max_budget] int32: the kept keys' places 16 e + s in the old table, ascending, then -1
+ *   n_kept      [n_rows] int32: n, or -1 for a row that is left out (a table outside the arrays or longer than max_blocks,
+ *               a budget outside its range, a new table that is too short or names what is no block of the pool): nothing
+ *               else of it is written, its kept are -1
+ * Entries that are no block of the pool count as empty.  No workspace.  EINVAL (shape, sizes, NULL pointers, k or v not
+ * 16-byte aligned, out over weights), EHIP. */
+typedef struct {
+    int32_t n_rows, n_kv_blocks, max_blocks, n_new_blocks, max_budget, sink, recent;
+    const int32_t *kv_indptr, *kv_blocks, *block_len, *new_indptr, *new_blocks, *budget;
+} tkv_evict_batch;
+int tkv_evict_keys(const tkv_shape* shape, const tkv_evict_batch* batch, const float* weights, float* out, int64_t keys, void* k,
+                   void* v, int32_t* kept, int32_t* n_kept, void* hip_stream);
+
 /* ======================================================================== decoder layer
  * The elementwise steps between a decoder layer's matrix products, one pass over memory each: fp32
  * arithmetic, bf16 results rounded to nearest even.  Tensors are contiguous device memory; enqueued on
@@ -497,6 +549,41 @@ int tkv_filter_sample(int32_t n_rows, int32_t vocab, int32_t logit_type, const v
                       int32_t max_potential, const float* d_uniform, const int32_t* d_draw_off, int32_t n_draws,
                       int32_t* d_token, int32_t* d_count, int32_t* d_n_groups, void* d_workspace, size_t bytes,
                       void* hip_stream);
+
+/* Logits under their rows' rules, for either sampler.  The tokens of the rows' paths lie in a pool [num_blocks][16] int32 under
+ * tables as the cache's (the same ones, or a block manager's of their own where keys are evicted); query token i of the batch
+ * follows the tokens of the keys that it would see in tkv_draft_verify.  For its logits l over the vocabulary:
+ *   j occurs among them:          l[j] = l[j] > 0 ? l[j] / repetition : l[j] * repetition
+ *   c > 0 times past the prompt:  l[j] -= frequency * c + presence
+ *   j is biased:                  l[j] += the last of the row's biases for j
+ *   j is not allowed:             l[j] = -inf, whatever it was
+ * in fp32, rounded once.  Out-of-vocabulary tokens count for nothing.
+ *   num_blocks, tokens   the pool;  batch   as in tkv_draft_verify (n_qtok rows of logits)
+ *   in, out        logits of token i at in + i * in_stride elements (stride >= vocab), fp32 or bf16 (in_type, out_type);
+ *                  out may be in if type and stride are the same, and must not overlap it otherwise
+ * The rules, all device data, each of them nullable (off):
+ *   prompt_len     [n_rows] int32 (off: 0): the first tokens of the path, which are the prompt
+ *   repetition     [n_rows] fp32, > 0 and finite (off: 1);  presence, frequency  [n_rows] fp32, finite (off: 0)
+ *   bias_indptr    [n_rows + 1] int32: row r's biases are bias_token, bias_value [bias_indptr[r] .. bias_indptr[r + 1]), of
+ *                  n_bias in all (0: no row has any)
+ *   grammar        [n_qtok] int32: each token's mask, allowed + grammar[i] * allowed_words, bit j % 32 of word j / 32 set
+ *                  where j is allowed; negative: none.  n_grammars masks of allowed_words >= ceil(vocab / 32) words
+ * A row whose settings are outside their ranges, whose biases are not inside the arrays, or whose table is not inside
+ * kv_blocks or is longer than max_blocks gets NaN, as does a token whose mask is not one of n_grammars (the samplers then say
+ * so); a row whose tokens are not inside the batch is left out, and rows of logits that are no row's token are not written.
+ * No workspace.  vocab <= 2,097,152.  EINVAL (sizes, types, strides, NULL pointers, tokens not 16-byte aligned), EHIP. */
+typedef struct {
+    const int32_t* prompt_len;
+    const float *repetition, *presence, *frequency;
+    const int32_t *bias_indptr, *bias_token;
+    const float* bias_value;
+    const int32_t* grammar;
+    const uint32_t* allowed;
+    int32_t n_bias, n_grammars, allowed_words;
+} tkv_logit_rules;
+int tkv_adjust_logits(int32_t num_blocks, const int32_t* tokens, const tkv_draft_batch* batch, const tkv_logit_rules* rules,
+                      int32_t vocab, int32_t in_type, const void* in, int64_t in_stride, int32_t out_type, void* out,
+                      int64_t out_stride, void* hip_stream);
 
 /* ======================================================================== search controller
  * Early pruning (Sec. 4.1) and lazy verification (Sec. 4.3) of a speculative beam search whose

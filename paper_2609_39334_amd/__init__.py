@@ -60,6 +60,18 @@ class tkv_draft_batch(ctypes.Structure):
                [(n, ctypes.c_void_p) for n in ("q_indptr", "kv_indptr", "kv_blocks", "block_len", "mask")]
 
 
+class tkv_evict_batch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_rows", "n_kv_blocks", "max_blocks", "n_new_blocks", "max_budget", "sink",
+                                              "recent")] + \
+               [(n, ctypes.c_void_p) for n in ("kv_indptr", "kv_blocks", "block_len", "new_indptr", "new_blocks", "budget")]
+
+
+class tkv_logit_rules(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("prompt_len", "repetition", "presence", "frequency", "bias_indptr", "bias_token",
+                                               "bias_value", "grammar", "allowed")] + \
+               [(n, ctypes.c_int32) for n in ("n_bias", "n_grammars", "allowed_words")]
+
+
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
 _PI32 = ctypes.POINTER(ctypes.c_int32)
@@ -101,6 +113,10 @@ _SIG = {
                                                  ctypes.POINTER(ctypes.c_size_t)]),
     "tkv_draft_verify": (ctypes.c_int, [ctypes.POINTER(tkv_shape), ctypes.POINTER(tkv_draft_batch), _P, _P, _P, _P, _P, _P,
                                         ctypes.c_size_t, _P]),
+    "tkv_key_weights": (ctypes.c_int, [ctypes.POINTER(tkv_shape), ctypes.POINTER(tkv_draft_batch), _P, _P, _P, _P, ctypes.c_float,
+                                       _P, _P, ctypes.c_int64, _P]),
+    "tkv_evict_keys": (ctypes.c_int, [ctypes.POINTER(tkv_shape), ctypes.POINTER(tkv_evict_batch), _P, _P, ctypes.c_int64, _P, _P,
+                                      _P, _P, _P]),
     "tkv_add_rmsnorm": (ctypes.c_int, [_I32, _I32, ctypes.c_float, _P, _P, _P, _P, _P]),
     "tkv_rope_append": (ctypes.c_int, [ctypes.POINTER(tkv_shape), _I32, _P, _P, _P, _P, _P, _P, _P, _P]),
     "tkv_norm_rope_append": (ctypes.c_int, [ctypes.POINTER(tkv_shape), _I32, _P, ctypes.c_int64, _P, _P, ctypes.c_float, _P, _P,
@@ -110,6 +126,8 @@ _SIG = {
     "tkv_filter_sample_workspace_bytes": (ctypes.c_size_t, [_I32, _I32]),
     "tkv_filter_sample": (ctypes.c_int, [_I32, _I32, _I32, _P, ctypes.c_int64, _P, _P, _P, _P, _I32, _P, _P, _I32, _P, _P, _P, _P,
                                          ctypes.c_size_t, _P]),
+    "tkv_adjust_logits": (ctypes.c_int, [_I32, _P, ctypes.POINTER(tkv_draft_batch), ctypes.POINTER(tkv_logit_rules), _I32, _I32, _P,
+                                         ctypes.c_int64, _I32, _P, ctypes.c_int64, _P]),
     "tkv_search_create": (ctypes.c_int, [_I32, _I32, _I32, _I32, ctypes.POINTER(_P)]),
     "tkv_search_destroy": (None, [_P]),
     "tkv_search_expand": (ctypes.c_int, [_P, _I32, _I32, _PI32]),
@@ -616,6 +634,73 @@ def tkv_draft_verify(q_indptr: torch.Tensor, kv_indptr: torch.Tensor, kv_blocks:
              0 if workspace is None else workspace.numel() * workspace.element_size())
 
 
+def tkv_key_weights(q_indptr: torch.Tensor, kv_indptr: torch.Tensor, kv_blocks: torch.Tensor, block_len: torch.Tensor,
+                    mask: torch.Tensor, max_q: int, max_blocks: int, q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor,
+                    out: torch.Tensor, before: Optional[torch.Tensor] = None, decay: float = 1.0,
+                    coef: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Adds the attention weight of a batch's queries to its rows' keys: out [n_rows, hkv, keys] fp32 (keys >= 16 max_blocks)
+    gets, at 16 e + s for the key in slot s of a row's entry e, decay * before (None: 0; may be out; not for the row's last
+    keys, which enter) + the sum of coef (None: 1) times the queries' weights.  lse [n, hq] is the attention's; the other
+    arguments are tkv_draft_verify's."""
+    fn = "tkv_key_weights"
+    if k.dim() != 4 or q.dim() != 3 or mask.dim() != 2 or out.dim() != 3:
+        raise ValueError(f"{fn}: k must be a pool [num_blocks, hkv, block_size, d], q [n, hq, d], mask [n, words], out [n_rows, "
+                         f"hkv, keys]")
+    nb, hkv, bs, d = k.shape
+    n, hq, words = q.shape[0], q.shape[1], mask.shape[1]
+    n_rows, n_kv, keys = q_indptr.numel() - 1, kv_blocks.numel(), out.shape[2]
+    index, sums = k.get_device(), (n_rows, hkv, keys)
+    _tensors(fn, index, ("k", k, torch.bfloat16, k.shape), ("q", q, torch.bfloat16, q.shape), ("lse", lse, torch.float32, (n, hq)),
+             ("q_indptr", q_indptr, torch.int32, (max(0, n_rows) + 1,)), ("kv_indptr", kv_indptr, torch.int32, (n_rows + 1,)),
+             ("kv_blocks", kv_blocks, torch.int32, (n_kv,)), ("block_len", block_len, torch.int32, (nb,)),
+             ("mask", mask, torch.int64, (n, words)), ("out", out, torch.float32, sums))
+    if before is not None:
+        _tensors(fn, index, ("before", before, torch.float32, sums))
+    if coef is not None:
+        _tensors(fn, index, ("coef", coef, torch.float32, (n,)))
+    call = _Call(fn, k, stream)
+    call.uses(q_indptr, kv_indptr, kv_blocks, block_len, mask, q, k, lse, out, before, coef)
+    sh = tkv_shape(hq, hkv, d, bs, nb)
+    batch = tkv_draft_batch(n_rows, n, int(max_q), n_kv, int(max_blocks), words, q_indptr.data_ptr(), kv_indptr.data_ptr(),
+                            kv_blocks.data_ptr(), block_len.data_ptr(), mask.data_ptr())
+    call.run(lib().tkv_key_weights, ctypes.byref(sh), ctypes.byref(batch), q.data_ptr(), k.data_ptr(), lse.data_ptr(),
+             None if coef is None else coef.data_ptr(), float(decay), None if before is None else before.data_ptr(),
+             out.data_ptr(), keys)
+
+
+def tkv_evict_keys(kv_indptr: torch.Tensor, kv_blocks: torch.Tensor, block_len: torch.Tensor, max_blocks: int,
+                   new_indptr: torch.Tensor, new_blocks: torch.Tensor, budget: torch.Tensor, sink: int, recent: int,
+                   weights: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, kept: torch.Tensor,
+                   n_kept: torch.Tensor, stream=None) -> None:
+    """Moves the keys that stay to new tables: of each row, and each KV head for itself, the first `sink`, the last `recent` and
+    the heaviest of those between, min(budget[r], keys) in all, to the slots of new_blocks[new_indptr[r] : new_indptr[r + 1]]
+    (blocks in no table of the call).  weights, out [n_rows, hkv, keys] fp32 as in tkv_key_weights: the kept keys' go to their
+    new places in out.  kept [n_rows, hkv, most] int32: their old places, then -1; n_kept [n_rows]: how many (-1: the row's
+    arrays do not fit, nothing was moved)."""
+    fn = "tkv_evict_keys"
+    if k.dim() != 4 or weights.dim() != 3 or kept.dim() != 3:
+        raise ValueError(f"{fn}: k must be a pool [num_blocks, hkv, block_size, d], weights [n_rows, hkv, keys], kept [n_rows, "
+                         f"hkv, most]")
+    nb, hkv, bs, d = k.shape
+    n_rows, n_kv, n_new = kv_indptr.numel() - 1, kv_blocks.numel(), new_blocks.numel()
+    keys, most, index = weights.shape[2], kept.shape[2], k.get_device()
+    rows = max(0, n_rows)
+    _tensors(fn, index, ("k", k, torch.bfloat16, k.shape), ("v", v, torch.bfloat16, k.shape),
+             ("kv_indptr", kv_indptr, torch.int32, (rows + 1,)), ("kv_blocks", kv_blocks, torch.int32, (n_kv,)),
+             ("block_len", block_len, torch.int32, (nb,)), ("new_indptr", new_indptr, torch.int32, (rows + 1,)),
+             ("new_blocks", new_blocks, torch.int32, (n_new,)), ("budget", budget, torch.int32, (rows,)),
+             ("weights", weights, torch.float32, (rows, hkv, keys)), ("out", out, torch.float32, (rows, hkv, keys)),
+             ("kept", kept, torch.int32, (rows, hkv, most)), ("n_kept", n_kept, torch.int32, (rows,)))
+    call = _Call(fn, k, stream)
+    call.uses(kv_indptr, kv_blocks, block_len, new_indptr, new_blocks, budget, weights, k, v, out, kept, n_kept)
+    sh = tkv_shape(hkv, hkv, d, bs, nb)
+    batch = tkv_evict_batch(n_rows, n_kv, int(max_blocks), n_new, most, int(sink), int(recent), kv_indptr.data_ptr(),
+                            kv_blocks.data_ptr(), block_len.data_ptr(), new_indptr.data_ptr(), new_blocks.data_ptr(),
+                            budget.data_ptr())
+    call.run(lib().tkv_evict_keys, ctypes.byref(sh), ctypes.byref(batch), weights.data_ptr(), out.data_ptr(), keys, k.data_ptr(),
+             v.data_ptr(), kept.data_ptr(), n_kept.data_ptr())
+
+
 def tkv_swiglu(gu: torch.Tensor, stream=None) -> torch.Tensor:
     """SiLU(gate) * up of gu [rows, 2 * inter] bf16 (gate first), in bf16."""
     rows, two = gu.shape
@@ -686,6 +771,75 @@ def tkv_filter_sample(logits: torch.Tensor, temperature: torch.Tensor, draw_off:
              int(max_potential), uniform.data_ptr(), draw_off.data_ptr(), n, tok.data_ptr(), cnt.data_ptr(), ng.data_ptr(),
              ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
     return tok, cnt, ng
+
+
+def _logit_rows(fn: str, name: str, t: torch.Tensor, rows: int, vocab: int, index: int) -> int:
+    """Checks logits [rows, vocab], fp32 or bf16, with contiguous rows on GPU `index`; returns the rows' stride."""
+    if (t.dim() != 2 or t.dtype not in (torch.float32, torch.bfloat16) or t.shape != (rows, vocab) or t.get_device() != index
+            or index < 0 or (t.numel() and ((vocab > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < vocab)))):
+        raise ValueError(f"{fn}: {name} must be a float32 or bfloat16 tensor of shape {(rows, vocab)} with contiguous rows on GPU "
+                         f"{max(index, 0)}, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
+    return t.stride(0) if rows > 1 else vocab
+
+
+def tkv_adjust_logits(q_indptr: torch.Tensor, kv_indptr: torch.Tensor, kv_blocks: torch.Tensor, block_len: torch.Tensor,
+                      mask: torch.Tensor, max_q: int, max_blocks: int, tokens: torch.Tensor, logits: torch.Tensor,
+                      prompt_len: Optional[torch.Tensor] = None, repetition: Optional[torch.Tensor] = None,
+                      presence: Optional[torch.Tensor] = None, frequency: Optional[torch.Tensor] = None,
+                      bias_indptr: Optional[torch.Tensor] = None, bias_token: Optional[torch.Tensor] = None,
+                      bias_value: Optional[torch.Tensor] = None, grammar: Optional[torch.Tensor] = None,
+                      allowed: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Logits [n_qtok, vocab] (fp32 or bf16) of a batch's query tokens under their rows' rules; each follows the tokens that it
+    sees of its row's path, which lie in the pool tokens [num_blocks, 16] int32 under the batch's tables.
+    repetition, presence, frequency [n_rows] fp32: penalties for tokens of the path, the last two for those past its first
+    prompt_len [n_rows] int32; bias_token int32, bias_value fp32: row r's biases at [bias_indptr[r], bias_indptr[r + 1]);
+    grammar [n_qtok] int32: each token's row of the masks allowed [masks, words] int32 (bit j % 32 of word j / 32: j is
+    allowed; negative: no mask).  None: off.  out: fp32 or bf16, made as logits are if not given, or logits itself."""
+    fn = "tkv_adjust_logits"
+    if tokens.dim() != 2 or mask.dim() != 2 or logits.dim() != 2:
+        raise ValueError(f"{fn}: tokens must be a pool [num_blocks, 16], mask [n, words], logits [n, vocab]")
+    if (bias_indptr is None) != (bias_token is None) or (bias_token is None) != (bias_value is None):
+        raise ValueError(f"{fn}: bias_indptr, bias_token and bias_value go together")
+    if grammar is not None and allowed is None:
+        raise ValueError(f"{fn}: a grammar needs the masks it names")
+    nb, n, words = tokens.shape[0], mask.shape[0], mask.shape[1]
+    n_rows, n_kv, vocab, index = q_indptr.numel() - 1, kv_blocks.numel(), logits.shape[1], tokens.get_device()
+    rows = max(0, n_rows)
+    _tensors(fn, index, ("tokens", tokens, torch.int32, (nb, 16)), ("q_indptr", q_indptr, torch.int32, (rows + 1,)),
+             ("kv_indptr", kv_indptr, torch.int32, (rows + 1,)), ("kv_blocks", kv_blocks, torch.int32, (n_kv,)),
+             ("block_len", block_len, torch.int32, (nb,)), ("mask", mask, torch.int64, (n, words)))
+    for name, t, dtype, size in (("prompt_len", prompt_len, torch.int32, rows), ("repetition", repetition, torch.float32, rows),
+                                 ("presence", presence, torch.float32, rows), ("frequency", frequency, torch.float32, rows),
+                                 ("bias_indptr", bias_indptr, torch.int32, rows + 1), ("grammar", grammar, torch.int32, n)):
+        if t is not None:
+            _tensors(fn, index, (name, t, dtype, (size,)))
+    n_bias = 0
+    if bias_token is not None:
+        n_bias = bias_token.numel()
+        _tensors(fn, index, ("bias_token", bias_token, torch.int32, (n_bias,)), ("bias_value", bias_value, torch.float32, (n_bias,)))
+    if allowed is not None:
+        if allowed.dim() != 2:
+            raise ValueError(f"{fn}: allowed must be [masks, words]")
+        _tensors(fn, index, ("allowed", allowed, torch.int32, allowed.shape))
+    stride = _logit_rows(fn, "logits", logits, n, vocab, index)
+    call = _Call(fn, tokens, stream)
+    if out is None:
+        out = call.empty((n, vocab), logits.dtype)
+    out_stride = _logit_rows(fn, "out", out, n, vocab, index)
+    call.uses(q_indptr, kv_indptr, kv_blocks, block_len, mask, tokens, logits, prompt_len, repetition, presence, frequency,
+              bias_indptr, bias_token, bias_value, grammar, allowed, out)
+
+    def ptr(t):
+        return None if t is None else t.data_ptr()
+    rules = tkv_logit_rules(ptr(prompt_len), ptr(repetition), ptr(presence), ptr(frequency), ptr(bias_indptr), ptr(bias_token),
+                            ptr(bias_value), ptr(grammar), ptr(allowed), n_bias, 0 if allowed is None else allowed.shape[0],
+                            0 if allowed is None else allowed.shape[1])
+    batch = tkv_draft_batch(n_rows, n, int(max_q), n_kv, int(max_blocks), words, q_indptr.data_ptr(), kv_indptr.data_ptr(),
+                            kv_blocks.data_ptr(), block_len.data_ptr(), mask.data_ptr())
+    call.run(lib().tkv_adjust_logits, nb, tokens.data_ptr(), ctypes.byref(batch), ctypes.byref(rules), vocab,
+             int(logits.dtype == torch.bfloat16), logits.data_ptr(), stride, int(out.dtype == torch.bfloat16), out.data_ptr(),
+             out_stride)
+    return out
 
 
 def tkv_plan_profile(plan: int, max_calls: int) -> None:

@@ -1,6 +1,7 @@
 // Error reporting shared by every C entry point (a thread-local message behind tkv_last_error()), and the host halves of
 // the entry points that take device data alone: their checks of arguments, and how a drafted batch is cut.
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
@@ -226,4 +227,118 @@ TKV_EXPORT int tkv_filter_sample(int32_t n_rows, int32_t vocab, int32_t logit_ty
     f.uniform = d_uniform, f.draw_off = d_draw_off;
     f.token = d_token, f.count = d_count, f.n_groups = d_n_groups, f.workspace = d_workspace;
     return tkv::launch_filter_sample(f, stream);
+}
+
+// ------------------------------------------------------------------ key weights, eviction, adjusted logits
+namespace {
+
+// Whether the tables' indices fit where 16 e + s is an int32.
+int check_tables(const char* fn, int32_t max_blocks, int64_t keys) {
+    if (max_blocks > INT32_MAX / tkv::kBlock) return tkv::set_error(TKV_EINVAL, "%s: max_blocks = %d is too many", fn, max_blocks);
+    if (keys < static_cast<int64_t>(max_blocks) * tkv::kBlock)
+        return tkv::set_error(TKV_EINVAL, "%s: %lld keys a row do not hold %d blocks", fn, static_cast<long long>(keys), max_blocks);
+    return TKV_OK;
+}
+
+bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
+
+}  // namespace
+
+TKV_EXPORT int tkv_key_weights(const tkv_shape* shape, const tkv_draft_batch* batch, const void* q, const void* k,
+                               const float* lse, const float* coef, float decay, const float* before, float* out,
+                               int64_t keys, void* stream) {
+    const char* fn = "tkv_key_weights";
+    tkv::clear_error();
+    if (const int rc = check_draft(fn, shape, batch)) return rc;
+    const tkv_draft_batch& b = *batch;
+    if (const int rc = check_tables(fn, b.max_blocks, keys)) return rc;
+    if (!std::isfinite(decay)) return tkv::set_error(TKV_EINVAL, "%s: decay is not finite", fn);
+    if (b.n_rows == 0 || b.n_qtok == 0) return TKV_OK;
+    if (!b.q_indptr || !b.kv_indptr || !b.block_len || !b.mask || (b.n_kv_blocks > 0 && !b.kv_blocks) || !q || !k || !lse || !out)
+        return tkv::set_error(TKV_EINVAL, "%s: NULL pointer", fn);
+    for (const void* p : {q, k})
+        if (!aligned16(p)) return tkv::set_error(TKV_EINVAL, "%s: q and k must be 16-byte aligned", fn);
+    for (const void* p : {static_cast<const void*>(lse), static_cast<const void*>(coef), static_cast<const void*>(before),
+                          static_cast<const void*>(out)})
+        if (!aligned4(p)) return tkv::set_error(TKV_EINVAL, "%s: tensors must be aligned to their type", fn);
+    if (!tkv::launch_key_weights) return tkv::set_error(TKV_EHIP, "%s: host-only build, no device", fn);
+    return tkv::launch_key_weights(*shape, b, q, k, lse, coef, decay, before, out, keys, stream);
+}
+
+TKV_EXPORT int tkv_evict_keys(const tkv_shape* shape, const tkv_evict_batch* batch, const float* weights, float* out,
+                              int64_t keys, void* k, void* v, int32_t* kept, int32_t* n_kept, void* stream) {
+    const char* fn = "tkv_evict_keys";
+    tkv::clear_error();
+    if (const int rc = check_pool(fn, shape)) return rc;
+    if (!batch) return tkv::set_error(TKV_EINVAL, "%s: batch is NULL", fn);
+    const tkv_evict_batch& b = *batch;
+    if (b.n_rows < 0 || b.n_kv_blocks < 0 || b.n_new_blocks < 0 || b.max_budget < 0 || b.sink < 0 || b.recent < 0)
+        return tkv::set_error(TKV_EINVAL, "%s: n_rows %d, n_kv_blocks %d, n_new_blocks %d, max_budget %d, sink %d, recent %d", fn,
+                              b.n_rows, b.n_kv_blocks, b.n_new_blocks, b.max_budget, b.sink, b.recent);
+    if (b.max_blocks < 1) return tkv::set_error(TKV_EINVAL, "%s: max_blocks = %d < 1", fn, b.max_blocks);
+    if (const int rc = check_tables(fn, b.max_blocks, keys)) return rc;
+    if (b.n_rows == 0) return TKV_OK;
+    if (!b.kv_indptr || !b.block_len || !b.new_indptr || !b.budget || (b.n_kv_blocks > 0 && !b.kv_blocks) ||
+        (b.n_new_blocks > 0 && !b.new_blocks) || !weights || !out || !k || !v || !n_kept || (b.max_budget > 0 && !kept))
+        return tkv::set_error(TKV_EINVAL, "%s: NULL pointer", fn);
+    for (const void* p : {static_cast<const void*>(k), static_cast<const void*>(v)})
+        if (!aligned16(p)) return tkv::set_error(TKV_EINVAL, "%s: k and v must be 16-byte aligned", fn);
+    for (const void* p : {static_cast<const void*>(weights), static_cast<const void*>(out), static_cast<const void*>(kept),
+                          static_cast<const void*>(n_kept)})
+        if (!aligned4(p)) return tkv::set_error(TKV_EINVAL, "%s: tensors must be aligned to their type", fn);
+    const __int128 bytes = static_cast<__int128>(b.n_rows) * shape->hkv * keys * 4;
+    const __int128 w = reinterpret_cast<uintptr_t>(weights), o = reinterpret_cast<uintptr_t>(out);
+    if (w < o + bytes && o < w + bytes) return tkv::set_error(TKV_EINVAL, "%s: out overlaps weights", fn);
+    if (!tkv::launch_evict_keys) return tkv::set_error(TKV_EHIP, "%s: host-only build, no device", fn);
+    return tkv::launch_evict_keys(*shape, b, weights, out, keys, k, v, kept, n_kept, stream);
+}
+
+TKV_EXPORT int tkv_adjust_logits(int32_t num_blocks, const int32_t* tokens, const tkv_draft_batch* batch,
+                                 const tkv_logit_rules* rules, int32_t vocab, int32_t in_type, const void* in,
+                                 int64_t in_stride, int32_t out_type, void* out, int64_t out_stride, void* stream) {
+    const char* fn = "tkv_adjust_logits";
+    tkv::clear_error();
+    // the batch's checks ask for a shape of attention heads: any will do
+    const tkv_shape one{1, 1, 64, tkv::kBlock, num_blocks};
+    if (const int rc = check_draft(fn, &one, batch)) return rc;
+    if (!rules) return tkv::set_error(TKV_EINVAL, "%s: rules is NULL", fn);
+    const tkv_draft_batch& b = *batch;
+    const tkv_logit_rules& u = *rules;
+    if (const int rc = check_tables(fn, b.max_blocks, INT64_MAX)) return rc;
+    if (vocab < 1 || vocab > kMaxFilterVocab) return tkv::set_error(TKV_EINVAL, "%s: vocabulary %d is not in [1, %d]", fn, vocab, kMaxFilterVocab);
+    for (const int32_t type : {in_type, out_type})
+        if (type != TKV_LOGITS_F32 && type != TKV_LOGITS_BF16) return tkv::set_error(TKV_EINVAL, "%s: logits' type %d", fn, type);
+    for (const int64_t stride : {in_stride, out_stride})
+        if (stride < vocab)
+            return tkv::set_error(TKV_EINVAL, "%s: stride %lld < vocab %d", fn, static_cast<long long>(stride), vocab);
+    if (u.n_bias < 0 || u.n_grammars < 0) return tkv::set_error(TKV_EINVAL, "%s: n_bias %d, n_grammars %d", fn, u.n_bias, u.n_grammars);
+    if (u.n_grammars > 0 && u.allowed_words < (vocab + 31) / 32)
+        return tkv::set_error(TKV_EINVAL, "%s: %d words do not hold %d tokens", fn, u.allowed_words, vocab);
+    if (b.n_rows == 0 || b.n_qtok == 0) return TKV_OK;
+    if (!tokens || !b.q_indptr || !b.kv_indptr || !b.block_len || !b.mask || (b.n_kv_blocks > 0 && !b.kv_blocks) || !in || !out ||
+        (u.n_bias > 0 && (!u.bias_indptr || !u.bias_token || !u.bias_value)) || (u.n_grammars > 0 && u.grammar && !u.allowed))
+        return tkv::set_error(TKV_EINVAL, "%s: NULL pointer", fn);
+    if (!aligned16(tokens)) return tkv::set_error(TKV_EINVAL, "%s: tokens must be 16-byte aligned", fn);
+    const int in_size = in_type == TKV_LOGITS_BF16 ? 2 : 4, out_size = out_type == TKV_LOGITS_BF16 ? 2 : 4;
+    if (reinterpret_cast<uintptr_t>(in) % in_size != 0 || reinterpret_cast<uintptr_t>(out) % out_size != 0)
+        return tkv::set_error(TKV_EINVAL, "%s: logits must be aligned to their type", fn);
+    const auto end = [&](const void* p, int64_t stride, int size) {
+        return static_cast<__int128>(reinterpret_cast<uintptr_t>(p)) +
+               (static_cast<__int128>(b.n_qtok - 1) * stride + vocab) * size;
+    };
+    const __int128 i0 = reinterpret_cast<uintptr_t>(in), o0 = reinterpret_cast<uintptr_t>(out);
+    const bool same = in == out && in_type == out_type && (in_stride == out_stride || b.n_qtok == 1);
+    // rows of one pitch may lie between each other
+    const __int128 pitch = static_cast<__int128>(in_stride) * in_size;
+    const __int128 off = ((o0 - i0) % pitch + pitch) % pitch;
+    const bool between = pitch == static_cast<__int128>(out_stride) * out_size && off >= static_cast<__int128>(vocab) * in_size &&
+                         pitch - off >= static_cast<__int128>(vocab) * out_size;
+    if (!same && !between && i0 < end(out, out_stride, out_size) && o0 < end(in, in_stride, in_size))
+        return tkv::set_error(TKV_EINVAL, "%s: out overlaps in", fn);
+    if (!tkv::launch_adjust_logits) return tkv::set_error(TKV_EHIP, "%s: host-only build, no device", fn);
+    tkv::AdjustCall f{};
+    f.b = b, f.u = u, f.num_blocks = num_blocks, f.vocab = vocab, f.tokens = tokens;
+    f.in = in, f.out = out, f.in_stride = in_stride, f.out_stride = out_stride;
+    f.in16 = in_type == TKV_LOGITS_BF16, f.out16 = out_type == TKV_LOGITS_BF16;
+    return tkv::launch_adjust_logits(f, stream);
 }

@@ -245,4 +245,23 @@ inline FilterLayout filter_layout(int32_t n_rows, int32_t vocab) {
     return l;
 }
 __attribute__((weak)) int launch_filter_sample(const FilterCall& f, void* stream);
+
+__attribute__((weak)) int launch_key_weights(const tkv_shape& s, const tkv_draft_batch& b, const void* q, const void* k,
+                                             const float* lse, const float* coef, float decay, const float* before, float* out,
+                                             int64_t keys, void* stream);
+__attribute__((weak)) int launch_evict_keys(const tkv_shape& s, const tkv_evict_batch& b, const float* weights, float* out,
+                                            int64_t keys, void* k, void* v, int32_t* kept, int32_t* n_kept, void* stream);
+
+// The arguments of tkv_adjust_logits.
+struct AdjustCall {
+    tkv_draft_batch b;
+    tkv_logit_rules u;
+    int32_t num_blocks, vocab;
+    const int32_t* tokens;
+    const void* in;
+    void* out;
+    int64_t in_stride, out_stride;
+    bool in16, out16;
+};
+__attribute__((weak)) int launch_adjust_logits(const AdjustCall& f, void* stream);
 }  // namespace tkv
