@@ -429,7 +429,8 @@ int tkv_draft_verify(const tkv_shape* shape, const tkv_draft_batch* batch, const
  *   before   [n_rows][hkv][keys] fp32 (nullable: zeros);  out  the same, and may be the same memory
  *   keys     at least 16 * max_blocks
  * What no key of a row's table has a place for is not written (slots past a block's length, entries that are no blocks, rows
- * that are left out: tokens or table outside the arrays, or longer than max_q or max_blocks).  K of the keys that a token
+ * that are left out: tokens or table outside the arrays, or longer than max_q or max_blocks; where kv_indptr decreases
+ * somewhere, so that rows share entries, rows behind it may be).  K of the keys that a token
  * sees must be finite; what the others hold does not matter.  Results do not depend on how the work is cut.  No workspace.
  * EINVAL (shape and batch as for tkv_draft_verify, keys, decay, NULL pointers, q or k not 16-byte aligned), EHIP. */
 int tkv_key_weights(const tkv_shape* shape, const tkv_draft_batch* batch, const void* q, const void* k, const float* lse,

@@ -13,6 +13,8 @@
 
 namespace {
 
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
 constexpr int kChoose = 1024, kChooseWaves = kChoose / 64;
 constexpr int kCached = 16384;  // entries whose lengths stay in LDS
 constexpr int kBins = 2048;
@@ -187,20 +189,20 @@ __global__ __launch_bounds__(kMove) void move(Args a) {
     const int i = kept[min(lane & 15, n - 1)];
     const int id = a.b.kv_blocks[a.b.kv_indptr[r] + (i >> 4)];
     const int64_t to = (static_cast<int64_t>(a.b.new_blocks[a.b.new_indptr[r] + j]) * a.hkv + g) * (16 * D);
-    uint4 kx[NI], vx[NI];
+    u32x4_t kx[NI], vx[NI];
 #pragma unroll
     for (int s = 0; s < NI; ++s) {
         const int row = s * RPI + lane / CPR;
         const int64_t from = (static_cast<int64_t>(__shfl(id, row)) * a.hkv + g) * (16 * D) + (__shfl(i, row) & 15) * D + lane % CPR * 8;
-        kx[s] = *reinterpret_cast<const uint4*>(a.k + from);
-        vx[s] = *reinterpret_cast<const uint4*>(a.v + from);
+        kx[s] = *reinterpret_cast<const u32x4_t*>(a.k + from);
+        vx[s] = *reinterpret_cast<const u32x4_t*>(a.v + from);
     }
 #pragma unroll
     for (int s = 0; s < NI; ++s) {
         const int row = s * RPI + lane / CPR;
         if (row >= n) continue;
-        *reinterpret_cast<uint4*>(a.k + to + row * D + lane % CPR * 8) = kx[s];
-        *reinterpret_cast<uint4*>(a.v + to + row * D + lane % CPR * 8) = vx[s];
+        *reinterpret_cast<u32x4_t*>(a.k + to + row * D + lane % CPR * 8) = kx[s];
+        *reinterpret_cast<u32x4_t*>(a.v + to + row * D + lane % CPR * 8) = vx[s];
     }
 }
 

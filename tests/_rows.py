@@ -66,9 +66,11 @@ class Rows:
     def path(self, r):
         """Row r's keys in order: their places 16 e + s in its table, and their slots in the pool."""
         t = self.tables[r]
-        at = [BS * e + s for e, b in enumerate(t) if 0 <= b < self.nb and 1 <= self.block_len[b] <= BS for s in range(self.block_len[b])]
-        at = np.asarray(at, np.int64)
-        return at, t[at // BS].astype(np.int64) * BS + at % BS if len(at) else at
+        inside = (t >= 0) & (t < self.nb)
+        lens = np.where(inside, self.block_len[np.where(inside, t, 0)], 0)
+        lens = np.where((lens >= 1) & (lens <= BS), lens, 0)
+        at = np.nonzero((np.arange(BS) < lens[:, None]).reshape(-1))[0]
+        return at, t[at // BS].astype(np.int64) * BS + at % BS
 
     def seen(self, r):
         """[L, N]: which of its keys each of row r's tokens sees."""

@@ -59,7 +59,8 @@ class Case(Rows):
     def want(self, out_rows=()):
         """What the call leaves behind; out_rows: those that it leaves out."""
         n = len(self.tables)
-        k, v, w = (t.cpu() for t in (self.k.view(torch.int16).clone(), self.v.view(torch.int16).clone(), self.weights))
+        old_k, old_v, w = self.k.view(torch.int16).cpu(), self.v.view(torch.int16).cpu(), self.weights.cpu()
+        k, v = old_k.clone(), old_v.clone()
         out = torch.full_like(w, 7.0)
         kept = torch.full((n, self.hkv, self.most), -1, dtype=torch.int32)
         n_kept = torch.zeros(n, dtype=torch.int32)
@@ -76,8 +77,8 @@ class Case(Rows):
                 out[r, h, :m] = w[r, h, at[pick]]
                 to, src = np.arange(m), slot[pick]
                 to = self.new[r][to // BS].astype(np.int64) * BS + to % BS
-                for new, old in ((k, self.k), (v, self.v)):
-                    new[to // BS, h, to % BS] = old.view(torch.int16).cpu()[src // BS, h, src % BS]
+                for new, old in ((k, old_k), (v, old_v)):
+                    new[to // BS, h, to % BS] = old[src // BS, h, src % BS]
         return {"kept": kept, "n_kept": n_kept, "out": out, "k": k, "v": v}
 
     def check(self, got, **more):

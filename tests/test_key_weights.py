@@ -225,6 +225,24 @@ def test_the_same_blocks_twice_and_many_rows():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("L", [2, 20])
+def test_tables_of_the_largest_capacity(L):
+    # maxima and arrays far above what the rows use (a captured call's capacity): hundreds of rows, empty ones among them
+    rng = np.random.default_rng(L)
+    c = Case([(int(n), L) for n in rng.integers(0, 200, 300)] + [(5000, L), (0, 1)], 12, 2, 64, extra_keys=16 * 3600)
+    spare = torch.zeros(3000, dtype=torch.int32, device="cuda")
+    a = c.arrays()
+    want = c.run()
+    c.check(want, rows=list(range(0, 300, 29)) + [255, 256, 300, 301])
+    got = c.run(kv_blocks=torch.cat([a["kv_blocks"], spare]), max_blocks=c.max_blocks + 3600, max_q=64)
+    for r in range(302):   # (another cut of the work, and for small drafts the other kernel: other orders of additions)
+        x, y = got[r], want[r]
+        assert torch.all((x - y).abs() <= 2.0 ** -16 * (1 + y.abs()))
+    few = c.run(kv_blocks=torch.cat([a["kv_blocks"], spare]), max_blocks=c.max_blocks + 3600)
+    c.check(few, rows=list(range(0, 300, 29)) + [255, 256, 300, 301])
+
+
+@pytest.mark.gpu
 def test_pools_and_weights_past_four_gib():
     hkv, d, nb = 8, 128, 140_000
     c = Case([(200, 5)], 16, hkv, d)
