@@ -3,7 +3,7 @@
 //
 // Two launches.  choose: a workgroup a (row, head) finds the weight of the last key that stays by radix selection over the
 // weights' bits (11, 11 and 10 of them, the counts in LDS), then lists the kept keys in path order; keys of equal weight
-// stay from the lowest index on.  move: a wave a new block copies the kept K and V rows.
+// stay from the lowest index on.  move: a wave a new block copies the kept K and V rows, and the weights.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cstdint>
@@ -14,15 +14,18 @@
 namespace {
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef f32x4_t f32x4_u __attribute__((aligned(4)));  // rows start anywhere
 
 constexpr int kChoose = 1024, kChooseWaves = kChoose / 64;
 constexpr int kCached = 16384;  // entries whose lengths stay in LDS
 constexpr int kBins = 2048;
+constexpr int kHeld = 32768;    // slots whose orders stay in LDS
 constexpr int kMove = 256, kMoveWaves = kMove / 64;
 
 struct Args {
     tkv_evict_batch b;
-    int32_t num_blocks, hkv, new_max;  // blocks of the longest new table
+    int32_t num_blocks, hkv, new_max, held;  // blocks of the longest new table; slots whose orders stay in LDS
     const float* weights;
     float* out;
     int64_t keys;
@@ -30,52 +33,54 @@ struct Args {
     int32_t *kept, *n_kept;
 };
 
-// Unsigned numbers in the order of the weights: NaN below everything, the two zeros equal.
+// A slot's order, an unsigned number: the weights' own (NaN below all others, the two zeros equal), 0 where there is no key,
+// kStays for a key that stays whatever its weight.
+constexpr uint32_t kStays = 0xffffffffu;
 __device__ __forceinline__ uint32_t order_of(float w) {
-    const uint32_t u = __float_as_uint(w);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return 0;
-    if (u == 0x80000000u) return u;
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    const uint32_t u = __float_as_uint(w + 0.f);  // (-0 + 0 is 0)
+    return w != w ? 1 : u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
 }
 
 __global__ __launch_bounds__(kChoose) void choose(Args a) {
+    extern __shared__ u32x4_t held[];  // the slots' orders, four by four, of the first a.held of them
     __shared__ uint8_t cached[kCached];
     __shared__ uint32_t hist[kBins];
-    __shared__ int part[kChooseWaves], part2[kChooseWaves], found[4];
-    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+    __shared__ int part[2][kChooseWaves], found[5];
+    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = blockIdx.x / a.hkv, g = blockIdx.x - r * a.hkv;
     const tkv::RowTable tab = tkv::row_table(a.b.kv_indptr, r, a.b.n_kv_blocks, a.b.max_blocks);
     const tkv::RowTable to = tkv::row_table(a.b.new_indptr, r, a.b.n_new_blocks, a.b.n_new_blocks);
     const int budget = a.b.budget[r];
     int32_t* kept = a.kept + (static_cast<int64_t>(r) * a.hkv + g) * a.b.max_budget;
-    const float* w = a.weights + (static_cast<int64_t>(r) * a.hkv + g) * a.keys;
-    float* out = a.out + (static_cast<int64_t>(r) * a.hkv + g) * a.keys;
+    const float* weights = a.weights + (static_cast<int64_t>(r) * a.hkv + g) * a.keys;
 
+    const int fresh = to.ok && tid < to.n ? a.b.new_blocks[to.first + tid] : -1;
     // the path's length, and where its keys between the first and the last begin and end
     bool ok = tab.ok && to.ok && budget >= 0 && budget <= a.b.max_budget;
-    const int sink = min(a.b.sink, budget);
-    int N = 0, lo = 0, hi = 16 * tab.n;
+    const int end = 16 * tab.n, sink = min(a.b.sink, budget), recent = min(a.b.recent, budget - sink);
+    int N = 0, lo = 0, hi = end;
     for (int base = 0; ok && base < tab.n; base += kChoose) {
         const int e = base + tid;
         int id, len = 0, total;
         if (e < tab.n) len = tkv::entry_len(a.b.kv_blocks, a.b.block_len, a.num_blocks, tab.first + e, id);
         if (e < kCached) cached[e] = static_cast<uint8_t>(len);
-        const int number = N + tkv::group_before<kChooseWaves>(len, total, part);
+        const int number = N + tkv::group_before<kChooseWaves>(len, total, part[0]);
         if (sink >= number && sink < number + len) found[0] = 16 * e + (sink - number);
         N += total;
+        if (tab.n <= kChoose) {  // one round: the end is known as well
+            const int last = N - recent;
+            if (last >= number && last < number + len) found[1] = 16 * e + (last - number);
+        }
         __syncthreads();
     }
     const int n = ok ? min(N, budget) : 0;
-    if (ok && N > budget && budget > 0) lo = found[0];
     // new blocks that are not of the pool
     {
-        int bad = 0;
-        for (int e = tid; e < (n + 15) / 16; e += kChoose)
-            if (e >= to.n || static_cast<uint32_t>(a.b.new_blocks[to.first + e]) >= static_cast<uint32_t>(a.num_blocks)) bad = 1;
-        int any;
-        tkv::group_before<kChooseWaves>(bad, any, part);
-        if (any) ok = false;
-        __syncthreads();
+        const int need = (n + 15) / 16;
+        int bad = need > to.n || (tid < need && static_cast<uint32_t>(fresh) >= static_cast<uint32_t>(a.num_blocks));
+        for (int e = kChoose + tid; e < min(need, to.n); e += kChoose)
+            if (static_cast<uint32_t>(a.b.new_blocks[to.first + e]) >= static_cast<uint32_t>(a.num_blocks)) bad = 1;
+        if (__syncthreads_or(bad)) ok = false;
     }
     const int n_out = ok ? n : 0;
     for (int i = n_out + tid; i < a.b.max_budget; i += kChoose) kept[i] = -1;
@@ -86,92 +91,130 @@ __global__ __launch_bounds__(kChoose) void choose(Args a) {
         int id;
         return e < kCached ? static_cast<int>(cached[e]) : tkv::entry_len(a.b.kv_blocks, a.b.block_len, a.num_blocks, tab.first + e, id);
     };
-    uint32_t last = 0;  // the order of the last key that stays, and how many of that order do
-    int equals = 0;
     if (N <= budget) {
-        lo = hi;
+        lo = end;
     } else {
-        const int recent = min(a.b.recent, budget - sink);
+        lo = found[0];
         int after = 0;
-        for (int base = (tab.n - 1) / kChoose * kChoose; recent > 0 && base >= 0 && after < recent; base -= kChoose) {
+        for (int base = (tab.n - 1) / kChoose * kChoose; tab.n > kChoose && recent > 0 && base >= 0 && after < recent; base -= kChoose) {
             const int e = base + tid;
             int total;
             const int len = e < tab.n ? len_of(e) : 0;
-            const int before = tkv::group_before<kChooseWaves>(len, total, part);
+            const int before = tkv::group_before<kChooseWaves>(len, total, part[0]);
             const int behind = after + total - before - len;  // keys behind this entry
             if (behind < recent && recent <= behind + len) found[1] = 16 * e + (len - (recent - behind));
             after += total;
             __syncthreads();
         }
         if (recent > 0) hi = found[1];
-        int left = budget - sink - recent;
-        if (left == 0) {
-            last = 0xffffffffu, equals = 0;  // (no weight has this order)
-        } else {
-            uint32_t high = 0;
-            for (int pass = 0; pass < 3; ++pass) {
-                const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
-                for (int i = tid; i < kBins; i += kChoose) hist[i] = 0;
-                __syncthreads();
-                for (int i = lo + tid; i < hi; i += kChoose) {
-                    if ((i & 15) >= len_of(i >> 4)) continue;
-                    const uint32_t o = order_of(w[i]);
-                    if (pass > 0 && (o ^ high) >> (shift + width) != 0) continue;
-                    atomicAdd(hist + (o >> shift & ((1u << width) - 1)), 1u);
-                }
-                __syncthreads();
-                // the bin, counted from the largest, in which the last one lies
-                const int top = (1 << width) - 1 - 2 * tid;
-                const int h0 = top >= 0 ? hist[top] : 0, h1 = top >= 1 ? hist[top - 1] : 0;
-                int total;
-                const int above = tkv::group_before<kChooseWaves>(h0 + h1, total, part);
-                if (above < left && left <= above + h0) found[2] = top, found[3] = left - above;
-                if (above + h0 < left && left <= above + h0 + h1) found[2] = top - 1, found[3] = left - above - h0;
-                __syncthreads();
-                high |= static_cast<uint32_t>(found[2]) << shift;
-                left = found[3];
-                __syncthreads();
-            }
-            last = high, equals = left;
+    }
+    // the orders of slots 4 q .. 4 q + 3, of one entry
+    const auto orders_at = [&](int q) {
+        const f32x4_t w = *reinterpret_cast<const f32x4_u*>(weights + 4 * static_cast<int64_t>(q));
+        const int len = len_of(q >> 2), slot = 4 * q & 15;
+        u32x4_t o;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = 4 * q + k;
+            o[k] = i < lo || i >= hi ? kStays : order_of(w[k]);
+            if (slot + k >= len) o[k] = 0;
+        }
+        return o;
+    };
+    const int quads = end / 4, in_lds = min(quads, a.held / 4);
+    const auto orders = [&](int q) { return q < in_lds ? held[q] : orders_at(q); };
+    for (int i = tid; i < kBins; i += kChoose) hist[i] = 0;
+    __syncthreads();
+    // equal weights are common: one addition where all lanes of a wave have the same bin
+    const auto add = [&](uint32_t bin) {
+        const uint32_t first = __builtin_amdgcn_readfirstlane(bin);
+        const uint64_t all = __builtin_amdgcn_ballot_w64(true);
+        if (__builtin_amdgcn_ballot_w64(bin != first) != 0)
+            atomicAdd(hist + bin, 1u);
+        else if (lane == __builtin_ctzll(all))
+            atomicAdd(hist + bin, static_cast<uint32_t>(__builtin_popcountll(all)));
+    };
+#pragma unroll 2
+    for (int q = tid; q < quads; q += kChoose) {
+        const u32x4_t o = orders_at(q);
+        if (q < in_lds) held[q] = o;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (o[k] != 0) add(o[k] >> 21);
+    }
+    // the order of the last key that stays, 11, 11 and 10 bits at a time, and how many of that order do
+    uint32_t last = 0;
+    int left = n;
+    for (int low = 21;;) {
+        __syncthreads();
+        // the bin, counted from the largest, in which it lies
+        const int most = low == 0 ? 0x3ff : 0x7ff, top = most - 2 * tid;
+        const int h0 = top >= 0 ? hist[top] : 0, h1 = top >= 1 ? hist[top - 1] : 0;
+        int total;
+        const int above = tkv::group_before<kChooseWaves>(h0 + h1, total, part[0]);
+        if (above < left && left <= above + h0) found[2] = top, found[3] = left - above, found[4] = h0;
+        if (above + h0 < left && left <= above + h0 + h1) found[2] = top - 1, found[3] = left - above - h0, found[4] = h1;
+        __syncthreads();
+        last |= static_cast<uint32_t>(found[2]) << low;
+        left = found[3];
+        if (low == 0) break;
+        if (found[4] == left) {  // the whole bin stays: those of its lowest order as well
+            last = max(last, 1u);
+            break;
+        }
+        const int shift = low;
+        low = low == 21 ? 10 : 0;
+        const uint32_t mask = low == 0 ? 0x3ff : 0x7ff;
+        for (int i = tid; i < kBins; i += kChoose) hist[i] = 0;
+        __syncthreads();
+#pragma unroll 2
+        for (int q = tid; q < quads; q += kChoose) {
+            const u32x4_t o = orders(q);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (o[k] != 0 && ((o[k] ^ last) >> shift) == 0) add(o[k] >> low & mask);
         }
     }
 
-    // the kept ones in path order: a wave a run of slots, counted first
-    const int end = 16 * tab.n, run = (end + 64 * kChooseWaves - 1) / (64 * kChooseWaves) * 64;
-    const int from = min(wid * run, end), until = min(from + run, end);
-    const auto look = [&](int i, bool& sure, bool& equal, float& x) {
-        const bool there = i < until && (i & 15) < len_of(i >> 4);
-        x = there ? w[i] : 0.f;
-        const bool between = i >= lo && i < hi;
-        const uint32_t o = order_of(x);
-        sure = there && (!between || o > last);
-        equal = there && between && o == last;
-    };
-    int n_sure = 0, n_equal = 0;
-    for (int i = from; i < until; i += 64) {
-        bool sure, equal;
-        float x;
-        look(i + lane, sure, equal, x);
-        n_sure += __builtin_popcountll(__builtin_amdgcn_ballot_w64(sure));
-        n_equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(equal));
+    // the kept ones in path order, a wave a run of slots, counted first
+    const int run = (quads + 64 * kChooseWaves - 1) / (64 * kChooseWaves) * 64;
+    const int from = min(wid * run, quads), until = min(from + run, quads);
+    int sures = 0, equals = 0;
+#pragma unroll 2
+    for (int q = from + lane; q < until; q += 64) {
+        const u32x4_t o = orders(q);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sures += o[k] > last, equals += o[k] == last;
     }
-    if (lane == 0) part[wid] = n_sure, part2[wid] = n_equal;
+    {
+        int all_sure, all_equal;
+        tkv::wave_before(sures, all_sure);
+        tkv::wave_before(equals, all_equal);
+        if (lane == 0) part[0][wid] = all_sure, part[1][wid] = all_equal;
+    }
     __syncthreads();
-    int sures = 0, same = 0;
-    for (int x = 0; x < wid; ++x) sures += part[x], same += part2[x];
-    for (int i = from; i < until; i += 64) {
-        bool sure, equal;
-        float x;
-        look(i + lane, sure, equal, x);
-        const uint64_t below = (uint64_t{1} << lane) - 1;
-        const uint64_t se = __builtin_amdgcn_ballot_w64(equal), ss = __builtin_amdgcn_ballot_w64(sure);
-        const int rank = same + __builtin_popcountll(se & below);
-        const int at = sures + __builtin_popcountll(ss & below) + min(rank, equals);
-        if (sure || (equal && rank < equals)) {
-            kept[at] = i + lane;
-            out[at] = x;
+    sures = 0, equals = 0;
+    for (int x = 0; x < wid; ++x) sures += part[0][x], equals += part[1][x];
+    const auto below = [](uint64_t m) {
+        return static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(m >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(m), 0)));
+    };
+#pragma unroll 2
+    for (int base = from; base < until; base += 64) {
+        const int q = base + lane;
+        const u32x4_t o = q < until ? orders(q) : u32x4_t{0, 0, 0, 0};
+        uint64_t s[4], e[4];
+        int at = sures, rank = equals;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            s[k] = __builtin_amdgcn_ballot_w64(o[k] > last), e[k] = __builtin_amdgcn_ballot_w64(o[k] == last);
+            at += below(s[k]), rank += below(e[k]);
+            sures += __builtin_popcountll(s[k]), equals += __builtin_popcountll(e[k]);
         }
-        sures += __builtin_popcountll(ss), same += __builtin_popcountll(se);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (o[k] > last || (o[k] == last && rank < left)) kept[at + min(rank, left)] = 4 * q + k;
+            at += o[k] > last, rank += o[k] == last;
+        }
     }
 }
 
@@ -185,8 +228,9 @@ __global__ __launch_bounds__(kMove) void move(Args a) {
     const int j = x * kMoveWaves + wid, n = a.n_kept[r] - 16 * j;
     if (n <= 0) return;
     // lane l holds the source of slot l % 16
-    const int32_t* kept = a.kept + (static_cast<int64_t>(r) * a.hkv + g) * a.b.max_budget + 16 * j;
-    const int i = kept[min(lane & 15, n - 1)];
+    const int64_t head = static_cast<int64_t>(r) * a.hkv + g;
+    const int i = a.kept[head * a.b.max_budget + 16 * j + min(lane & 15, n - 1)];
+    if (lane < min(16, n)) a.out[head * a.keys + 16 * j + lane] = a.weights[head * a.keys + i];
     const int id = a.b.kv_blocks[a.b.kv_indptr[r] + (i >> 4)];
     const int64_t to = (static_cast<int64_t>(a.b.new_blocks[a.b.new_indptr[r] + j]) * a.hkv + g) * (16 * D);
     u32x4_t kx[NI], vx[NI];
@@ -221,7 +265,8 @@ int tkv::launch_evict_keys(const tkv_shape& s, const tkv_evict_batch& b, const f
     const int64_t moves = rows * ((a.new_max + kMoveWaves - 1) / kMoveWaves);
     if (rows > INT32_MAX || moves > INT32_MAX)
         return set_error(TKV_EINVAL, "tkv_evict_keys: %lld workgroups are too many", static_cast<long long>(std::max(rows, moves)));
-    choose<<<dim3(static_cast<unsigned>(rows)), dim3(kChoose), 0, st>>>(a);
+    a.held = std::min(kHeld, 16 * b.max_blocks);
+    choose<<<dim3(static_cast<unsigned>(rows)), dim3(kChoose), static_cast<size_t>(a.held) * 4, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return set_error(TKV_EHIP, "tkv_evict_keys launch: %s", hipGetErrorString(e));
     if (moves == 0) return TKV_OK;
