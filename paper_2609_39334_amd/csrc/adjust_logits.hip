@@ -8,19 +8,19 @@
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "internal.h"
 #include "rows.h"
 
 namespace {
 
-constexpr int kThreads = 512, kWaves = kThreads / 64;
 constexpr int kTile = 8192;                        // tokens of the vocabulary a workgroup
-constexpr int kLoads = kTile / (4 * kThreads);     // four tokens a load
 constexpr int kMaxDraft = 1024;
-constexpr uint32_t kInPrompt = 0x80000000u, kTimes = 0x7fffffffu;  // a count: seen in the prompt; occurrences past it
+constexpr int kBatch = 4;                          // entries of a table a thread looks at together
 constexpr int32_t kPast = 1 << 30;                 // a drafted token past the prompt
 
+typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x4_t __attribute__((ext_vector_type(4)));
@@ -31,7 +31,8 @@ typedef u16x4_t u16x4_u __attribute__((aligned(2)));
 struct Args {
     tkv_draft_batch b;
     tkv_logit_rules u;
-    int32_t num_blocks, vocab, n_tiles, groups, per;  // groups of `per` query tokens of a row
+    int32_t num_blocks, vocab, n_tiles, groups, per, units;  // groups of `per` query tokens of a row; groups or tokens in all
+    bool spread, search;
     const int32_t* tokens;
     const void* in;
     void* out;
@@ -82,28 +83,77 @@ __device__ __forceinline__ void store4(void* row, int c, int n, f32x4_t x) {
     }
 }
 
-template <bool IN16, bool OUT16, bool BIAS>
+// What a tile's tokens have of something, a number of 16 bits each (two in a word of LDS) or of 32.
+template <bool WIDE>
+struct Cells {
+    using Four = std::conditional_t<WIDE, uint4, uint2>;
+    static constexpr int kWords = WIDE ? kTile : kTile / 2;
+    static constexpr uint32_t kPrompt = WIDE ? 0x80000000u : 0x8000u, kTimes = kPrompt - 1;  // seen in the prompt; times past it
+    uint32_t* at;
+    static __device__ __forceinline__ int shift(uint32_t i) { return WIDE ? 0 : 16 * (i & 1); }
+    __device__ __forceinline__ uint32_t* word(uint32_t i) const { return at + (WIDE ? i : i >> 1); }
+    __device__ __forceinline__ void clear(int tid, int threads) const {
+        for (int i = tid * 4; i < kWords; i += threads * 4) *reinterpret_cast<uint4*>(at + i) = uint4{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ void more(uint32_t i) const { atomicAdd(word(i), 1u << shift(i)); }
+    __device__ __forceinline__ void less(uint32_t i) const { atomicSub(word(i), 1u << shift(i)); }
+    __device__ __forceinline__ bool mark(uint32_t i) const {  // whether it was not marked before
+        return !(atomicOr(word(i), kPrompt << shift(i)) >> shift(i) & kPrompt);
+    }
+    __device__ __forceinline__ void unmark(uint32_t i) const { atomicAnd(word(i), ~(kPrompt << shift(i))); }
+    __device__ __forceinline__ void raise(uint32_t i, uint32_t to) const {  // to the largest of those given
+        if (WIDE) {
+            atomicMax(word(i), to);
+            return;
+        }
+        uint32_t old = *word(i);
+        while ((old >> shift(i) & 0xffff) < to) {
+            const uint32_t seen = atomicCAS(word(i), old, (old & ~(0xffffu << shift(i))) | to << shift(i));
+            if (seen == old) break;
+            old = seen;
+        }
+    }
+    __device__ __forceinline__ void four(int i, uint32_t (&x)[4]) const {
+        const Four f = *reinterpret_cast<const Four*>(word(i));
+        if constexpr (WIDE)
+            x[0] = f.x, x[1] = f.y, x[2] = f.z, x[3] = f.w;
+        else
+            x[0] = f.x & 0xffff, x[1] = f.x >> 16, x[2] = f.y & 0xffff, x[3] = f.y >> 16;
+    }
+};
+
+template <bool IN16, bool OUT16, bool BIAS, bool WIDE, int kThreads>
 __global__ __launch_bounds__(kThreads) void adjust(Args a) {
-    __shared__ __attribute__((aligned(16))) uint32_t count[kTile];
-    __shared__ __attribute__((aligned(16))) int32_t given[BIAS ? kTile : 4];  // a token's last bias, as its number + 1
+    using Cell = Cells<WIDE>;
+    constexpr int kWaves = kThreads / 64, kLoads = kTile / (4 * kThreads);  // four tokens a load
+    __shared__ __attribute__((aligned(16))) uint32_t counted[Cell::kWords];
+    __shared__ __attribute__((aligned(16))) uint32_t biases[BIAS ? Cell::kWords : 4];
     __shared__ int32_t drafted[kMaxDraft];  // a drafted token's place in the tile, with kPast; -1: not in it
-    __shared__ int part[2][kWaves];
+    __shared__ int part[kWaves];
+    const Cell count{counted}, given{biases};  // given: a token's last bias, as its number + 1
     const int tid = threadIdx.x;
-    const int tile = blockIdx.x % a.n_tiles, g = blockIdx.x / a.n_tiles;
-    const int r = g / a.groups;
+    int tile = blockIdx.x % a.n_tiles, g = blockIdx.x / a.n_tiles;
+    if (a.spread) {  // a row's tiles on one XCD, whose L2 then holds its path
+        const int of8 = blockIdx.x >> 3;
+        tile = of8 % a.n_tiles, g = of8 / a.n_tiles * 8 + (blockIdx.x & 7);
+        if (g >= a.units) return;
+    }
+    // what the row is: all of it is asked for before anything is waited for
+    int r = g % a.b.n_rows;
+    if (a.search) {  // g is a query token: its row
+        __shared__ int row;
+        if (tid == 0) row = INT32_MAX;
+        __syncthreads();
+        for (int r0 = 0; r0 < a.b.n_rows; r0 += kThreads) {
+            const int mine = r0 + tid;
+            const tkv::RowTokens m = mine < a.b.n_rows ? tkv::row_tokens(a.b, mine) : tkv::RowTokens{};
+            if (m.ok && g >= m.q0 && g < m.q0 + m.L) atomicMin(&row, mine);
+            if (__syncthreads_or(m.ok && g >= m.q0 && g < m.q0 + m.L)) break;
+        }
+        r = __builtin_amdgcn_readfirstlane(row);
+        if (r == INT32_MAX) return;
+    }
     const tkv::RowTokens t = tkv::row_tokens(a.b, r);
-    const int first = (g - r * a.groups) * a.per;
-    if (!t.ok || first >= t.L) return;
-    const int end = min(t.L, first + a.per);
-    const int c0 = tile * kTile, n = min(kTile, a.vocab - c0);
-    const char* in = static_cast<const char*>(a.in) + (static_cast<int64_t>(t.q0 + first) * a.in_stride + c0) * (IN16 ? 2 : 4);
-    char* out = static_cast<char*>(a.out) + (static_cast<int64_t>(t.q0 + first) * a.out_stride + c0) * (OUT16 ? 2 : 4);
-    const int64_t in_step = a.in_stride * (IN16 ? 2 : 4), out_step = a.out_stride * (OUT16 ? 2 : 4);
-
-    f32x4_t x[kLoads];
-#pragma unroll
-    for (int k = 0; k < kLoads; ++k) x[k] = load4<IN16>(in, (k * kThreads + tid) * 4, n);
-
     const tkv::RowTable tab = tkv::row_table(a.b.kv_indptr, r, a.b.n_kv_blocks, a.b.max_blocks);
     const float rep = a.u.repetition ? a.u.repetition[r] : 1.f;
     const float pres = a.u.presence ? a.u.presence[r] : 0.f;
@@ -111,107 +161,156 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
     const int prompt = a.u.prompt_len ? a.u.prompt_len[r] : 0;
     tkv::RowTable bias{0, 0, true};
     if (BIAS) bias = tkv::row_table(a.u.bias_indptr, r, a.u.n_bias, a.u.n_bias);
+    const int first = a.search ? g - t.q0 : g / a.b.n_rows * a.per;
+    if (!t.ok || first >= t.L) return;
+    const int end = a.search ? first + 1 : min(t.L, first + a.per);
+    const int c0 = tile * kTile, n = min(kTile, a.vocab - c0);
+    const char* in = static_cast<const char*>(a.in) + (static_cast<int64_t>(t.q0 + first) * a.in_stride + c0) * (IN16 ? 2 : 4);
+    char* out = static_cast<char*>(a.out) + (static_cast<int64_t>(t.q0 + first) * a.out_stride + c0) * (OUT16 ? 2 : 4);
+    const int64_t in_step = a.in_stride * (IN16 ? 2 : 4), out_step = a.out_stride * (OUT16 ? 2 : 4);
     const bool ok = tab.ok && bias.ok && rep > 0.f && rep < INFINITY && fabsf(pres) < INFINITY && fabsf(freq) < INFINITY;
     const bool counts = ok && (rep != 1.f || pres != 0.f || freq != 0.f);
     const bool biased = BIAS && ok && bias.n > 0;
 
+    // a thread a run of entries, kBatch of them at once; the first one's tokens are on their way before it is known where the run
+    // begins in the path
+    const int run = (tab.n + kThreads - 1) / kThreads;
+    const int e0 = tab.first + min(tid * run, tab.n), e1 = tab.first + min(tid * run + run, tab.n);
+    int id[kBatch], len[kBatch], keys = 0;
+    const auto look = [&](int e) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) id[k] = e + k < e1 ? a.b.kv_blocks[e + k] : -1;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const bool there = static_cast<uint32_t>(id[k]) < static_cast<uint32_t>(a.num_blocks);
+            len[k] = there ? a.b.block_len[id[k]] : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) len[k] = len[k] >= 1 && len[k] <= tkv::kBlock ? len[k] : 0;
+    };
+    i32x4_t tok[4];
+    const auto fetch = [&](int block) __attribute__((always_inline)) {
+        const i32x4_t* p = reinterpret_cast<const i32x4_t*>(a.tokens + static_cast<int64_t>(block) * tkv::kBlock);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tok[q] = p[q];
+    };
     if (counts) {
-        for (int c = tid * 4; c < kTile; c += kThreads * 4) *reinterpret_cast<uint4*>(count + c) = uint4{0, 0, 0, 0};
+        for (int e = e0 + (run - 1) / kBatch * kBatch; e >= e0; e -= kBatch) {  // the first ones last: they stay
+            look(e);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) keys += len[k];
+        }
+        if (len[0] > 0) fetch(id[0]);
+    }
+    // a query token's logits, its grammar's words, and which of this thread's drafted tokens it sees
+    f32x4_t x[kLoads];
+    uint32_t words[kLoads], sees;
+    bool fine, masked;
+    const auto ask = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) x[k] = load4<IN16>(in, (k * kThreads + tid) * 4, n);
+        const int64_t q = t.q0 + i;
+        const int grammar = a.u.grammar ? a.u.grammar[q] : -1;
+        fine = ok && grammar < a.u.n_grammars;
+        masked = fine && grammar >= 0;
+        if (masked) {
+            const uint32_t* allowed = a.u.allowed + static_cast<int64_t>(grammar) * a.u.allowed_words;
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) {
+                const int c = (k * kThreads + tid) * 4;
+                if (c < n) words[k] = allowed[(c0 + c) >> 5];
+            }
+        }
+        sees = 0;
+        if (counts) {
+            const uint64_t* mask = a.b.mask + q * a.b.mask_words;
+            if (t.L == 1)
+                sees = static_cast<uint32_t>(mask[0] & 1);
+            else
+                for (int j = tid, b = 0; j < t.L; j += kThreads, ++b) sees |= static_cast<uint32_t>(mask[j >> 6] >> (j & 63) & 1) << b;
+        }
+    };
+    ask(first);
+    if (counts) {
+        count.clear(tid, kThreads);
         for (int j = tid; j < t.L; j += kThreads) drafted[j] = -1;
     }
-    if (biased)
-        for (int c = tid * 4; c < kTile; c += kThreads * 4) *reinterpret_cast<uint4*>(given + c) = uint4{0, 0, 0, 0};
-    if (counts || biased) __syncthreads();
+    if (biased) given.clear(tid, kThreads);
+    if (biased && !counts) __syncthreads();
+    if (counts) {
+        int N;
+        int number = tkv::group_before<kWaves>(keys, N, part);  // (its barrier is the one after the clearing)
+        const int context = N - t.L;
+        for (int e = e0; e < e1; e += kBatch) {
+            if (e > e0) look(e);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                if (len[k] == 0) continue;
+                if (e > e0 || k > 0) fetch(id[k]);
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                    const uint32_t at = static_cast<uint32_t>(tok[q >> 2][q & 3]) - static_cast<uint32_t>(c0);
+                    if (q >= len[k] || at >= static_cast<uint32_t>(n)) continue;
+                    const bool past = number + q >= prompt;
+                    if (number + q >= context && (t.L > 1 || !sees)) {
+                        if (t.L > 1) drafted[number + q - context] = static_cast<int32_t>(at) | (past ? kPast : 0);
+                    } else if (past) {
+                        count.more(at);
+                    } else {
+                        count.mark(at);
+                    }
+                }
+                number += len[k];
+            }
+        }
+    }
     if (biased) {
         for (int e = tid; e < bias.n; e += kThreads) {
             const uint32_t at = static_cast<uint32_t>(a.u.bias_token[bias.first + e]) - static_cast<uint32_t>(c0);
-            if (at < static_cast<uint32_t>(n)) atomicMax(given + at, e + 1);
+            if (at < static_cast<uint32_t>(n)) given.raise(at, static_cast<uint32_t>(e) + 1);
         }
     }
-    if (counts) {
-        int N = 0;
-        if (tab.n > kThreads) {
-            int mine = 0, id;
-            for (int e = tid; e < tab.n; e += kThreads) mine += tkv::entry_len(a.b.kv_blocks, a.b.block_len, a.num_blocks, tab.first + e, id);
-            tkv::group_before<kWaves>(mine, N, part[1]);
-        }
-        int run = 0;
-        for (int base = 0; base < tab.n; base += kThreads) {
-            int id = 0, len = 0, total;
-            if (base + tid < tab.n) len = tkv::entry_len(a.b.kv_blocks, a.b.block_len, a.num_blocks, tab.first + base + tid, id);
-            int4 tok[4];
-            if (len > 0) {
-                const int4* p = reinterpret_cast<const int4*>(a.tokens + static_cast<int64_t>(id) * tkv::kBlock);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) tok[q] = p[q];
-            }
-            const int before = run + tkv::group_before<kWaves>(len, total, part[0]);
-            if (tab.n <= kThreads) N = total;
-            run += total;
-            const int context = N - t.L;
-            if (len > 0) {
-#pragma unroll
-                for (int q = 0; q < 16; ++q) {
-                    const uint32_t at = static_cast<uint32_t>((&tok[0].x)[q]) - static_cast<uint32_t>(c0);
-                    if (q >= len || at >= static_cast<uint32_t>(n)) continue;
-                    const int number = before + q;
-                    if (number >= context)
-                        drafted[number - context] = static_cast<int32_t>(at) | (number >= prompt ? kPast : 0);
-                    else if (number >= prompt)
-                        atomicAdd(count + at, 1u);
-                    else
-                        atomicOr(count + at, kInPrompt);
-                }
-            }
-            __syncthreads();  // (part is free again; after the last round: everything is counted)
-        }
-    }
-    if (biased) __syncthreads();
+    if (counts || biased) __syncthreads();
 
     const float inv = 1.f / rep;
-    for (int i = first; i < end; ++i) {
-        const int64_t q = t.q0 + i;
+    for (int i = first;;) {
+        const bool tree = counts && t.L > 1;
         uint32_t put = 0;  // which of this thread's drafted tokens were the first to be seen in the prompt
-        if (counts) {
-            const uint64_t* mask = a.b.mask + q * a.b.mask_words;
-            int b = 0;
-            for (int j = tid; j < t.L; j += kThreads, ++b) {
+        if (tree) {
+            for (int j = tid, b = 0; j < t.L; j += kThreads, ++b) {
                 const int32_t d = drafted[j];
-                if (d < 0 || !(mask[j >> 6] >> (j & 63) & 1)) continue;
+                if (d < 0 || !(sees >> b & 1)) continue;
                 if (d & kPast)
-                    atomicAdd(count + (d & ~kPast), 1u);
-                else if (!(atomicOr(count + d, kInPrompt) & kInPrompt))
+                    count.more(d & ~kPast);
+                else if (count.mark(d))
                     put |= 1u << b;
             }
             __syncthreads();
         }
-        const int grammar = a.u.grammar ? a.u.grammar[q] : -1;
-        const bool fine = ok && grammar < a.u.n_grammars;
-        const uint32_t* allowed = grammar >= 0 && fine ? a.u.allowed + static_cast<int64_t>(grammar) * a.u.allowed_words : nullptr;
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
             const int c = (k * kThreads + tid) * 4;
             if (c >= n) continue;
             f32x4_t y = x[k];
             if (counts) {
-                const uint4 s4 = *reinterpret_cast<const uint4*>(count + c);
-                const uint32_t* s = &s4.x;
+                uint32_t s[4];
+                count.four(c, s);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if (s[e] != 0) y[e] = y[e] > 0.f ? y[e] * inv : y[e] * rep;
-                    const uint32_t times = s[e] & kTimes;
+                    const uint32_t times = s[e] & Cell::kTimes;
                     if (times != 0) y[e] = y[e] - freq * static_cast<float>(times) - pres;
                 }
             }
             if (biased) {
-                const int4 w4 = *reinterpret_cast<const int4*>(given + c);
-                const int32_t* w = &w4.x;
+                uint32_t w[4];
+                given.four(c, w);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (w[e] != 0) y[e] += a.u.bias_value[bias.first + w[e] - 1];
+                    if (w[e] != 0) y[e] += a.u.bias_value[bias.first + static_cast<int>(w[e]) - 1];
             }
-            if (allowed) {
-                const uint32_t bits = allowed[(c0 + c) >> 5] >> ((c0 + c) & 31);
+            if (masked) {
+                const uint32_t bits = words[k] >> ((c0 + c) & 31);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (!(bits >> e & 1)) y[e] = -INFINITY;
@@ -219,21 +318,19 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
             if (!fine) y = f32x4_t{NAN, NAN, NAN, NAN};
             store4<OUT16>(out, c, n, y);
         }
+        if (++i == end) break;
         in += in_step, out += out_step;
-        if (i + 1 == end) break;
-#pragma unroll
-        for (int k = 0; k < kLoads; ++k) x[k] = load4<IN16>(in, (k * kThreads + tid) * 4, n);
-        if (counts) {
+        const uint32_t seen = sees;
+        ask(i);
+        if (tree) {
             __syncthreads();
-            int b = 0;
-            const uint64_t* mask = a.b.mask + q * a.b.mask_words;
-            for (int j = tid; j < t.L; j += kThreads, ++b) {
+            for (int j = tid, b = 0; j < t.L; j += kThreads, ++b) {
                 const int32_t d = drafted[j];
-                if (d < 0 || !(mask[j >> 6] >> (j & 63) & 1)) continue;
+                if (d < 0 || !(seen >> b & 1)) continue;
                 if (d & kPast)
-                    atomicSub(count + (d & ~kPast), 1u);
+                    count.less(d & ~kPast);
                 else if (put >> b & 1)
-                    atomicAnd(count + d, kTimes);
+                    count.unmark(d);
             }
             __syncthreads();
         }
@@ -249,20 +346,39 @@ int tkv::launch_adjust_logits(const AdjustCall& f, void* stream) {
     a.num_blocks = f.num_blocks, a.vocab = f.vocab, a.tokens = f.tokens;
     a.in = f.in, a.out = f.out, a.in_stride = f.in_stride, a.out_stride = f.out_stride;
     a.n_tiles = (f.vocab + kTile - 1) / kTile;
-    const int64_t units = static_cast<int64_t>(a.n_tiles) * f.b.n_qtok;
-    a.per = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, f.b.max_q), units / 2048)));
+    const int64_t tiles = static_cast<int64_t>(a.n_tiles) * f.b.n_qtok;
+    a.per = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, f.b.max_q), tiles / 4096)));
     a.groups = (f.b.max_q + a.per - 1) / a.per;
-    const int64_t grid = static_cast<int64_t>(a.n_tiles) * a.groups * f.b.n_rows;
-    if (grid > INT32_MAX)
-        return set_error(TKV_EINVAL, "tkv_adjust_logits: %lld workgroups are too many", static_cast<long long>(grid));
-    const auto run = [&](auto kernel) { kernel<<<dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, st>>>(a); };
-    const bool bias = f.u.n_bias > 0;
-    if (f.in16)
-        f.out16 ? (bias ? run(adjust<true, true, true>) : run(adjust<true, true, false>))
-                : (bias ? run(adjust<true, false, true>) : run(adjust<true, false, false>));
-    else
-        f.out16 ? (bias ? run(adjust<false, true, true>) : run(adjust<false, true, false>))
-                : (bias ? run(adjust<false, false, true>) : run(adjust<false, false, false>));
+    a.search = f.b.max_q > 1 && a.per == 1;
+    int64_t all = a.search ? f.b.n_qtok : static_cast<int64_t>(a.groups) * f.b.n_rows;
+    const int64_t most = (all + 7) / 8 * 8 * a.n_tiles;
+    if (most > INT32_MAX)
+        return set_error(TKV_EINVAL, "tkv_adjust_logits: %lld workgroups are too many", static_cast<long long>(most));
+    a.units = static_cast<int32_t>(all);
+    a.spread = all >= 64;
+    if (a.spread) all = (all + 7) / 8 * 8;
+    const bool bias = f.u.n_bias > 0, wide = f.b.max_blocks > 0x7fff / kBlock || f.u.n_bias >= 0xffff;
+    const bool many = all * a.n_tiles >= 768;
+    const auto run = [&](auto kernel, int threads) {
+        kernel<<<dim3(static_cast<unsigned>(all * a.n_tiles)), dim3(threads), 0, st>>>(a);
+    };
+    const auto typed = [&](auto has_bias, auto is_wide, auto n_threads) {
+        constexpr bool B = decltype(has_bias)::value, W = decltype(is_wide)::value;
+        constexpr int T = decltype(n_threads)::value;
+        if (f.in16)
+            f.out16 ? run(adjust<true, true, B, W, T>, T) : run(adjust<true, false, B, W, T>, T);
+        else
+            f.out16 ? run(adjust<false, true, B, W, T>, T) : run(adjust<false, false, B, W, T>, T);
+    };
+    const auto sized = [&](auto has_bias) {
+        if (wide)
+            typed(has_bias, std::true_type{}, std::integral_constant<int, 512>{});
+        else if (many)
+            typed(has_bias, std::false_type{}, std::integral_constant<int, 256>{});
+        else
+            typed(has_bias, std::false_type{}, std::integral_constant<int, 512>{});
+    };
+    bias ? sized(std::true_type{}) : sized(std::false_type{});
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? TKV_OK : set_error(TKV_EHIP, "tkv_adjust_logits launch: %s", hipGetErrorString(e));
 }

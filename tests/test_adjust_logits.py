@@ -141,6 +141,17 @@ def test_long_paths():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("m", [60000, 70000])
+def test_biases_for_every_token(m):
+    # many times over: the last one counts
+    c = Case([(300, 2), (50, 1)], 9001, 5)
+    c.rules["bias_indptr"] = np.array([0, m, m + 10], np.int32)
+    c.rules["bias_token"] = c.rng.integers(0, 9001, m + 10).astype(np.int32)
+    c.rules["bias_value"] = c.rng.normal(size=m + 10).astype(np.float32)
+    c.check(c.run())
+
+
+@pytest.mark.gpu
 def test_rules_that_are_off():
     names = ["prompt_len", "repetition", "presence", "frequency", "bias", "grammar"]
     for off in [names] + [[x] for x in names] + [names[:4], names[4:], names[1:]]:
