@@ -26,13 +26,14 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kFewChunk = 256;    // most entries a workgroup of weigh_few
 constexpr int kManyChunk = 16;    // entries a workgroup of weigh_many
-constexpr int kWords = 5;         // words of a mask that 256 consecutive bits can touch
+constexpr int kWords = 9;         // words of 32 bits that 256 consecutive bits can touch
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Args {
     tkv_draft_batch b;
     int32_t num_blocks, hq, hkv, G, chunk, n_chunks;  // entries a chunk, chunks of the longest table
     bool search;                                      // units are counted over the rows
+    uint32_t inv_g;                                   // 2^31 / G, rounded up
     float sl2, decay;                                 // log2(e) / sqrt(d)
     const uint16_t *q, *k;
     const float *lse, *coef, *before;
@@ -52,7 +53,7 @@ __device__ __forceinline__ Unit unit_of(const Args& a) {
     u.r = -1;
     int x = blockIdx.x;
     if (!a.search) {
-        u.e0 = x % a.n_chunks * a.chunk;
+        u.e0 = (a.n_chunks - 1 - x % a.n_chunks) * a.chunk;  // (a row's last keys, with masks, first)
         x /= a.n_chunks;
         u.g = x % a.hkv, u.r = x / a.hkv;
     } else {
@@ -99,24 +100,33 @@ __device__ __forceinline__ Unit unit_of(const Args& a) {
 // The chunk's blocks: {id, 32 (first key's number among the drafted ones, at least -64) + length}; n: entries of the chunk, at
 // most as many as threads.  Ends in a barrier.
 __device__ __forceinline__ void list_blocks(const Args& a, const Unit& u, int n, int2* list, int* part) {
-    const int tid = threadIdx.x;
-    int id = 0, len = 0, total;
-    if (tid < n && u.e0 + tid < u.tab.n)
-        len = tkv::entry_len(a.b.kv_blocks, a.b.block_len, a.num_blocks, u.tab.first + u.e0 + tid, id);
+    const int tid = threadIdx.x, step = min(kThreads, u.t.L);
+    const int mine = u.e0 + tid, later = u.e0 + n + tid;
+    int id = -1, behind = -1, len = 0, more = 0, total;
+    if (tid < n && mine < u.tab.n) id = a.b.kv_blocks[u.tab.first + mine];
+    if (tid < step && later < u.tab.n) behind = a.b.kv_blocks[u.tab.first + later];
+    if (static_cast<uint32_t>(id) < static_cast<uint32_t>(a.num_blocks)) len = a.b.block_len[id];
+    if (static_cast<uint32_t>(behind) < static_cast<uint32_t>(a.num_blocks)) more = a.b.block_len[behind];
+    len = len >= 1 && len <= tkv::kBlock ? len : 0;
+    more = more >= 1 && more <= tkv::kBlock ? more : 0;
+    const int before = tkv::group_before<kWaves>(more << 16 | len, total, part) & 0xffff;
     // keys behind the chunk, exact below the row's tokens
-    int after = 0;
-    const int step = min(kThreads, u.t.L);
-    for (int next = u.e0 + n; after < u.t.L && next < u.tab.n; next += step) {
-        int other, more = 0;
-        if (next + tid < u.tab.n && tid < step)
-            more = tkv::entry_len(a.b.kv_blocks, a.b.block_len, a.num_blocks, u.tab.first + next + tid, other);
-        tkv::group_before<kWaves>(more, total, part);
+    int after = total >> 16;
+    for (int next = u.e0 + n + step; after < u.t.L && next < u.tab.n; next += step) {
+        int other, sum = 0;
         __syncthreads();
-        after += total;
+        if (tid < step && next + tid < u.tab.n)
+            sum = tkv::entry_len(a.b.kv_blocks, a.b.block_len, a.num_blocks, u.tab.first + next + tid, other);
+        tkv::group_before<kWaves>(sum, sum, part);
+        after += sum;
     }
-    const int before = tkv::group_before<kWaves>(len, total, part);
-    if (tid < n) list[tid] = int2{id, 32 * max(u.t.L - (after + total - before), -64) + len};
+    if (tid < n) list[tid] = int2{id, 32 * max(u.t.L - (after + (total & 0xffff) - before), -64) + len};
     __syncthreads();
+}
+
+// Query row qr of a (row, KV head) is head qr % G of token qr / G (rows below 2^16, G at most 64).
+__device__ __forceinline__ int token_of(const Args& a, int qr) {
+    return static_cast<int>(__umulhi(static_cast<uint32_t>(2 * qr), a.inv_g));
 }
 
 // What is subtracted from a query row's score, in units of log2: infinite for a row that gives nothing.
@@ -137,17 +147,18 @@ __global__ __launch_bounds__(kThreads, 3) void weigh_few(Args a) {
     const int rows = u.t.L * a.G, nu = (rows + 7) / 8;
     bf16x8_t qf[KS];
     {
-        const int qr = min(col, rows - 1), i = qr / a.G;
+        const int qr = min(col, rows - 1), i = token_of(a, qr);
         const uint16_t* row = a.q + (static_cast<int64_t>(u.t.q0 + i) * a.hq + u.g * a.G + (qr - i * a.G)) * D + 8 * hi;
 #pragma unroll
         for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8_t*>(row + 16 * s);
     }
     // x[4 v + e] of a product is query row 8 v + 4 hi + e
     float off[16];
+    {
+        const int i = token_of(a, min(col, rows - 1));
+        const float mine = col < rows ? offset_of(a, u.t.q0 + i, u.g * a.G + (col - i * a.G)) : INFINITY;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        const int row = 8 * (e >> 2) + 4 * hi + (e & 3), i = row / a.G;
-        off[e] = row < rows ? offset_of(a, u.t.q0 + i, u.g * a.G + (row - i * a.G)) : INFINITY;
+        for (int e = 0; e < 16; ++e) off[e] = __shfl(mine, 8 * (e >> 2) + 4 * hi + (e & 3));
     }
     const int n = min(a.chunk, u.tab.n - u.e0), pairs = (n + 1) / 2;
     list_blocks(a, u, a.chunk, list, part);
@@ -185,7 +196,7 @@ __global__ __launch_bounds__(kThreads, 3) void weigh_few(Args a) {
             for (int e = 0; e < 4 * nu; ++e) {
                 const int row = 8 * (e >> 2) + 4 * hi + (e & 3);
                 if (there && row < rows &&
-                    (j < 0 || a.b.mask[static_cast<int64_t>(u.t.q0 + row / a.G) * a.b.mask_words + (j >> 6)] >> (j & 63) & 1))
+                    (j < 0 || a.b.mask[static_cast<int64_t>(u.t.q0 + token_of(a, row)) * a.b.mask_words + (j >> 6)] >> (j & 63) & 1))
                     sees |= 1u << e;
             }
 #pragma unroll
@@ -212,11 +223,11 @@ __global__ __launch_bounds__(kThreads, 3) void weigh_few(Args a) {
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
+__global__ __launch_bounds__(kThreads, 3) void weigh_many(Args a) {
     constexpr int KS = D / 16, CPR = D / 8, kPieces = 32 * CPR / kThreads;  // 16-byte pieces a row, pieces of a tile a thread
     __shared__ __attribute__((aligned(16))) uint16_t qs[2][32 * D];
     __shared__ __attribute__((aligned(16))) float offs[2][32];
-    __shared__ uint64_t bits[2][32][kWords];  // the rows' masks from the chunk's first drafted key on
+    __shared__ uint32_t bits[2][32][kWords];  // the rows' masks from the chunk's first drafted key on
     __shared__ int2 list[kManyChunk];
     __shared__ int part[kWaves];
     const Unit u = unit_of(a);
@@ -224,11 +235,30 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, hi = lane >> 5;
     const int rows = u.t.L * a.G, n_tiles = (rows + 31) / 32;
+
+    // a tile of 32 query rows, their 16-byte pieces XOR-swizzled by row so that the operand reads meet no bank conflict
+    u32x4_t qx[kPieces];
+    float ox = 0.f;
+    uint32_t bx[2] = {0, 0};
+    const auto fetch_q = [&](int tile) __attribute__((always_inline)) {
+#pragma unroll
+        for (int y = 0; y < kPieces; ++y) {
+            const int x = y * kThreads + tid, qr = min(32 * tile + x / CPR, rows - 1), i = token_of(a, qr);
+            qx[y] = *reinterpret_cast<const u32x4_t*>(a.q + (static_cast<int64_t>(u.t.q0 + i) * a.hq + u.g * a.G + (qr - i * a.G)) * D + x % CPR * 8);
+        }
+        if (tid < 32) {
+            const int qr = 32 * tile + tid, i = token_of(a, min(qr, rows - 1));
+            ox = qr < rows ? offset_of(a, u.t.q0 + i, u.g * a.G + (qr - i * a.G)) : INFINITY;
+        }
+    };
+    fetch_q(0);
     list_blocks(a, u, kManyChunk, list, part);
 
     bf16x8_t kf[2][KS];
     int j[2], place[2];
     bool there[2];
+    int low = INT32_MAX, high = -1;  // the wave's drafted keys
+    bool context = false;            // whether it has others
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int e = 4 * wid + 2 * h + (col >> 4), slot = col & 15;
@@ -244,41 +274,30 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
             for (int s = 0; s < KS; ++s) kf[h][s] = *reinterpret_cast<const bf16x8_t*>(row + 16 * s);
         }
     }
-    // whether the chunk holds drafted keys, and the mask's words from the first of them on
-    bool some = false;
-    int w0 = 0;
-    {
-        int lowest = INT32_MAX;
-        for (int e = 0; e < kManyChunk; ++e) {
-            const int2 d = list[e];
-            if ((d.y & 31) == 0) continue;
-            const int last = (d.y >> 5) + (d.y & 31) - 1;
-            if (last >= 0) some = true, lowest = min(lowest, max(d.y >> 5, 0));
-        }
-        if (some) w0 = lowest >> 6;
+    int lowest = INT32_MAX;  // the chunk's first drafted key
+    for (int e = kManyChunk - 1; e >= 0; --e) {
+        const int first = list[e].y >> 5, len = list[e].y & 31;
+        if (len == 0) continue;
+        if (first + len > 0) lowest = max(first, 0);
+        if (e >> 2 != wid) continue;
+        if (first < 0) context = true;
+        if (first + len > 0) low = max(first, 0), high = max(high, first + len - 1);
     }
-    const bool drafted = __builtin_amdgcn_ballot_w64((there[0] && j[0] >= 0) || (there[1] && j[1] >= 0)) != 0;
-
-    // a tile of 32 query rows, their 16-byte pieces XOR-swizzled by row so that the operand reads meet no bank conflict
-    u32x4_t qx[kPieces];
-    float ox = 0.f;
-    uint64_t bx = 0;
-    const auto fetch = [&](int tile) {
+    lowest = __builtin_amdgcn_readfirstlane(lowest), low = __builtin_amdgcn_readfirstlane(low);
+    high = __builtin_amdgcn_readfirstlane(high), context = __builtin_amdgcn_readfirstlane(context);
+    const bool some = lowest < INT32_MAX, drafted = high >= 0;
+    const int w0 = some ? lowest >> 5 : 0;
+    const auto fetch_bits = [&](int tile) __attribute__((always_inline)) {
+        if (!some) return;
+        const uint32_t* masks = reinterpret_cast<const uint32_t*>(a.b.mask);
 #pragma unroll
-        for (int y = 0; y < kPieces; ++y) {
-            const int x = y * kThreads + tid, qr = min(32 * tile + x / CPR, rows - 1), i = qr / a.G;
-            qx[y] = *reinterpret_cast<const u32x4_t*>(a.q + (static_cast<int64_t>(u.t.q0 + i) * a.hq + u.g * a.G + (qr - i * a.G)) * D + x % CPR * 8);
-        }
-        if (tid < 32) {
-            const int qr = 32 * tile + tid, i = qr / a.G;
-            ox = qr < rows ? offset_of(a, u.t.q0 + i, u.g * a.G + (qr - i * a.G)) : INFINITY;
-        }
-        if (some && tid < 32 * kWords) {
-            const int qr = min(32 * tile + tid / kWords, rows - 1), w = w0 + tid % kWords;
-            bx = w < a.b.mask_words && 32 * tile + tid / kWords < rows ? a.b.mask[static_cast<int64_t>(u.t.q0 + qr / a.G) * a.b.mask_words + w] : 0;
+        for (int y = 0; y < 2; ++y) {
+            const int x = y * kThreads + tid, qr = 32 * tile + x / kWords, w = w0 + x % kWords;
+            bx[y] = x < 32 * kWords && w < 2 * a.b.mask_words && qr < rows
+                        ? masks[static_cast<int64_t>(u.t.q0 + token_of(a, qr)) * (2 * a.b.mask_words) + w] : 0;
         }
     };
-    const auto put = [&](int buf) {
+    const auto put = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int y = 0; y < kPieces; ++y) {
             const int x = y * kThreads + tid, row = x / CPR;
@@ -286,43 +305,60 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
             *reinterpret_cast<u32x4_t*>(qs[buf] + row * D + ((x % CPR) ^ swz) * 8) = qx[y];
         }
         if (tid < 32) offs[buf][tid] = ox;
-        if (some && tid < 32 * kWords) bits[buf][tid / kWords][tid % kWords] = bx;
+        if (some) {
+            bits[buf][tid / kWords][tid % kWords] = bx[0];
+            if (tid + kThreads < 32 * kWords) bits[buf][(tid + kThreads) / kWords][(tid + kThreads) % kWords] = bx[1];
+        }
     };
     const int swz = D == 128 ? col & 15 : (col >> 1) & 7;
     float sum[2] = {0.f, 0.f};
-    fetch(0);
+    fetch_bits(0);
     put(0);
     for (int t = 0; t < n_tiles; ++t) {
         const int buf = t & 1;
-        if (t + 1 < n_tiles) fetch(t + 1);
+        if (t + 1 < n_tiles) fetch_q(t + 1), fetch_bits(t + 1);
         __syncthreads();
-        f32x16_t x0{}, x1{};
-        const uint16_t* row = qs[buf] + col * D;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            const bf16x8_t qf = *reinterpret_cast<const bf16x8_t*>(row + ((2 * s + hi) ^ swz) * 8);
-            x0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[0][s], x0, 0, 0, 0);
-            x1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[1][s], x1, 0, 0, 0);
+        // whether the tile's rows (padding aside) see all of the wave's drafted keys, or none
+        bool all = true, none = false;
+        if (drafted) {
+            bool every = true, any = false;
+            for (int w = low >> 5; w <= high >> 5; ++w) {
+                const uint32_t from = w == low >> 5 ? ~0u << (low & 31) : ~0u, to = w == high >> 5 ? ~0u >> (31 - (high & 31)) : ~0u;
+                const uint32_t seen = bits[buf][col][w - w0] & from & to;
+                every = every && seen == (from & to), any = any || seen != 0;
+            }
+            all = __builtin_amdgcn_ballot_w64(!every && 32 * t + col < rows) == 0;
+            none = !context && __builtin_amdgcn_ballot_w64(any && 32 * t + col < rows) == 0;
         }
-        // x[4 v + e] is query row 8 v + 4 hi + e of the tile
+        if (!none) {
+            f32x16_t x0{}, x1{};
+            const uint16_t* row = qs[buf] + col * D;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const f32x4_t o = *reinterpret_cast<const f32x4_t*>(offs[buf] + 8 * v + 4 * hi);
-            if (!drafted) {
+            for (int s = 0; s < KS; ++s) {
+                const bf16x8_t qf = *reinterpret_cast<const bf16x8_t*>(row + ((2 * s + hi) ^ swz) * 8);
+                x0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[0][s], x0, 0, 0, 0);
+                x1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[1][s], x1, 0, 0, 0);
+            }
+            // x[4 v + e] is query row 8 v + 4 hi + e of the tile
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    sum[0] += __builtin_amdgcn_exp2f(fmaf(x0[4 * v + e], a.sl2, -o[e]));
-                    sum[1] += __builtin_amdgcn_exp2f(fmaf(x1[4 * v + e], a.sl2, -o[e]));
-                }
-            } else {
+            for (int v = 0; v < 4; ++v) {
+                const f32x4_t o = *reinterpret_cast<const f32x4_t*>(offs[buf] + 8 * v + 4 * hi);
+                if (all) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint64_t* m = bits[buf][8 * v + 4 * hi + e];
+                    for (int e = 0; e < 4; ++e) {
+                        sum[0] += __builtin_amdgcn_exp2f(fmaf(x0[4 * v + e], a.sl2, -o[e]));
+                        sum[1] += __builtin_amdgcn_exp2f(fmaf(x1[4 * v + e], a.sl2, -o[e]));
+                    }
+                } else {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const bool sees = there[h] && (j[h] < 0 || (m[(j[h] >> 6) - w0] >> (j[h] & 63) & 1));
-                        const float p = __builtin_amdgcn_exp2f(fmaf(h == 0 ? x0[4 * v + e] : x1[4 * v + e], a.sl2, -o[e]));
-                        sum[h] += sees ? p : 0.f;
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t* m = bits[buf][8 * v + 4 * hi + e];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const bool sees = there[h] && (j[h] < 0 || (m[(j[h] >> 5) - w0] >> (j[h] & 31) & 1));
+                            const float p = __builtin_amdgcn_exp2f(fmaf(h == 0 ? x0[4 * v + e] : x1[4 * v + e], a.sl2, -o[e]));
+                            sum[h] += sees ? p : 0.f;
+                        }
                     }
                 }
             }
@@ -347,6 +383,7 @@ int tkv::launch_key_weights(const tkv_shape& s, const tkv_draft_batch& b, const 
     Args a{};
     a.b = b;
     a.num_blocks = s.num_blocks, a.hq = s.hq, a.hkv = s.hkv, a.G = s.hq / s.hkv;
+    a.inv_g = ((1u << 31) + a.G - 1) / a.G;
     a.sl2 = kLog2e / sqrtf(static_cast<float>(s.d));
     a.decay = decay;
     a.q = static_cast<const uint16_t*>(q), a.k = static_cast<const uint16_t*>(k);
