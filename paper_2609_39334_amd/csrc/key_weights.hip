@@ -97,18 +97,26 @@ __device__ __forceinline__ Unit unit_of(const Args& a) {
     return u;
 }
 
-// The chunk's blocks: {id, 32 (first key's number among the drafted ones, at least -64) + length}; n: entries of the chunk, at
-// most as many as threads.  Ends in a barrier.
-__device__ __forceinline__ void list_blocks(const Args& a, const Unit& u, int n, int2* list, int* part) {
+// A thread's part of a chunk's table, in two steps so that other loads can go between: the block and length of entry `tid` of
+// the chunk's n (at most as many as threads), and the length of entry `tid` behind it.
+struct Look {
+    int id, behind, len, more;
+};
+__device__ __forceinline__ void look_ids(const Args& a, const Unit& u, int n, Look& k) {
+    const int tid = threadIdx.x, mine = u.e0 + tid, later = u.e0 + n + tid;
+    k.id = tid < n && mine < u.tab.n ? a.b.kv_blocks[u.tab.first + mine] : -1;
+    k.behind = tid < u.t.L && later < u.tab.n ? a.b.kv_blocks[u.tab.first + later] : -1;
+}
+__device__ __forceinline__ void look_lens(const Args& a, Look& k) {
+    k.len = 0, k.more = 0;
+    if (static_cast<uint32_t>(k.id) < static_cast<uint32_t>(a.num_blocks)) k.len = a.b.block_len[k.id];
+    if (static_cast<uint32_t>(k.behind) < static_cast<uint32_t>(a.num_blocks)) k.more = a.b.block_len[k.behind];
+}
+// The chunk's blocks: {id, 32 (first key's number among the drafted ones, at least -64) + length}.  Ends in a barrier.
+__device__ __forceinline__ void list_blocks(const Args& a, const Unit& u, int n, const Look& k, int2* list, int* part) {
     const int tid = threadIdx.x, step = min(kThreads, u.t.L);
-    const int mine = u.e0 + tid, later = u.e0 + n + tid;
-    int id = -1, behind = -1, len = 0, more = 0, total;
-    if (tid < n && mine < u.tab.n) id = a.b.kv_blocks[u.tab.first + mine];
-    if (tid < step && later < u.tab.n) behind = a.b.kv_blocks[u.tab.first + later];
-    if (static_cast<uint32_t>(id) < static_cast<uint32_t>(a.num_blocks)) len = a.b.block_len[id];
-    if (static_cast<uint32_t>(behind) < static_cast<uint32_t>(a.num_blocks)) more = a.b.block_len[behind];
-    len = len >= 1 && len <= tkv::kBlock ? len : 0;
-    more = more >= 1 && more <= tkv::kBlock ? more : 0;
+    const int len = k.len >= 1 && k.len <= tkv::kBlock ? k.len : 0, more = k.more >= 1 && k.more <= tkv::kBlock ? k.more : 0;
+    int total;
     const int before = tkv::group_before<kWaves>(more << 16 | len, total, part) & 0xffff;
     // keys behind the chunk, exact below the row's tokens
     int after = total >> 16;
@@ -120,7 +128,7 @@ __device__ __forceinline__ void list_blocks(const Args& a, const Unit& u, int n,
         tkv::group_before<kWaves>(sum, sum, part);
         after += sum;
     }
-    if (tid < n) list[tid] = int2{id, 32 * max(u.t.L - (after + (total & 0xffff) - before), -64) + len};
+    if (tid < n) list[tid] = int2{k.id, 32 * max(u.t.L - (after + (total & 0xffff) - before), -64) + len};
     __syncthreads();
 }
 
@@ -129,10 +137,12 @@ __device__ __forceinline__ int token_of(const Args& a, int qr) {
     return static_cast<int>(__umulhi(static_cast<uint32_t>(2 * qr), a.inv_g));
 }
 
-// What is subtracted from a query row's score, in units of log2: infinite for a row that gives nothing.
-__device__ __forceinline__ float offset_of(const Args& a, int64_t token, int head) {
-    const float z = a.lse[token * a.hq + head], c = a.coef ? a.coef[token] : 1.f;
-    return fabsf(z) < INFINITY && c > 0.f ? z * kLog2e - (a.coef ? log2f(c) : 0.f) : INFINITY;
+// What is subtracted from a query row's score, in units of log2: infinite for a row that gives nothing (the logarithm of a
+// coefficient below 2^-126 is -infinity).
+__device__ __forceinline__ float offset_of(float z, float c) {
+    float x = z * kLog2e - __builtin_amdgcn_logf(c);
+    asm volatile("" : "+v"(x));  // (computed in any case: a branch would end the block that the compiler schedules as one)
+    return fabsf(z) < INFINITY && c > 0.f ? x : INFINITY;
 }
 
 template <int D>
@@ -145,6 +155,8 @@ __global__ __launch_bounds__(kThreads, 3) void weigh_few(Args a) {
     const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, hi = lane >> 5;
     const int rows = u.t.L * a.G, nu = (rows + 7) / 8;
+    Look look;
+    look_ids(a, u, a.chunk, look);
     bf16x8_t qf[KS];
     {
         const int qr = min(col, rows - 1), i = token_of(a, qr);
@@ -152,16 +164,19 @@ __global__ __launch_bounds__(kThreads, 3) void weigh_few(Args a) {
 #pragma unroll
         for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const bf16x8_t*>(row + 16 * s);
     }
+    look_lens(a, look);
     // x[4 v + e] of a product is query row 8 v + 4 hi + e
     float off[16];
     {
-        const int i = token_of(a, min(col, rows - 1));
-        const float mine = col < rows ? offset_of(a, u.t.q0 + i, u.g * a.G + (col - i * a.G)) : INFINITY;
+        const int qr = min(col, rows - 1), i = token_of(a, qr);
+        const int64_t token = u.t.q0 + i;
+        const float z = a.lse[token * a.hq + u.g * a.G + (qr - i * a.G)], c = a.coef ? a.coef[token] : 1.f;
+        const float mine = col < rows ? offset_of(z, c) : INFINITY;
 #pragma unroll
         for (int e = 0; e < 16; ++e) off[e] = __shfl(mine, 8 * (e >> 2) + 4 * hi + (e & 3));
     }
     const int n = min(a.chunk, u.tab.n - u.e0), pairs = (n + 1) / 2;
-    list_blocks(a, u, a.chunk, list, part);
+    list_blocks(a, u, a.chunk, look, list, part);
 
     float* out = a.out + (static_cast<int64_t>(u.r) * a.hkv + u.g) * a.keys + 16 * static_cast<int64_t>(u.e0);
     const float* before = a.before ? a.before + (out - a.out) : nullptr;
@@ -223,10 +238,10 @@ __global__ __launch_bounds__(kThreads, 3) void weigh_few(Args a) {
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads, 3) void weigh_many(Args a) {
+__global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
     constexpr int KS = D / 16, CPR = D / 8, kPieces = 32 * CPR / kThreads;  // 16-byte pieces a row, pieces of a tile a thread
     __shared__ __attribute__((aligned(16))) uint16_t qs[2][32 * D];
-    __shared__ __attribute__((aligned(16))) float offs[2][32];
+    __shared__ __attribute__((aligned(16))) float offs[4][32];
     __shared__ uint32_t bits[2][32][kWords];  // the rows' masks from the chunk's first drafted key on
     __shared__ int2 list[kManyChunk];
     __shared__ int part[kWaves];
@@ -236,142 +251,213 @@ __global__ __launch_bounds__(kThreads, 3) void weigh_many(Args a) {
     const int col = lane & 31, hi = lane >> 5;
     const int rows = u.t.L * a.G, n_tiles = (rows + 31) / 32;
 
-    // a tile of 32 query rows, their 16-byte pieces XOR-swizzled by row so that the operand reads meet no bank conflict
-    u32x4_t qx[kPieces];
-    float ox = 0.f;
-    uint32_t bx[2] = {0, 0};
-    const auto fetch_q = [&](int tile) __attribute__((always_inline)) {
+    // a tile of 32 query rows, their 16-byte pieces XOR-swizzled by row so that the operand reads meet no bank conflict; two tiles
+    // are on their way (tile t in set t % 2), and what follows from their loads is left until these are back
+    u32x4_t qx[2][kPieces];
+    float zx[2], cx[2];  // of row `col`
+    uint32_t bx[2][2];
+    const uint16_t* q0 = a.q + (static_cast<int64_t>(u.t.q0) * a.hq + u.g * a.G) * D + tid % CPR * 8;
+    const float* lse = a.lse + static_cast<int64_t>(u.t.q0) * a.hq + u.g * a.G;
+    const float* coef = a.coef ? a.coef + u.t.q0 : lse;  // (lse where there are none: its values are masked out)
+    const uint32_t given = a.coef ? ~0u : 0u;
+    const auto fetch_q = [&](int tile, int set) __attribute__((always_inline)) {
 #pragma unroll
         for (int y = 0; y < kPieces; ++y) {
-            const int x = y * kThreads + tid, qr = min(32 * tile + x / CPR, rows - 1), i = token_of(a, qr);
-            qx[y] = *reinterpret_cast<const u32x4_t*>(a.q + (static_cast<int64_t>(u.t.q0 + i) * a.hq + u.g * a.G + (qr - i * a.G)) * D + x % CPR * 8);
+            const int qr = min(32 * tile + (y * kThreads + tid) / CPR, rows - 1), i = token_of(a, qr);
+            qx[set][y] = *reinterpret_cast<const u32x4_t*>(q0 + (i * (a.hq - a.G) + qr) * D);  // (below 2^10 256 128 elements)
         }
-        if (tid < 32) {
-            const int qr = 32 * tile + tid, i = token_of(a, min(qr, rows - 1));
-            ox = qr < rows ? offset_of(a, u.t.q0 + i, u.g * a.G + (qr - i * a.G)) : INFINITY;
-        }
+        // (every wave reads the rows' lse and coefficients, so that a step has no branches)
+        const int qr = min(32 * tile + col, rows - 1), i = token_of(a, qr);
+        zx[set] = lse[i * (a.hq - a.G) + qr];
+        cx[set] = coef[i];
     };
-    fetch_q(0);
-    list_blocks(a, u, kManyChunk, list, part);
-
-    bf16x8_t kf[2][KS];
-    int j[2], place[2];
-    bool there[2];
-    int low = INT32_MAX, high = -1;  // the wave's drafted keys
-    bool context = false;            // whether it has others
+    // the table first, then its lengths, then the keys (rows past a block's length are read, and nothing made of them): loads
+    // come back in order
+    Look look;
+    look_ids(a, u, kManyChunk, look);
+    int own[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int e = 4 * wid + 2 * h + (col >> 4), slot = col & 15;
-        const int2 d = list[e];
-        there[h] = slot < (d.y & 31);
-        j[h] = (d.y >> 5) + slot;
-        place[h] = 16 * e + slot;
+        const int e = u.e0 + 4 * wid + 2 * h + (col >> 4);
+        own[h] = e < u.tab.n ? a.b.kv_blocks[u.tab.first + e] : -1;
+    }
+    fetch_q(0, 0);
+    look_lens(a, look);
+    bf16x8_t kf[2][KS];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
         for (int s = 0; s < KS; ++s) kf[h][s] = bf16x8_t{};
-        if (there[h]) {
-            const uint16_t* row = a.k + (static_cast<int64_t>(d.x) * a.hkv + u.g) * (16 * D) + slot * D + 8 * hi;
+        if (static_cast<uint32_t>(own[h]) < static_cast<uint32_t>(a.num_blocks)) {
+            const uint16_t* row = a.k + (static_cast<int64_t>(own[h]) * a.hkv + u.g) * (16 * D) + (col & 15) * D + 8 * hi;
 #pragma unroll
             for (int s = 0; s < KS; ++s) kf[h][s] = *reinterpret_cast<const bf16x8_t*>(row + 16 * s);
         }
     }
-    int lowest = INT32_MAX;  // the chunk's first drafted key
-    for (int e = kManyChunk - 1; e >= 0; --e) {
-        const int first = list[e].y >> 5, len = list[e].y & 31;
-        if (len == 0) continue;
-        if (first + len > 0) lowest = max(first, 0);
-        if (e >> 2 != wid) continue;
-        if (first < 0) context = true;
-        if (first + len > 0) low = max(first, 0), high = max(high, first + len - 1);
+    list_blocks(a, u, kManyChunk, look, list, part);
+
+    const int64_t at = (static_cast<int64_t>(u.r) * a.hkv + u.g) * a.keys + 16 * static_cast<int64_t>(u.e0);
+    int j[2], place[2];
+    bool there[2];
+    float had[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int e = 4 * wid + 2 * h + (col >> 4), slot = col & 15, d = list[e].y;
+        there[h] = slot < (d & 31);
+        j[h] = (d >> 5) + slot;
+        place[h] = 16 * e + slot;
+        had[h] = there[h] && j[h] < 0 && a.before ? a.before[at + place[h]] : 0.f;
     }
-    lowest = __builtin_amdgcn_readfirstlane(lowest), low = __builtin_amdgcn_readfirstlane(low);
-    high = __builtin_amdgcn_readfirstlane(high), context = __builtin_amdgcn_readfirstlane(context);
-    const bool some = lowest < INT32_MAX, drafted = high >= 0;
-    const int w0 = some ? lowest >> 5 : 0;
-    const auto fetch_bits = [&](int tile) __attribute__((always_inline)) {
-        if (!some) return;
+    // the chunk's first drafted key, the wave's first and last one, and whether the wave has others: lane l looks at entry l
+    int lowest = 0, low = 0, high = -1;
+    bool context, some;
+    {
+        const int d = list[lane & 15].y, first = d >> 5, len = d & 31;
+        const uint32_t has = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(len > 0 && first + len > 0)) & 0xffff;
+        const uint32_t mine = has >> (4 * wid) & 15;
+        context = (static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(len > 0 && first < 0)) >> (4 * wid) & 15) != 0;
+        some = has != 0;
+        if (some) lowest = max(__builtin_amdgcn_readlane(first, __builtin_ctz(has)), 0);
+        if (mine != 0) {
+            low = max(__builtin_amdgcn_readlane(first, 4 * wid + __builtin_ctz(mine)), 0);
+            high = __builtin_amdgcn_readlane(first + len, 4 * wid + 31 - __builtin_clz(mine)) - 1;
+        }
+    }
+    const bool drafted = high >= 0;
+    const int w0 = lowest >> 5;
+    // where a lane's bits are; context is seen by all
+    int word[2];
+    uint32_t always[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) word[h] = there[h] && j[h] >= 0 ? (j[h] >> 5) - w0 : 0, always[h] = there[h] && j[h] < 0 ? ~0u : 0u;
+    const auto fetch_bits = [&](int tile, int set) __attribute__((always_inline)) {
+        bx[set][0] = 0, bx[set][1] = 0;
         const uint32_t* masks = reinterpret_cast<const uint32_t*>(a.b.mask);
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
             const int x = y * kThreads + tid, qr = 32 * tile + x / kWords, w = w0 + x % kWords;
-            bx[y] = x < 32 * kWords && w < 2 * a.b.mask_words && qr < rows
-                        ? masks[static_cast<int64_t>(u.t.q0 + token_of(a, qr)) * (2 * a.b.mask_words) + w] : 0;
+            if (x < 32 * kWords && w < 2 * a.b.mask_words && qr < rows)
+                bx[set][y] = masks[static_cast<int64_t>(u.t.q0 + token_of(a, qr)) * (2 * a.b.mask_words) + w];
         }
     };
-    const auto put = [&](int buf) __attribute__((always_inline)) {
+    const auto put = [&](int tile, int set) __attribute__((always_inline)) {
 #pragma unroll
         for (int y = 0; y < kPieces; ++y) {
             const int x = y * kThreads + tid, row = x / CPR;
             const int swz = D == 128 ? row & 15 : (row >> 1) & 7;
-            *reinterpret_cast<u32x4_t*>(qs[buf] + row * D + ((x % CPR) ^ swz) * 8) = qx[y];
+            *reinterpret_cast<u32x4_t*>(qs[set] + row * D + ((x % CPR) ^ swz) * 8) = qx[set][y];
         }
-        if (tid < 32) offs[buf][tid] = ox;
-        if (some) {
-            bits[buf][tid / kWords][tid % kWords] = bx[0];
-            if (tid + kThreads < 32 * kWords) bits[buf][(tid + kThreads) / kWords][(tid + kThreads) % kWords] = bx[1];
-        }
+        const float c = __uint_as_float((__float_as_uint(cx[set]) & given) | (__float_as_uint(1.f) & ~given));
+        const float off = offset_of(zx[set], c);
+        offs[tile & 3][col] = 32 * tile + col < rows ? off : INFINITY;
+    };
+    const auto put_bits = [&](int set) __attribute__((always_inline)) {
+        bits[set][tid / kWords][tid % kWords] = bx[set][0];
+        if (tid + kThreads < 32 * kWords) bits[set][(tid + kThreads) / kWords][(tid + kThreads) % kWords] = bx[set][1];
     };
     const int swz = D == 128 ? col & 15 : (col >> 1) & 7;
     float sum[2] = {0.f, 0.f};
-    fetch_bits(0);
-    put(0);
-    for (int t = 0; t < n_tiles; ++t) {
-        const int buf = t & 1;
-        if (t + 1 < n_tiles) fetch_q(t + 1), fetch_bits(t + 1);
+    // x[4 v + e] of a product is query row 8 v + 4 hi + e of the tile
+    const auto multiply = [&](int tile, f32x16_t (&x)[2]) __attribute__((always_inline)) {
+        const uint16_t* row = qs[tile & 1] + col * D;
+        x[0] = f32x16_t{}, x[1] = f32x16_t{};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const bf16x8_t qf = *reinterpret_cast<const bf16x8_t*>(row + ((2 * s + hi) ^ swz) * 8);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) x[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[h][s], x[h], 0, 0, 0);
+        }
+    };
+    const auto add = [&](int tile, const f32x16_t (&x)[2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const f32x4_t o = *reinterpret_cast<const f32x4_t*>(offs[tile & 3] + 8 * v + 4 * hi);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(x[h][4 * v + e], a.sl2, -o[e]));
+                sum[h] += (p[0] + p[1]) + (p[2] + p[3]);
+            }
+        }
+    };
+    if (!some) {
+        // a tile's products beside the exponentials of the one before
+        f32x16_t x[2][2];
+        const auto step = [&](int t, int set) __attribute__((always_inline)) {  // set: t % 2
+            fetch_q(t + 2, set);  // (tiles past the last read its last row again, and give nothing)
+            __syncthreads();
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(t, x[set]);
+            add(t - 1, x[set ^ 1]);
+            put(t + 1, set ^ 1);
+        };
+        put(0, 0);
+        fetch_q(1, 1);
+        fetch_q(2, 0);
         __syncthreads();
-        // whether the tile's rows (padding aside) see all of the wave's drafted keys, or none
-        bool all = true, none = false;
-        if (drafted) {
-            bool every = true, any = false;
-            for (int w = low >> 5; w <= high >> 5; ++w) {
+        multiply(0, x[0]);
+        put(1, 1);
+        int t = 1;
+        for (; t + 1 < n_tiles; t += 2) {
+            step(t, 1);
+            step(t + 1, 0);
+        }
+        if (t < n_tiles) {
+            step(t, 1);
+            add(t, x[1]);
+        } else {
+            add(t - 1, x[0]);
+        }
+    } else {
+        const auto step = [&](int t, int set) __attribute__((always_inline)) {
+            if (t + 2 < n_tiles) fetch_q(t + 2, set), fetch_bits(t + 2, set);
+            __syncthreads();
+            // whether the tile's rows (padding aside) see all of the wave's drafted keys, or none
+            bool every = true, any = !drafted;
+            for (int w = low >> 5; drafted && w <= high >> 5; ++w) {
                 const uint32_t from = w == low >> 5 ? ~0u << (low & 31) : ~0u, to = w == high >> 5 ? ~0u >> (31 - (high & 31)) : ~0u;
-                const uint32_t seen = bits[buf][col][w - w0] & from & to;
+                const uint32_t seen = bits[set][col][w - w0] & from & to;
                 every = every && seen == (from & to), any = any || seen != 0;
             }
-            all = __builtin_amdgcn_ballot_w64(!every && 32 * t + col < rows) == 0;
-            none = !context && __builtin_amdgcn_ballot_w64(any && 32 * t + col < rows) == 0;
-        }
-        if (!none) {
-            f32x16_t x0{}, x1{};
-            const uint16_t* row = qs[buf] + col * D;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const bf16x8_t qf = *reinterpret_cast<const bf16x8_t*>(row + ((2 * s + hi) ^ swz) * 8);
-                x0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[0][s], x0, 0, 0, 0);
-                x1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[1][s], x1, 0, 0, 0);
-            }
-            // x[4 v + e] is query row 8 v + 4 hi + e of the tile
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const f32x4_t o = *reinterpret_cast<const f32x4_t*>(offs[buf] + 8 * v + 4 * hi);
+            const bool all = __builtin_amdgcn_ballot_w64(!every && 32 * t + col < rows) == 0;
+            const bool none = !context && drafted && __builtin_amdgcn_ballot_w64(any && 32 * t + col < rows) == 0;
+            if (!none) {
+                f32x16_t x[2];
+                multiply(t, x);
                 if (all) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        sum[0] += __builtin_amdgcn_exp2f(fmaf(x0[4 * v + e], a.sl2, -o[e]));
-                        sum[1] += __builtin_amdgcn_exp2f(fmaf(x1[4 * v + e], a.sl2, -o[e]));
-                    }
+                    add(t, x);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t* m = bits[buf][8 * v + 4 * hi + e];
+                    for (int v = 0; v < 4; ++v) {
+                        const f32x4_t o = *reinterpret_cast<const f32x4_t*>(offs[t & 3] + 8 * v + 4 * hi);
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const bool sees = there[h] && (j[h] < 0 || (m[(j[h] >> 5) - w0] >> (j[h] & 31) & 1));
-                            const float p = __builtin_amdgcn_exp2f(fmaf(h == 0 ? x0[4 * v + e] : x1[4 * v + e], a.sl2, -o[e]));
-                            sum[h] += sees ? p : 0.f;
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t* m = bits[set][8 * v + 4 * hi + e];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const uint32_t sees = (m[word[h]] | always[h]) >> (j[h] & 31) & 1;
+                                const float p = __builtin_amdgcn_exp2f(fmaf(x[h][4 * v + e], a.sl2, -o[e]));
+                                sum[h] += sees != 0 ? p : 0.f;
+                            }
                         }
                     }
                 }
             }
+            if (t + 1 < n_tiles) put(t + 1, set ^ 1), put_bits(set ^ 1);
+        };
+        fetch_bits(0, 0);
+        put(0, 0), put_bits(0);
+        if (n_tiles > 1) fetch_q(1, 1), fetch_bits(1, 1);
+        for (int t = 0; t < n_tiles; t += 2) {
+            step(t, 0);
+            if (t + 1 < n_tiles) step(t + 1, 1);
         }
-        if (t + 1 < n_tiles) put(buf ^ 1);
     }
-    const int64_t at = (static_cast<int64_t>(u.r) * a.hkv + u.g) * a.keys + 16 * static_cast<int64_t>(u.e0);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        float w = sum[h] + __shfl_xor(sum[h], 32);
-        if (!there[h] || hi != 0) continue;
-        if (j[h] < 0 && a.before) w = fmaf(a.decay, a.before[at + place[h]], w);
-        a.out[at + place[h]] = w;
+        const float w = sum[h] + __shfl_xor(sum[h], 32);
+        if (there[h] && hi == 0) a.out[at + place[h]] = fmaf(a.decay, had[h], w);
     }
 }
 
