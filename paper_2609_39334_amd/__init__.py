@@ -1043,9 +1043,10 @@ class DraftBatch:
     """The device arrays of a drafted batch for tkv_draft_verify, in one upload: row r's block table (its last keys are the
     drafted tokens), the parents of its drafted tokens (earlier ones, or -1 for the context), and every block's length.
     A batch serves every layer.  positions, depth: each token's position in its path (int64, device) and its
-    number of drafted ancestors (host)."""
+    number of drafted ancestors (host).  evicted: how many keys each row's path has lost (tkv_evict_keys), which its tokens'
+    positions still count (None: none)."""
 
-    def __init__(self, tables, parents, block_len, device="cuda"):
+    def __init__(self, tables, parents, block_len, device="cuda", evicted=None):
         if len(tables) != len(parents):
             raise ValueError("DraftBatch: a table and a tree for every row")
         lens, n_blk = [len(p) for p in parents], [len(t) for t in tables]
@@ -1064,6 +1065,10 @@ class DraftBatch:
         context = [int(bl[_i32(t)].sum()) - n for t, n in zip(tables, lens)]
         if any(c < 0 for c in context):
             raise ValueError("DraftBatch: a row's path is shorter than its draft")
+        if evicted is not None:
+            if len(evicted) != len(tables) or any(int(e) < 0 for e in evicted):
+                raise ValueError("DraftBatch: a number of evicted keys, 0 or more, for every row")
+            context = [c + int(e) for c, e in zip(context, evicted)]
         positions = np.repeat(np.asarray(context, np.int64), lens) + self.depth
         mask = np.concatenate([m for m, _ in trees]) if trees else np.zeros((0, words), np.uint64)
         parts = [positions.astype(np.int64).view(np.int32), mask.view(np.int32).reshape(-1),
@@ -1079,6 +1084,63 @@ class DraftBatch:
     def verify(self, q, k, v, o, lse=None, workspace=None, stream=None):
         tkv_draft_verify(self.q_indptr, self.kv_indptr, self.kv_blocks, self.block_len, self.mask, self.max_q, self.max_blocks,
                          q, k, v, o, lse, workspace, stream)
+
+    def key_weights(self, q, k, lse, out, before=None, decay=1.0, coef=None, stream=None):
+        tkv_key_weights(self.q_indptr, self.kv_indptr, self.kv_blocks, self.block_len, self.mask, self.max_q, self.max_blocks,
+                        q, k, lse, out, before, decay, coef, stream)
+
+    def adjust_logits(self, tokens, logits, **rules):
+        """tkv_adjust_logits with this batch's tables (those of the tokens' pool); its rules, out and stream by name."""
+        return tkv_adjust_logits(self.q_indptr, self.kv_indptr, self.kv_blocks, self.block_len, self.mask, self.max_q,
+                                 self.max_blocks, tokens, logits, **rules)
+
+
+class EvictBatch:
+    """The device arrays of an eviction (tkv_evict_keys), in one upload: row r's path in tables[r] keeps at most budget[r]
+    keys a KV head, in the blocks new_tables[r] (as many as they need, in no other table of the batch: e.g. of a sequence that
+    BlockManager.extend made without a parent and with seal=False).  A batch serves every layer.  n_kept: how many each row
+    keeps, evicted: how many it loses (host)."""
+
+    def __init__(self, tables, new_tables, budget, block_len, device="cuda"):
+        if not len(tables) == len(new_tables) == len(budget):
+            raise ValueError("EvictBatch: a table, a new table and a budget for every row")
+        bl, budget = _i32(block_len), [int(b) for b in budget]
+        old, new = [_i32(t) for t in tables], [_i32(t) for t in new_tables]
+        if any(b < 0 for b in budget):
+            raise ValueError("EvictBatch: a budget below 0")
+        every = np.concatenate(old + new) if tables else np.zeros(0, np.int32)
+        if len(every) and (every.min() < 0 or every.max() >= len(bl)):
+            raise ValueError("EvictBatch: a table names a block outside block_len")
+        if any(len(t) and (bl[t].min() < 0 or bl[t].max() > 16) for t in old):
+            raise ValueError("EvictBatch: a table's block has a length outside [0, 16]")
+        fresh = np.concatenate(new) if new else np.zeros(0, np.int32)
+        if len(np.unique(fresh)) < len(fresh) or (len(fresh) and np.isin(fresh, np.concatenate(old)).any()):
+            raise ValueError("EvictBatch: a block of a new table is in another table too, or twice in its own")
+        lens = [int(bl[t].sum()) for t in old]
+        self.n_kept = [min(n, b) for n, b in zip(lens, budget)]
+        self.evicted = [n - m for n, m in zip(lens, self.n_kept)]
+        for t, m in zip(new, self.n_kept):
+            if 16 * len(t) < m:
+                raise ValueError(f"EvictBatch: {len(t)} blocks do not hold {m} keys")
+        self.max_blocks, self.most = max([len(t) for t in old], default=1) or 1, max(budget, default=0)
+        parts = [np.cumsum([0] + [len(t) for t in old]).astype(np.int32), np.cumsum([0] + [len(t) for t in new]).astype(np.int32),
+                 np.asarray(budget, np.int32), np.concatenate(old) if old else fresh, fresh, bl]
+        flat = torch.from_numpy(np.concatenate(parts)).to(device)
+        at = np.cumsum([0] + [len(p) for p in parts])
+        self.kv_indptr, self.new_indptr, self.budget, self.kv_blocks, self.new_blocks, self.block_len = \
+            [flat[a:b] for a, b in zip(at[:-1], at[1:])]
+
+    def evict(self, weights, k, v, sink=0, recent=0, out=None, kept=None, n_kept=None, stream=None):
+        """One layer's eviction; returns (weights at their new places, kept, n_kept), made if not given (weights past a row's kept
+        ones are not written)."""
+        call = _Call("EvictBatch.evict", k, stream)
+        rows, hkv = self.budget.numel(), k.shape[1]
+        out = call.empty(weights.shape, torch.float32) if out is None else out
+        kept = call.empty((rows, hkv, self.most), torch.int32) if kept is None else kept
+        n_kept = call.empty((rows,), torch.int32) if n_kept is None else n_kept
+        tkv_evict_keys(self.kv_indptr, self.kv_blocks, self.block_len, self.max_blocks, self.new_indptr, self.new_blocks, self.budget,
+                       sink, recent, weights, k, v, out, kept, n_kept, stream)
+        return out, kept, n_kept
 
 
 class Search:

@@ -16,7 +16,9 @@ then logits = RMSNorm(x) W_lm, and the CD branching sampler draws each row's pot
 (tkv_cd_sample, library kernel).  One plan serves every layer: the block tables are the same in all
 of them, only the pools differ.  Shapes with qk_norm normalise each query and key head first
 (tkv_norm_rope_append).  verify_draft is the same forward pass over small trees of drafted tokens
-(tkv_draft_verify), and sample_filtered draws from their truncated distributions (tkv_filter_sample).
+(tkv_draft_verify), and sample_filtered draws from their truncated distributions (tkv_filter_sample).  For long generations
+verify_draft adds up what each key's attention weights have been (tkv_key_weights), evict moves the keys that stay to shorter
+tables (tkv_evict_keys), and sample_filtered draws under penalties, biases and grammars (tkv_adjust_logits).
 
 The dense products are plain GEMMs and run in the platform BLAS (hipBLASLt through torch.mm); what lies
 between them are library kernels of one pass over memory each.  Precision: the residual stream and every
@@ -25,11 +27,11 @@ output to bf16 (as the attention kernel rounds o).  No biases; weights are N(0, 
 """
 from __future__ import annotations
 
-from typing import List, NamedTuple
+from typing import List, NamedTuple, Optional
 
 import torch
 
-from . import (DraftBatch, Plan, tkv_add_rmsnorm, tkv_cd_sample, tkv_filter_sample, tkv_norm_rope_append, tkv_rope_append,
+from . import (DraftBatch, EvictBatch, Plan, tkv_add_rmsnorm, tkv_cd_sample, tkv_filter_sample, tkv_norm_rope_append, tkv_rope_append,
                tkv_swiglu)
 
 
@@ -94,12 +96,32 @@ class SyntheticDecoder:
         return self._on(stream, lambda: self._forward(tokens, positions, dst, plan.decode, k_pools, v_pools, on_layer).float())
 
     def verify_draft(self, tokens: torch.Tensor, dst: torch.Tensor, batch: DraftBatch, k_pools: List[torch.Tensor],
-                     v_pools: List[torch.Tensor], stream=None, on_layer=None) -> torch.Tensor:
+                     v_pools: List[torch.Tensor], stream=None, on_layer=None, weights: Optional[List[torch.Tensor]] = None,
+                     decay: float = 1.0, coef: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Logits [n_qtok, vocab] (bf16, as tkv_filter_sample takes them) after each drafted token of a batch.
 
         tokens: [n_qtok] int64; dst: [n_qtok] int32 pool slots of the drafted tokens, the last keys of their
-        rows' tables in order; pools and stream as for step."""
-        return self._on(stream, lambda: self._forward(tokens, batch.positions, dst, batch.verify, k_pools, v_pools, on_layer))
+        rows' tables in order; pools and stream as for step.  weights[l]: layer l's key weights [n_rows, hkv, keys] fp32, to
+        which the tokens' attention is added in place (decay and coef as for tkv_key_weights)."""
+        def attend(layers):
+            lse = torch.empty((tokens.numel(), self.shape.hq), dtype=torch.float32, device=tokens.device)
+
+            def run(q, k, v, o):
+                w = next(layers)
+                batch.verify(q, k, v, o, lse)
+                batch.key_weights(q, k, lse, w, before=w, decay=decay, coef=coef)
+            return run
+        return self._on(stream, lambda: self._forward(tokens, batch.positions, dst,
+                                                      batch.verify if weights is None else attend(iter(weights)),
+                                                      k_pools, v_pools, on_layer))
+
+    def evict(self, batch: EvictBatch, weights: List[torch.Tensor], k_pools: List[torch.Tensor], v_pools: List[torch.Tensor],
+              sink: int = 0, recent: int = 0, stream=None) -> List[torch.Tensor]:
+        """Every layer's eviction; returns the layers' key weights, kept keys' at their new places and zeros behind them.
+        stream as for step."""
+        def run():
+            return tuple(batch.evict(w, k, v, sink, recent, out=torch.zeros_like(w))[0] for w, k, v in zip(weights, k_pools, v_pools))
+        return list(self._on(stream, run))
 
     @staticmethod
     def _on(stream, run, device=None):
@@ -143,7 +165,12 @@ class SyntheticDecoder:
         return tkv_cd_sample(logits.contiguous(), temperature, draw_off, uniform, max_potential, stream)
 
     def sample_filtered(self, logits, temperature, draw_off, uniform, max_potential, top_k=None, top_p=None, min_p=None,
-                        stream=None):
-        """Draws under per-row temperature, top-k, top-p and min-p: (tokens, counts, groups per row).  stream as for step."""
-        return self._on(stream, lambda: tkv_filter_sample(logits, temperature, draw_off, uniform, max_potential, top_k, top_p, min_p,
-                                                          stream=stream), logits.device)
+                        stream=None, history: Optional[DraftBatch] = None, said: Optional[torch.Tensor] = None, rules=None):
+        """Draws under per-row temperature, top-k, top-p and min-p: (tokens, counts, groups per row).  stream as for step.
+        With a history (the batch over the tables of `said`, the pool [num_blocks, 16] of the paths' tokens) the logits are
+        adjusted first: rules holds tkv_adjust_logits' settings by name."""
+        def run():
+            x = logits if history is None else history.adjust_logits(said, logits, out=torch.empty_like(logits, dtype=torch.float32),
+                                                                     stream=stream, **(rules or {}))
+            return tkv_filter_sample(x, temperature, draw_off, uniform, max_potential, top_k, top_p, min_p, stream=stream)
+        return self._on(stream, run, logits.device)
