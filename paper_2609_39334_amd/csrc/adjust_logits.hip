@@ -188,11 +188,12 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) len[k] = len[k] >= 1 && len[k] <= tkv::kBlock ? len[k] : 0;
     };
-    i32x4_t tok[4];
-    const auto fetch = [&](int block) __attribute__((always_inline)) {
-        const i32x4_t* p = reinterpret_cast<const i32x4_t*>(a.tokens + static_cast<int64_t>(block) * tkv::kBlock);
+    i32x4_t tok[2][4];  // an entry's tokens, and the next one's on their way
+    const auto fetch = [&](int k) __attribute__((always_inline)) {
+        if (len[k] == 0) return;
+        const i32x4_t* p = reinterpret_cast<const i32x4_t*>(a.tokens + static_cast<int64_t>(id[k]) * tkv::kBlock);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) tok[q] = p[q];
+        for (int q = 0; q < 4; ++q) tok[k & 1][q] = p[q];
     };
     if (counts) {
         for (int e = e0 + (run - 1) / kBatch * kBatch; e >= e0; e -= kBatch) {  // the first ones last: they stay
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) keys += len[k];
         }
-        if (len[0] > 0) fetch(id[0]);
+        fetch(0);
     }
     // a query token's logits, its grammar's words, and which of this thread's drafted tokens it sees
     f32x4_t x[kLoads];
@@ -242,14 +243,17 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
         int number = tkv::group_before<kWaves>(keys, N, part);  // (its barrier is the one after the clearing)
         const int context = N - t.L;
         for (int e = e0; e < e1; e += kBatch) {
-            if (e > e0) look(e);
+            if (e > e0) {
+                look(e);
+                fetch(0);
+            }
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
+                if (k + 1 < kBatch) fetch(k + 1);
                 if (len[k] == 0) continue;
-                if (e > e0 || k > 0) fetch(id[k]);
 #pragma unroll
                 for (int q = 0; q < 16; ++q) {
-                    const uint32_t at = static_cast<uint32_t>(tok[q >> 2][q & 3]) - static_cast<uint32_t>(c0);
+                    const uint32_t at = static_cast<uint32_t>(tok[k & 1][q >> 2][q & 3]) - static_cast<uint32_t>(c0);
                     if (q >= len[k] || at >= static_cast<uint32_t>(n)) continue;
                     const bool past = number + q >= prompt;
                     if (number + q >= context && (t.L > 1 || !sees)) {
