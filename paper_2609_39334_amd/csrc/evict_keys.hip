@@ -20,6 +20,7 @@ typedef f32x4_t f32x4_u __attribute__((aligned(4)));  // rows start anywhere
 constexpr int kChoose = 1024, kChooseWaves = kChoose / 64;
 constexpr int kCached = 16384;  // entries whose lengths stay in LDS
 constexpr int kBins = 2048;
+constexpr int kEarly = 2;       // slots of a thread, in fours, whose weights are asked for first
 constexpr int kHeld = 32768;    // slots whose orders stay in LDS
 constexpr int kMove = 256, kMoveWaves = kMove / 64;
 
@@ -55,62 +56,49 @@ __global__ __launch_bounds__(kChoose) void choose(Args a) {
     const float* weights = a.weights + (static_cast<int64_t>(r) * a.hkv + g) * a.keys;
 
     const int fresh = to.ok && tid < to.n ? a.b.new_blocks[to.first + tid] : -1;
-    // the path's length, and where its keys between the first and the last begin and end
+    const int quads = 4 * tab.n, in_lds = min(quads, a.held / 4);
+    const auto weights_of = [&](int q) { return *reinterpret_cast<const f32x4_u*>(weights + 4 * static_cast<int64_t>(q)); };
+    f32x4_t early[kEarly];  // (asked for before anything is known of the path)
+#pragma unroll
+    for (int k = 0; k < kEarly; ++k) early[k] = tid + k * kChoose < quads ? weights_of(tid + k * kChoose) : f32x4_t{};
+    for (int i = tid; i < kBins; i += kChoose) hist[i] = 0;
+
+    // the path's length, and where its keys between the first and the last begin and end: a thread a run of entries
     bool ok = tab.ok && to.ok && budget >= 0 && budget <= a.b.max_budget;
     const int end = 16 * tab.n, sink = min(a.b.sink, budget), recent = min(a.b.recent, budget - sink);
-    int N = 0, lo = 0, hi = end;
-    for (int base = 0; ok && base < tab.n; base += kChoose) {
-        const int e = base + tid;
-        int id, len = 0, total;
-        if (e < tab.n) len = tkv::entry_len(a.b.kv_blocks, a.b.block_len, a.num_blocks, tab.first + e, id);
+    const auto look = [&](int e) {
+        int id;
+        return tkv::entry_len(a.b.kv_blocks, a.b.block_len, a.num_blocks, tab.first + e, id);
+    };
+    const auto len_of = [&](int e) { return e < kCached ? static_cast<int>(cached[e]) : look(e); };
+    const int stretch = (tab.n + kChoose - 1) / kChoose, e0 = min(tid * stretch, tab.n), e1 = min(e0 + stretch, tab.n);
+    int mine = 0, N;
+#pragma unroll 2
+    for (int e = e0; e < e1; ++e) {
+        const int len = look(e);
         if (e < kCached) cached[e] = static_cast<uint8_t>(len);
-        const int number = N + tkv::group_before<kChooseWaves>(len, total, part[0]);
+        mine += len;
+    }
+    int number = tkv::group_before<kChooseWaves>(mine, N, part[0]);
+    for (int e = e0; e < e1; ++e) {
+        const int len = len_of(e);
         if (sink >= number && sink < number + len) found[0] = 16 * e + (sink - number);
-        N += total;
-        if (tab.n <= kChoose) {  // one round: the end is known as well
-            const int last = N - recent;
-            if (last >= number && last < number + len) found[1] = 16 * e + (last - number);
-        }
-        __syncthreads();
+        if (N - recent >= number && N - recent < number + len) found[1] = 16 * e + (N - recent - number);
+        number += len;
     }
-    const int n = ok ? min(N, budget) : 0;
+    const int n = ok ? min(N, budget) : 0, need = (n + 15) / 16;
     // new blocks that are not of the pool
-    {
-        const int need = (n + 15) / 16;
-        int bad = need > to.n || (tid < need && static_cast<uint32_t>(fresh) >= static_cast<uint32_t>(a.num_blocks));
-        for (int e = kChoose + tid; e < min(need, to.n); e += kChoose)
-            if (static_cast<uint32_t>(a.b.new_blocks[to.first + e]) >= static_cast<uint32_t>(a.num_blocks)) bad = 1;
-        if (__syncthreads_or(bad)) ok = false;
-    }
+    int bad = need > to.n || (tid < need && static_cast<uint32_t>(fresh) >= static_cast<uint32_t>(a.num_blocks));
+    for (int e = kChoose + tid; e < min(need, to.n); e += kChoose)
+        if (static_cast<uint32_t>(a.b.new_blocks[to.first + e]) >= static_cast<uint32_t>(a.num_blocks)) bad = 1;
+    if (__syncthreads_or(bad)) ok = false;
     const int n_out = ok ? n : 0;
     for (int i = n_out + tid; i < a.b.max_budget; i += kChoose) kept[i] = -1;
     if (g == 0 && tid == 0) a.n_kept[r] = ok ? n : -1;
     if (n_out == 0) return;
-
-    const auto len_of = [&](int e) {
-        int id;
-        return e < kCached ? static_cast<int>(cached[e]) : tkv::entry_len(a.b.kv_blocks, a.b.block_len, a.num_blocks, tab.first + e, id);
-    };
-    if (N <= budget) {
-        lo = end;
-    } else {
-        lo = found[0];
-        int after = 0;
-        for (int base = (tab.n - 1) / kChoose * kChoose; tab.n > kChoose && recent > 0 && base >= 0 && after < recent; base -= kChoose) {
-            const int e = base + tid;
-            int total;
-            const int len = e < tab.n ? len_of(e) : 0;
-            const int before = tkv::group_before<kChooseWaves>(len, total, part[0]);
-            const int behind = after + total - before - len;  // keys behind this entry
-            if (behind < recent && recent <= behind + len) found[1] = 16 * e + (len - (recent - behind));
-            after += total;
-            __syncthreads();
-        }
-        if (recent > 0) hi = found[1];
-    }
+    const int lo = N <= budget ? end : found[0], hi = N <= budget || recent == 0 ? end : found[1];
     // the orders of slots 4 q .. 4 q + 3, of one entry
-    const auto orders_at = [&](int q) {
-        const f32x4_t w = *reinterpret_cast<const f32x4_u*>(weights + 4 * static_cast<int64_t>(q));
+    const auto orders_of = [&](int q, f32x4_t w) {
         const int len = len_of(q >> 2), slot = 4 * q & 15;
         u32x4_t o;
 #pragma unroll
@@ -121,10 +109,7 @@ __global__ __launch_bounds__(kChoose) void choose(Args a) {
         }
         return o;
     };
-    const int quads = end / 4, in_lds = min(quads, a.held / 4);
-    const auto orders = [&](int q) { return q < in_lds ? held[q] : orders_at(q); };
-    for (int i = tid; i < kBins; i += kChoose) hist[i] = 0;
-    __syncthreads();
+    const auto orders = [&](int q) { return q < in_lds ? held[q] : orders_of(q, weights_of(q)); };
     // equal weights are common: one addition where all lanes of a wave have the same bin
     const auto add = [&](uint32_t bin) {
         const uint32_t first = __builtin_amdgcn_readfirstlane(bin);
@@ -134,13 +119,21 @@ __global__ __launch_bounds__(kChoose) void choose(Args a) {
         else if (lane == __builtin_ctzll(all))
             atomicAdd(hist + bin, static_cast<uint32_t>(__builtin_popcountll(all)));
     };
-#pragma unroll 2
-    for (int q = tid; q < quads; q += kChoose) {
-        const u32x4_t o = orders_at(q);
+    const auto fill = [&](int q, f32x4_t w) {
+        const u32x4_t o = orders_of(q, w);
         if (q < in_lds) held[q] = o;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (o[k] != 0) add(o[k] >> 21);
+    };
+#pragma unroll
+    for (int k = 0; k < kEarly; ++k)
+        if (tid + k * kChoose < quads) fill(tid + k * kChoose, early[k]);
+    f32x4_t next = tid + kEarly * kChoose < quads ? weights_of(tid + kEarly * kChoose) : f32x4_t{};
+    for (int q = tid + kEarly * kChoose; q < quads; q += kChoose) {
+        const f32x4_t w = next;
+        if (q + kChoose < quads) next = weights_of(q + kChoose);
+        fill(q, w);
     }
     // the order of the last key that stays, 11, 11 and 10 bits at a time, and how many of that order do
     uint32_t last = 0;
