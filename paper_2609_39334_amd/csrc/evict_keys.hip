@@ -18,8 +18,9 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef f32x4_t f32x4_u __attribute__((aligned(4)));  // rows start anywhere
 
 constexpr int kChoose = 1024, kChooseWaves = kChoose / 64;
-constexpr int kCached = 16384;  // entries whose lengths stay in LDS
+constexpr int kCached = 8192;   // entries whose lengths stay in LDS
 constexpr int kBins = 2048;
+constexpr int kListed = 2048;   // most slots of a bin that are listed
 constexpr int kEarly = 2;       // slots of a thread, in fours, whose weights are asked for first
 constexpr int kHeld = 32768;    // slots whose orders stay in LDS
 constexpr int kMove = 256, kMoveWaves = kMove / 64;
@@ -46,7 +47,7 @@ __global__ __launch_bounds__(kChoose) void choose(Args a) {
     extern __shared__ u32x4_t held[];  // the slots' orders, four by four, of the first a.held of them
     __shared__ uint8_t cached[kCached];
     __shared__ uint32_t hist[kBins];
-    __shared__ int part[2][kChooseWaves], found[5];
+    __shared__ int part[kChooseWaves], tally[2][kChooseWaves], found[6], list[kListed];
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = blockIdx.x / a.hkv, g = blockIdx.x - r * a.hkv;
     const tkv::RowTable tab = tkv::row_table(a.b.kv_indptr, r, a.b.n_kv_blocks, a.b.max_blocks);
@@ -79,7 +80,7 @@ __global__ __launch_bounds__(kChoose) void choose(Args a) {
         if (e < kCached) cached[e] = static_cast<uint8_t>(len);
         mine += len;
     }
-    int number = tkv::group_before<kChooseWaves>(mine, N, part[0]);
+    int number = tkv::group_before<kChooseWaves>(mine, N, part);
     for (int e = e0; e < e1; ++e) {
         const int len = len_of(e);
         if (sink >= number && sink < number + len) found[0] = 16 * e + (sink - number);
@@ -135,18 +136,24 @@ __global__ __launch_bounds__(kChoose) void choose(Args a) {
         if (q + kChoose < quads) next = weights_of(q + kChoose);
         fill(q, w);
     }
-    // the order of the last key that stays, 11, 11 and 10 bits at a time, and how many of that order do
+    // The order of the last key that stays, 11, 11 and 10 bits at a time, and how many of that order do.  Where the first bin
+    // that is not kept whole is small, its slots are listed as they are counted, and the rest goes by the list.
+    const int run = (quads + 64 * kChooseWaves - 1) / (64 * kChooseWaves) * 64;  // a wave a run of slots, in fours
+    const int from = min(wid * run, quads), until = min(from + run, quads);
+    const auto order = [&](int i) { return i < 4 * in_lds ? reinterpret_cast<const uint32_t*>(held)[i] : orders(i >> 2)[i & 3]; };
     uint32_t last = 0;
-    int left = n;
+    int left = n, n_listed = 0;
+    bool listed = false;
     for (int low = 21;;) {
         __syncthreads();
         // the bin, counted from the largest, in which it lies
         const int most = low == 0 ? 0x3ff : 0x7ff, top = most - 2 * tid;
         const int h0 = top >= 0 ? hist[top] : 0, h1 = top >= 1 ? hist[top - 1] : 0;
         int total;
-        const int above = tkv::group_before<kChooseWaves>(h0 + h1, total, part[0]);
+        const int above = tkv::group_before<kChooseWaves>(h0 + h1, total, part);
         if (above < left && left <= above + h0) found[2] = top, found[3] = left - above, found[4] = h0;
         if (above + h0 < left && left <= above + h0 + h1) found[2] = top - 1, found[3] = left - above - h0, found[4] = h1;
+        if (tid == 0) found[5] = 0;
         __syncthreads();
         last |= static_cast<uint32_t>(found[2]) << low;
         left = found[3];
@@ -159,35 +166,63 @@ __global__ __launch_bounds__(kChoose) void choose(Args a) {
         low = low == 21 ? 10 : 0;
         const uint32_t mask = low == 0 ? 0x3ff : 0x7ff;
         for (int i = tid; i < kBins; i += kChoose) hist[i] = 0;
+        if (low == 10) listed = found[4] <= kListed, n_listed = found[4];
         __syncthreads();
-#pragma unroll 2
-        for (int q = tid; q < quads; q += kChoose) {
-            const u32x4_t o = orders(q);
+        if (low == 10 && listed) {
+            int sures = 0, all;
+            for (int q = from + lane; q < until; q += 64) {
+                const u32x4_t o = orders(q);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (o[k] != 0 && ((o[k] ^ last) >> shift) == 0) add(o[k] >> low & mask);
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t bin = o[k] >> 21, here = last >> 21;
+                    sures += bin > here;
+                    if (o[k] != 0 && bin == here) {
+                        list[atomicAdd(found + 5, 1)] = 4 * q + k;
+                        atomicAdd(hist + (o[k] >> 10 & 0x7ff), 1u);
+                    }
+                }
+            }
+            tkv::wave_before(sures, all);
+            if (lane == 0) tally[0][wid] = all, tally[1][wid] = 0;
+        } else if (listed) {
+            for (int c = tid; c < n_listed; c += kChoose) {
+                const uint32_t o = order(list[c]);
+                if ((o ^ last) >> shift == 0) atomicAdd(hist + (o >> low & mask), 1u);
+            }
+        } else {
+#pragma unroll 2
+            for (int q = tid; q < quads; q += kChoose) {
+                const u32x4_t o = orders(q);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (o[k] != 0 && ((o[k] ^ last) >> shift) == 0) add(o[k] >> low & mask);
+            }
         }
     }
 
-    // the kept ones in path order, a wave a run of slots, counted first
-    const int run = (quads + 64 * kChooseWaves - 1) / (64 * kChooseWaves) * 64;
-    const int from = min(wid * run, quads), until = min(from + run, quads);
-    int sures = 0, equals = 0;
+    // the kept ones in path order, counted first
+    if (listed) {
+        for (int c = tid; c < n_listed; c += kChoose) {
+            const int i = list[c];
+            const uint32_t o = order(i);
+            if (o > last) atomicAdd(&tally[0][(i >> 2) / run], 1);
+            if (o == last) atomicAdd(&tally[1][(i >> 2) / run], 1);
+        }
+    } else {
+        int sures = 0, equals = 0, all_sure, all_equal;
 #pragma unroll 2
-    for (int q = from + lane; q < until; q += 64) {
-        const u32x4_t o = orders(q);
+        for (int q = from + lane; q < until; q += 64) {
+            const u32x4_t o = orders(q);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sures += o[k] > last, equals += o[k] == last;
-    }
-    {
-        int all_sure, all_equal;
+            for (int k = 0; k < 4; ++k) sures += o[k] > last, equals += o[k] == last;
+        }
         tkv::wave_before(sures, all_sure);
         tkv::wave_before(equals, all_equal);
-        if (lane == 0) part[0][wid] = all_sure, part[1][wid] = all_equal;
+        if (lane == 0) tally[0][wid] = all_sure, tally[1][wid] = all_equal;
     }
     __syncthreads();
-    sures = 0, equals = 0;
-    for (int x = 0; x < wid; ++x) sures += part[0][x], equals += part[1][x];
+    int sures = 0, equals = 0;
+    for (int x = 0; x < wid; ++x) sures += tally[0][x], equals += tally[1][x];
     const auto below = [](uint64_t m) {
         return static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(m >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(m), 0)));
     };
