@@ -17,6 +17,10 @@ namespace {
 
 constexpr int kTile = 8192;                        // tokens of the vocabulary a workgroup
 constexpr int kMaxDraft = 1024;
+// Logits of many rows do not stay in the caches until they are drawn from.  Written past them from 8 MiB on: 238 bf16 rows of
+// 32,003 21.4 us, 22.8 into them (45.5 and 46.5 with the draws after them); five of 151,936 cost a draw 0.9 us more.  Read
+// past them where both pass 192 MiB: 1,000 fp32 rows of 151,936 234 us, 244 with the stores alone, 252 through the caches.
+constexpr int64_t kPastOut = 8 << 20, kPastIn = 192 << 20;
 constexpr int kBatch = 4;                          // entries of a table a thread looks at together
 constexpr int32_t kPast = 1 << 30;                 // a drafted token past the prompt
 
@@ -33,20 +37,26 @@ struct Args {
     tkv_logit_rules u;
     int32_t num_blocks, vocab, n_tiles, groups, per, units;  // groups of `per` query tokens of a row; groups or tokens in all
     bool spread, search;
+    bool past_in, past_out;  // logits read and written past the caches
     const int32_t* tokens;
     const void* in;
     void* out;
     int64_t in_stride, out_stride;
 };
 
-template <bool B16>
+// PAST: past the caches.
+template <bool B16, bool PAST>
 __device__ __forceinline__ f32x4_t load4(const void* row, int c, int n) {
+    const auto get = [](const auto* p) {
+        if constexpr (PAST) return __builtin_nontemporal_load(p);
+        else return *p;
+    };
     f32x4_t x{0.f, 0.f, 0.f, 0.f};
     if constexpr (B16) {
         const uint16_t* p = static_cast<const uint16_t*>(row) + c;
         u16x4_t v{0, 0, 0, 0};
         if (c + 4 <= n)
-            v = *reinterpret_cast<const u16x4_u*>(p);
+            v = get(reinterpret_cast<const u16x4_u*>(p));
         else
             for (int e = 0; e < 3; ++e)
                 if (c + e < n) v[e] = p[e];
@@ -55,7 +65,7 @@ __device__ __forceinline__ f32x4_t load4(const void* row, int c, int n) {
     } else {
         const float* p = static_cast<const float*>(row) + c;
         if (c + 4 <= n)
-            x = *reinterpret_cast<const f32x4_u*>(p);
+            x = get(reinterpret_cast<const f32x4_u*>(p));
         else
             for (int e = 0; e < 3; ++e)
                 if (c + e < n) x[e] = p[e];
@@ -64,19 +74,28 @@ __device__ __forceinline__ f32x4_t load4(const void* row, int c, int n) {
 }
 
 template <bool B16>
-__device__ __forceinline__ void store4(void* row, int c, int n, f32x4_t x) {
+__device__ __forceinline__ void store4(void* row, int c, int n, f32x4_t x, bool past) {
+    const auto set = [past](auto* p, auto v) {
+        if (past) {
+            asm volatile("");  // (the branches would be made one, and the store an ordinary one)
+            __builtin_nontemporal_store(v, p);
+            asm volatile("");
+        } else {
+            *p = v;
+        }
+    };
     if constexpr (B16) {
         uint16_t* p = static_cast<uint16_t*>(row) + c;
         const u16x4_t v = __builtin_bit_cast(u16x4_t, __builtin_convertvector(x, bf16x4_t));
         if (c + 4 <= n)
-            *reinterpret_cast<u16x4_u*>(p) = v;
+            set(reinterpret_cast<u16x4_u*>(p), v);
         else
             for (int e = 0; e < 3; ++e)
                 if (c + e < n) p[e] = v[e];
     } else {
         float* p = static_cast<float*>(row) + c;
         if (c + 4 <= n)
-            *reinterpret_cast<f32x4_u*>(p) = x;
+            set(reinterpret_cast<f32x4_u*>(p), x);
         else
             for (int e = 0; e < 3; ++e)
                 if (c + e < n) p[e] = x[e];
@@ -208,8 +227,15 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
     uint32_t words[kLoads], sees;
     bool fine, masked;
     const auto ask = [&](int i) __attribute__((always_inline)) {
+        if (a.past_in) {
+            asm volatile("");  // (as for the stores)
 #pragma unroll
-        for (int k = 0; k < kLoads; ++k) x[k] = load4<IN16>(in, (k * kThreads + tid) * 4, n);
+            for (int k = 0; k < kLoads; ++k) x[k] = load4<IN16, true>(in, (k * kThreads + tid) * 4, n);
+            asm volatile("");
+        } else {
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) x[k] = load4<IN16, false>(in, (k * kThreads + tid) * 4, n);
+        }
         const int64_t q = t.q0 + i;
         const int grammar = a.u.grammar ? a.u.grammar[q] : -1;
         fine = ok && grammar < a.u.n_grammars;
@@ -320,7 +346,7 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
                     if (!(bits >> e & 1)) y[e] = -INFINITY;
             }
             if (!fine) y = f32x4_t{NAN, NAN, NAN, NAN};
-            store4<OUT16>(out, c, n, y);
+            store4<OUT16>(out, c, n, y, a.past_out);
         }
         if (++i == end) break;
         in += in_step, out += out_step;
@@ -350,6 +376,9 @@ int tkv::launch_adjust_logits(const AdjustCall& f, void* stream) {
     a.num_blocks = f.num_blocks, a.vocab = f.vocab, a.tokens = f.tokens;
     a.in = f.in, a.out = f.out, a.in_stride = f.in_stride, a.out_stride = f.out_stride;
     a.n_tiles = (f.vocab + kTile - 1) / kTile;
+    const int64_t logits = static_cast<int64_t>(f.vocab) * f.b.n_qtok, out_bytes = logits * (f.out16 ? 2 : 4);
+    a.past_out = out_bytes >= kPastOut;
+    a.past_in = out_bytes + logits * (f.in16 ? 2 : 4) >= kPastIn;
     const int64_t tiles = static_cast<int64_t>(a.n_tiles) * f.b.n_qtok;
     a.per = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, f.b.max_q), tiles / 4096)));
     a.groups = (f.b.max_q + a.per - 1) / a.per;

@@ -24,6 +24,10 @@ constexpr int kListed = 2048;   // most slots of a bin that are listed
 constexpr int kEarly = 2;       // slots of a thread, in fours, whose weights are asked for first
 constexpr int kHeld = 32768;    // slots whose orders stay in LDS
 constexpr int kMove = 256, kMoveWaves = kMove / 64;
+// The old rows are not read again, so they are read past the caches (64 rows of up to 6,144 keys, 1,024 of which stay, 12/2/128
+// heads: 36 us a call, 43 through them); the new ones are next read by attention, and written past the caches only where they
+// do not fit them (32 rows of eight heads, 2,000 keys each, 250 MiB: 127 us, 131 into them; those 64 rows 40 us).
+constexpr int64_t kPast = 192 << 20;
 
 struct Args {
     tkv_evict_batch b;
@@ -33,6 +37,7 @@ struct Args {
     int64_t keys;
     uint16_t *k, *v;
     int32_t *kept, *n_kept;
+    bool past;  // the kept keys are written past the caches
 };
 
 // A slot's order, an unsigned number: the weights' own (NaN below all others, the two zeros equal), 0 where there is no key,
@@ -266,15 +271,23 @@ __global__ __launch_bounds__(kMove) void move(Args a) {
     for (int s = 0; s < NI; ++s) {
         const int row = s * RPI + lane / CPR;
         const int64_t from = (static_cast<int64_t>(__shfl(id, row)) * a.hkv + g) * (16 * D) + (__shfl(i, row) & 15) * D + lane % CPR * 8;
-        kx[s] = *reinterpret_cast<const u32x4_t*>(a.k + from);
-        vx[s] = *reinterpret_cast<const u32x4_t*>(a.v + from);
+        kx[s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(a.k + from));
+        vx[s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(a.v + from));
     }
 #pragma unroll
     for (int s = 0; s < NI; ++s) {
         const int row = s * RPI + lane / CPR;
         if (row >= n) continue;
-        *reinterpret_cast<u32x4_t*>(a.k + to + row * D + lane % CPR * 8) = kx[s];
-        *reinterpret_cast<u32x4_t*>(a.v + to + row * D + lane % CPR * 8) = vx[s];
+        u32x4_t* kt = reinterpret_cast<u32x4_t*>(a.k + to + row * D + lane % CPR * 8);
+        u32x4_t* vt = reinterpret_cast<u32x4_t*>(a.v + to + row * D + lane % CPR * 8);
+        if (a.past) {
+            asm volatile("");  // (the branches would be made one, and the stores ordinary ones)
+            __builtin_nontemporal_store(kx[s], kt);
+            __builtin_nontemporal_store(vx[s], vt);
+            asm volatile("");
+        } else {
+            *kt = kx[s], *vt = vx[s];
+        }
     }
 }
 
@@ -293,6 +306,7 @@ int tkv::launch_evict_keys(const tkv_shape& s, const tkv_evict_batch& b, const f
     const int64_t moves = rows * ((a.new_max + kMoveWaves - 1) / kMoveWaves);
     if (rows > INT32_MAX || moves > INT32_MAX)
         return set_error(TKV_EINVAL, "tkv_evict_keys: %lld workgroups are too many", static_cast<long long>(std::max(rows, moves)));
+    a.past = rows * b.max_budget * s.d * 4 >= kPast;
     a.held = std::min(kHeld, 16 * b.max_blocks);
     choose<<<dim3(static_cast<unsigned>(rows)), dim3(kChoose), static_cast<size_t>(a.held) * 4, st>>>(a);
     hipError_t e = hipGetLastError();
