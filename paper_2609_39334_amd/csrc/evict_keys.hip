@@ -31,7 +31,7 @@ constexpr int64_t kPast = 192 << 20;
 
 struct Args {
     tkv_evict_batch b;
-    int32_t num_blocks, hkv, new_max, held;  // blocks of the longest new table; slots whose orders stay in LDS
+    int32_t num_blocks, hkv, new_max, per_row, held;  // blocks of the longest new table, workgroups that move it; slots whose orders stay in LDS
     const float* weights;
     float* out;
     int64_t keys;
@@ -255,7 +255,7 @@ template <int D>
 __global__ __launch_bounds__(kMove) void move(Args a) {
     constexpr int CPR = D / 8, RPI = 64 / CPR, NI = 16 / RPI;  // 16-byte pieces a row, rows a load, loads a block
     const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-    const int per_row = (a.new_max + kMoveWaves - 1) / kMoveWaves;
+    const int per_row = a.per_row;
     const int x = blockIdx.x % per_row, u = blockIdx.x / per_row;
     const int g = u % a.hkv, r = u / a.hkv;
     const int j = x * kMoveWaves + wid, n = a.n_kept[r] - 16 * j;
@@ -303,7 +303,8 @@ int tkv::launch_evict_keys(const tkv_shape& s, const tkv_evict_batch& b, const f
     a.weights = weights, a.out = out, a.keys = keys;
     a.k = static_cast<uint16_t*>(k), a.v = static_cast<uint16_t*>(v), a.kept = kept, a.n_kept = n_kept;
     const int64_t rows = static_cast<int64_t>(b.n_rows) * s.hkv;
-    const int64_t moves = rows * ((a.new_max + kMoveWaves - 1) / kMoveWaves);
+    a.per_row = (a.new_max + kMoveWaves - 1) / kMoveWaves | 1;  // (odd: a row's blocks would go to the same XCDs as the other rows')
+    const int64_t moves = a.new_max > 0 ? rows * a.per_row : 0;
     if (rows > INT32_MAX || moves > INT32_MAX)
         return set_error(TKV_EINVAL, "tkv_evict_keys: %lld workgroups are too many", static_cast<long long>(std::max(rows, moves)));
     a.past = rows * b.max_budget * s.d * 4 >= kPast;

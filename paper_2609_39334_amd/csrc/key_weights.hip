@@ -24,7 +24,7 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kFewChunk = 256;    // most entries a workgroup of weigh_few
+constexpr int kFewChunk = 64;     // most entries a workgroup of weigh_few
 constexpr int kManyChunk = 16;    // entries a workgroup of weigh_many
 constexpr int kWords = 9;         // words of 32 bits that 256 consecutive bits can touch
 constexpr float kLog2e = 1.4426950408889634f;
@@ -167,10 +167,12 @@ __global__ __launch_bounds__(kThreads, 3) void weigh_few(Args a) {
     look_lens(a, look);
     // x[4 v + e] of a product is query row 8 v + 4 hi + e
     float off[16];
+    uint32_t mask;  // of row `col`: a row's tokens are at most 32
     {
         const int qr = min(col, rows - 1), i = token_of(a, qr);
         const int64_t token = u.t.q0 + i;
         const float z = a.lse[token * a.hq + u.g * a.G + (qr - i * a.G)], c = a.coef ? a.coef[token] : 1.f;
+        mask = col < rows ? static_cast<uint32_t>(a.b.mask[token * a.b.mask_words]) : 0;
         const float mine = col < rows ? offset_of(z, c) : INFINITY;
 #pragma unroll
         for (int e = 0; e < 16; ++e) off[e] = __shfl(mine, 8 * (e >> 2) + 4 * hi + (e & 3));
@@ -206,18 +208,11 @@ __global__ __launch_bounds__(kThreads, 3) void weigh_few(Args a) {
                     for (int e = 4 * v; e < 4 * v + 4; ++e) sum += __builtin_amdgcn_exp2f(fmaf(x[e], a.sl2, -off[e]));
                 }
         } else {
-            uint32_t sees = 0;  // the rows that see this lane's key
-#pragma unroll 1
-            for (int e = 0; e < 4 * nu; ++e) {
-                const int row = 8 * (e >> 2) + 4 * hi + (e & 3);
-                if (there && row < rows &&
-                    (j < 0 || a.b.mask[static_cast<int64_t>(u.t.q0 + token_of(a, row)) * a.b.mask_words + (j >> 6)] >> (j & 63) & 1))
-                    sees |= 1u << e;
-            }
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
+                const uint32_t row = __shfl(mask, 8 * (e >> 2) + 4 * hi + (e & 3));
                 const float w = __builtin_amdgcn_exp2f(fmaf(x[e], a.sl2, -off[e]));
-                sum += sees >> e & 1 ? w : 0.f;
+                sum += there && (j < 0 || (row >> (j & 31) & 1)) ? w : 0.f;
             }
         }
         sum += __shfl_xor(sum, 32);
@@ -480,7 +475,7 @@ int tkv::launch_key_weights(const tkv_shape& s, const tkv_draft_batch& b, const 
         const int64_t even = static_cast<int64_t>(b.n_kv_blocks) * s.hkv / 768;
         a.chunk = static_cast<int32_t>(std::max<int64_t>(8, std::min<int64_t>(kFewChunk, (even + 7) / 8 * 8)));
     }
-    a.n_chunks = (b.max_blocks + a.chunk - 1) / a.chunk;
+    a.n_chunks = (b.max_blocks + a.chunk - 1) / a.chunk | 1;  // (odd: a row's chunks would go to the same XCDs as the other rows')
     const int64_t direct = static_cast<int64_t>(a.n_chunks) * b.n_rows * s.hkv;
     const int64_t counted = (b.n_kv_blocks / a.chunk + static_cast<int64_t>(b.n_rows)) * s.hkv;
     a.search = direct > 4 * counted;
