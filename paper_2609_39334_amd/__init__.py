@@ -1132,9 +1132,9 @@ class EvictBatch:
         for t, m in zip(new, self.n_kept):
             if 16 * len(t) < m:
                 raise ValueError(f"EvictBatch: {len(t)} blocks do not hold {m} keys")
-        self.max_blocks, self.most = max([len(t) for t in old], default=1) or 1, max(budget, default=0)
+        self.max_blocks, self.most = max([len(t) for t in old], default=1) or 1, max(self.n_kept, default=0)
         parts = [np.cumsum([0] + [len(t) for t in old]).astype(np.int32), np.cumsum([0] + [len(t) for t in new]).astype(np.int32),
-                 np.asarray(budget, np.int32), np.concatenate(old) if old else fresh, fresh, bl]
+                 np.asarray(self.n_kept, np.int32), np.concatenate(old) if old else fresh, fresh, bl]
         flat = torch.from_numpy(np.concatenate(parts)).to(device)
         at = np.cumsum([0] + [len(p) for p in parts])
         self.kv_indptr, self.new_indptr, self.budget, self.kv_blocks, self.new_blocks, self.block_len = \

@@ -222,9 +222,9 @@ def test_draws_under_rules_on_another_stream():
 
 def test_evict_batch():
     bl = np.array([16, 16, 5, 3, 0, 0, 0], np.int32)
-    e = tkv.EvictBatch([[0, 3], [1, 2], []], [[4], [5, 6], []], [10, 100, 0], bl, device="cpu")
-    assert e.n_kept == [10, 21, 0] and e.evicted == [9, 0, 0] and (e.max_blocks, e.most) == (2, 100)
-    assert e.kv_indptr.tolist() == [0, 2, 4, 4] and e.new_indptr.tolist() == [0, 1, 3, 3] and e.budget.tolist() == [10, 100, 0]
+    e = tkv.EvictBatch([[0, 3], [1, 2], []], [[4], [5, 6], []], [10, 1 << 40, 0], bl, device="cpu")  # (a budget of any size)
+    assert e.n_kept == [10, 21, 0] and e.evicted == [9, 0, 0] and (e.max_blocks, e.most) == (2, 21)
+    assert e.kv_indptr.tolist() == [0, 2, 4, 4] and e.new_indptr.tolist() == [0, 1, 3, 3] and e.budget.tolist() == [10, 21, 0]
     assert e.kv_blocks.tolist() == [0, 3, 1, 2] and e.new_blocks.tolist() == [4, 5, 6] and e.block_len.tolist() == bl.tolist()
     none = tkv.EvictBatch([], [], [], bl, device="cpu")
     assert none.kv_indptr.tolist() == [0] and none.n_kept == [] and none.max_blocks == 1
