@@ -187,7 +187,7 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
     const char* in = static_cast<const char*>(a.in) + (static_cast<int64_t>(t.q0 + first) * a.in_stride + c0) * (IN16 ? 2 : 4);
     char* out = static_cast<char*>(a.out) + (static_cast<int64_t>(t.q0 + first) * a.out_stride + c0) * (OUT16 ? 2 : 4);
     const int64_t in_step = a.in_stride * (IN16 ? 2 : 4), out_step = a.out_stride * (OUT16 ? 2 : 4);
-    const bool ok = tab.ok && bias.ok && rep > 0.f && rep < INFINITY && fabsf(pres) < INFINITY && fabsf(freq) < INFINITY;
+    const bool ok = tab.ok && bias.ok && rep >= 0x1p-126f && rep <= 0x1p126f && fabsf(pres) < INFINITY && fabsf(freq) < INFINITY;
     const bool counts = ok && (rep != 1.f || pres != 0.f || freq != 0.f);
     const bool biased = BIAS && ok && bias.n > 0;
 
@@ -385,7 +385,7 @@ int tkv::launch_adjust_logits(const AdjustCall& f, void* stream) {
     a.search = f.b.max_q > 1 && a.per == 1;
     int64_t all = a.search ? f.b.n_qtok : static_cast<int64_t>(a.groups) * f.b.n_rows;
     const int64_t most = (all + 7) / 8 * 8 * a.n_tiles;
-    if (most > INT32_MAX)
+    if (most > static_cast<int64_t>(UINT32_MAX) / 512)
         return set_error(TKV_EINVAL, "tkv_adjust_logits: %lld workgroups are too many", static_cast<long long>(most));
     a.units = static_cast<int32_t>(all);
     a.spread = all >= 64;

@@ -188,7 +188,7 @@ def test_settings_outside_their_ranges():
     want = c.run().clone()
     n = c.q_ptr
     bad = {k: v.copy() for k, v in c.rules.items()}
-    for i, x in enumerate((0.0, -1.0, np.nan, np.inf)):
+    for i, x in enumerate((0.0, 1e-39, np.nan, np.inf)):
         bad["repetition"][i] = x
     bad["presence"][4], bad["frequency"][5] = np.inf, np.nan
     bad["grammar"][n[6]] = 5
@@ -354,7 +354,8 @@ def test_bad_arguments_are_refused():
                 dict(x=one + 2), dict(y=far + 1), dict(stride=99), dict(out_stride=99), dict(n_bias=-1), dict(n_bias=1),
                 dict(n_grammars=-1), dict(n_grammars=1, grammar=one, allowed=None, allowed_words=4),
                 dict(n_grammars=1, grammar=one, allowed=one, allowed_words=3), dict(rules=False),
-                dict(y=one + 4), dict(y=one, t_out=1), dict(y=one, out_stride=101), dict(y=one + 4 * 399)):
+                dict(y=one + 4), dict(y=one, t_out=1), dict(y=one, out_stride=101), dict(y=one + 4 * 399),
+                dict(n_rows=1 << 24, n_qtok=1 << 24, max_q=1, y=1 << 50)):
         assert call(**bad) == tkv.TKV_EINVAL, bad
     assert call(n_rows=0) == tkv.TKV_OK and call(n_qtok=0) == tkv.TKV_OK
     assert L.tkv_adjust_logits(4, one, None, None, 100, 0, one, 100, 0, far, 100, None) == tkv.TKV_EINVAL
