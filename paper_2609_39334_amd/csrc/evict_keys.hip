@@ -305,7 +305,7 @@ int tkv::launch_evict_keys(const tkv_shape& s, const tkv_evict_batch& b, const f
     const int64_t rows = static_cast<int64_t>(b.n_rows) * s.hkv;
     a.per_row = (a.new_max + kMoveWaves - 1) / kMoveWaves | 1;  // (odd: a row's blocks would go to the same XCDs as the other rows')
     const int64_t moves = a.new_max > 0 ? rows * a.per_row : 0;
-    if (rows > INT32_MAX || moves > INT32_MAX)
+    if (rows > static_cast<int64_t>(UINT32_MAX) / kChoose || moves > static_cast<int64_t>(UINT32_MAX) / kMove)
         return set_error(TKV_EINVAL, "tkv_evict_keys: %lld workgroups are too many", static_cast<long long>(std::max(rows, moves)));
     a.past = rows * b.max_budget * s.d * 4 >= kPast;
     a.held = std::min(kHeld, 16 * b.max_blocks);

@@ -293,7 +293,7 @@ def test_bad_arguments_are_refused():
     for bad in (dict(n_rows=-1), dict(n_kv=-1), dict(max_blocks=0), dict(n_new=-1), dict(most=-1), dict(sink=-1), dict(recent=-1),
                 dict(ptr=None), dict(new=None), dict(w=None), dict(w=one + 2), dict(out=None), dict(out=one), dict(out=one + 2 * 144 * 4 - 4),
                 dict(keys=143), dict(k=None), dict(k=one + 8), dict(kept=None), dict(kept=one + 2), dict(n_kept=None),
-                dict(max_blocks=1 << 28, keys=1 << 40)):
+                dict(max_blocks=1 << 28, keys=1 << 40), dict(n_rows=1 << 22, out=1 << 50), dict(n_rows=1 << 19, most=1 << 20, n_new=1 << 20, out=1 << 50)):
         assert call(**bad) == tkv.TKV_EINVAL, bad
     assert call(n_rows=0) == tkv.TKV_OK
     assert L.tkv_evict_keys(None, None, one, one, 1, one, one, one, one, None) == tkv.TKV_EINVAL
