@@ -423,10 +423,10 @@ int tkv_draft_verify(const tkv_shape* shape, const tkv_draft_batch* batch, const
  * in fp32, the first term for the keys of the context alone: a key among the row's last L enters with this call.
  *   q, k     as in tkv_draft_verify;  lse  [n_qtok][hq] fp32, of the same attention (natural log); a query head whose lse is
  *            not finite gives nothing
- *   coef     [n_qtok] fp32, >= 0 (nullable: 1): 0 leaves a token out (a draft that was not accepted, padding); a
- *            coefficient that is not above 0 leaves it out too
+ *   coef     [n_qtok] fp32, finite (nullable: 1): 0 leaves a token out (a draft that was not accepted, padding, whose q
+ *            may then hold anything); so does one below 2^-126 or NaN
  *   decay    finite; before is not read where it is 0
- *   before   [n_rows][hkv][keys] fp32 (nullable: zeros);  out  the same, and may be the same memory
+ *   before   [n_rows][hkv][keys] fp32 (nullable: zeros);  out  the same; it may be before, and must not overlap it otherwise
  *   keys     at least 16 * max_blocks
  * What no key of a row's table has a place for is not written (slots past a block's length, entries that are no blocks, rows
  * that are left out: tokens or table outside the arrays, or longer than max_q or max_blocks; where kv_indptr decreases

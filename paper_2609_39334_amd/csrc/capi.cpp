@@ -240,6 +240,13 @@ int check_tables(const char* fn, int32_t max_blocks, int64_t keys) {
     return TKV_OK;
 }
 
+// Whether two arrays of rows x heads x keys fp32 share memory.
+bool overlap(const float* a, const float* b, int32_t rows, int32_t heads, int64_t keys) {
+    const __int128 bytes = static_cast<__int128>(rows) * heads * keys * 4;
+    const __int128 x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + bytes && y < x + bytes;
+}
+
 bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
 }  // namespace
@@ -261,6 +268,8 @@ TKV_EXPORT int tkv_key_weights(const tkv_shape* shape, const tkv_draft_batch* ba
     for (const void* p : {static_cast<const void*>(lse), static_cast<const void*>(coef), static_cast<const void*>(before),
                           static_cast<const void*>(out)})
         if (!aligned4(p)) return tkv::set_error(TKV_EINVAL, "%s: tensors must be aligned to their type", fn);
+    if (before && before != out && overlap(before, out, b.n_rows, shape->hkv, keys))
+        return tkv::set_error(TKV_EINVAL, "%s: out overlaps before", fn);
     if (!tkv::launch_key_weights) return tkv::set_error(TKV_EHIP, "%s: host-only build, no device", fn);
     return tkv::launch_key_weights(*shape, b, q, k, lse, coef, decay, before, out, keys, stream);
 }
@@ -286,9 +295,7 @@ TKV_EXPORT int tkv_evict_keys(const tkv_shape* shape, const tkv_evict_batch* bat
     for (const void* p : {static_cast<const void*>(weights), static_cast<const void*>(out), static_cast<const void*>(kept),
                           static_cast<const void*>(n_kept)})
         if (!aligned4(p)) return tkv::set_error(TKV_EINVAL, "%s: tensors must be aligned to their type", fn);
-    const __int128 bytes = static_cast<__int128>(b.n_rows) * shape->hkv * keys * 4;
-    const __int128 w = reinterpret_cast<uintptr_t>(weights), o = reinterpret_cast<uintptr_t>(out);
-    if (w < o + bytes && o < w + bytes) return tkv::set_error(TKV_EINVAL, "%s: out overlaps weights", fn);
+    if (overlap(weights, out, b.n_rows, shape->hkv, keys)) return tkv::set_error(TKV_EINVAL, "%s: out overlaps weights", fn);
     if (!tkv::launch_evict_keys) return tkv::set_error(TKV_EHIP, "%s: host-only build, no device", fn);
     return tkv::launch_evict_keys(*shape, b, weights, out, keys, k, v, kept, n_kept, stream);
 }

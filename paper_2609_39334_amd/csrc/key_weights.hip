@@ -174,6 +174,10 @@ __global__ __launch_bounds__(kThreads, 3) void weigh_few(Args a) {
         const float z = a.lse[token * a.hq + u.g * a.G + (qr - i * a.G)], c = a.coef ? a.coef[token] : 1.f;
         mask = col < rows ? static_cast<uint32_t>(a.b.mask[token * a.b.mask_words]) : 0;
         const float mine = col < rows ? offset_of(z, c) : INFINITY;
+        if (mine == INFINITY) {  // a row that gives nothing may hold anything
+#pragma unroll
+            for (int s = 0; s < KS; ++s) qf[s] = bf16x8_t{};
+        }
 #pragma unroll
         for (int e = 0; e < 16; ++e) off[e] = __shfl(mine, 8 * (e >> 2) + 4 * hi + (e & 3));
     }
@@ -336,15 +340,19 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
         }
     };
     const auto put = [&](int tile, int set) __attribute__((always_inline)) {
+        const float c = __uint_as_float((__float_as_uint(cx[set]) & given) | (__float_as_uint(1.f) & ~given));
+        float off = offset_of(zx[set], c);
+        off = 32 * tile + col < rows ? off : INFINITY;
+        offs[tile & 3][col] = off;
+        // a row that gives nothing may hold anything: zeros in its place
+        const uint32_t none = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(off == INFINITY));
 #pragma unroll
         for (int y = 0; y < kPieces; ++y) {
             const int x = y * kThreads + tid, row = x / CPR;
             const int swz = D == 128 ? row & 15 : (row >> 1) & 7;
-            *reinterpret_cast<u32x4_t*>(qs[set] + row * D + ((x % CPR) ^ swz) * 8) = qx[set][y];
+            const uint32_t keep = (none >> row & 1) - 1;
+            *reinterpret_cast<u32x4_t*>(qs[set] + row * D + ((x % CPR) ^ swz) * 8) = qx[set][y] & keep;
         }
-        const float c = __uint_as_float((__float_as_uint(cx[set]) & given) | (__float_as_uint(1.f) & ~given));
-        const float off = offset_of(zx[set], c);
-        offs[tile & 3][col] = 32 * tile + col < rows ? off : INFINITY;
     };
     const auto put_bits = [&](int set) __attribute__((always_inline)) {
         bits[set][tid / kWords][tid % kWords] = bx[set][0];
@@ -480,7 +488,7 @@ int tkv::launch_key_weights(const tkv_shape& s, const tkv_draft_batch& b, const 
     const int64_t counted = (b.n_kv_blocks / a.chunk + static_cast<int64_t>(b.n_rows)) * s.hkv;
     a.search = direct > 4 * counted;
     const int64_t grid = a.search ? counted : direct;
-    if (grid > INT32_MAX)
+    if (grid > static_cast<int64_t>(UINT32_MAX) / kThreads)
         return set_error(TKV_EINVAL, "tkv_key_weights: %lld workgroups are too many", static_cast<long long>(grid));
     const auto run = [&](auto kernel) { kernel<<<dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, st>>>(a); };
     if (s.d == 128)

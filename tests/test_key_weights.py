@@ -133,6 +133,25 @@ def test_old_weights_coefficients_and_decay():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("L", [3, 40])
+def test_tokens_that_are_left_out_may_hold_anything(L):
+    # padding: no coefficient, or no attention
+    c = Case([(300, L), (20, L), (1200, L)], 8, 2, 64)
+    out = torch.arange(0, 3 * L, 3, device="cuda")
+    for what in ("coef", "lse"):
+        if what == "coef":
+            c.coef[out] = 0.0
+        else:
+            c.coef = torch.ones_like(c.coef)
+            c.lse[out] = torch.tensor([float("nan"), float("inf"), -float("inf")], device="cuda").repeat(L)[:len(out), None]
+        c.q[out] = 1.0
+        want = c.run()
+        for x in (float("nan"), float("inf"), -float("inf")):
+            c.q[out] = x
+            assert torch.equal(c.run(), want)
+
+
+@pytest.mark.gpu
 def test_queries_without_keys_give_nothing():
     # masks that hide everything: lse is -inf
     c = Case([(0, 1), (0, 40), (5, 3)], 8, 2, 64, bits=True, seed=5)
@@ -333,7 +352,8 @@ def test_bad_arguments_are_refused():
     for bad in (dict(n_rows=-1), dict(n_qtok=-1), dict(max_q=0), dict(max_q=1025), dict(max_q=65), dict(n_kv=-1), dict(max_blocks=0),
                 dict(words=0), dict(ptr=None), dict(q=None), dict(q=one + 8), dict(lse=None), dict(lse=one + 2), dict(coef=one + 1),
                 dict(before=one + 2), dict(out=None), dict(out=one + 2), dict(keys=143), dict(keys=-1), dict(decay=float("nan")),
-                dict(decay=float("inf")), dict(max_blocks=1 << 28, keys=1 << 40)):
+                dict(decay=float("inf")), dict(max_blocks=1 << 28, keys=1 << 40), dict(before=one + 4), dict(before=one + 2 * 144 * 4 - 4),
+                dict(out=one + 4, before=one), dict(n_rows=1 << 30), dict(n_rows=1 << 24)):
         assert call(**bad) == tkv.TKV_EINVAL, bad
     assert call(n_rows=0) == tkv.TKV_OK and call(n_qtok=0) == tkv.TKV_OK
     assert L.tkv_key_weights(None, None, one, one, one, None, 1.0, None, one, 1, None) == tkv.TKV_EINVAL
