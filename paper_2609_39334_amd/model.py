@@ -103,6 +103,9 @@ class SyntheticDecoder:
         tokens: [n_qtok] int64; dst: [n_qtok] int32 pool slots of the drafted tokens, the last keys of their
         rows' tables in order; pools and stream as for step.  weights[l]: layer l's key weights [n_rows, hkv, keys] fp32, to
         which the tokens' attention is added in place (decay and coef as for tkv_key_weights)."""
+        if weights is not None and len(weights) != len(self.layers):
+            raise ValueError(f"verify_draft: key weights of {len(weights)} layers, {len(self.layers)} expected")
+
         def attend(layers):
             lse = torch.empty((tokens.numel(), self.shape.hq), dtype=torch.float32, device=tokens.device)
 
@@ -119,6 +122,10 @@ class SyntheticDecoder:
               sink: int = 0, recent: int = 0, stream=None) -> List[torch.Tensor]:
         """Every layer's eviction; returns the layers' key weights, kept keys' at their new places and zeros behind them.
         stream as for step."""
+        if not len(weights) == len(k_pools) == len(v_pools) == len(self.layers):
+            raise ValueError(f"evict: weights, K and V pools of {len(weights)}, {len(k_pools)} and {len(v_pools)} layers, "
+                             f"{len(self.layers)} expected")
+
         def run():
             return tuple(batch.evict(w, k, v, sink, recent, out=torch.zeros_like(w))[0] for w, k, v in zip(weights, k_pools, v_pools))
         return list(self._on(stream, run))

@@ -187,6 +187,11 @@ def test_the_model_after_an_eviction():
     for stream in (other, None):
         short = model.evict(e, weights, *pools, sink=2, recent=8, stream=stream)
     assert all(0 < float(s.sum()) < b for s, b in zip(short, before))
+    for args in ((e, weights[:1], *pools), (e, weights, pools[0][:1], pools[1]), (e, weights + weights, *pools)):
+        with pytest.raises(ValueError):
+            model.evict(*args)
+    with pytest.raises(ValueError):
+        verify(seqs, None, weights[:1])
     kp, vp = ([_np(p) for p in ps] for ps in pools)
     ctx = [_slots(bm.table(s), bm.block_len()) for s in new]
     got, _, batch = verify(new, e.evicted, short)
