@@ -5,6 +5,16 @@
 // often each of them occurs in the row's context, adds the drafted tokens that a query token sees (and takes them out again
 // before the next one), and passes once over the tile's logits.  Counts are whole numbers, so the order in which threads add
 // them changes nothing.
+//
+// Logits are read and written once and that bounds large calls: 1,000 rows of 151,936 in fp32 take 231 us, 5.3 TB/s, a large
+// copy's rate.  Every tile walks its row's path (4 bytes a token, from L2 after the first), which bounds few rows: five of 151,936,
+// bf16, paths of 200 to 1,000 tokens 9 us; 16 rows with paths of 8,000 to 30,000 tokens 18 us, about four entries of a table a
+// thread; 16 trees of 4 to 32 tokens, 32,003, bf16 to fp32, 20 us: the row, its table, lengths, tokens
+// and counts are a chain, before which the logits are asked for.
+//
+// Measured for the choices below (threads / tile, before logits went past the caches): 256 / 8,192 with many tiles, the 1,000 rows 239 to 249 us; 512 / 8,192 250;
+// 256 / 4,096 261; 512 / 16,384 246; 1,024 / 8,192 446; 1,024 / 16,384 310.  512 / 8,192 with few: the five rows 8.7 us, by 256 11.0; the
+// paths of 30,000 tokens 18 and 26.  (256 rows with paths of 8,000 to 16,000 tokens: 143 by 512, 120 by 256.)
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cstdint>
@@ -379,6 +389,9 @@ int tkv::launch_adjust_logits(const AdjustCall& f, void* stream) {
     const int64_t logits = static_cast<int64_t>(f.vocab) * f.b.n_qtok, out_bytes = logits * (f.out16 ? 2 : 4);
     a.past_out = out_bytes >= kPastOut;
     a.past_in = out_bytes + logits * (f.in16 ? 2 : 4) >= kPastIn;
+    // The query tokens of a tree that share a workgroup's counts: few enough that 4,096 workgroups are left.  (64 trees of 16 to 32
+    // tokens, 152,064, bf16 to fp32: one 397 us, two 378, four 355, eight 344; 319 by this rule, 327 with 2,048 left.)  With one, a
+    // workgroup finds its token's row, so that none is without work in rows shorter than max_q.
     const int64_t tiles = static_cast<int64_t>(a.n_tiles) * f.b.n_qtok;
     a.per = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, f.b.max_q), tiles / 4096)));
     a.groups = (f.b.max_q + a.per - 1) / a.per;
@@ -388,10 +401,11 @@ int tkv::launch_adjust_logits(const AdjustCall& f, void* stream) {
     if (most > static_cast<int64_t>(UINT32_MAX) / 512)
         return set_error(TKV_EINVAL, "tkv_adjust_logits: %lld workgroups are too many", static_cast<long long>(most));
     a.units = static_cast<int32_t>(all);
-    a.spread = all >= 64;
+    a.spread = all >= 64;  // (fewer units would leave XCDs without work at the end)
     if (a.spread) all = (all + 7) / 8 * 8;
+    // Numbers of 16 bits while no path and no list of biases can pass them: 32 KB of LDS for the two instead of 64.
     const bool bias = f.u.n_bias > 0, wide = f.b.max_blocks > 0x7fff / kBlock || f.u.n_bias >= 0xffff;
-    const bool many = all * a.n_tiles >= 768;
+    const bool many = all * a.n_tiles >= 768;  // (three a CU)
     const auto run = [&](auto kernel, int threads) {
         kernel<<<dim3(static_cast<unsigned>(all * a.n_tiles)), dim3(threads), 0, st>>>(a);
     };

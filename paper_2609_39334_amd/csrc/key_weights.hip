@@ -6,9 +6,21 @@
 // operand.  The coefficient goes into the exponent (lse - log c, infinite where nothing counts).  A key of a row and head
 // belongs to one wave, whose order of additions is fixed: no atomics.
 //
+// A call has to read each key once (2 d bytes a KV head) and two floats a key are read and written; it multiplies 2 d hq
+// times and takes hq exponentials a key and token.  Few tokens are bound by memory, many by their exponentials and products.
+//
 // Two kernels.  weigh_few: rows of up to 32 queries a KV head (single tokens, small drafts) hold the queries in registers and
 // stream K, the next 32 keys on their way.  weigh_many: 64 keys a wave stay in registers, and the queries pass in tiles of 32
-// through LDS, double-buffered, shared by the four waves.
+// through LDS, double-buffered, shared by the four waves.  Up to 32 queries the first is faster: 64 single tokens under 300 to
+// 6,144 keys (12/2/128 heads) 24 us, 36 by the second; 1,000 tokens under 30 to 300 keys 29 and 45; 28/4 heads 27 and 36.
+//
+// Measured (times of the kernel alone): those 64 tokens 21 us, 102 MB, 4.9 TB/s.  32 tokens under one path of 30,000 keys, 28/4/128:
+// 17 us; 472 workgroups are less than two a CU, so it is a workgroup's own time: about 7 us until its first product (table,
+// lengths, keys and first queries, a chain) and seven tiles of 0.8 to 1 us.  8 rows of 64 to 256 tokens
+// under 2,000 to 12,000 keys, 32/8/128 (67.8 GFLOP): 111 us, 610 TFLOP/s; MFMAs are busy 31% of it and the vector units 53%
+// (a product of 32 x 64 scores is 256 cycles of MFMA beside 16 x 64 exponentials, 512 cycles of a quarter-rate unit); the products
+// alone take 103 us.  Tried there: eight waves of 32 keys (123 us, 119 then), two groups of keys one after the other in a
+// workgroup (141), three waves a SIMD (127 to 133, registers spill), chunks slowest in the grid (130 to 141).
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cstdint>
@@ -24,7 +36,10 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kFewChunk = 64;     // most entries a workgroup of weigh_few
+// Most entries a workgroup of weigh_few, and workgroups aimed at: three a CU, what their registers allow.  (64 tokens under 300
+// to 6,144 keys: 600 workgroups 26.2 us, 768 24.2, 1,024 27.0, 1,536 28.7.  Arrays ten times as long as the tables in them, as a
+// captured call may have: 36 us, 178 without the limit.)
+constexpr int kFewChunk = 64, kFewGroups = 768;
 constexpr int kManyChunk = 16;    // entries a workgroup of weigh_many
 constexpr int kWords = 9;         // words of 32 bits that 256 consecutive bits can touch
 constexpr float kLog2e = 1.4426950408889634f;
@@ -271,7 +286,8 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
         cx[set] = coef[i];
     };
     // the table first, then its lengths, then the keys (rows past a block's length are read, and nothing made of them): loads
-    // come back in order
+    // come back in order.  (K is read in four pieces of 32 bytes a line: past the caches each piece is fetched for itself, 40 us
+    // for 25.)
     Look look;
     look_ids(a, u, kManyChunk, look);
     int own[2];
@@ -480,10 +496,13 @@ int tkv::launch_key_weights(const tkv_shape& s, const tkv_draft_batch& b, const 
     const bool few = static_cast<int64_t>(b.max_q) * a.G <= 32;
     a.chunk = kManyChunk;
     if (few) {
-        const int64_t even = static_cast<int64_t>(b.n_kv_blocks) * s.hkv / 768;
+        const int64_t even = static_cast<int64_t>(b.n_kv_blocks) * s.hkv / kFewGroups;
         a.chunk = static_cast<int32_t>(std::max<int64_t>(8, std::min<int64_t>(kFewChunk, (even + 7) / 8 * 8)));
     }
-    a.n_chunks = (b.max_blocks + a.chunk - 1) / a.chunk | 1;  // (odd: a row's chunks would go to the same XCDs as the other rows')
+    // Workgroup b runs on XCD b % 8: an odd number of chunks, or the rows' first chunks, which all rows have, would share one.
+    a.n_chunks = (b.max_blocks + a.chunk - 1) / a.chunk | 1;
+    // A workgroup finds its row by division where that leaves few without work, or counts the rows' chunks up to its own: one row of
+    // 30,000 keys beside 300 of 30 to 300 takes 23 us counted and 75 divided, 1,000 rows of like lengths 52 and 29.
     const int64_t direct = static_cast<int64_t>(a.n_chunks) * b.n_rows * s.hkv;
     const int64_t counted = (b.n_kv_blocks / a.chunk + static_cast<int64_t>(b.n_rows)) * s.hkv;
     a.search = direct > 4 * counted;
