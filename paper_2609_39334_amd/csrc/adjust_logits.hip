@@ -119,13 +119,14 @@ struct Cells {
     static constexpr int kWords = WIDE ? kTile : kTile / 2;
     static constexpr uint32_t kPrompt = WIDE ? 0x80000000u : 0x8000u, kTimes = kPrompt - 1;  // seen in the prompt; times past it
     uint32_t* at;
-    static __device__ __forceinline__ int shift(uint32_t i) { return WIDE ? 0 : 16 * (i & 1); }
+    static __device__ __forceinline__ int shift(uint32_t i) { return WIDE ? 0 : i << 4 & 31; }
     __device__ __forceinline__ uint32_t* word(uint32_t i) const { return at + (WIDE ? i : i >> 1); }
     __device__ __forceinline__ void clear(int tid, int threads) const {
         for (int i = tid * 4; i < kWords; i += threads * 4) *reinterpret_cast<uint4*>(at + i) = uint4{0, 0, 0, 0};
     }
     __device__ __forceinline__ void more(uint32_t i) const { atomicAdd(word(i), 1u << shift(i)); }
     __device__ __forceinline__ void less(uint32_t i) const { atomicSub(word(i), 1u << shift(i)); }
+    __device__ __forceinline__ void set(uint32_t i) const { atomicOr(word(i), kPrompt << shift(i)); }
     __device__ __forceinline__ bool mark(uint32_t i) const {  // whether it was not marked before
         return !(atomicOr(word(i), kPrompt << shift(i)) >> shift(i) & kPrompt);
     }
@@ -217,12 +218,12 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) len[k] = len[k] >= 1 && len[k] <= tkv::kBlock ? len[k] : 0;
     };
-    i32x4_t tok[2][4];  // an entry's tokens, and the next one's on their way
-    const auto fetch = [&](int k) __attribute__((always_inline)) {
-        if (len[k] == 0) return;
-        const i32x4_t* p = reinterpret_cast<const i32x4_t*>(a.tokens + static_cast<int64_t>(id[k]) * tkv::kBlock);
+    i32x4_t tok[4];  // the next entry's tokens
+    const auto fetch = [&](int block, int m) __attribute__((always_inline)) {
+        if (m == 0) return;
+        const i32x4_t* p = reinterpret_cast<const i32x4_t*>(a.tokens + static_cast<int64_t>(block) * tkv::kBlock);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) tok[k & 1][q] = p[q];
+        for (int q = 0; q < 4; ++q) tok[q] = p[q];
     };
     if (counts) {
         for (int e = e0 + (run - 1) / kBatch * kBatch; e >= e0; e -= kBatch) {  // the first ones last: they stay
@@ -230,7 +231,7 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) keys += len[k];
         }
-        fetch(0);
+        fetch(id[0], len[0]);
     }
     // a query token's logits, its grammar's words, and which of this thread's drafted tokens it sees
     f32x4_t x[kLoads];
@@ -277,30 +278,38 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
     if (counts) {
         int N;
         int number = tkv::group_before<kWaves>(keys, N, part);  // (its barrier is the one after the clearing)
-        const int context = N - t.L;
-        for (int e = e0; e < e1; e += kBatch) {
-            if (e > e0) {
-                look(e);
-                fetch(0);
+        const int context = t.L == 1 && sees ? N : N - t.L;  // (a single token counts or does not)
+        // the tokens of an entry whose bits are set, by what is done with each of them
+        const auto every = [&](const i32x4_t (&x)[4], uint32_t others, auto what) __attribute__((always_inline)) {
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                const uint32_t other = static_cast<uint32_t>(static_cast<int32_t>(others << (31 - q)) >> 31);
+                const uint32_t at = (static_cast<uint32_t>(x[q >> 2][q & 3]) - static_cast<uint32_t>(c0)) | other;
+                if (at < static_cast<uint32_t>(n)) what(at);
             }
+        };
+        for (int e = 0; e < run; e += kBatch) {
+            if (e > 0) {
+                look(e0 + e);
+                fetch(id[0], len[0]);
+            }
+            // (not unrolled: the instructions of one entry are 3 KB, and first reads of them are waited for)
+#pragma unroll 1
+            for (int k = 0; k < kBatch && e + k < run; ++k) {
+                const int m = k == 0 ? len[0] : k == 1 ? len[1] : k == 2 ? len[2] : len[3];
+                const int block = k == 0 ? id[0] : k == 1 ? id[1] : k == 2 ? id[2] : id[3];
+                i32x4_t now[4];
 #pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-                if (k + 1 < kBatch) fetch(k + 1);
-                if (len[k] == 0) continue;
-#pragma unroll
-                for (int q = 0; q < 16; ++q) {
-                    const uint32_t at = static_cast<uint32_t>(tok[k & 1][q >> 2][q & 3]) - static_cast<uint32_t>(c0);
-                    if (q >= len[k] || at >= static_cast<uint32_t>(n)) continue;
-                    const bool past = number + q >= prompt;
-                    if (number + q >= context && (t.L > 1 || !sees)) {
-                        if (t.L > 1) drafted[number + q - context] = static_cast<int32_t>(at) | (past ? kPast : 0);
-                    } else if (past) {
-                        count.more(at);
-                    } else {
-                        count.mark(at);
-                    }
+                for (int q = 0; q < 4; ++q) now[q] = tok[q];
+                if (k + 1 < kBatch) fetch(k == 0 ? id[1] : k == 1 ? id[2] : id[3], k == 0 ? len[1] : k == 1 ? len[2] : len[3]);
+                const int sure = min(max(context - number, 0), m), old = min(max(prompt - number, 0), sure);
+                if (old < sure) every(now, ~((1u << sure) - (1u << old)), [&](uint32_t at) { count.more(at); });
+                if (old > 0) every(now, ~((1u << old) - 1), [&](uint32_t at) { count.set(at); });
+                for (int q = sure; t.L > 1 && q < m; ++q) {
+                    const uint32_t at = static_cast<uint32_t>(a.tokens[static_cast<int64_t>(block) * tkv::kBlock + q]) - static_cast<uint32_t>(c0);
+                    if (at < static_cast<uint32_t>(n)) drafted[number + q - context] = static_cast<int32_t>(at) | (number + q >= prompt ? kPast : 0);
                 }
-                number += len[k];
+                number += m;
             }
         }
     }

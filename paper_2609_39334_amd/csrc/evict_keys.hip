@@ -29,7 +29,7 @@ constexpr int kChoose = 1024, kChooseWaves = kChoose / 64;
 constexpr int kCached = 8192;   // entries whose lengths stay in LDS
 constexpr int kBins = 2048;
 constexpr int kListed = 2048;   // most slots of a bin that are listed (30,000 keys: 26 us a call, 28 without the list)
-constexpr int kEarly = 2;       // slots of a thread, in fours, whose weights are asked for first: 8,192 of a row
+constexpr int kEarly = 4;       // slots of a thread, in fours, whose weights are on their way at once: 16,384 of a row
 constexpr int kHeld = 32768;    // slots whose orders stay in LDS, 128 KB; others are read again for every pass
 constexpr int kMove = 256, kMoveWaves = kMove / 64;
 // The old rows are not read again, so they are read past the caches (64 rows of up to 6,144 keys, 1,024 of which stay, 12/2/128
@@ -136,18 +136,25 @@ __global__ __launch_bounds__(kChoose) void choose(Args a) {
     const auto fill = [&](int q, f32x4_t w) {
         const u32x4_t o = orders_of(q, w);
         if (q < in_lds) held[q] = o;
+        const uint32_t first = __builtin_amdgcn_readfirstlane(o[0]) >> 21;
+        const uint32_t apart = (o[0] >> 21 ^ first) | ((o[0] ^ o[1]) | (o[0] ^ o[2]) | (o[0] ^ o[3])) >> 21;
+        if (first != 0 && __builtin_amdgcn_ballot_w64(apart != 0) == 0) {
+            const uint64_t all = __builtin_amdgcn_ballot_w64(true);
+            if (lane == __builtin_ctzll(all)) atomicAdd(hist + first, static_cast<uint32_t>(4 * __builtin_popcountll(all)));
+        } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (o[k] != 0) add(o[k] >> 21);
+            for (int k = 0; k < 4; ++k)
+                if (o[k] != 0) atomicAdd(hist + (o[k] >> 21), 1u);
+        }
     };
+    for (int q = tid; q < quads; q += kEarly * kChoose) {
 #pragma unroll
-    for (int k = 0; k < kEarly; ++k)
-        if (tid + k * kChoose < quads) fill(tid + k * kChoose, early[k]);
-    f32x4_t next = tid + kEarly * kChoose < quads ? weights_of(tid + kEarly * kChoose) : f32x4_t{};
-    for (int q = tid + kEarly * kChoose; q < quads; q += kChoose) {
-        const f32x4_t w = next;
-        if (q + kChoose < quads) next = weights_of(q + kChoose);
-        fill(q, w);
+        for (int k = 0; k < kEarly; ++k) {
+            const int mine = q + k * kChoose, later = mine + kEarly * kChoose;
+            const f32x4_t w = early[k];
+            if (later < quads) early[k] = weights_of(later);
+            if (mine < quads) fill(mine, w);
+        }
     }
     // The order of the last key that stays, 11, 11 and 10 bits at a time, and how many of that order do.  Where the first bin
     // that is not kept whole is small, its slots are listed as they are counted, and the rest goes by the list.
@@ -182,21 +189,21 @@ __global__ __launch_bounds__(kChoose) void choose(Args a) {
         if (low == 10) listed = found[4] <= kListed, n_listed = found[4];
         __syncthreads();
         if (low == 10 && listed) {
-            int sures = 0, all;
-            for (int q = from + lane; q < until; q += 64) {
-                const u32x4_t o = orders(q);
+            const uint32_t least = max(last, 1u), most_of = last | 0x1fffff;
+            int sures = 0;
+            for (int base = from; base < until; base += 64) {
+                const int q = base + lane;
+                const u32x4_t o = q < until ? orders(q) : u32x4_t{0, 0, 0, 0};
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const uint32_t bin = o[k] >> 21, here = last >> 21;
-                    sures += bin > here;
-                    if (o[k] != 0 && bin == here) {
+                    sures += __builtin_popcountll(__builtin_amdgcn_ballot_w64(o[k] > most_of));
+                    if (o[k] - least <= most_of - least) {
                         list[atomicAdd(found + 5, 1)] = 4 * q + k;
                         atomicAdd(hist + (o[k] >> 10 & 0x7ff), 1u);
                     }
                 }
             }
-            tkv::wave_before(sures, all);
-            if (lane == 0) tally[0][wid] = all, tally[1][wid] = 0;
+            if (lane == 0) tally[0][wid] = sures, tally[1][wid] = 0;
         } else if (listed) {
             for (int c = tid; c < n_listed; c += kChoose) {
                 const uint32_t o = order(list[c]);
@@ -222,22 +229,24 @@ __global__ __launch_bounds__(kChoose) void choose(Args a) {
             if (o == last) atomicAdd(&tally[1][(i >> 2) / run], 1);
         }
     } else {
-        int sures = 0, equals = 0, all_sure, all_equal;
-#pragma unroll 2
-        for (int q = from + lane; q < until; q += 64) {
-            const u32x4_t o = orders(q);
+        int sures = 0, equals = 0;
+        for (int base = from; base < until; base += 64) {
+            const int q = base + lane;
+            const u32x4_t o = q < until ? orders(q) : u32x4_t{0, 0, 0, 0};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sures += o[k] > last, equals += o[k] == last;
+            for (int k = 0; k < 4; ++k) {
+                sures += __builtin_popcountll(__builtin_amdgcn_ballot_w64(o[k] > last));
+                equals += __builtin_popcountll(__builtin_amdgcn_ballot_w64(o[k] == last));
+            }
         }
-        tkv::wave_before(sures, all_sure);
-        tkv::wave_before(equals, all_equal);
-        if (lane == 0) tally[0][wid] = all_sure, tally[1][wid] = all_equal;
+        if (lane == 0) tally[0][wid] = sures, tally[1][wid] = equals;
     }
     __syncthreads();
     int sures = 0, equals = 0;
     for (int x = 0; x < wid; ++x) sures += tally[0][x], equals += tally[1][x];
-    const auto below = [](uint64_t m) {
-        return static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(m >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(m), 0)));
+    // x and the lanes of m before this one
+    const auto below = [](uint64_t m, int x) {
+        return static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(m >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(m), x)));
     };
 #pragma unroll 2
     for (int base = from; base < until; base += 64) {
@@ -248,8 +257,20 @@ __global__ __launch_bounds__(kChoose) void choose(Args a) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             s[k] = __builtin_amdgcn_ballot_w64(o[k] > last), e[k] = __builtin_amdgcn_ballot_w64(o[k] == last);
-            at += below(s[k]), rank += below(e[k]);
-            sures += __builtin_popcountll(s[k]), equals += __builtin_popcountll(e[k]);
+            at = below(s[k], at);
+            sures += __builtin_popcountll(s[k]);
+        }
+        if ((e[0] | e[1] | e[2] | e[3]) == 0) {
+            at += min(rank, left);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (o[k] > last) kept[at++] = 4 * q + k;
+            continue;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            rank = below(e[k], rank);
+            equals += __builtin_popcountll(e[k]);
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {

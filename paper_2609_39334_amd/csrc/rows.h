@@ -43,16 +43,17 @@ __device__ __forceinline__ int entry_len(const int32_t* blocks, const int32_t* b
     return len >= 1 && len <= kBlock ? len : 0;
 }
 
-// Sum over the lanes before this one; total: over all.
+// Sum over the lanes before this one; total: over all.  All lanes are active.  By data-parallel moves: sums within the rows of
+// 16 lanes, then row 0's to row 1 and row 2's to row 3, then the first half's to the second.
 __device__ __forceinline__ int wave_before(int v, int& total) {
-    const int lane = threadIdx.x & 63;
     int incl = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int u = __shfl_up(incl, o);
-        if (lane >= o) incl += u;
-    }
-    total = __shfl(incl, 63);
+    incl += __builtin_amdgcn_update_dpp(0, incl, 0x111, 0xf, 0xf, true);   // row_shr:1
+    incl += __builtin_amdgcn_update_dpp(0, incl, 0x112, 0xf, 0xf, true);   // row_shr:2
+    incl += __builtin_amdgcn_update_dpp(0, incl, 0x114, 0xf, 0xf, true);   // row_shr:4
+    incl += __builtin_amdgcn_update_dpp(0, incl, 0x118, 0xf, 0xf, true);   // row_shr:8
+    incl += __builtin_amdgcn_update_dpp(0, incl, 0x142, 0xa, 0xf, false);  // row_bcast:15
+    incl += __builtin_amdgcn_update_dpp(0, incl, 0x143, 0xc, 0xf, false);  // row_bcast:31
+    total = __builtin_amdgcn_readlane(incl, 63);
     return incl - v;
 }
 
