@@ -193,6 +193,7 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
     if (BIAS) bias = tkv::row_table(a.u.bias_indptr, r, a.u.n_bias, a.u.n_bias);
     const int first = a.search ? g - t.q0 : g / a.b.n_rows * a.per;
     if (!t.ok || first >= t.L) return;
+    const int32_t early = BIAS && tid < bias.n ? a.u.bias_token[bias.first + tid] : -1;
     const int end = a.search ? first + 1 : min(t.L, first + a.per);
     const int c0 = tile * kTile, n = min(kTile, a.vocab - c0);
     const char* in = static_cast<const char*>(a.in) + (static_cast<int64_t>(t.q0 + first) * a.in_stride + c0) * (IN16 ? 2 : 4);
@@ -248,6 +249,7 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
             for (int k = 0; k < kLoads; ++k) x[k] = load4<IN16, false>(in, (k * kThreads + tid) * 4, n);
         }
         const int64_t q = t.q0 + i;
+        // (asked for behind the logits, which it then waits for: ahead of them, 1,000 rows take 247 us for 230)
         const int grammar = a.u.grammar ? a.u.grammar[q] : -1;
         fine = ok && grammar < a.u.n_grammars;
         masked = fine && grammar >= 0;
@@ -285,7 +287,7 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
             for (int q = 0; q < 16; ++q) {
                 const uint32_t other = static_cast<uint32_t>(static_cast<int32_t>(others << (31 - q)) >> 31);
                 const uint32_t at = (static_cast<uint32_t>(x[q >> 2][q & 3]) - static_cast<uint32_t>(c0)) | other;
-                if (at < static_cast<uint32_t>(n)) what(at);
+                if (at < static_cast<uint32_t>(n)) what(at, q);
             }
         };
         for (int e = 0; e < run; e += kBatch) {
@@ -297,25 +299,24 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
 #pragma unroll 1
             for (int k = 0; k < kBatch && e + k < run; ++k) {
                 const int m = k == 0 ? len[0] : k == 1 ? len[1] : k == 2 ? len[2] : len[3];
-                const int block = k == 0 ? id[0] : k == 1 ? id[1] : k == 2 ? id[2] : id[3];
                 i32x4_t now[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) now[q] = tok[q];
                 if (k + 1 < kBatch) fetch(k == 0 ? id[1] : k == 1 ? id[2] : id[3], k == 0 ? len[1] : k == 1 ? len[2] : len[3]);
                 const int sure = min(max(context - number, 0), m), old = min(max(prompt - number, 0), sure);
-                if (old < sure) every(now, ~((1u << sure) - (1u << old)), [&](uint32_t at) { count.more(at); });
-                if (old > 0) every(now, ~((1u << old) - 1), [&](uint32_t at) { count.set(at); });
-                for (int q = sure; t.L > 1 && q < m; ++q) {
-                    const uint32_t at = static_cast<uint32_t>(a.tokens[static_cast<int64_t>(block) * tkv::kBlock + q]) - static_cast<uint32_t>(c0);
-                    if (at < static_cast<uint32_t>(n)) drafted[number + q - context] = static_cast<int32_t>(at) | (number + q >= prompt ? kPast : 0);
-                }
+                if (old < sure) every(now, ~((1u << sure) - (1u << old)), [&](uint32_t at, int) { count.more(at); });
+                if (old > 0) every(now, ~((1u << old) - 1), [&](uint32_t at, int) { count.set(at); });
+                if (sure < m && t.L > 1)
+                    every(now, ~((1u << m) - (1u << sure)), [&](uint32_t at, int q) {
+                        drafted[number + q - context] = static_cast<int32_t>(at) | (number + q >= prompt ? kPast : 0);
+                    });
                 number += m;
             }
         }
     }
     if (biased) {
         for (int e = tid; e < bias.n; e += kThreads) {
-            const uint32_t at = static_cast<uint32_t>(a.u.bias_token[bias.first + e]) - static_cast<uint32_t>(c0);
+            const uint32_t at = static_cast<uint32_t>(e == tid ? early : a.u.bias_token[bias.first + e]) - static_cast<uint32_t>(c0);
             if (at < static_cast<uint32_t>(n)) given.raise(at, static_cast<uint32_t>(e) + 1);
         }
     }
