@@ -24,6 +24,7 @@
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "internal.h"
 #include "rows.h"
@@ -41,6 +42,7 @@ constexpr int kThreads = 256, kWaves = 4;
 // captured call may have: 36 us, 178 without the limit.)
 constexpr int kFewChunk = 64, kFewGroups = 768;
 constexpr int kManyChunk = 16;    // entries a workgroup of weigh_many
+constexpr int kAhead = 8;         // tiles whose masks are looked up together
 constexpr int kWords = 9;         // words of 32 bits that 256 consecutive bits can touch
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -160,6 +162,9 @@ __device__ __forceinline__ float offset_of(float z, float c) {
     return fabsf(z) < INFINITY && c > 0.f ? x : INFINITY;
 }
 
+// All bits as bit i of x.
+__device__ __forceinline__ uint32_t every_bit(uint32_t x, int i) { return static_cast<uint32_t>(static_cast<int32_t>(x << (31 - i)) >> 31); }
+
 template <int D>
 __global__ __launch_bounds__(kThreads, 3) void weigh_few(Args a) {
     constexpr int KS = D / 16;
@@ -256,7 +261,8 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
     constexpr int KS = D / 16, CPR = D / 8, kPieces = 32 * CPR / kThreads;  // 16-byte pieces a row, pieces of a tile a thread
     __shared__ __attribute__((aligned(16))) uint16_t qs[2][32 * D];
     __shared__ __attribute__((aligned(16))) float offs[4][32];
-    __shared__ uint32_t bits[2][32][kWords];  // the rows' masks from the chunk's first drafted key on
+    extern __shared__ uint32_t bits[];  // the tokens' masks from the chunk's first drafted key on, kWords each
+    __shared__ uint32_t seen[kWaves][kAhead][64];  // tile t's at t % kAhead: which of its rows see each of a wave's keys
     __shared__ int2 list[kManyChunk];
     __shared__ int part[kWaves];
     const Unit u = unit_of(a);
@@ -269,7 +275,6 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
     // are on their way (tile t in set t % 2), and what follows from their loads is left until these are back
     u32x4_t qx[2][kPieces];
     float zx[2], cx[2];  // of row `col`
-    uint32_t bx[2][2];
     const uint16_t* q0 = a.q + (static_cast<int64_t>(u.t.q0) * a.hq + u.g * a.G) * D + tid % CPR * 8;
     const float* lse = a.lse + static_cast<int64_t>(u.t.q0) * a.hq + u.g * a.G;
     const float* coef = a.coef ? a.coef + u.t.q0 : lse;  // (lse where there are none: its values are masked out)
@@ -323,38 +328,13 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
         place[h] = 16 * e + slot;
         had[h] = there[h] && j[h] < 0 && a.before ? a.before[at + place[h]] : 0.f;
     }
-    // the chunk's first drafted key, the wave's first and last one, and whether the wave has others: lane l looks at entry l
-    int lowest = 0, low = 0, high = -1;
-    bool context, some;
+    // the chunk's first drafted key, -1: it has none; lane l looks at entry l
+    int first_drafted;
     {
         const int d = list[lane & 15].y, first = d >> 5, len = d & 31;
         const uint32_t has = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(len > 0 && first + len > 0)) & 0xffff;
-        const uint32_t mine = has >> (4 * wid) & 15;
-        context = (static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(len > 0 && first < 0)) >> (4 * wid) & 15) != 0;
-        some = has != 0;
-        if (some) lowest = max(__builtin_amdgcn_readlane(first, __builtin_ctz(has)), 0);
-        if (mine != 0) {
-            low = max(__builtin_amdgcn_readlane(first, 4 * wid + __builtin_ctz(mine)), 0);
-            high = __builtin_amdgcn_readlane(first + len, 4 * wid + 31 - __builtin_clz(mine)) - 1;
-        }
+        first_drafted = has != 0 ? max(__builtin_amdgcn_readlane(first, __builtin_ctz(has)), 0) : -1;
     }
-    const bool drafted = high >= 0;
-    const int w0 = lowest >> 5;
-    // where a lane's bits are; context is seen by all
-    int word[2];
-    uint32_t always[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) word[h] = there[h] && j[h] >= 0 ? (j[h] >> 5) - w0 : 0, always[h] = there[h] && j[h] < 0 ? ~0u : 0u;
-    const auto fetch_bits = [&](int tile, int set) __attribute__((always_inline)) {
-        bx[set][0] = 0, bx[set][1] = 0;
-        const uint32_t* masks = reinterpret_cast<const uint32_t*>(a.b.mask);
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const int x = y * kThreads + tid, qr = 32 * tile + x / kWords, w = w0 + x % kWords;
-            if (x < 32 * kWords && w < 2 * a.b.mask_words && qr < rows)
-                bx[set][y] = masks[static_cast<int64_t>(u.t.q0 + token_of(a, qr)) * (2 * a.b.mask_words) + w];
-        }
-    };
     const auto put = [&](int tile, int set) __attribute__((always_inline)) {
         const float c = __uint_as_float((__float_as_uint(cx[set]) & given) | (__float_as_uint(1.f) & ~given));
         float off = offset_of(zx[set], c);
@@ -370,10 +350,6 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
             *reinterpret_cast<u32x4_t*>(qs[set] + row * D + ((x % CPR) ^ swz) * 8) = qx[set][y] & keep;
         }
     };
-    const auto put_bits = [&](int set) __attribute__((always_inline)) {
-        bits[set][tid / kWords][tid % kWords] = bx[set][0];
-        if (tid + kThreads < 32 * kWords) bits[set][(tid + kThreads) / kWords][(tid + kThreads) % kWords] = bx[set][1];
-    };
     const int swz = D == 128 ? col & 15 : (col >> 1) & 7;
     float sum[2] = {0.f, 0.f};
     // x[4 v + e] of a product is query row 8 v + 4 hi + e of the tile
@@ -387,7 +363,7 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
             for (int h = 0; h < 2; ++h) x[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[h][s], x[h], 0, 0, 0);
         }
     };
-    const auto add = [&](int tile, const f32x16_t (&x)[2]) __attribute__((always_inline)) {
+    const auto add = [&](int tile, const f32x16_t (&x)[2], const uint32_t (&sees)[2], auto masked) __attribute__((always_inline)) {
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const f32x4_t o = *reinterpret_cast<const f32x4_t*>(offs[tile & 3] + 8 * v + 4 * hi);
@@ -395,27 +371,58 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
             for (int h = 0; h < 2; ++h) {
                 float p[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(x[h][4 * v + e], a.sl2, -o[e]));
+                for (int e = 0; e < 4; ++e) {
+                    p[e] = __builtin_amdgcn_exp2f(fmaf(x[h][4 * v + e], a.sl2, -o[e]));
+                    if (masked) p[e] = __uint_as_float(__float_as_uint(p[e]) & every_bit(sees[h], 8 * v + e));
+                }
                 sum[h] += (p[0] + p[1]) + (p[2] + p[3]);
             }
         }
     };
-    if (!some) {
-        // a tile's products beside the exponentials of the one before
+    // this lane's word of `seen` for tiles t to t + kAhead - 1, of key 64 wid + lane of the chunk
+    int word = 0, bit = 0;
+    uint32_t context = 0;
+    const auto look_seen = [&](int t) {
+        for (int tile = t; tile < min(t + kAhead, n_tiles); ++tile) {
+            const int from = token_of(a, 32 * tile), to = token_of(a, min(32 * tile + 31, rows - 1));
+            uint32_t s = context;
+            for (int i = from; i <= to; i += 4) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int lo = max((i + k) * a.G - 32 * tile, 0), end = min((i + k + 1) * a.G - 32 * tile, 32);  // its rows
+                    const uint32_t mine = i + k <= to ? (~0u >> (32 - end)) & (~0u << lo) : 0;
+                    s |= every_bit(bits[min(i + k, to) * kWords + word], bit) & mine;
+                }
+            }
+            seen[wid][tile % kAhead][lane] = s;
+        }
+    };
+    // a tile's products beside the exponentials of the one before
+    const auto walk = [&](auto masked) __attribute__((always_inline)) {
         f32x16_t x[2][2];
+        uint32_t sees[2][2];
+        const auto begin = [&](int t, int set) __attribute__((always_inline)) {
+            if (masked) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) sees[set][h] = seen[wid][t % kAhead][32 * h + col] >> (4 * hi);
+            }
+            multiply(t, x[set]);
+        };
         const auto step = [&](int t, int set) __attribute__((always_inline)) {  // set: t % 2
             fetch_q(t + 2, set);  // (tiles past the last read its last row again, and give nothing)
+            if (masked && t % kAhead == 0) look_seen(t);
             __syncthreads();
             __builtin_amdgcn_sched_barrier(0);
-            multiply(t, x[set]);
-            add(t - 1, x[set ^ 1]);
+            begin(t, set);
+            add(t - 1, x[set ^ 1], sees[set ^ 1], masked);
             put(t + 1, set ^ 1);
         };
         put(0, 0);
         fetch_q(1, 1);
         fetch_q(2, 0);
         __syncthreads();
-        multiply(0, x[0]);
+        if (masked) look_seen(0);
+        begin(0, 0);
         put(1, 1);
         int t = 1;
         for (; t + 1 < n_tiles; t += 2) {
@@ -424,54 +431,25 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
         }
         if (t < n_tiles) {
             step(t, 1);
-            add(t, x[1]);
+            add(t, x[1], sees[1], masked);
         } else {
-            add(t - 1, x[0]);
+            add(t - 1, x[0], sees[0], masked);
         }
+    };
+    if (first_drafted < 0) {
+        walk(std::false_type{});
     } else {
-        const auto step = [&](int t, int set) __attribute__((always_inline)) {
-            if (t + 2 < n_tiles) fetch_q(t + 2, set), fetch_bits(t + 2, set);
-            __syncthreads();
-            // whether the tile's rows (padding aside) see all of the wave's drafted keys, or none
-            bool every = true, any = !drafted;
-            for (int w = low >> 5; drafted && w <= high >> 5; ++w) {
-                const uint32_t from = w == low >> 5 ? ~0u << (low & 31) : ~0u, to = w == high >> 5 ? ~0u >> (31 - (high & 31)) : ~0u;
-                const uint32_t seen = bits[set][col][w - w0] & from & to;
-                every = every && seen == (from & to), any = any || seen != 0;
-            }
-            const bool all = __builtin_amdgcn_ballot_w64(!every && 32 * t + col < rows) == 0;
-            const bool none = !context && drafted && __builtin_amdgcn_ballot_w64(any && 32 * t + col < rows) == 0;
-            if (!none) {
-                f32x16_t x[2];
-                multiply(t, x);
-                if (all) {
-                    add(t, x);
-                } else {
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        const f32x4_t o = *reinterpret_cast<const f32x4_t*>(offs[t & 3] + 8 * v + 4 * hi);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t* m = bits[set][8 * v + 4 * hi + e];
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const uint32_t sees = (m[word[h]] | always[h]) >> (j[h] & 31) & 1;
-                                const float p = __builtin_amdgcn_exp2f(fmaf(x[h][4 * v + e], a.sl2, -o[e]));
-                                sum[h] += sees != 0 ? p : 0.f;
-                            }
-                        }
-                    }
-                }
-            }
-            if (t + 1 < n_tiles) put(t + 1, set ^ 1), put_bits(set ^ 1);
-        };
-        fetch_bits(0, 0);
-        put(0, 0), put_bits(0);
-        if (n_tiles > 1) fetch_q(1, 1), fetch_bits(1, 1);
-        for (int t = 0; t < n_tiles; t += 2) {
-            step(t, 0);
-            if (t + 1 < n_tiles) step(t + 1, 1);
+        const int w0 = first_drafted >> 5;
+        const int64_t words = 2 * static_cast<int64_t>(a.b.mask_words);
+        const uint32_t* masks = reinterpret_cast<const uint32_t*>(a.b.mask) + u.t.q0 * words;
+        for (int m = tid; m < u.t.L * kWords; m += kThreads) {
+            const int w = w0 + m % kWords;
+            bits[m] = w < words ? masks[m / kWords * words + w] : 0;
         }
+        const int d = list[4 * wid + (lane >> 4)].y, mine = (d >> 5) + (lane & 15);
+        context = mine < 0 ? ~0u : 0;
+        if (mine >= 0 && (lane & 15) < (d & 31)) word = (mine >> 5) - w0, bit = mine & 31;
+        walk(std::true_type{});
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -509,7 +487,8 @@ int tkv::launch_key_weights(const tkv_shape& s, const tkv_draft_batch& b, const 
     const int64_t grid = a.search ? counted : direct;
     if (grid > static_cast<int64_t>(UINT32_MAX) / kThreads)
         return set_error(TKV_EINVAL, "tkv_key_weights: %lld workgroups are too many", static_cast<long long>(grid));
-    const auto run = [&](auto kernel) { kernel<<<dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, st>>>(a); };
+    const size_t lds = few ? 0 : static_cast<size_t>(b.max_q) * kWords * 4;  // of 62 KB with the rest, at most
+    const auto run = [&](auto kernel) { kernel<<<dim3(static_cast<unsigned>(grid)), dim3(kThreads), lds, st>>>(a); };
     if (s.d == 128)
         few ? run(weigh_few<128>) : run(weigh_many<128>);
     else
