@@ -14,13 +14,15 @@
 // through LDS, double-buffered, shared by the four waves.  Up to 32 queries the first is faster: 64 single tokens under 300 to
 // 6,144 keys (12/2/128 heads) 24 us, 36 by the second; 1,000 tokens under 30 to 300 keys 29 and 45; 28/4 heads 27 and 36.
 //
-// Measured (times of the kernel alone): those 64 tokens 21 us, 102 MB, 4.9 TB/s.  32 tokens under one path of 30,000 keys, 28/4/128:
-// 17 us; 472 workgroups are less than two a CU, so it is a workgroup's own time: about 7 us until its first product (table,
-// lengths, keys and first queries, a chain) and seven tiles of 0.8 to 1 us.  8 rows of 64 to 256 tokens
-// under 2,000 to 12,000 keys, 32/8/128 (67.8 GFLOP): 111 us, 610 TFLOP/s; MFMAs are busy 31% of it and the vector units 53%
-// (a product of 32 x 64 scores is 256 cycles of MFMA beside 16 x 64 exponentials, 512 cycles of a quarter-rate unit); the products
-// alone take 103 us.  Tried there: eight waves of 32 keys (123 us, 119 then), two groups of keys one after the other in a
-// workgroup (141), three waves a SIMD (127 to 133, registers spill), chunks slowest in the grid (130 to 141).
+// Measured (times of calls one after the other): those 64 tokens 23 us, 102 MB, 4.5 TB/s.  32 tokens under one path of 30,000 keys,
+// 28/4/128: 17 us; 472 workgroups are less than two a CU, so it is a workgroup's own time: about 6 us until its first product
+// (table, lengths, keys and first queries, a chain) and seven tiles of 1 us, 1.5 where there are masks.  8 rows of 64 to 256
+// tokens under 2,000 to 12,000 keys, 32/8/128 (67.8 GFLOP): 100 us, 675 TFLOP/s; MFMAs were busy 31% and the vector units 53% of 110 (a product of
+// 32 x 64 scores is 512 cycles of a SIMD's MFMAs, its exponentials 512 of a quarter-rate unit and about as many of others).
+// Tried there, against 119 to 123 at the time: eight waves of 32 keys (123), two groups of keys one after the other in a
+// workgroup (141), three waves a SIMD (127 to 133, registers spill in the steps), chunks slowest in the grid (130 to 141), products
+// alone (103).  Masks tested score by score in a step of its own took 1.8 us a tile and these two calls 19.4 and 111 us; a lane's key
+// has one word a tile instead, a bit a row, looked up for eight tiles at once and laid over the exponentials.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cstdint>
@@ -43,6 +45,7 @@ constexpr int kThreads = 256, kWaves = 4;
 constexpr int kFewChunk = 64, kFewGroups = 768;
 constexpr int kManyChunk = 16;    // entries a workgroup of weigh_many
 constexpr int kAhead = 8;         // tiles whose masks are looked up together
+constexpr int kTokens = 8;        // of which masks are looked up together
 constexpr int kWords = 9;         // words of 32 bits that 256 consecutive bits can touch
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -163,7 +166,9 @@ __device__ __forceinline__ float offset_of(float z, float c) {
 }
 
 // All bits as bit i of x.
-__device__ __forceinline__ uint32_t every_bit(uint32_t x, int i) { return static_cast<uint32_t>(static_cast<int32_t>(x << (31 - i)) >> 31); }
+__device__ __forceinline__ uint32_t every_bit(uint32_t x, int i) {
+    return static_cast<uint32_t>(__builtin_amdgcn_sbfe(static_cast<int>(x), i, 1));
+}
 
 template <int D>
 __global__ __launch_bounds__(kThreads, 3) void weigh_few(Args a) {
@@ -256,8 +261,10 @@ __global__ __launch_bounds__(kThreads, 3) void weigh_few(Args a) {
     }
 }
 
+// (Three waves a SIMD for heads of 64: 32 rows of 40 to 100 tokens, eight heads of their own, 22 us, 25 with two; ten values are
+// spilled ahead of the steps under masks and come back behind them.)
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void weigh_many(Args a) {
     constexpr int KS = D / 16, CPR = D / 8, kPieces = 32 * CPR / kThreads;  // 16-byte pieces a row, pieces of a tile a thread
     __shared__ __attribute__((aligned(16))) uint16_t qs[2][32 * D];
     __shared__ __attribute__((aligned(16))) float offs[4][32];
@@ -316,18 +323,11 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
     }
     list_blocks(a, u, kManyChunk, look, list, part);
 
-    const int64_t at = (static_cast<int64_t>(u.r) * a.hkv + u.g) * a.keys + 16 * static_cast<int64_t>(u.e0);
-    int j[2], place[2];
-    bool there[2];
-    float had[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int e = 4 * wid + 2 * h + (col >> 4), slot = col & 15, d = list[e].y;
-        there[h] = slot < (d & 31);
-        j[h] = (d >> 5) + slot;
-        place[h] = 16 * e + slot;
-        had[h] = there[h] && j[h] < 0 && a.before ? a.before[at + place[h]] : 0.f;
-    }
+    // what is read and written is key 64 wid + lane of the chunk
+    const int entry = 4 * wid + (lane >> 4), slot = lane & 15;
+    const int64_t at = (static_cast<int64_t>(u.r) * a.hkv + u.g) * a.keys + 16 * static_cast<int64_t>(u.e0 + entry) + slot;
+    const int number = (list[entry].y >> 5) + slot;
+    const float had = slot < (list[entry].y & 31) && number < 0 && a.before ? a.before[at] : 0.f;
     // the chunk's first drafted key, -1: it has none; lane l looks at entry l
     int first_drafted;
     {
@@ -385,13 +385,15 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
     const auto look_seen = [&](int t) {
         for (int tile = t; tile < min(t + kAhead, n_tiles); ++tile) {
             const int from = token_of(a, 32 * tile), to = token_of(a, min(32 * tile + 31, rows - 1));
-            uint32_t s = context;
-            for (int i = from; i <= to; i += 4) {
+            const uint64_t group = ~0ull >> (64 - a.G);  // a token's rows, from its first one at `at` of the tile
+            int at = from * a.G - 32 * tile;
+            uint32_t s = context | (every_bit(bits[from * kWords + word], bit) & static_cast<uint32_t>(group >> -at));
+            const uint32_t* m = bits + (from + 1) * kWords + word;
+            for (int i = from + 1; i <= to; i += kTokens, m += kTokens * kWords) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int lo = max((i + k) * a.G - 32 * tile, 0), end = min((i + k + 1) * a.G - 32 * tile, 32);  // its rows
-                    const uint32_t mine = i + k <= to ? (~0u >> (32 - end)) & (~0u << lo) : 0;
-                    s |= every_bit(bits[min(i + k, to) * kWords + word], bit) & mine;
+                for (int k = 0; k < kTokens; ++k) {  // (what is behind the last token has no rows here)
+                    at += a.G;
+                    s |= every_bit(m[k * kWords], bit) & static_cast<uint32_t>(group << min(at, 32));
                 }
             }
             seen[wid][tile % kAhead][lane] = s;
@@ -410,7 +412,7 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
         };
         const auto step = [&](int t, int set) __attribute__((always_inline)) {  // set: t % 2
             fetch_q(t + 2, set);  // (tiles past the last read its last row again, and give nothing)
-            if (masked && t % kAhead == 0) look_seen(t);
+            if (masked && set == 0 && t % kAhead == 0) look_seen(t);
             __syncthreads();
             __builtin_amdgcn_sched_barrier(0);
             begin(t, set);
@@ -442,20 +444,23 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many(Args a) {
         const int w0 = first_drafted >> 5;
         const int64_t words = 2 * static_cast<int64_t>(a.b.mask_words);
         const uint32_t* masks = reinterpret_cast<const uint32_t*>(a.b.mask) + u.t.q0 * words;
-        for (int m = tid; m < u.t.L * kWords; m += kThreads) {
-            const int w = w0 + m % kWords;
-            bits[m] = w < words ? masks[m / kWords * words + w] : 0;
+        for (int m0 = tid; m0 < u.t.L * kWords; m0 += 4 * kThreads) {
+            uint32_t x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int m = m0 + k * kThreads, w = w0 + m % kWords;
+                x[k] = m < u.t.L * kWords && w < words ? masks[m / kWords * words + w] : 0;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (m0 + k * kThreads < u.t.L * kWords) bits[m0 + k * kThreads] = x[k];
         }
-        const int d = list[4 * wid + (lane >> 4)].y, mine = (d >> 5) + (lane & 15);
-        context = mine < 0 ? ~0u : 0;
-        if (mine >= 0 && (lane & 15) < (d & 31)) word = (mine >> 5) - w0, bit = mine & 31;
+        context = number < 0 ? ~0u : 0;
+        if (number >= 0 && slot < (list[entry].y & 31)) word = (number >> 5) - w0, bit = number & 31;
         walk(std::true_type{});
     }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const float w = sum[h] + __shfl_xor(sum[h], 32);
-        if (there[h] && hi == 0) a.out[at + place[h]] = fmaf(a.decay, had[h], w);
-    }
+    const float w0 = sum[0] + __shfl_xor(sum[0], 32), w1 = sum[1] + __shfl_xor(sum[1], 32);
+    if (slot < (list[entry].y & 31)) a.out[at] = fmaf(a.decay, had, hi == 0 ? w0 : w1);
 }
 
 }  // namespace
@@ -487,7 +492,7 @@ int tkv::launch_key_weights(const tkv_shape& s, const tkv_draft_batch& b, const 
     const int64_t grid = a.search ? counted : direct;
     if (grid > static_cast<int64_t>(UINT32_MAX) / kThreads)
         return set_error(TKV_EINVAL, "tkv_key_weights: %lld workgroups are too many", static_cast<long long>(grid));
-    const size_t lds = few ? 0 : static_cast<size_t>(b.max_q) * kWords * 4;  // of 62 KB with the rest, at most
+    const size_t lds = few ? 0 : static_cast<size_t>(b.max_q + kTokens) * kWords * 4;  // (62 KB with the rest, at most)
     const auto run = [&](auto kernel) { kernel<<<dim3(static_cast<unsigned>(grid)), dim3(kThreads), lds, st>>>(a); };
     if (s.d == 128)
         few ? run(weigh_few<128>) : run(weigh_many<128>);

@@ -101,6 +101,14 @@ def test_ragged_rows_and_any_mask(hq, hkv, d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d", [(64, 1, 64), (33, 1, 128), (62, 2, 64), (5, 5, 128), (9, 3, 64), (40, 8, 128)])
+def test_any_masks_of_groups_of_any_size(hq, hkv, d):
+    # tiles of 32 query rows that begin and end inside a token's group, masks looked up for several tiles at once
+    c = Case([(5, 60), (300, 40), (0, 257), (77, 33), (1000, 130)], hq, hkv, d, seed=hq, bits=True, extra_words=2)
+    c.check(c.run())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows", [[(30000, 1)], [(20000, 40)], [(9000, 9), (10, 1), (0, 2), (17000, 3)], [(4000, 300)],
                                   [(70, 1024)], [(1, 1)] * 3])
 def test_long_and_short_paths(rows):
