@@ -6,15 +6,16 @@
 // before the next one), and passes once over the tile's logits.  Counts are whole numbers, so the order in which threads add
 // them changes nothing.
 //
-// Logits are read and written once and that bounds large calls: 1,000 rows of 151,936 in fp32 take 231 us, 5.3 TB/s, a large
-// copy's rate.  Every tile walks its row's path (4 bytes a token, from L2 after the first), which bounds few rows: five of 151,936,
-// bf16, paths of 200 to 1,000 tokens 9 us; 16 rows with paths of 8,000 to 30,000 tokens 18 us, about four entries of a table a
-// thread; 16 trees of 4 to 32 tokens, 32,003, bf16 to fp32, 20 us: the row, its table, lengths, tokens
-// and counts are a chain, before which the logits are asked for.
+// Logits are read and written once and that bounds large calls: 1,000 rows of 151,936 in fp32 take 228 us, 5.35 TB/s, a large
+// copy's rate.  Every tile walks its row's path (4 bytes a token, from L2 after the first), which bounds few rows: five of
+// 151,936, bf16, paths of 200 to 1,000 tokens 9 us; 16 rows with paths of 8,000 to 30,000 tokens 16 us, about four entries of a
+// table a thread, eleven instructions a token (by 25, 18); 16 trees of 4 to 32 tokens, 32,003, bf16 to fp32, 19 us: the row, its
+// table, lengths, tokens and counts are a chain, before which the logits are asked for.
 //
-// Measured for the choices below (threads / tile, before logits went past the caches): 256 / 8,192 with many tiles, the 1,000 rows 239 to 249 us; 512 / 8,192 250;
-// 256 / 4,096 261; 512 / 16,384 246; 1,024 / 8,192 446; 1,024 / 16,384 310.  512 / 8,192 with few: the five rows 8.7 us, by 256 11.0; the
-// paths of 30,000 tokens 18 and 26.  (256 rows with paths of 8,000 to 16,000 tokens: 143 by 512, 120 by 256.)
+// Measured for the choices below (threads / tile, before logits went past the caches): 256 / 8,192 with many tiles, the 1,000 rows
+// 239 to 249 us; 512 / 8,192 250; 256 / 4,096 261; 512 / 16,384 246; 1,024 / 8,192 446; 1,024 / 16,384 310.  512 / 8,192 with few:
+// the five rows 8.7 us, by 256 11.0; the paths of 30,000 tokens 18 and 26.  (256 rows with paths of 8,000 to 16,000 tokens: 143 by
+// 512, 120 by 256.)
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cstdint>

@@ -6,12 +6,12 @@
 // stay from the lowest index on.  move: a wave a new block copies the kept K and V rows, and the weights.
 //
 // A call has to read the weights once and to read and write what is kept, 8 d bytes a key: large calls are bound by memory in
-// move, small ones by the chain of choose's steps.  One row of 30,000 keys, 2,048 of which stay (28/4/128): choose 21 us on 4 CUs,
-// move 4.3.  64 rows of up to 6,144 keys, 1,024 of which
-// stay (12/2/128): 11.6 and 24 us.  32 rows of 2,000 to 12,000 keys, 2,000 of which stay (32/8/128, 535 MB): 16 and 107 us,
-// 4.9 TB/s in move, a large copy's rate being 5.2.  One kernel for both leaves too few workgroups for the copies: 48 us for
-// the first, 48 against 43 for the second, 128 against 131 for the third (before reads went past the caches).  The orders of
-// 32 slots a thread in registers, unrolled, took 27 us for 1,000 keys (instruction fetches) against 8.5.
+// move, small ones by the chain of choose's steps.  One row of 30,000 keys, 2,048 of which stay (28/4/128): choose 19 us on 4 CUs
+// (6 to cut, 4 for the orders and the first counts, which a CU's own rate bounds), move 4.3.  64 rows of up to 6,144 keys, 1,024
+// of which stay (12/2/128): 10.6 and 24 us.  32 rows of 2,000 to 12,000 keys, 2,000 of which stay (32/8/128, 535 MB): 14 and 107
+// us, 4.9 TB/s in move, a large copy's rate being 5.2.  One kernel for both leaves too few workgroups for the copies: 48 us for
+// the first, 48 against 43 for the second, 128 against 131 for the third (before reads went past the caches).  The orders of 32
+// slots a thread in registers, unrolled, took 27 us for 1,000 keys (instruction fetches) against 8.5.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cstdint>
@@ -29,7 +29,7 @@ constexpr int kChoose = 1024, kChooseWaves = kChoose / 64;
 constexpr int kCached = 8192;   // entries whose lengths stay in LDS
 constexpr int kBins = 2048;
 constexpr int kListed = 2048;   // most slots of a bin that are listed (30,000 keys: 26 us a call, 28 without the list)
-constexpr int kEarly = 4;       // slots of a thread, in fours, whose weights are on their way at once: 16,384 of a row
+constexpr int kEarly = 4;       // slots of a thread, in fours, whose weights are on their way at once: 16,384 of a row (32,768: 0.4 us slower)
 constexpr int kHeld = 32768;    // slots whose orders stay in LDS, 128 KB; others are read again for every pass
 constexpr int kMove = 256, kMoveWaves = kMove / 64;
 // The old rows are not read again, so they are read past the caches (64 rows of up to 6,144 keys, 1,024 of which stay, 12/2/128

@@ -6,23 +6,23 @@
 // operand.  The coefficient goes into the exponent (lse - log c, infinite where nothing counts).  A key of a row and head
 // belongs to one wave, whose order of additions is fixed: no atomics.
 //
-// A call has to read each key once (2 d bytes a KV head) and two floats a key are read and written; it multiplies 2 d hq
-// times and takes hq exponentials a key and token.  Few tokens are bound by memory, many by their exponentials and products.
+// A call has to read each key once (2 d bytes a KV head) and two floats a key are read and written; it multiplies 2 d hq times and
+// takes hq exponentials a key and token.  Few tokens are bound by memory, many by their exponentials and products.
 //
 // Two kernels.  weigh_few: rows of up to 32 queries a KV head (single tokens, small drafts) hold the queries in registers and
 // stream K, the next 32 keys on their way.  weigh_many: 64 keys a wave stay in registers, and the queries pass in tiles of 32
 // through LDS, double-buffered, shared by the four waves.  Up to 32 queries the first is faster: 64 single tokens under 300 to
 // 6,144 keys (12/2/128 heads) 24 us, 36 by the second; 1,000 tokens under 30 to 300 keys 29 and 45; 28/4 heads 27 and 36.
 //
-// Measured (times of calls one after the other): those 64 tokens 23 us, 102 MB, 4.5 TB/s.  32 tokens under one path of 30,000 keys,
-// 28/4/128: 17 us; 472 workgroups are less than two a CU, so it is a workgroup's own time: about 6 us until its first product
-// (table, lengths, keys and first queries, a chain) and seven tiles of 1 us, 1.5 where there are masks.  8 rows of 64 to 256
-// tokens under 2,000 to 12,000 keys, 32/8/128 (67.8 GFLOP): 100 us, 675 TFLOP/s; MFMAs were busy 31% and the vector units 53% of 110 (a product of
-// 32 x 64 scores is 512 cycles of a SIMD's MFMAs, its exponentials 512 of a quarter-rate unit and about as many of others).
-// Tried there, against 119 to 123 at the time: eight waves of 32 keys (123), two groups of keys one after the other in a
-// workgroup (141), three waves a SIMD (127 to 133, registers spill in the steps), chunks slowest in the grid (130 to 141), products
-// alone (103).  Masks tested score by score in a step of its own took 1.8 us a tile and these two calls 19.4 and 111 us; a lane's key
-// has one word a tile instead, a bit a row, looked up for eight tiles at once and laid over the exponentials.
+// Measured (times of calls one after the other): those 64 tokens 23 us, 102 MB, 4.5 TB/s.  32 tokens under one path of 30,000
+// keys, 28/4/128: 17 us; 472 workgroups are less than two a CU, so it is a workgroup's own time: about 6 us until its first
+// product (table, lengths, keys and first queries, a chain) and seven tiles of 1 us, 1.5 where there are masks.  8 rows of 64 to
+// 256 tokens under 2,000 to 12,000 keys, 32/8/128 (67.8 GFLOP): 100 us, 675 TFLOP/s; MFMAs were busy 31% and the vector units 53%
+// of 110 (a product of 32 x 64 scores is 512 cycles of a SIMD's MFMAs, its exponentials 512 of a quarter-rate unit and about as
+// many of others). Tried there, against 119 to 123 at the time: eight waves of 32 keys (123), two groups of keys one after the
+// other in a workgroup (141), three waves a SIMD (127 to 133, registers spill in the steps), chunks slowest in the grid (130 to
+// 141), products alone (103).  Masks tested score by score in a step of its own took 1.8 us a tile and these two calls 19.4 and
+// 111 us; a lane's key has one word a tile instead, a bit a row, looked up for eight tiles at once and laid over the exponentials.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cstdint>
