@@ -406,6 +406,10 @@ int tkv::launch_adjust_logits(const AdjustCall& f, void* stream) {
     const int64_t tiles = static_cast<int64_t>(a.n_tiles) * f.b.n_qtok;
     a.per = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, f.b.max_q), tiles / 4096)));
     a.groups = (f.b.max_q + a.per - 1) / a.per;
+    // Groups go by max_q: where it is far above the rows' tokens (a captured call's, say) most have no work, and a group a token is
+    // faster.  (Those 64 trees under a max_q of 256, 1.3 groups a token: 334 us, 382 by tokens; 1,024, 5.2: 488 and 374.  300 rows of
+    // up to 8 tokens under 64, 2.4: 316 and 345; 64 rows of up to 12 under 1,024, 62: 825 and 137.)
+    if (static_cast<int64_t>(a.groups) * f.b.n_rows > 4 * static_cast<int64_t>(f.b.n_qtok)) a.per = 1;
     a.search = f.b.max_q > 1 && a.per == 1;
     int64_t all = a.search ? f.b.n_qtok : static_cast<int64_t>(a.groups) * f.b.n_rows;
     const int64_t most = (all + 7) / 8 * 8 * a.n_tiles;

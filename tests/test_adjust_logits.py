@@ -249,6 +249,16 @@ def test_rows_outside_the_arrays():
 
 
 @pytest.mark.gpu
+def test_max_q_above_the_rows_lengths():
+    # two tokens share a workgroup's counts, or none do where max_q leaves most groups without tokens: the same bits
+    c = Case([(50 + 3 * r, 11 - r % 2) for r in range(42)], 151936, seed=2, extra_words=15)
+    want = c.run().clone()
+    c.check(want, rows=[0, 17, 41])
+    for max_q in (64, 400, 1024):
+        assert torch.equal(c.run(max_q=max_q).view(torch.int32), want.view(torch.int32)), max_q
+
+
+@pytest.mark.gpu
 def test_many_rows_and_pools_past_four_gib():
     rng = np.random.default_rng(5)
     c = Case([(int(n), int(L)) for n, L in zip(rng.integers(0, 90, 700), rng.integers(1, 3, 700))], 601, 9)
