@@ -418,11 +418,15 @@ int tkv::launch_adjust_logits(const AdjustCall& f, void* stream) {
     a.units = static_cast<int32_t>(all);
     a.spread = all >= 64;  // (fewer units would leave XCDs without work at the end)
     if (a.spread) all = (all + 7) / 8 * 8;
-    // Numbers of 16 bits while no path and no list of biases can pass them: 32 KB of LDS for the two instead of 64.
-    const bool bias = f.u.n_bias > 0, wide = f.b.max_blocks > 0x7fff / kBlock || f.u.n_bias >= 0xffff;
-    const bool many = all * a.n_tiles >= 768;  // (three a CU)
+    // Numbers of 32 bits where a path or a list of biases can pass 16, and where two workgroups a CU are enough: they take fewer
+    // instructions, but 64 KB of LDS for the two instead of 32.  (Bf16 rows of 151,936 with paths of 200 to 4,000 tokens, in 32 and
+    // 16 bits: 152 workgroups 9.2 and 9.3 us, 494 11.9 and 12.2, 570 16.1 and 14.3; 304 with paths of 8,000 to 30,000 14.6 and 16.0.)
+    // 512 threads up to three workgroups a CU, 256 beyond: 646 13.9 and 14.6 us, 760 14.3 and 15.1, 1,026 19.0 and 18.2.
+    const int64_t workgroups = all * a.n_tiles;
+    const bool bias = f.u.n_bias > 0, wide = workgroups <= 512 || f.b.max_blocks > 0x7fff / kBlock || f.u.n_bias >= 0xffff;
+    const bool many = workgroups >= 768;
     const auto run = [&](auto kernel, int threads) {
-        kernel<<<dim3(static_cast<unsigned>(all * a.n_tiles)), dim3(threads), 0, st>>>(a);
+        kernel<<<dim3(static_cast<unsigned>(workgroups)), dim3(threads), 0, st>>>(a);
     };
     const auto typed = [&](auto has_bias, auto is_wide, auto n_threads) {
         constexpr bool B = decltype(has_bias)::value, W = decltype(is_wide)::value;

@@ -152,6 +152,25 @@ def test_biases_for_every_token(m):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("in16,out16", TYPES)
+@pytest.mark.parametrize("others", [2, 15])
+def test_counts_and_biases_at_the_limit_of_16_bits(others, in16, out16):
+    # enough workgroups for numbers of 16 bits: one token 32,752 times over (with the drafted ones), as many biases as they hold
+    c = Case([(2047 * BS - 32, 32)] + [(40 + r, 2) for r in range(others)], 151936, others, in16, out16, full_blocks=True, bias=0.0)
+    path = c.path(0)[1]
+    c.tokens.reshape(-1)[path] = 42
+    c.rules["prompt_len"][:], c.rules["frequency"][:] = 0, 0.001
+    m = 65534
+    c.rules["bias_indptr"][2:] = m
+    c.rules["bias_token"] = c.rng.integers(0, 9001, m).astype(np.int32)
+    c.rules["bias_value"] = c.rng.normal(size=m).astype(np.float32)
+    assert c.max_blocks == 2047
+    c.check(c.run(), rows=[0, 1, others])
+    off = ("bias_indptr", "bias_token", "bias_value")
+    c.check(c.run(without=off), off, rows=[1, others])
+
+
+@pytest.mark.gpu
 def test_rules_that_are_off():
     names = ["prompt_len", "repetition", "presence", "frequency", "bias", "grammar"]
     for off in [names] + [[x] for x in names] + [names[:4], names[4:], names[1:]]:
