@@ -431,7 +431,8 @@ int tkv_draft_verify(const tkv_shape* shape, const tkv_draft_batch* batch, const
  * What no key of a row's table has a place for is not written (slots past a block's length, entries that are no blocks, rows
  * that are left out: tokens or table outside the arrays, or longer than max_q or max_blocks; where kv_indptr decreases
  * somewhere, so that rows share entries, rows behind it may be).  K of the keys that a token
- * sees must be finite; what the others hold does not matter.  Results do not depend on how the work is cut.  No workspace.
+ * sees must be finite; what the others hold does not matter.  The order of a key's additions follows from the call's sizes
+ * (n_rows, n_kv_blocks, max_q, heads) and its row alone: the same call gives the same bits.  No workspace.
  * EINVAL (shape and batch as for tkv_draft_verify, keys, decay, NULL pointers, q or k not 16-byte aligned), EHIP. */
 int tkv_key_weights(const tkv_shape* shape, const tkv_draft_batch* batch, const void* q, const void* k, const float* lse,
                     const float* coef, float decay, const float* before, float* out, int64_t keys, void* hip_stream);

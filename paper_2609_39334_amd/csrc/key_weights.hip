@@ -9,10 +9,11 @@
 // A call has to read each key once (2 d bytes a KV head) and two floats a key are read and written; it multiplies 2 d hq times and
 // takes hq exponentials a key and token.  Few tokens are bound by memory, many by their exponentials and products.
 //
-// Two kernels.  weigh_few: rows of up to 32 queries a KV head (single tokens, small drafts) hold the queries in registers and
+// Three kernels.  weigh_few: rows of up to 32 queries a KV head (single tokens, small drafts) hold the queries in registers and
 // stream K, the next 32 keys on their way.  weigh_many: 64 keys a wave stay in registers, and the queries pass in tiles of 32
-// through LDS, double-buffered, shared by the four waves.  Up to 32 queries the first is faster: 64 single tokens under 300 to
-// 6,144 keys (12/2/128 heads) 24 us, 36 by the second; 1,000 tokens under 30 to 300 keys 29 and 45; 28/4 heads 27 and 36.
+// through LDS, double-buffered, shared by the four waves.  weigh_split: where there are few keys, the tiles are shared out among
+// the waves.  Up to 32 queries the first is faster: 64 single tokens under 300 to 6,144 keys (12/2/128 heads) 24 us, 36 by the
+// second; 1,000 tokens under 30 to 300 keys 29 and 45; 28/4 heads 27 and 36.
 //
 // Measured (times of calls one after the other): those 64 tokens 23 us, 102 MB, 4.5 TB/s.  32 tokens under one path of 30,000
 // keys, 28/4/128: 17 us; 472 workgroups are less than two a CU, so it is a workgroup's own time: about 6 us until its first
@@ -44,6 +45,9 @@ constexpr int kThreads = 256, kWaves = 4;
 // captured call may have: 36 us, 178 without the limit.)
 constexpr int kFewChunk = 64, kFewGroups = 768;
 constexpr int kManyChunk = 16;    // entries a workgroup of weigh_many
+constexpr int kSplitChunk = 4;    // entries a workgroup of weigh_split
+constexpr int kSplitGroups = 512;
+constexpr int kSplitWords = 3;    // words of 32 bits that 64 consecutive bits can touch
 constexpr int kAhead = 8;         // tiles whose masks are looked up together
 constexpr int kTokens = 8;        // of which masks are looked up together
 constexpr int kWords = 9;         // words of 32 bits that 256 consecutive bits can touch
@@ -168,6 +172,51 @@ __device__ __forceinline__ float offset_of(float z, float c) {
 // All bits as bit i of x.
 __device__ __forceinline__ uint32_t every_bit(uint32_t x, int i) {
     return static_cast<uint32_t>(__builtin_amdgcn_sbfe(static_cast<int>(x), i, 1));
+}
+
+// Which of a tile's rows see a key that its tokens' bit `bit` of bits[token * words + word] stands for.
+__device__ __forceinline__ uint32_t rows_that_see(const Args& a, int tile, int rows, const uint32_t* bits, int words, int word,
+                                                  int bit) {
+    const int from = token_of(a, 32 * tile), to = token_of(a, min(32 * tile + 31, rows - 1));
+    const uint64_t group = ~0ull >> (64 - a.G);  // a token's rows, from its first one at `at` of the tile
+    int at = from * a.G - 32 * tile;
+    const uint32_t* m = bits + from * words + word;
+    uint32_t s = every_bit(*m, bit) & static_cast<uint32_t>(group >> -at);
+    m += words;
+    for (int i = from + 1; i <= to; i += kTokens, m += kTokens * words) {
+#pragma unroll
+        for (int k = 0; k < kTokens; ++k) {  // (what is behind the last token has no rows here)
+            at += a.G;
+            s |= every_bit(m[k * words], bit) & static_cast<uint32_t>(group << min(at, 32));
+        }
+    }
+    return s;
+}
+
+// The first drafted key of a chunk of n entries (at most 64), -1: it has none.  Lane l looks at entry l.
+__device__ __forceinline__ int first_drafted_of(const int2* list, int n) {
+    const int lane = threadIdx.x & 63, d = list[min(lane, n - 1)].y, first = d >> 5, len = d & 31;
+    const uint64_t has = __builtin_amdgcn_ballot_w64(lane < n && len > 0 && first + len > 0);
+    return has != 0 ? max(__builtin_amdgcn_readlane(first, __builtin_ctzll(has)), 0) : -1;
+}
+
+// The tokens' masks from word w0 on, `words` words each, to bits.
+template <int W>
+__device__ __forceinline__ void stage_masks(const Args& a, const Unit& u, int w0, uint32_t* bits) {
+    const int64_t words = 2 * static_cast<int64_t>(a.b.mask_words);
+    const uint32_t* masks = reinterpret_cast<const uint32_t*>(a.b.mask) + u.t.q0 * words;
+    const int n = u.t.L * W;
+    for (int m0 = threadIdx.x; m0 < n; m0 += 4 * kThreads) {
+        uint32_t x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int m = m0 + k * kThreads, w = w0 + m % W;
+            x[k] = m < n && w < words ? masks[m / W * words + w] : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (m0 + k * kThreads < n) bits[m0 + k * kThreads] = x[k];
+    }
 }
 
 template <int D>
@@ -328,13 +377,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void weigh_many(Args a) 
     const int64_t at = (static_cast<int64_t>(u.r) * a.hkv + u.g) * a.keys + 16 * static_cast<int64_t>(u.e0 + entry) + slot;
     const int number = (list[entry].y >> 5) + slot;
     const float had = slot < (list[entry].y & 31) && number < 0 && a.before ? a.before[at] : 0.f;
-    // the chunk's first drafted key, -1: it has none; lane l looks at entry l
-    int first_drafted;
-    {
-        const int d = list[lane & 15].y, first = d >> 5, len = d & 31;
-        const uint32_t has = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(len > 0 && first + len > 0)) & 0xffff;
-        first_drafted = has != 0 ? max(__builtin_amdgcn_readlane(first, __builtin_ctz(has)), 0) : -1;
-    }
+    const int first_drafted = first_drafted_of(list, kManyChunk);
     const auto put = [&](int tile, int set) __attribute__((always_inline)) {
         const float c = __uint_as_float((__float_as_uint(cx[set]) & given) | (__float_as_uint(1.f) & ~given));
         float off = offset_of(zx[set], c);
@@ -384,19 +427,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void weigh_many(Args a) 
     uint32_t context = 0;
     const auto look_seen = [&](int t) {
         for (int tile = t; tile < min(t + kAhead, n_tiles); ++tile) {
-            const int from = token_of(a, 32 * tile), to = token_of(a, min(32 * tile + 31, rows - 1));
-            const uint64_t group = ~0ull >> (64 - a.G);  // a token's rows, from its first one at `at` of the tile
-            int at = from * a.G - 32 * tile;
-            uint32_t s = context | (every_bit(bits[from * kWords + word], bit) & static_cast<uint32_t>(group >> -at));
-            const uint32_t* m = bits + (from + 1) * kWords + word;
-            for (int i = from + 1; i <= to; i += kTokens, m += kTokens * kWords) {
-#pragma unroll
-                for (int k = 0; k < kTokens; ++k) {  // (what is behind the last token has no rows here)
-                    at += a.G;
-                    s |= every_bit(m[k * kWords], bit) & static_cast<uint32_t>(group << min(at, 32));
-                }
-            }
-            seen[wid][tile % kAhead][lane] = s;
+            seen[wid][tile % kAhead][lane] = context | rows_that_see(a, tile, rows, bits, kWords, word, bit);
         }
     };
     // a tile's products beside the exponentials of the one before
@@ -442,25 +473,124 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void weigh_many(Args a) 
         walk(std::false_type{});
     } else {
         const int w0 = first_drafted >> 5;
-        const int64_t words = 2 * static_cast<int64_t>(a.b.mask_words);
-        const uint32_t* masks = reinterpret_cast<const uint32_t*>(a.b.mask) + u.t.q0 * words;
-        for (int m0 = tid; m0 < u.t.L * kWords; m0 += 4 * kThreads) {
-            uint32_t x[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int m = m0 + k * kThreads, w = w0 + m % kWords;
-                x[k] = m < u.t.L * kWords && w < words ? masks[m / kWords * words + w] : 0;
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (m0 + k * kThreads < u.t.L * kWords) bits[m0 + k * kThreads] = x[k];
-        }
+        stage_masks<kWords>(a, u, w0, bits);
         context = number < 0 ? ~0u : 0;
         if (number >= 0 && slot < (list[entry].y & 31)) word = (number >> 5) - w0, bit = number & 31;
         walk(std::true_type{});
     }
     const float w0 = sum[0] + __shfl_xor(sum[0], 32), w1 = sum[1] + __shfl_xor(sum[1], 32);
     if (slot < (list[entry].y & 31)) a.out[at] = fmaf(a.decay, had, hi == 0 ? w0 : w1);
+}
+
+// weigh_many for few keys: 64 of them a workgroup, which all its waves hold, and a wave takes every fourth tile of queries, straight
+// into the operand.  The waves' sums meet in LDS at the end, in their order.
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void weigh_split(Args a) {
+    constexpr int KS = D / 16;
+    extern __shared__ uint32_t bits[];  // the tokens' masks from the chunk's first drafted key on, kSplitWords each
+    __shared__ __attribute__((aligned(16))) float offs[kWaves][32];
+    __shared__ float sums[kWaves][64];
+    __shared__ int2 list[kSplitChunk];
+    __shared__ int part[kWaves];
+    const Unit u = unit_of(a);
+    if (!u.ok) return;
+    const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, hi = lane >> 5;
+    const int rows = u.t.L * a.G, n_tiles = (rows + 31) / 32;
+    const uint16_t* q0 = a.q + (static_cast<int64_t>(u.t.q0) * a.hq + u.g * a.G) * D + 8 * hi;
+    const float* lse = a.lse + static_cast<int64_t>(u.t.q0) * a.hq + u.g * a.G;
+    bf16x8_t qf[2][KS];
+    float z[2], c[2];  // of row `col`
+    const auto fetch_q = [&](int tile, int set) __attribute__((always_inline)) {
+        const int qr = min(32 * tile + col, rows - 1), i = token_of(a, qr), head = i * (a.hq - a.G) + qr;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[set][s] = *reinterpret_cast<const bf16x8_t*>(q0 + head * D + 16 * s);  // (below 2^10 256 128)
+        z[set] = lse[head];
+        c[set] = a.coef ? a.coef[u.t.q0 + i] : 1.f;
+    };
+    Look look;
+    look_ids(a, u, kSplitChunk, look);
+    int own[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int e = u.e0 + 2 * h + (col >> 4);
+        own[h] = e < u.tab.n ? a.b.kv_blocks[u.tab.first + e] : -1;
+    }
+    fetch_q(wid, 0);
+    look_lens(a, look);
+    bf16x8_t kf[2][KS];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) kf[h][s] = bf16x8_t{};
+        if (static_cast<uint32_t>(own[h]) < static_cast<uint32_t>(a.num_blocks)) {
+            const uint16_t* row = a.k + (static_cast<int64_t>(own[h]) * a.hkv + u.g) * (16 * D) + (col & 15) * D + 8 * hi;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kf[h][s] = *reinterpret_cast<const bf16x8_t*>(row + 16 * s);
+        }
+    }
+    list_blocks(a, u, kSplitChunk, look, list, part);
+
+    // what is read and written, and whose masks a lane looks up, is key `lane` of the chunk
+    const int entry = lane >> 4, slot = lane & 15, number = (list[entry].y >> 5) + slot;
+    const bool there = slot < (list[entry].y & 31);
+    const int64_t at = (static_cast<int64_t>(u.r) * a.hkv + u.g) * a.keys + 16 * static_cast<int64_t>(u.e0 + entry) + slot;
+    const float had = wid == 0 && there && number < 0 && a.before ? a.before[at] : 0.f;
+    const int first_drafted = first_drafted_of(list, kSplitChunk);
+    const bool masked = first_drafted >= 0;
+    const uint32_t context = number < 0 ? ~0u : 0;
+    int word = 0, bit = 0;
+    if (masked) {
+        const int w0 = first_drafted >> 5;
+        stage_masks<kSplitWords>(a, u, w0, bits);
+        if (number >= 0 && there) word = (number >> 5) - w0, bit = number & 31;
+        __syncthreads();
+    }
+    float sum[2] = {0.f, 0.f};
+    const auto step = [&](int t, int set) __attribute__((always_inline)) {
+        fetch_q(t + kWaves, set ^ 1);  // (tiles past the last read its last row again)
+        float off = offset_of(z[set], c[set]);
+        off = 32 * t + col < rows ? off : INFINITY;
+        if (off == INFINITY) {  // a row that gives nothing may hold anything
+#pragma unroll
+            for (int s = 0; s < KS; ++s) qf[set][s] = bf16x8_t{};
+        }
+        offs[wid][col] = off;
+        f32x16_t x[2] = {f32x16_t{}, f32x16_t{}};
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) x[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[set][s], kf[h][s], x[h], 0, 0, 0);
+        uint32_t sees[2] = {~0u, ~0u};
+        if (masked) {
+            const uint32_t s = context | rows_that_see(a, t, rows, bits, kSplitWords, word, bit);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) sees[h] = __shfl(s, 32 * h + col) >> (4 * hi);
+        }
+        // x[h][4 v + e] is query row 8 v + 4 hi + e of the tile
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const f32x4_t o = *reinterpret_cast<const f32x4_t*>(offs[wid] + 8 * v + 4 * hi);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[e] = __builtin_amdgcn_exp2f(fmaf(x[h][4 * v + e], a.sl2, -o[e]));
+                    p[e] = __uint_as_float(__float_as_uint(p[e]) & every_bit(sees[h], 8 * v + e));
+                }
+                sum[h] += (p[0] + p[1]) + (p[2] + p[3]);
+            }
+        }
+    };
+    for (int t = wid; t < n_tiles; t += 2 * kWaves) {
+        step(t, 0);
+        if (t + kWaves < n_tiles) step(t + kWaves, 1);
+    }
+    const float w0 = sum[0] + __shfl_xor(sum[0], 32), w1 = sum[1] + __shfl_xor(sum[1], 32);
+    sums[wid][lane] = hi == 0 ? w0 : w1;
+    __syncthreads();
+    if (wid == 0 && there) a.out[at] = fmaf(a.decay, had, (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]));
 }
 
 }  // namespace
@@ -477,7 +607,13 @@ int tkv::launch_key_weights(const tkv_shape& s, const tkv_draft_batch& b, const 
     a.q = static_cast<const uint16_t*>(q), a.k = static_cast<const uint16_t*>(k);
     a.lse = lse, a.coef = coef, a.before = decay != 0.f ? before : nullptr, a.out = out, a.keys = keys;
     const bool few = static_cast<int64_t>(b.max_q) * a.G <= 32;
-    a.chunk = kManyChunk;
+    // weigh_split where its workgroups run all at once, two a CU, and a wave has a tile at least.  (32/4/128 heads, many and split: one
+    // row of 3,550 keys and 32, 64, 128 tokens 13.9 and 9.1, 22.4 and 12.6, 40.2 and 17.9 us; two such rows, 458 workgroups, 15.1 and
+    // 13.4, 23.7 and 18.7, 41.4 and 26.6; three rows 15.4 and 23.0, 24.2 and 30.4, 42.8 and 46.2.  Two rows of 16 tokens, four tiles,
+    // 10.5 and 11.4; two tiles 7.1 and 9.1.  Nine rows of 200 tokens under 1,200 keys, 14/2/64: 55 and 24.)
+    const bool split = !few && (static_cast<int64_t>(b.max_q) * a.G + 31) / 32 >= kWaves &&
+                       (b.n_kv_blocks / kSplitChunk + static_cast<int64_t>(b.n_rows)) * s.hkv <= kSplitGroups;
+    a.chunk = split ? kSplitChunk : kManyChunk;
     if (few) {
         const int64_t even = static_cast<int64_t>(b.n_kv_blocks) * s.hkv / kFewGroups;
         a.chunk = static_cast<int32_t>(std::max<int64_t>(8, std::min<int64_t>(kFewChunk, (even + 7) / 8 * 8)));
@@ -492,12 +628,12 @@ int tkv::launch_key_weights(const tkv_shape& s, const tkv_draft_batch& b, const 
     const int64_t grid = a.search ? counted : direct;
     if (grid > static_cast<int64_t>(UINT32_MAX) / kThreads)
         return set_error(TKV_EINVAL, "tkv_key_weights: %lld workgroups are too many", static_cast<long long>(grid));
-    const size_t lds = few ? 0 : static_cast<size_t>(b.max_q + kTokens) * kWords * 4;  // (62 KB with the rest, at most)
+    const size_t lds = few ? 0 : static_cast<size_t>(b.max_q + kTokens) * (split ? kSplitWords : kWords) * 4;  // (62 KB with all)
     const auto run = [&](auto kernel) { kernel<<<dim3(static_cast<unsigned>(grid)), dim3(kThreads), lds, st>>>(a); };
     if (s.d == 128)
-        few ? run(weigh_few<128>) : run(weigh_many<128>);
+        few ? run(weigh_few<128>) : split ? run(weigh_split<128>) : run(weigh_many<128>);
     else
-        few ? run(weigh_few<64>) : run(weigh_many<64>);
+        few ? run(weigh_few<64>) : split ? run(weigh_split<64>) : run(weigh_many<64>);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? TKV_OK : set_error(TKV_EHIP, "tkv_key_weights launch: %s", hipGetErrorString(e));
 }

@@ -18,6 +18,11 @@ from _rows import BS, Rows, dev
 HEADS = [(28, 4, 128), (4, 4, 64), (16, 1, 64), (12, 2, 128), (15, 5, 64), (64, 1, 128), (40, 8, 128), (8, 2, 64)]
 
 
+def more_entries(c):
+    """Entries of no row behind the tables: the work is cut for as many keys as the arrays hold."""
+    return {"kv_blocks": torch.cat([c.arrays()["kv_blocks"], torch.zeros(4096, dtype=torch.int32, device="cuda")])}
+
+
 class Case(Rows):
     def __init__(self, rows, hq, hkv, d, seed=0, extra_keys=0, **more):
         super().__init__(rows, seed, **more)
@@ -88,6 +93,7 @@ class Case(Rows):
 def test_drafts_of_one_size(hq, hkv, d, L):
     c = Case([(n, L) for n in (0, 1, 15, 16, 17, 100, 700)], hq, hkv, d, seed=L, extra_keys=L)
     c.check(c.run())
+    c.check(c.run(**more_entries(c)))
 
 
 @pytest.mark.gpu
@@ -106,6 +112,7 @@ def test_any_masks_of_groups_of_any_size(hq, hkv, d):
     # tiles of 32 query rows that begin and end inside a token's group, masks looked up for several tiles at once
     c = Case([(5, 60), (300, 40), (0, 257), (77, 33), (1000, 130)], hq, hkv, d, seed=hq, bits=True, extra_words=2)
     c.check(c.run())
+    c.check(c.run(**more_entries(c)))
 
 
 @pytest.mark.gpu
@@ -114,6 +121,13 @@ def test_any_masks_of_groups_of_any_size(hq, hkv, d):
 def test_long_and_short_paths(rows):
     c = Case(rows, 12, 2, 128, seed=3)
     c.check(c.run())
+    c.check(c.run(**more_entries(c)))
+
+
+@pytest.mark.gpu
+def test_few_rows_in_tables_of_a_large_capacity():
+    c = Case([(200, 40), (0, 1), (30, 70), (900, 33)], 12, 2, 64, seed=8, extra_keys=16 * 5000)
+    c.check(c.run(max_blocks=c.max_blocks + 5000))
 
 
 @pytest.mark.gpu
@@ -157,6 +171,11 @@ def test_tokens_that_are_left_out_may_hold_anything(L):
         for x in (float("nan"), float("inf"), -float("inf")):
             c.q[out] = x
             assert torch.equal(c.run(), want)
+        if L > 3:  # the kernel for many keys
+            c.q[out] = 1.0
+            want = c.run(**more_entries(c))
+            c.q[out] = float("nan")
+            assert torch.equal(c.run(**more_entries(c)), want)
 
 
 @pytest.mark.gpu
