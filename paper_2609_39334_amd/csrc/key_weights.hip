@@ -18,7 +18,7 @@
 // Measured (times of calls one after the other): those 64 tokens 23 us, 102 MB, 4.5 TB/s.  32 tokens under one path of 30,000
 // keys, 28/4/128: 17 us; 472 workgroups are less than two a CU, so it is a workgroup's own time: about 6 us until its first
 // product (table, lengths, keys and first queries, a chain) and seven tiles of 1 us, 1.5 where there are masks.  8 rows of 64 to
-// 256 tokens under 2,000 to 12,000 keys, 32/8/128 (67.8 GFLOP): 100 us, 675 TFLOP/s; MFMAs were busy 31% and the vector units 53%
+// 256 tokens under 2,000 to 12,000 keys, 32/8/128 (67.8 GFLOP): 100 to 104 us, 650 to 675 TFLOP/s; MFMAs were busy 31% and the vector units 53%
 // of 110 (a product of 32 x 64 scores is 512 cycles of a SIMD's MFMAs, its exponentials 512 of a quarter-rate unit and about as
 // many of others). Tried there, against 119 to 123 at the time: eight waves of 32 keys (123), two groups of keys one after the
 // other in a workgroup (141), three waves a SIMD (127 to 133, registers spill in the steps), chunks slowest in the grid (130 to
