@@ -1096,6 +1096,7 @@ class DraftBatch:
                          q, k, v, o, lse, workspace, stream)
 
     def key_weights(self, q, k, lse, out, before=None, decay=1.0, coef=None, stream=None):
+        """tkv_key_weights of this batch, after its attention wrote lse; out may be before."""
         tkv_key_weights(self.q_indptr, self.kv_indptr, self.kv_blocks, self.block_len, self.mask, self.max_q, self.max_blocks,
                         q, k, lse, out, before, decay, coef, stream)
 

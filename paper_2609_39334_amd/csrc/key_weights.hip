@@ -46,11 +46,10 @@ constexpr int kThreads = 256, kWaves = 4;
 constexpr int kFewChunk = 64, kFewGroups = 768;
 constexpr int kManyChunk = 16;    // entries a workgroup of weigh_many
 constexpr int kSplitChunk = 4;    // entries a workgroup of weigh_split
-constexpr int kSplitGroups = 512;
-constexpr int kSplitWords = 3;    // words of 32 bits that 64 consecutive bits can touch
+constexpr int kSplitGroups = 512; // most workgroups of weigh_split: two a CU
+constexpr int kWords = 9, kSplitWords = 3;  // words of 32 bits that 256 and 64 consecutive bits can touch
 constexpr int kAhead = 8;         // tiles whose masks are looked up together
-constexpr int kTokens = 8;        // of which masks are looked up together
-constexpr int kWords = 9;         // words of 32 bits that 256 consecutive bits can touch
+constexpr int kTokens = 8;        // tokens whose masks are read together
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Args {
@@ -622,11 +621,12 @@ int tkv::launch_key_weights(const tkv_shape& s, const tkv_draft_batch& b, const 
     a.n_chunks = (b.max_blocks + a.chunk - 1) / a.chunk | 1;
     // A workgroup finds its row by division where that leaves few without work, or counts the rows' chunks up to its own: one row of
     // 30,000 keys beside 300 of 30 to 300 takes 23 us counted and 75 divided, 1,000 rows of like lengths 52 and 29.
-    const int64_t direct = static_cast<int64_t>(a.n_chunks) * b.n_rows * s.hkv;
+    const int64_t heads = static_cast<int64_t>(b.n_rows) * s.hkv, most = static_cast<int64_t>(UINT32_MAX) / kThreads;
+    const int64_t direct = a.n_chunks * std::min(heads, most + 1);  // (2^25 2^24 at most)
     const int64_t counted = (b.n_kv_blocks / a.chunk + static_cast<int64_t>(b.n_rows)) * s.hkv;
     a.search = direct > 4 * counted;
     const int64_t grid = a.search ? counted : direct;
-    if (grid > static_cast<int64_t>(UINT32_MAX) / kThreads)
+    if (grid > most || heads > most)
         return set_error(TKV_EINVAL, "tkv_key_weights: %lld workgroups are too many", static_cast<long long>(grid));
     const size_t lds = few ? 0 : static_cast<size_t>(b.max_q + kTokens) * (split ? kSplitWords : kWords) * 4;  // (62 KB with all)
     const auto run = [&](auto kernel) { kernel<<<dim3(static_cast<unsigned>(grid)), dim3(kThreads), lds, st>>>(a); };

@@ -380,7 +380,8 @@ def test_bad_arguments_are_refused():
                 dict(words=0), dict(ptr=None), dict(q=None), dict(q=one + 8), dict(lse=None), dict(lse=one + 2), dict(coef=one + 1),
                 dict(before=one + 2), dict(out=None), dict(out=one + 2), dict(keys=143), dict(keys=-1), dict(decay=float("nan")),
                 dict(decay=float("inf")), dict(max_blocks=1 << 28, keys=1 << 40), dict(before=one + 4), dict(before=one + 2 * 144 * 4 - 4),
-                dict(out=one + 4, before=one), dict(n_rows=1 << 30), dict(n_rows=1 << 24)):
+                dict(out=one + 4, before=one), dict(n_rows=1 << 30), dict(n_rows=1 << 24),
+                dict(n_rows=(1 << 31) - 1, max_blocks=(1 << 27) - 1, keys=1 << 31)):
         assert call(**bad) == tkv.TKV_EINVAL, bad
     assert call(n_rows=0) == tkv.TKV_OK and call(n_qtok=0) == tkv.TKV_OK
     assert L.tkv_key_weights(None, None, one, one, one, None, 1.0, None, one, 1, None) == tkv.TKV_EINVAL
