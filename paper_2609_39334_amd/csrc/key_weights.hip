@@ -184,7 +184,7 @@ __device__ __forceinline__ uint32_t rows_that_see(const Args& a, int tile, int r
     m += words;
     for (int i = from + 1; i <= to; i += kTokens, m += kTokens * words) {
 #pragma unroll
-        for (int k = 0; k < kTokens; ++k) {  // (what is behind the last token has no rows here)
+        for (int k = 0; k < kTokens; ++k) {  // (tokens behind the tile's last have no rows here, or masks of zeros)
             at += a.G;
             s |= every_bit(m[k * words], bit) & static_cast<uint32_t>(group << min(at, 32));
         }
@@ -199,18 +199,19 @@ __device__ __forceinline__ int first_drafted_of(const int2* list, int n) {
     return has != 0 ? max(__builtin_amdgcn_readlane(first, __builtin_ctzll(has)), 0) : -1;
 }
 
-// The tokens' masks from word w0 on, `words` words each, to bits.
+// The tokens' masks from word w0 on, `words` words each, to bits, and kTokens masks of zeros behind them: a row's last tile may end
+// inside, and its rows past the last token must not be seen to see (their products are 0 K, which is not 0 under any K).
 template <int W>
 __device__ __forceinline__ void stage_masks(const Args& a, const Unit& u, int w0, uint32_t* bits) {
     const int64_t words = 2 * static_cast<int64_t>(a.b.mask_words);
     const uint32_t* masks = reinterpret_cast<const uint32_t*>(a.b.mask) + u.t.q0 * words;
-    const int n = u.t.L * W;
+    const int given = u.t.L * W, n = given + kTokens * W;
     for (int m0 = threadIdx.x; m0 < n; m0 += 4 * kThreads) {
         uint32_t x[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int m = m0 + k * kThreads, w = w0 + m % W;
-            x[k] = m < n && w < words ? masks[m / W * words + w] : 0;
+            x[k] = m < given && w < words ? masks[m / W * words + w] : 0;
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k)

@@ -253,6 +253,34 @@ def test_blocks_that_are_none_and_rows_outside_the_arrays():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,d", [(28, 4, 128), (14, 2, 64), (10, 2, 128), (9, 3, 64), (6, 2, 64)])
+def test_hidden_keys_under_partial_tiles_may_hold_anything(hq, hkv, d):
+    # a row's last tile of 32 query rows ends inside; what a call whose masks are all ones leaves on the chip must not count there
+    rng, rows = np.random.default_rng(hq), 128 // hkv
+    c = Case([(30, int(n)) for n in rng.integers(34, 60, rows)], hq, hkv, d, seed=2)
+    infinite = c.k.clone()
+    for r, L in enumerate(c.L):
+        columns, a = rng.choice(L, 6, replace=False), c.q_ptr[r]
+        for j in columns:
+            c.masks[r][:, 0] &= ~(np.uint64(1) << np.uint64(j))
+        slot = c.path(r)[1][30 + columns]
+        for k, x in ((c.k, float("nan")), (infinite, float("inf"))):
+            k[dev(slot // BS), :, dev(slot % BS)] = x
+        c.lse[a:a + L] = torch.logsumexp(c.scores(r)[0], -1).permute(2, 0, 1).reshape(L, hq).float()
+    for more, n in ((lambda x: {}, rows), (more_entries, 2048 // hkv)):   # few keys (the waves share out the tiles), many
+        ones = Case([(36, 60)] * n, hq, hkv, d, seed=1)
+        for m in ones.masks:
+            m[:] = np.uint64(2**64 - 1)
+        theirs, mine = dict(ones.arrays(), **more(ones), max_q=60), dict(c.arrays(), **more(c), max_q=60)
+        ones.run(**theirs)
+        first = c.run(**mine)
+        c.check(first)
+        assert torch.equal(c.run(**mine), first)
+        ones.run(**theirs)
+        assert torch.equal(c.run(k=infinite, **mine), first)
+
+
+@pytest.mark.gpu
 def test_the_same_blocks_twice_and_many_rows():
     c = Case([(100, 4), (200, 4), (50, 2)], 12, 2, 128)
     c.tables[0] = np.concatenate([c.tables[1][:3], c.tables[1][:3], c.tables[0]])
