@@ -430,9 +430,10 @@ int tkv_draft_verify(const tkv_shape* shape, const tkv_draft_batch* batch, const
  *   keys     at least 16 * max_blocks
  * What no key of a row's table has a place for is not written (slots past a block's length, entries that are no blocks, rows
  * that are left out: tokens or table outside the arrays, or longer than max_q or max_blocks; where kv_indptr decreases
- * somewhere, so that rows share entries, rows behind it may be).  K of the keys that a token
- * sees must be finite; what the others hold does not matter.  The order of a key's additions follows from the call's sizes
- * (n_rows, n_kv_blocks, max_q, heads) and its row alone: the same call gives the same bits.  No workspace.
+ * somewhere, so that rows share entries, rows behind it may be).  A row without tokens takes no step and is left out as well:
+ * its weights are not decayed, and out keeps what it held there, so where rows pause out has to be before.  K of the keys that
+ * a token sees must be finite; what the others hold does not matter.  The order of a key's additions follows from the call's
+ * sizes (n_rows, n_kv_blocks, max_q, heads) and its row alone: the same call gives the same bits.  No workspace.
  * EINVAL (shape and batch as for tkv_draft_verify, keys, decay, NULL pointers, q or k not 16-byte aligned), EHIP. */
 int tkv_key_weights(const tkv_shape* shape, const tkv_draft_batch* batch, const void* q, const void* k, const float* lse,
                     const float* coef, float decay, const float* before, float* out, int64_t keys, void* hip_stream);

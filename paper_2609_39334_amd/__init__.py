@@ -642,7 +642,8 @@ def tkv_key_weights(q_indptr: torch.Tensor, kv_indptr: torch.Tensor, kv_blocks: 
     """Adds the attention weight of a batch's queries to its rows' keys: out [n_rows, hkv, keys] fp32 (keys >= 16 max_blocks)
     gets, at 16 e + s for the key in slot s of a row's entry e, decay * before (None: 0; may be out; not for the row's last
     keys, which enter) + the sum of coef (None: 1) times the queries' weights.  lse [n, hq] is the attention's; the other
-    arguments are tkv_draft_verify's."""
+    arguments are tkv_draft_verify's.  A row without tokens is left out, its weights not decayed and its part of out not
+    written: where rows pause, out has to be before."""
     fn = "tkv_key_weights"
     if k.dim() != 4 or q.dim() != 3 or mask.dim() != 2 or out.dim() != 3:
         raise ValueError(f"{fn}: k must be a pool [num_blocks, hkv, block_size, d], q [n, hq, d], mask [n, words], out [n_rows, "

@@ -281,6 +281,24 @@ def test_hidden_keys_under_partial_tiles_may_hold_anything(hq, hkv, d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("L,more", [(3, lambda c: {}), (40, lambda c: {}), (40, more_entries)], ids=["few", "split", "many"])
+def test_rows_without_tokens_are_left_out(L, more):
+    # rows that pause among others: in place their weights stay as they are, elsewhere nothing is written for them
+    c = Case([(100, 0), (300, L), (0, 0), (77, 0), (500, L), (40, 0)], 8, 2, 64, seed=L)
+    out = c.run(**more(c))
+    c.check(out, rows=[1, 4])
+    assert torch.all(out[[0, 2, 3, 5]] == 7)
+    own = c.before.clone()
+    c.run(out=own, before=own, **more(c))
+    assert torch.equal(own[[0, 2, 3, 5]], c.before[[0, 2, 3, 5]])
+    for r in (1, 4):
+        at = dev(c.path(r)[0])
+        assert torch.equal(own[r][:, at], out[r][:, at])
+    none = Case([(30, 0), (5, 0)], 8, 2, 64)
+    assert torch.all(none.run() == 7)
+
+
+@pytest.mark.gpu
 def test_the_same_blocks_twice_and_many_rows():
     c = Case([(100, 4), (200, 4), (50, 2)], 12, 2, 128)
     c.tables[0] = np.concatenate([c.tables[1][:3], c.tables[1][:3], c.tables[0]])
