@@ -176,6 +176,8 @@ class SyntheticDecoder:
         """Draws under per-row temperature, top-k, top-p and min-p: (tokens, counts, groups per row).  stream as for step.
         With a history (the batch over the tables of `said`, the pool [num_blocks, 16] of the paths' tokens) the logits are
         adjusted first: rules holds tkv_adjust_logits' settings by name."""
+        if (history is None) != (said is None) or (rules and history is None):
+            raise ValueError("sample_filtered: rules need a history and its tokens, and these two go together")
         def run():
             x = logits if history is None else history.adjust_logits(said, logits, out=torch.empty_like(logits, dtype=torch.float32),
                                                                      stream=stream, **(rules or {}))

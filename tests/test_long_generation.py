@@ -225,6 +225,18 @@ def test_draws_under_rules_on_another_stream():
         assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_rules_and_histories_go_together():
+    # no draw from logits that silently miss their rules (refused before any device access: no GPU needed)
+    model = SyntheticDecoder(DecoderShape(layers=1, hidden=64, hq=1, hkv=1, d=64, inter=64, vocab=64), device="cpu")
+    history = tkv.DraftBatch([[0]], [[-1]], np.full(1, 16, np.int32), device="cpu")
+    said, rules = torch.zeros((1, BS), dtype=torch.int32), {"repetition": torch.full((1,), 1.5)}
+    logits, one, off = torch.zeros((1, 64)), torch.ones(1), torch.tensor([0, 1], dtype=torch.int32)
+    for some in (dict(rules=rules), dict(said=said), dict(rules=rules, said=said), dict(history=history),
+                 dict(history=history, rules=rules)):
+        with pytest.raises(ValueError, match="go together"):
+            model.sample_filtered(logits, one, off, one * 0.5, 1, **some)
+
+
 def test_evict_batch():
     bl = np.array([16, 16, 5, 3, 0, 0, 0], np.int32)
     e = tkv.EvictBatch([[0, 3], [1, 2], []], [[4], [5, 6], []], [10, 1 << 40, 0], bl, device="cpu")  # (a budget of any size)
