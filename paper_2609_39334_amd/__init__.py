@@ -537,6 +537,10 @@ class _Call:
                 _check(entry(*args, self.handle))
 
 
+def _past_32_bits(fn: str) -> ValueError:
+    return ValueError(f"{fn}: a size or a number is no whole number of 32 bits")
+
+
 def _tensors(fn: str, index: int, *specs) -> None:
     """Checks (name, tensor, dtype, shape): contiguous, of that type and shape, on GPU `index`."""
     for name, t, dtype, shape in specs:
@@ -664,9 +668,13 @@ def tkv_key_weights(q_indptr: torch.Tensor, kv_indptr: torch.Tensor, kv_blocks: 
     _tensors(fn, index, *specs)
     call = _Call(fn, k, stream)
     call.uses(q_indptr, kv_indptr, kv_blocks, block_len, mask, q, k, lse, out, before, coef)
-    batch = _pack_draft(n_rows, n, max_q, n_kv, max_blocks, words, q_indptr.data_ptr(), kv_indptr.data_ptr(),
-                        kv_blocks.data_ptr(), block_len.data_ptr(), mask.data_ptr())
-    call.run(lib().tkv_key_weights, _pack_shape(hq, hkv, d, bs, nb), batch, q.data_ptr(), k.data_ptr(), lse.data_ptr(),
+    try:
+        shape = _pack_shape(hq, hkv, d, bs, nb)
+        batch = _pack_draft(n_rows, n, max_q, n_kv, max_blocks, words, q_indptr.data_ptr(), kv_indptr.data_ptr(),
+                            kv_blocks.data_ptr(), block_len.data_ptr(), mask.data_ptr())
+    except struct.error:
+        raise _past_32_bits(fn) from None
+    call.run(lib().tkv_key_weights, shape, batch, q.data_ptr(), k.data_ptr(), lse.data_ptr(),
              None if coef is None else coef.data_ptr(), decay, None if before is None else before.data_ptr(), out.data_ptr(), keys)
 
 
@@ -695,10 +703,14 @@ def tkv_evict_keys(kv_indptr: torch.Tensor, kv_blocks: torch.Tensor, block_len: 
              ("kept", kept, torch.int32, (rows, hkv, most)), ("n_kept", n_kept, torch.int32, (rows,)))
     call = _Call(fn, k, stream)
     call.uses(kv_indptr, kv_blocks, block_len, new_indptr, new_blocks, budget, weights, k, v, out, kept, n_kept)
-    batch = _pack_evict(n_rows, n_kv, max_blocks, n_new, most, sink, recent, kv_indptr.data_ptr(), kv_blocks.data_ptr(),
-                        block_len.data_ptr(), new_indptr.data_ptr(), new_blocks.data_ptr(), budget.data_ptr())
-    call.run(lib().tkv_evict_keys, _pack_shape(hkv, hkv, d, bs, nb), batch, weights.data_ptr(), out.data_ptr(), keys, k.data_ptr(),
-             v.data_ptr(), kept.data_ptr(), n_kept.data_ptr())
+    try:
+        shape = _pack_shape(hkv, hkv, d, bs, nb)
+        batch = _pack_evict(n_rows, n_kv, max_blocks, n_new, most, sink, recent, kv_indptr.data_ptr(), kv_blocks.data_ptr(),
+                            block_len.data_ptr(), new_indptr.data_ptr(), new_blocks.data_ptr(), budget.data_ptr())
+    except struct.error:
+        raise _past_32_bits(fn) from None
+    call.run(lib().tkv_evict_keys, shape, batch, weights.data_ptr(), out.data_ptr(), keys, k.data_ptr(), v.data_ptr(),
+             kept.data_ptr(), n_kept.data_ptr())
 
 
 def tkv_swiglu(gu: torch.Tensor, stream=None) -> torch.Tensor:
@@ -839,15 +851,20 @@ def tkv_adjust_logits(q_indptr: torch.Tensor, kv_indptr: torch.Tensor, kv_blocks
         p8 = allowed.data_ptr()
     _tensors(fn, index, *specs)
     stride = _logit_rows(fn, "logits", logits, n, vocab, index)
+    if vocab >> 31:  # (an int32 argument of a call would be cut to 32 bits without a word)
+        raise _past_32_bits(fn)
     call = _Call(fn, tokens, stream)
     if out is None:
         out = call.empty((n, vocab), logits.dtype)
     out_stride = _logit_rows(fn, "out", out, n, vocab, index)
     call.uses(q_indptr, kv_indptr, kv_blocks, block_len, mask, tokens, logits, prompt_len, repetition, presence, frequency,
               bias_indptr, bias_token, bias_value, grammar, allowed, out)
-    rules = _pack_rules(p0, p1, p2, p3, p4, p5, p6, p7, p8, n_bias, n_masks, mask_words)
-    batch = _pack_draft(n_rows, n, max_q, n_kv, max_blocks, words, q_indptr.data_ptr(), kv_indptr.data_ptr(),
-                        kv_blocks.data_ptr(), block_len.data_ptr(), mask.data_ptr())
+    try:
+        rules = _pack_rules(p0, p1, p2, p3, p4, p5, p6, p7, p8, n_bias, n_masks, mask_words)
+        batch = _pack_draft(n_rows, n, max_q, n_kv, max_blocks, words, q_indptr.data_ptr(), kv_indptr.data_ptr(),
+                            kv_blocks.data_ptr(), block_len.data_ptr(), mask.data_ptr())
+    except struct.error:
+        raise _past_32_bits(fn) from None
     call.run(lib().tkv_adjust_logits, nb, tokens.data_ptr(), batch, rules, vocab, logits.dtype is torch.bfloat16, logits.data_ptr(),
              stride, out.dtype is torch.bfloat16, out.data_ptr(), out_stride)
     return out

@@ -225,6 +225,29 @@ def test_draws_under_rules_on_another_stream():
         assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+@pytest.mark.gpu
+def test_numbers_past_32_bits_are_refused():
+    dev = lambda *x, dtype=torch.int32: torch.tensor(x, dtype=dtype, device="cuda")
+    rows = dict(kv_indptr=dev(0, 2), kv_blocks=dev(0, 1), block_len=dev(16, 4, 0), max_blocks=2)
+    k, w = torch.zeros((3, 2, BS, 64), device="cuda").bfloat16(), torch.zeros((1, 2, 32), device="cuda")
+    batch = dict(rows, q_indptr=dev(0, 1), mask=dev(1, dtype=torch.int64)[None], max_q=1)
+    weigh = dict(batch, q=torch.zeros((1, 2, 64), device="cuda").bfloat16(), k=k, lse=torch.zeros((1, 2), device="cuda"), out=w)
+    evict = dict(rows, new_indptr=dev(0, 1), new_blocks=dev(2), budget=dev(4), sink=1, recent=1, weights=w, k=k, v=k.clone(),
+                 out=w.clone(), kept=torch.zeros((1, 2, 4), dtype=torch.int32, device="cuda"), n_kept=dev(0))
+    adjust = dict(batch, tokens=torch.zeros((3, BS), dtype=torch.int32, device="cuda"), logits=torch.zeros((1, 100), device="cuda"))
+    for call, args, names in ((tkv.tkv_key_weights, weigh, ("max_q", "max_blocks")),
+                              (tkv.tkv_evict_keys, evict, ("max_blocks", "sink", "recent")),
+                              (tkv.tkv_adjust_logits, adjust, ("max_q", "max_blocks"))):
+        call(**args)
+        for name in names:
+            for bad in (1 << 31, -(1 << 31) - 1, (1 << 32) + 2):
+                with pytest.raises(ValueError, match="32 bits"):
+                    call(**dict(args, **{name: bad}))
+    wide = torch.empty((1, (1 << 32) + 100), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="32 bits"):
+        tkv.tkv_adjust_logits(**dict(adjust, logits=wide, out=wide))
+
+
 def test_rules_and_histories_go_together():
     # no draw from logits that silently miss their rules (refused before any device access: no GPU needed)
     model = SyntheticDecoder(DecoderShape(layers=1, hidden=64, hq=1, hkv=1, d=64, inter=64, vocab=64), device="cpu")
