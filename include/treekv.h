@@ -572,8 +572,8 @@ int tkv_filter_sample(int32_t n_rows, int32_t vocab, int32_t logit_type, const v
  *   grammar        [n_qtok] int32: each token's mask, allowed + grammar[i] * allowed_words, bit j % 32 of word j / 32 set
  *                  where j is allowed; negative: none.  n_grammars masks of allowed_words >= ceil(vocab / 32) words
  * A row whose settings are outside their ranges, whose biases are not inside the arrays, or whose table is not inside
- * kv_blocks or is longer than max_blocks gets NaN, as does a token whose mask is not one of n_grammars (the samplers then say
- * so); a row whose tokens are not inside the batch is left out, and rows of logits that are no row's token are not written.
+ * kv_blocks or is longer than max_blocks gets NaN alone, as does a token whose mask is not one of n_grammars (both samplers then
+ * give it d_n_groups -1); a row whose tokens are not inside the batch is left out, and rows of logits that are no row's token are not written.
  * No workspace.  vocab <= 2,097,152.  EINVAL (sizes, types, strides, NULL pointers, tokens not 16-byte aligned), EHIP. */
 typedef struct {
     const int32_t* prompt_len;

@@ -236,6 +236,28 @@ def test_settings_outside_their_ranges():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("vocab", [9001, 70000])
+def test_the_samplers_say_which_rows_are_refused(vocab):
+    # the operator's output as it is: every token of a refused row, and the one whose grammar is none, draws nothing
+    c = Case([(100, 2)] * 12, vocab, 2, grammar=0.0)
+    finite = c.logits.nan_to_num(1.0, 5.0, -5.0)
+    u = {k: v.copy() for k, v in c.rules.items()}
+    u["bias_value"] = np.where(np.isfinite(u["bias_value"]), u["bias_value"], -4.0).astype(np.float32)
+    u["allowed"][1, :] = -1   # all tokens
+    u["grammar"][:] = np.where(np.arange(24) % 2, 1, -1)
+    u["repetition"][1], u["presence"][4], u["frequency"][7], u["grammar"][17] = np.nan, np.inf, -np.inf, 5
+    u["bias_indptr"][-1] += 1
+    want = [-1 if i // 2 in (1, 4, 7, 11) or i == 17 else 1 for i in range(24)]
+    got = c.run(logits=finite, **{k: dev(v) for k, v in u.items()}, out=torch.empty_like(finite))
+    off, half = torch.arange(25, dtype=torch.int32, device="cuda"), torch.full((24,), 0.5, device="cuda")
+    tok, _, groups = tkv.tkv_filter_sample(got, torch.ones(24, device="cuda"), off, half, 1)
+    assert groups.tolist() == want and [t >= 0 for t in tok.tolist()] == [g == 1 for g in want]
+    tok, _, groups = tkv.tkv_cd_sample(got, 1.0, off, half, 1)
+    assert groups.tolist() == want
+    assert torch.equal(got.isnan().all(1), dev(np.array(want) < 0)) and torch.equal(got.isnan().any(1), got.isnan().all(1))
+
+
+@pytest.mark.gpu
 def test_rows_outside_the_arrays():
     c = Case([(100, 4), (160, 6), (100, 8), (1500, 5), (90, 3), (90, 2)], 900, 3)
     same = lambda x, y: torch.equal(x.nan_to_num(9), y.nan_to_num(9))
