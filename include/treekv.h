@@ -565,7 +565,7 @@ int tkv_filter_sample(int32_t n_rows, int32_t vocab, int32_t logit_type, const v
  *   in, out        logits of token i at in + i * in_stride elements (stride >= vocab), fp32 or bf16 (in_type, out_type);
  *                  out may be in if type and stride are the same, and must not overlap it otherwise
  * The rules, all device data, each of them nullable (off):
- *   prompt_len     [n_rows] int32 (off: 0): the first tokens of the path, which are the prompt
+ *   prompt_len     [n_rows] int32 (off: 0): the first tokens of the path, which are the prompt (below 0: none)
  *   repetition     [n_rows] fp32 in [2^-126, 2^126] (off: 1);  presence, frequency  [n_rows] fp32, finite (off: 0)
  *   bias_indptr    [n_rows + 1] int32: row r's biases are bias_token, bias_value [bias_indptr[r] .. bias_indptr[r + 1]), of
  *                  n_bias in all (0: no row has any)

@@ -304,7 +304,9 @@ __global__ __launch_bounds__(kThreads) void adjust(Args a) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q) now[q] = tok[q];
                 if (k + 1 < kBatch) fetch(k == 0 ? id[1] : k == 1 ? id[2] : id[3], k == 0 ? len[1] : k == 1 ? len[2] : len[3]);
-                const int sure = min(max(context - number, 0), m), old = min(max(prompt - number, 0), sure);
+                const int sure = min(max(context - number, 0), m);
+                // (prompt is any number: a difference that cuts off where it would leave 32 bits)
+                const int old = min(max(__builtin_elementwise_sub_sat(prompt, number), 0), sure);
                 if (old < sure) every(now, ~((1u << sure) - (1u << old)), [&](uint32_t at, int) { count.more(at); });
                 if (old > 0) every(now, ~((1u << old) - 1), [&](uint32_t at, int) { count.set(at); });
                 if (sure < m && t.L > 1)

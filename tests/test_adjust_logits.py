@@ -202,6 +202,15 @@ def test_in_place_and_rows_between_each_other(in16):
 
 
 @pytest.mark.gpu
+def test_prompt_lengths_of_any_size():
+    # below 0 is no prompt, past the path's end all of it
+    c = Case([(300, 3), (2000, 1), (40, 2), (700, 12), (50, 1)], 501, 4)
+    c.rules["frequency"][:], c.rules["presence"][:] = 0.25, 0.5
+    c.rules["prompt_len"][:] = [-2**31, -2**31 + 40, -1, 2**31 - 1, -2**31]
+    c.check(c.run())
+
+
+@pytest.mark.gpu
 def test_settings_outside_their_ranges():
     c = Case([(100, 2)] * 12, 9001, 2, grammar=0.0)
     want = c.run().clone()
