@@ -432,8 +432,9 @@ int tkv_draft_verify(const tkv_shape* shape, const tkv_draft_batch* batch, const
  * that are left out: tokens or table outside the arrays, or longer than max_q or max_blocks; where kv_indptr decreases
  * somewhere, so that rows share entries, rows behind it may be).  A row without tokens takes no step and is left out as well:
  * its weights are not decayed, and out keeps what it held there, so where rows pause out has to be before.  K of the keys that
- * a token sees must be finite; what the others hold does not matter.  The order of a key's additions follows from the call's
- * sizes (n_rows, n_kv_blocks, max_q, heads) and its row alone: the same call gives the same bits.  No workspace.
+ * a token sees (one that coef leaves out as well) must be finite; what the others hold does not matter.  The order of a key's
+ * additions follows from the call's sizes (n_rows, n_kv_blocks, max_q, heads) and its row alone: the same call gives the same
+ * bits.  No workspace.
  * EINVAL (shape and batch as for tkv_draft_verify, keys, decay, NULL pointers, q or k not 16-byte aligned), EHIP. */
 int tkv_key_weights(const tkv_shape* shape, const tkv_draft_batch* batch, const void* q, const void* k, const float* lse,
                     const float* coef, float decay, const float* before, float* out, int64_t keys, void* hip_stream);
@@ -442,6 +443,8 @@ int tkv_key_weights(const tkv_shape* shape, const tkv_draft_batch* batch, const 
  * them if N <= budget[r], else the first min(sink, n), of the rest the last min(recent, ...), and of those between the
  * ones with the largest weights, the lowest index first among equal weights (NaN is below everything).  They go, in path
  * order, to the slots 0 .. n - 1 of the row's new table (16 a block; block_len is the caller's to bring up to date).
+ * Every row gets a copy of its own: rows that shared blocks share none afterwards, and where n over all rows is more than the
+ * blocks that they held between them, the cache grows.
  *   n_rows, n_kv_blocks, max_blocks, kv_indptr, kv_blocks, block_len   the rows' tables, as in tkv_draft_batch
  *   new_indptr  [n_rows + 1] device: row r's new table is new_blocks[new_indptr[r] .. new_indptr[r + 1]), at least
  *               ceil(n / 16) blocks of the pool (tkv_bm_extend of n tokens without a parent and with seal = 0), each
@@ -560,7 +563,8 @@ int tkv_filter_sample(int32_t n_rows, int32_t vocab, int32_t logit_type, const v
  *   c > 0 times past the prompt:  l[j] -= frequency * c + presence
  *   j is biased:                  l[j] += the last of the row's biases for j
  *   j is not allowed:             l[j] = -inf, whatever it was
- * in fp32, rounded once.  Out-of-vocabulary tokens count for nothing.
+ * in fp32 (the quotient as l[j] times the rounded 1 / repetition), and at the end rounded once to out's type.
+ * Out-of-vocabulary tokens count for nothing.
  *   num_blocks, tokens   the pool;  batch   as in tkv_draft_verify (n_qtok rows of logits)
  *   in, out        logits of token i at in + i * in_stride elements (stride >= vocab), fp32 or bf16 (in_type, out_type);
  *                  out may be in if type and stride are the same, and must not overlap it otherwise

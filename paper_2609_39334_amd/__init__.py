@@ -1127,8 +1127,9 @@ class DraftBatch:
 class EvictBatch:
     """The device arrays of an eviction (tkv_evict_keys), in one upload: row r's path in tables[r] keeps at most budget[r]
     keys a KV head, in the blocks new_tables[r] (as many as they need, in no other table of the batch: e.g. of a sequence that
-    BlockManager.extend made without a parent and with seal=False).  A batch serves every layer.  n_kept: how many each row
-    keeps, evicted: how many it loses (host)."""
+    BlockManager.extend made without a parent and with seal=False).  Rows that share blocks each keep copies of their own: a
+    shared prefix is worth evicting where it and the rest are more than what all rows keep.  A batch serves every layer.
+    n_kept: how many each row keeps, evicted: how many it loses (host)."""
 
     def __init__(self, tables, new_tables, budget, block_len, device="cuda"):
         if not len(tables) == len(new_tables) == len(budget):

@@ -4,7 +4,8 @@
 // with lse from the attention call before.  S = Q K^T runs on v_mfma_f32_32x32x16_bf16 with the queries as its rows, so that a
 // lane holds one key's scores against 16 queries and their sum stays in the lane; K goes from the pool straight into the
 // operand.  The coefficient goes into the exponent (lse - log c, infinite where nothing counts).  A key of a row and head
-// belongs to one wave, whose order of additions is fixed: no atomics.
+// belongs to one wave, in weigh_split to one workgroup, whose order of additions is fixed: no atomics.  The kernels' orders
+// differ, and which one runs follows from the call's sizes: the same row may get other last bits in a call of other sizes.
 //
 // A call has to read each key once (2 d bytes a KV head) and two floats a key are read and written; it multiplies 2 d hq times and
 // takes hq exponentials a key and token.  Few tokens are bound by memory, many by their exponentials and products.
@@ -18,8 +19,8 @@
 // Measured (times of calls one after the other): those 64 tokens 23 us, 102 MB, 4.5 TB/s.  32 tokens under one path of 30,000
 // keys, 28/4/128: 17 us; 472 workgroups are less than two a CU, so it is a workgroup's own time: about 6 us until its first
 // product (table, lengths, keys and first queries, a chain) and seven tiles of 1 us, 1.5 where there are masks.  8 rows of 64 to
-// 256 tokens under 2,000 to 12,000 keys, 32/8/128 (67.8 GFLOP): 100 to 104 us, 650 to 675 TFLOP/s; MFMAs were busy 31% and the vector units 53%
-// of 110 (a product of 32 x 64 scores is 512 cycles of a SIMD's MFMAs, its exponentials 512 of a quarter-rate unit and about as
+// 256 tokens under 2,000 to 12,000 keys, 32/8/128 (67.8 GFLOP): 100 to 104 us, 650 to 675 TFLOP/s; MFMAs were busy 29% and the vector units 50%
+// of the counted cycles (a product of 32 x 64 scores is 512 cycles of a SIMD's MFMAs, its exponentials 512 of a quarter-rate unit and about as
 // many of others). Tried there, against 119 to 123 at the time: eight waves of 32 keys (123), two groups of keys one after the
 // other in a workgroup (141), three waves a SIMD (127 to 133, registers spill in the steps), chunks slowest in the grid (130 to
 // 141), products alone (103).  Masks tested score by score in a step of its own took 1.8 us a tile and these two calls 19.4 and
